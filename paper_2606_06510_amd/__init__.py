@@ -7,3 +7,6 @@ from ._lib import *  # noqa: F401,F403
 from ._lib import load, Ozaki2Error, LIB_PATH  # noqa: F401
 from .tensor import (colmajor_empty, to_device_colmajor, from_device_colmajor,  # noqa: F401
                      matmul, gemv, Plan, words_to_ints)
+from .layers import (ExpertOrder, linear, linear_backward, grouped_linear,  # noqa: F401
+                     grouped_linear_backward, expert_sort, expert_gather, expert_combine,
+                     expert_combine_backward)

@@ -46,6 +46,20 @@ OZ2_Q_STAGE_TIMES = 10
 # the six stages OZ2_Q_STAGE_TIMES reports, in its order
 STAGE_NAMES = ["scan_codes", "maxmag_gemm", "split", "residue_gemm", "reconstruct", "fallback"]
 
+# include/ozaki2/layers.h
+OZ2_F32 = 0
+OZ2_F16 = 1
+OZ2_BF16 = 2
+
+OZ2_ACT_NONE = 0
+OZ2_ACT_RELU = 1
+OZ2_ACT_GELU = 2
+OZ2_ACT_GELU_TANH = 3
+OZ2_ACT_SILU = 4
+
+OZ2_MAX_EXPERTS = 1024
+OZ2_MAX_TOPK = 64
+
 EXPORTS = [
     "ozaki2_dgemm", "ozaki2_dgemm_ex", "ozaki2_dgemm_static", "ozaki2_dgemm_strided_batched",
     "ozaki2_workspace_bytes", "ozaki2_moduli", "ozaki2_plan_create",
@@ -60,6 +74,16 @@ PROBE_EXPORTS = [
     "ozaki2_probe_e4m3", "ozaki2_probe_accum", "ozaki2_probe_copy", "ozaki2_probe_mfma_peak",
     "ozaki2_probe_mfma_digits", "ozaki2_probe_copy_peak", "ozaki2_probe_crt",
     "ozaki2_probe_batched_integers",
+]
+
+# include/ozaki2/layers.h
+LAYER_EXPORTS = [
+    "ozaki2_linear", "ozaki2_linear_workspace_bytes", "ozaki2_linear_backward",
+    "ozaki2_linear_backward_workspace_bytes", "ozaki2_grouped_linear",
+    "ozaki2_grouped_linear_workspace_bytes", "ozaki2_grouped_linear_backward",
+    "ozaki2_grouped_linear_backward_workspace_bytes", "ozaki2_expert_sort",
+    "ozaki2_expert_sort_workspace_bytes", "ozaki2_expert_gather", "ozaki2_expert_combine",
+    "ozaki2_expert_combine_backward",
 ]
 
 
@@ -115,6 +139,20 @@ def load():
         "ozaki2_probe_copy_peak": (i, [sz, i, ctypes.POINTER(ctypes.c_double)]),
         "ozaki2_probe_crt": (i, [i, p, p, i, p, p, p]),
         "ozaki2_probe_batched_integers": (i, [i, i, i, p, i, ll, p, i, ll, i, i, p, p]),
+        "ozaki2_linear": (i, [i] * 6 + [p, ll, p, ll, p, p, ll, p, ll, p, ll, p, sz, p]),
+        "ozaki2_linear_workspace_bytes": (sz, [i] * 5),
+        "ozaki2_linear_backward": (i, [i] * 6 + [p, ll] * 6 + [p, p, sz, p]),
+        "ozaki2_linear_backward_workspace_bytes": (sz, [i] * 6),
+        "ozaki2_grouped_linear": (i, [i] * 7 + [p, p, ll, p, ll, ll, p, ll, p, ll, p, ll, p, sz, p]),
+        "ozaki2_grouped_linear_workspace_bytes": (sz, [i] * 6),
+        "ozaki2_grouped_linear_backward": (
+            i, [i] * 7 + [p, p, ll, p, ll, p, ll, ll, p, ll, p, ll, p, ll, ll, p, ll, p, sz, p]),
+        "ozaki2_grouped_linear_backward_workspace_bytes": (sz, [i] * 7),
+        "ozaki2_expert_sort": (i, [i, i, i, p, i, ll, p, p, p, p, sz, p]),
+        "ozaki2_expert_sort_workspace_bytes": (sz, [i] * 3),
+        "ozaki2_expert_gather": (i, [i] * 4 + [p, ll, p, p, p, p, ll, p]),
+        "ozaki2_expert_combine": (i, [i] * 4 + [p, ll, p, p, p, p, ll, p, ll, p]),
+        "ozaki2_expert_combine_backward": (i, [i] * 4 + [p, ll, p, ll, p, p, p, p, ll, p, p]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -266,6 +304,93 @@ def ozaki2_status_string(status):
 
 def ozaki2_finalize():
     load().ozaki2_finalize()
+
+
+# ------------------------------------------------- layers (ozaki2/layers.h), same names
+
+def ozaki2_linear(dtype, activation, gated, rows, out, inp, x, ldx, w, ldw, bias, residual, ldr, y,
+                  ldy, z, ldz, workspace, ws_bytes, stream=None):
+    return _check("ozaki2_linear", load().ozaki2_linear(
+        dtype, activation, gated, rows, out, inp, _ptr(x), ldx, _ptr(w), ldw, _ptr(bias),
+        _ptr(residual), ldr, _ptr(y), ldy, _ptr(z), ldz, _ptr(workspace), ws_bytes,
+        _stream(stream)))
+
+
+def ozaki2_linear_workspace_bytes(dtype, gated, rows, out, inp):
+    return load().ozaki2_linear_workspace_bytes(dtype, gated, rows, out, inp)
+
+
+def ozaki2_linear_backward(dtype, activation, gated, rows, out, inp, dy, lddy, x, ldx, w, ldw, z,
+                           ldz, dx, lddx, dw, lddw, dbias, workspace, ws_bytes, stream=None):
+    return _check("ozaki2_linear_backward", load().ozaki2_linear_backward(
+        dtype, activation, gated, rows, out, inp, _ptr(dy), lddy, _ptr(x), ldx, _ptr(w), ldw,
+        _ptr(z), ldz, _ptr(dx), lddx, _ptr(dw), lddw, _ptr(dbias), _ptr(workspace), ws_bytes,
+        _stream(stream)))
+
+
+def ozaki2_linear_backward_workspace_bytes(dtype, activation, gated, rows, out, inp):
+    return load().ozaki2_linear_backward_workspace_bytes(dtype, activation, gated, rows, out, inp)
+
+
+def ozaki2_grouped_linear(dtype, activation, gated, rows, groups, out, inp, offsets, x, ldx, w,
+                          ldw, stride_w, bias, stride_bias, y, ldy, z, ldz, workspace, ws_bytes,
+                          stream=None):
+    return _check("ozaki2_grouped_linear", load().ozaki2_grouped_linear(
+        dtype, activation, gated, rows, groups, out, inp, _ptr(offsets), _ptr(x), ldx, _ptr(w),
+        ldw, stride_w, _ptr(bias), stride_bias, _ptr(y), ldy, _ptr(z), ldz, _ptr(workspace),
+        ws_bytes, _stream(stream)))
+
+
+def ozaki2_grouped_linear_workspace_bytes(dtype, gated, rows, groups, out, inp):
+    return load().ozaki2_grouped_linear_workspace_bytes(dtype, gated, rows, groups, out, inp)
+
+
+def ozaki2_grouped_linear_backward(dtype, activation, gated, rows, groups, out, inp, offsets, dy,
+                                   lddy, x, ldx, w, ldw, stride_w, z, ldz, dx, lddx, dw, lddw,
+                                   stride_dw, dbias, stride_dbias, workspace, ws_bytes,
+                                   stream=None):
+    return _check("ozaki2_grouped_linear_backward", load().ozaki2_grouped_linear_backward(
+        dtype, activation, gated, rows, groups, out, inp, _ptr(offsets), _ptr(dy), lddy, _ptr(x),
+        ldx, _ptr(w), ldw, stride_w, _ptr(z), ldz, _ptr(dx), lddx, _ptr(dw), lddw, stride_dw,
+        _ptr(dbias), stride_dbias, _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def ozaki2_grouped_linear_backward_workspace_bytes(dtype, activation, gated, rows, groups, out,
+                                                   inp):
+    return load().ozaki2_grouped_linear_backward_workspace_bytes(dtype, activation, gated, rows,
+                                                                 groups, out, inp)
+
+
+def ozaki2_expert_sort(tokens, top_k, num_experts, experts, wide_ids, ldexperts, offsets, rows,
+                       slots, workspace, ws_bytes, stream=None):
+    return _check("ozaki2_expert_sort", load().ozaki2_expert_sort(
+        tokens, top_k, num_experts, _ptr(experts), wide_ids, ldexperts, _ptr(offsets), _ptr(rows),
+        _ptr(slots), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def ozaki2_expert_sort_workspace_bytes(tokens, top_k, num_experts):
+    return load().ozaki2_expert_sort_workspace_bytes(tokens, top_k, num_experts)
+
+
+def ozaki2_expert_gather(dtype, tokens, top_k, width, x, ldx, slots, kept, weights, xs, ldxs,
+                         stream=None):
+    return _check("ozaki2_expert_gather", load().ozaki2_expert_gather(
+        dtype, tokens, top_k, width, _ptr(x), ldx, _ptr(slots), _ptr(kept), _ptr(weights),
+        _ptr(xs), ldxs, _stream(stream)))
+
+
+def ozaki2_expert_combine(dtype, tokens, top_k, width, ys, ldys, slots, kept, weights, residual,
+                          ldr, y, ldy, stream=None):
+    return _check("ozaki2_expert_combine", load().ozaki2_expert_combine(
+        dtype, tokens, top_k, width, _ptr(ys), ldys, _ptr(slots), _ptr(kept), _ptr(weights),
+        _ptr(residual), ldr, _ptr(y), ldy, _stream(stream)))
+
+
+def ozaki2_expert_combine_backward(dtype, tokens, top_k, width, dy, lddy, ys, ldys, slots, kept,
+                                   weights, dys, lddys, dweights, stream=None):
+    return _check("ozaki2_expert_combine_backward", load().ozaki2_expert_combine_backward(
+        dtype, tokens, top_k, width, _ptr(dy), lddy, _ptr(ys), ldys, _ptr(slots), _ptr(kept),
+        _ptr(weights), _ptr(dys), lddys, _ptr(dweights), _stream(stream)))
 
 
 # ------------------------------------------------------------ probes (ozaki2_probes.h)

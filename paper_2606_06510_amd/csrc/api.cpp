@@ -470,10 +470,8 @@ int oz2_device_cus() {
   return cus;
 }
 
-namespace {
-
 // gfx950 check, cached per device
-int device_ok() {
+int oz2_device_ok() {
   static std::mutex mu;
   static int cache[64];
   static bool init = false;
@@ -489,6 +487,8 @@ int device_ok() {
   }
   return cache[dev] == 1 ? OZ2_OK : OZ2_E_UNSUPPORTED;
 }
+
+namespace {
 
 bool overlaps(const void* a, size_t abytes, const void* b, size_t bbytes) {
   uintptr_t a0 = (uintptr_t)a, a1 = a0 + abytes, b0 = (uintptr_t)b, b1 = b0 + bbytes;
@@ -763,7 +763,7 @@ int ozaki2_plan_create(ozaki2_plan_t* out, int m, int n, int k, int num_moduli, 
     delete p;
     return OZ2_E_WORKSPACE;
   }
-  int st = device_ok();
+  int st = oz2_device_ok();
   if (st != OZ2_OK) {
     delete p;
     return st;
@@ -862,7 +862,7 @@ int ozaki2_dgemm_ex(int m, int n, int k, const double* A, int lda, const double*
   int st = check_mats(m, n, k, A, lda, B, ldb, C, ldc);
   if (st != OZ2_OK) return st;
   if (m == 0 || n == 0) return OZ2_OK;
-  st = device_ok();
+  st = oz2_device_ok();
   if (st != OZ2_OK) return st;
   hipStream_t s = (hipStream_t)stream;
   if (k == 0) {
@@ -908,7 +908,7 @@ int ozaki2_dgemm(int m, int n, int k, const double* A, int lda, const double* B,
   if (m == 0 || n == 0) return OZ2_OK;
   size_t need = ozaki2_workspace_bytes(m, n, k, num_moduli, route_flags(m, n, k, num_moduli, 0));
   if (need == 0) return OZ2_E_INVALID;
-  st = device_ok();
+  st = oz2_device_ok();
   if (st != OZ2_OK) return st;
   std::lock_guard<std::mutex> g(g_pool_mu);
   void* ws = nullptr;
@@ -926,7 +926,7 @@ int ozaki2_dgemm_static(int m, int n, int k, const double* A, int lda, const dou
   const size_t need = ozaki2_workspace_bytes(m, n, k, num_moduli, 0);
   if (need == 0) return OZ2_E_INVALID;
   if (need > OZ2_STATIC_SCRATCH_BYTES) return OZ2_E_WORKSPACE;
-  st = device_ok();
+  st = oz2_device_ok();
   if (st != OZ2_OK) return st;
   void* ws = nullptr;
   st = scratch_address(&ws);
@@ -950,7 +950,7 @@ int ozaki2_dgemm_strided_batched(int m, int n, int k, const double* A, int lda, 
     // one launch for all problems: every stage inside one workgroup per problem
     Oz2Const c;
     if (!make_const(num_moduli, c)) return OZ2_E_INVALID;
-    st = device_ok();
+    st = oz2_device_ok();
     if (st != OZ2_OK) return st;
     const hipError_t e = oz2_launch_batched(c, m, n, k, batch, A, lda, strideA, B, ldb, strideB, C,
                                             ldc, strideC, nullptr, (hipStream_t)stream);
@@ -961,7 +961,7 @@ int ozaki2_dgemm_strided_batched(int m, int n, int k, const double* A, int lda, 
                     C + (size_t)b * strideC, ldc);
     if (st != OZ2_OK) return st;
   }
-  st = device_ok();
+  st = oz2_device_ok();
   if (st != OZ2_OK) return st;
   hipStream_t s = (hipStream_t)stream;
   if (k == 0) {
@@ -1026,7 +1026,7 @@ int ozaki2_gemv_batched(int m, int k, int nrhs, const double* A, int lda, const 
   if (m == 0 || nrhs == 0) return OZ2_OK;
   hipStream_t s = (hipStream_t)stream;
   if (k == 0) {
-    st = device_ok();
+    st = oz2_device_ok();
     return st != OZ2_OK ? st : hip_status(oz2_launch_fill(Y, m, nrhs, ldy, s));
   }
   Oz2Const c;
@@ -1034,7 +1034,7 @@ int ozaki2_gemv_batched(int m, int k, int nrhs, const double* A, int lda, const 
   if (!make_const(num_moduli, c) || !gemv_shape(m, k, nrhs, flags, g)) return OZ2_E_INVALID;
   const Oz2Layout L = make_gemv_layout(g, c);
   if (!workspace || ws_bytes < L.total || ((uintptr_t)workspace & 255)) return OZ2_E_WORKSPACE;
-  st = device_ok();
+  st = oz2_device_ok();
   if (st != OZ2_OK) return st;
   uint8_t* ws = (uint8_t*)workspace;
   const Oz2Dims& d = g.d;
@@ -1231,7 +1231,7 @@ int ozaki2_probe_crt(int num_moduli, const short* residues, const int* shifts, i
   Oz2Const c;
   if (n < 0 || !make_const(num_moduli, c)) return OZ2_E_INVALID;
   if (n > 0 && (!residues || !shifts || !words || !rounded)) return OZ2_E_INVALID;
-  const int st = device_ok();
+  const int st = oz2_device_ok();
   if (st != OZ2_OK) return st;
   return hip_status(oz2_launch_crt_probe(c, (const int16_t*)residues, shifts, n, (uint32_t*)words,
                                          rounded, (hipStream_t)stream));
@@ -1246,7 +1246,7 @@ int ozaki2_probe_batched_integers(int m, int n, int k, const double* A, int lda,
     return OZ2_E_INVALID;
   if (batch == 0) return OZ2_OK;
   if (!A || !B || !words) return OZ2_E_INVALID;
-  int st = device_ok();
+  int st = oz2_device_ok();
   if (st != OZ2_OK) return st;
   // C is not written on this path (the kernel writes the integers instead)
   const hipError_t e = oz2_launch_batched(c, m, n, k, batch, A, lda, strideA, B, ldb, strideB, nullptr,

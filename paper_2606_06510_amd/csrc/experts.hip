@@ -1,0 +1,376 @@
+// Tokens in the order of their experts and back: a stable counting sort of the
+// token-expert pairs, the tokens' rows at their places, their weighted sum, and
+// the gradients.  All of it moves data once; nothing here is bound by arithmetic.
+#include <algorithm>
+
+#include "oz2_layers.h"
+
+namespace {
+
+// ---------------------------------------------------------------- sort
+// Key of pair p: its expert, or E where dropped.  The stable order of keys
+// 0..E by counting: place = (pairs of lower keys) + (earlier pairs of the key).
+// A workgroup takes a contiguous range of pairs, each of its waves a contiguous
+// part, so "earlier" is: earlier workgroups (counted by a first launch), earlier
+// waves (counted in LDS), and earlier lanes (a ballot per bit of the key).
+constexpr int SORT_NT = 512, SORT_W = SORT_NT / 64;
+
+struct SortArgs {
+  const void* ids;
+  ll ld;
+  int k, E, pairs, chunk;   // chunk: pairs per workgroup, a multiple of SORT_NT
+  bool wide;
+};
+
+__device__ __forceinline__ int key_of(const SortArgs& a, int p) {
+  const int t = p / a.k;
+  const ll at = (ll)t * a.ld + (p - t * a.k);
+  const ll v = a.wide ? ((const ll*)a.ids)[at] : (ll)((const int*)a.ids)[at];
+  return v >= 0 && v < a.E ? (int)v : a.E;
+}
+
+__global__ void __launch_bounds__(SORT_NT)
+k_sort_count(SortArgs a, int* __restrict__ counts) {
+  __shared__ int h[OZ2_MAX_EXPERTS + 1];
+  for (int e = threadIdx.x; e <= a.E; e += SORT_NT) h[e] = 0;
+  __syncthreads();
+  const int p0 = blockIdx.x * a.chunk, p1 = min(a.pairs, p0 + a.chunk);
+  for (int p = p0 + (int)threadIdx.x; p < p1; p += SORT_NT) atomicAdd(&h[key_of(a, p)], 1);
+  __syncthreads();
+  for (int e = threadIdx.x; e <= a.E; e += SORT_NT) counts[(ll)blockIdx.x * (a.E + 1) + e] = h[e];
+}
+
+__global__ void __launch_bounds__(SORT_NT)
+k_sort_place(SortArgs a, const int* __restrict__ counts, int* __restrict__ offsets,
+             int* __restrict__ rows, int* __restrict__ slots) {
+  __shared__ int at[SORT_W][OZ2_MAX_EXPERTS + 1];   // counts, then next place, of each wave and key
+  __shared__ int tot[OZ2_MAX_EXPERTS + 1];
+  __shared__ int wsum[SORT_W];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, K = a.E + 1;
+  for (int i = tid; i < SORT_W * K; i += SORT_NT) at[i / K][i % K] = 0;
+  __syncthreads();
+  const int part = a.chunk / SORT_W, p0 = blockIdx.x * a.chunk + w * part;
+  const int p1 = min(a.pairs, p0 + part);
+  for (int p = p0 + lane; p < p1; p += 64) atomicAdd(&at[w][key_of(a, p)], 1);
+  __syncthreads();
+  // pairs of each key in all, and in earlier workgroups
+  for (int e = tid; e < K; e += SORT_NT) {
+    int all = 0, before = 0;
+    if (gridDim.x == 1) {
+#pragma unroll
+      for (int v = 0; v < SORT_W; ++v) all += at[v][e];
+    } else {
+      for (int b = 0; b < (int)gridDim.x; ++b) {
+        const int c = counts[(ll)b * K + e];
+        all += c;
+        before += b < (int)blockIdx.x ? c : 0;
+      }
+    }
+    tot[e] = all;
+    // exclusive over the waves, from the earlier workgroups' pairs on
+#pragma unroll
+    for (int v = 0; v < SORT_W; ++v) {
+      const int c = at[v][e];
+      at[v][e] = before;
+      before += c;
+    }
+  }
+  __syncthreads();
+  // exclusive sums of tot: each thread `per` consecutive keys
+  const int per = (K + SORT_NT - 1) / SORT_NT;
+  int mine = 0;
+  for (int i = 0; i < per; ++i) {
+    const int e = tid * per + i;
+    if (e < K) mine += tot[e];
+  }
+  int incl = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int up = __shfl_up(incl, d);
+    if (lane >= d) incl += up;
+  }
+  if (lane == 63) wsum[w] = incl;
+  __syncthreads();
+  int excl = incl - mine;
+  for (int v = 0; v < w; ++v) excl += wsum[v];
+  for (int i = 0; i < per; ++i) {
+    const int e = tid * per + i;
+    if (e < K) {
+      const int c = tot[e];
+      tot[e] = excl;
+      if (blockIdx.x == 0) offsets[e] = excl;   // offsets[E]: the pairs kept
+      excl += c;
+    }
+  }
+  __syncthreads();
+  const int bits = 32 - __clz(a.E);   // of keys 0..E
+  for (int q = p0; q < p1; q += 64) {
+    const int p = q + lane;
+    const bool live = p < p1;
+    const int key = live ? key_of(a, p) : 0;
+    unsigned long long same = __ballot(live);
+    for (int b = 0; b < bits; ++b) {
+      const bool one = (key >> b) & 1;
+      const unsigned long long m = __ballot(one);
+      same &= one ? m : ~m;
+    }
+    const int rank = __popcll(same & ((1ull << lane) - 1));
+    if (live) {
+      const int place = tot[key] + at[w][key] + rank;
+      rows[place] = p;
+      slots[p] = place;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (live && rank == 0) at[w][key] += __popcll(same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+}
+
+// ---------------------------------------------------------------- rows
+// LPR lanes walk the 16-byte pieces of one token's row; a token's row is read
+// once and meets all of its places.  All rows may start at any element.
+template <int LPR>
+__device__ __forceinline__ bool token_of(int tokens, int& t, int& lane) {
+  const ll id = (ll)blockIdx.x * 256 + threadIdx.x;
+  t = (int)min(id / LPR, (ll)tokens);
+  lane = (int)(id % LPR);
+  return t < tokens;
+}
+
+template <class T, int LPR>
+__global__ void __launch_bounds__(256)
+k_gather(Oz2Tokens a, const T* __restrict__ x, ll ldx, T* __restrict__ xs, ll ldxs) {
+  constexpr int P = 16 / sizeof(T);
+  int t, lane;
+  if (!token_of<LPR>(a.tokens, t, lane)) return;
+  const int pairs = a.tokens * a.top_k, kept = min(*a.kept, pairs);
+  const int pieces = (a.width + P - 1) / P;
+  const int* sl = a.slots + (ll)t * a.top_k;
+  const float* wt = a.weights ? a.weights + (ll)t * a.top_k : nullptr;
+  for (int c = lane + LPR * (int)blockIdx.y; c < pieces; c += LPR * (int)gridDim.y) {
+    const int valid = a.width - c * P;
+    const Piece<T, P> v = load_piece<T>(x + t * ldx + (ll)c * P, valid);
+    for (int j = 0; j < a.top_k; ++j) {
+      const int s = sl[j];
+      if (s < 0 || s >= pairs) continue;
+      Piece<T, P> o = v;
+      if (s >= kept) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) o.v[i] = (T)0.0f;
+      } else if (wt) {
+        const float f = wt[j];
+#pragma unroll
+        for (int i = 0; i < P; ++i) o.v[i] = from_f<T>(f * to_f(v.v[i]));
+      }
+      store_piece(xs + s * ldxs + (ll)c * P, o, valid);
+    }
+  }
+}
+
+template <class T, int LPR>
+__global__ void __launch_bounds__(256)
+k_combine(Oz2Tokens a, const T* __restrict__ ys, ll ldys, const T* res, ll ldr, T* y, ll ldy) {
+  constexpr int P = 16 / sizeof(T), UN = 4;
+  int t, lane;
+  if (!token_of<LPR>(a.tokens, t, lane)) return;
+  const int kept = min(*a.kept, a.tokens * a.top_k);
+  const int pieces = (a.width + P - 1) / P;
+  const int* sl = a.slots + (ll)t * a.top_k;
+  const float* wt = a.weights ? a.weights + (ll)t * a.top_k : nullptr;
+  for (int c = lane + LPR * (int)blockIdx.y; c < pieces; c += LPR * (int)gridDim.y) {
+    const int valid = a.width - c * P;
+    float sum[P];
+    if (res) {
+      const Piece<T, P> r = load_piece<T>(res + t * ldr + (ll)c * P, valid);
+#pragma unroll
+      for (int i = 0; i < P; ++i) sum[i] = to_f(r.v[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < P; ++i) sum[i] = 0.0f;
+    }
+    for (int j0 = 0; j0 < a.top_k; j0 += UN) {   // UN rows in flight
+      Piece<T, P> v[UN];
+      float f[UN];
+      bool on[UN];
+#pragma unroll
+      for (int u = 0; u < UN; ++u) {
+        const int j = j0 + u;
+        const int s = j < a.top_k ? sl[j] : -1;
+        on[u] = s >= 0 && s < kept;
+        f[u] = on[u] && wt ? wt[j] : 1.0f;
+        if (on[u]) v[u] = load_piece<T>(ys + s * ldys + (ll)c * P, valid);
+      }
+#pragma unroll
+      for (int u = 0; u < UN; ++u)
+        if (on[u]) {
+#pragma unroll
+          for (int i = 0; i < P; ++i) sum[i] += f[u] * to_f(v[u].v[i]);
+        }
+    }
+    Piece<T, P> o;
+#pragma unroll
+    for (int i = 0; i < P; ++i) o.v[i] = from_f<T>(sum[i]);
+    store_piece(y + t * ldy + (ll)c * P, o, valid);
+  }
+}
+
+// UN places at a time: dY's piece is read once for them.  The dot products are
+// joined over the LPR lanes in a fixed order.
+template <class T, int LPR>
+__global__ void __launch_bounds__(256)
+k_combine_backward(Oz2Tokens a, const T* __restrict__ dy, ll lddy, const T* __restrict__ ys, ll ldys,
+                   T* __restrict__ dys, ll lddys, float* __restrict__ dw) {
+  constexpr int P = 16 / sizeof(T), UN = 4;
+  __shared__ float red[4][UN];
+  int t, lane;
+  const bool live = token_of<LPR>(a.tokens, t, lane);
+  if (LPR <= 64 && !live) return;   // LPR = 256: one token per workgroup, all live
+  const int pairs = a.tokens * a.top_k, kept = min(*a.kept, pairs);
+  const int pieces = (a.width + P - 1) / P;
+  const int* sl = a.slots + (ll)t * a.top_k;
+  const float* wt = a.weights + (ll)t * a.top_k;
+  for (int j0 = 0; j0 < a.top_k; j0 += UN) {
+    int s[UN];
+    float f[UN], dot[UN];
+#pragma unroll
+    for (int u = 0; u < UN; ++u) {
+      const int j = j0 + u;
+      s[u] = j < a.top_k ? sl[j] : -1;
+      if (s[u] >= pairs) s[u] = -1;
+      f[u] = s[u] >= 0 && s[u] < kept ? wt[j] : 0.0f;
+      dot[u] = 0.0f;
+    }
+    for (int c = lane; c < pieces; c += LPR) {
+      const int valid = a.width - c * P;
+      const Piece<T, P> g = load_piece<T>(dy + t * lddy + (ll)c * P, valid);
+      Piece<T, P> v[UN];
+      if (dw) {
+#pragma unroll
+        for (int u = 0; u < UN; ++u)
+          if (s[u] >= 0 && s[u] < kept) v[u] = load_piece<T>(ys + s[u] * ldys + (ll)c * P, valid);
+      }
+#pragma unroll
+      for (int u = 0; u < UN; ++u) {
+        if (s[u] < 0) continue;
+        const bool on = s[u] < kept;
+        if (dw && on) {
+#pragma unroll
+          for (int i = 0; i < P; ++i) dot[u] += to_f(g.v[i]) * to_f(v[u].v[i]);
+        }
+        if (dys) {
+          Piece<T, P> o;
+#pragma unroll
+          for (int i = 0; i < P; ++i) o.v[i] = from_f<T>(on ? f[u] * to_f(g.v[i]) : 0.0f);
+          store_piece(dys + s[u] * lddys + (ll)c * P, o, valid);
+        }
+      }
+    }
+    if (!dw) continue;
+#pragma unroll
+    for (int u = 0; u < UN; ++u)
+#pragma unroll
+      for (int d = 1; d < (LPR < 64 ? LPR : 64); d <<= 1) dot[u] += __shfl_xor(dot[u], d);
+    if (LPR > 64) {
+      if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+        for (int u = 0; u < UN; ++u) red[threadIdx.x >> 6][u] = dot[u];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < UN; ++u) dot[u] = (red[0][u] + red[1][u]) + (red[2][u] + red[3][u]);
+      __syncthreads();
+    }
+    if (lane == 0) {
+#pragma unroll
+      for (int u = 0; u < UN; ++u)
+        if (j0 + u < a.top_k) dw[(ll)t * a.top_k + j0 + u] = dot[u];
+    }
+  }
+}
+
+// workgroups over the tokens, and over pieces of long rows until the chip is full
+dim3 row_grid(int tokens, int lpr, int pieces) {
+  const ll bx = ((ll)tokens * lpr + 255) / 256;
+  const int want = (int)std::max<ll>(1, 2 * oz2_device_cus() / bx);
+  return dim3((unsigned)bx, (unsigned)std::min(want, (pieces + lpr - 1) / lpr));
+}
+
+int lanes_per_row(int pieces) { return pieces <= 8 ? 8 : pieces <= 16 ? 16 : pieces <= 32 ? 32 : 64; }
+
+}  // namespace
+
+#define OZ2_TYPE(dtype, ...)                               \
+  do {                                                     \
+    if ((dtype) == OZ2_F32) { typedef float T; __VA_ARGS__; }    \
+    else if ((dtype) == OZ2_F16) { typedef _Float16 T; __VA_ARGS__; } \
+    else { typedef __bf16 T; __VA_ARGS__; }                \
+  } while (0)
+#define OZ2_LANES(lpr, kern, ...)                          \
+  do {                                                     \
+    if ((lpr) == 8) { auto* f = kern<T, 8>; __VA_ARGS__; }       \
+    else if ((lpr) == 16) { auto* f = kern<T, 16>; __VA_ARGS__; } \
+    else if ((lpr) == 32) { auto* f = kern<T, 32>; __VA_ARGS__; } \
+    else { auto* f = kern<T, 64>; __VA_ARGS__; }                 \
+  } while (0)
+
+// workgroups of the sort: one where its own loop is shorter than a second launch
+int oz2_sort_blocks(ll pairs) {
+  if (pairs <= 4096) return 1;
+  return (int)std::min<ll>(128, (pairs + 2047) / 2048);
+}
+
+hipError_t oz2_launch_sort(int tokens, int top_k, int E, const void* ids, bool wide, ll ld, int* offsets,
+                           int* rows, int* slots, int* counts, hipStream_t s) {
+  const ll pairs = (ll)tokens * top_k;
+  int nb = oz2_sort_blocks(pairs);
+  const ll chunk = std::max<ll>(1, ((pairs + nb - 1) / nb + SORT_NT - 1) / SORT_NT) * SORT_NT;
+  nb = std::max(1, (int)((pairs + chunk - 1) / chunk));
+  SortArgs a{ids, ld, top_k, E, (int)pairs, (int)chunk, wide};
+  if (nb > 1) {
+    hipLaunchKernelGGL(k_sort_count, dim3(nb), dim3(SORT_NT), 0, s, a, counts);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(k_sort_place, dim3(nb), dim3(SORT_NT), 0, s, a, counts, offsets, rows, slots);
+  return hipGetLastError();
+}
+
+hipError_t oz2_launch_gather(int dtype, const Oz2Tokens& t, const void* x, ll ldx, void* xs, ll ldxs,
+                             hipStream_t s) {
+  OZ2_TYPE(dtype, {
+    const int pieces = (t.width + 16 / (int)sizeof(T) - 1) / (16 / (int)sizeof(T));
+    const int lpr = lanes_per_row(pieces);
+    OZ2_LANES(lpr, k_gather, hipLaunchKernelGGL(f, row_grid(t.tokens, lpr, pieces), dim3(256), 0, s, t,
+                                                (const T*)x, ldx, (T*)xs, ldxs));
+  });
+  return hipGetLastError();
+}
+
+hipError_t oz2_launch_combine(int dtype, const Oz2Tokens& t, const void* ys, ll ldys, const void* res,
+                              ll ldr, void* y, ll ldy, hipStream_t s) {
+  OZ2_TYPE(dtype, {
+    const int pieces = (t.width + 16 / (int)sizeof(T) - 1) / (16 / (int)sizeof(T));
+    const int lpr = lanes_per_row(pieces);
+    OZ2_LANES(lpr, k_combine, hipLaunchKernelGGL(f, row_grid(t.tokens, lpr, pieces), dim3(256), 0, s, t,
+                                                 (const T*)ys, ldys, (const T*)res, ldr, (T*)y, ldy));
+  });
+  return hipGetLastError();
+}
+
+hipError_t oz2_launch_combine_backward(int dtype, const Oz2Tokens& t, const void* dy, ll lddy,
+                                       const void* ys, ll ldys, void* dys, ll lddys, float* dw,
+                                       hipStream_t s) {
+  OZ2_TYPE(dtype, {
+    const int pieces = (t.width + 16 / (int)sizeof(T) - 1) / (16 / (int)sizeof(T));
+    if (pieces > 128) {
+      hipLaunchKernelGGL((k_combine_backward<T, 256>), dim3(t.tokens), dim3(256), 0, s, t, (const T*)dy,
+                         lddy, (const T*)ys, ldys, (T*)dys, lddys, dw);
+    } else {
+      const int lpr = lanes_per_row(pieces);
+      const unsigned bx = (unsigned)(((ll)t.tokens * lpr + 255) / 256);
+      OZ2_LANES(lpr, k_combine_backward, hipLaunchKernelGGL(f, dim3(bx), dim3(256), 0, s, t, (const T*)dy,
+                                                            lddy, (const T*)ys, ldys, (T*)dys, lddys, dw));
+    }
+  });
+  return hipGetLastError();
+}

@@ -1,0 +1,571 @@
+// Products of the layer operators on the matrix cores:
+//   D[i][j] = sum over l of A(i, l) B(j, l),
+// forward (A = X, B = W, both contiguous along l), the gradient of X (B = W
+// contiguous along j) and of W (A = dZ contiguous along i, B = X along j), each
+// for one product or for groups of rows.
+//
+// A stage is 64 bytes of l (32 entries of 16 bits, 16 of 32) for all rows of the
+// workgroup's tiles, in LDS in the layout of its source, read as 16-byte
+// fragments: lane (r = L%16, g = L/16) of a block of 16 rows holds row r and l =
+// 8 g .. 8 g + 7 (16 bits) or 4 g .. 4 g + 3 (32 bits) of the stage, which is one
+// 16x16x32 instruction or four 16x16x4 ones.  Rows contiguous along l give a
+// fragment as one read; the others through the transposing LDS read (16 bits:
+// its 16 lanes read 4 l x 16 columns and each receives one column) or as four
+// words (32 bits).
+//
+// The instruction's first operand is B, so that a lane's accumulators are
+// consecutive columns j of one row i of D.  Where B's rows are contiguous along l
+// (forward) the loader also deals them out so that the lane's 16 accumulators of
+// a 64-column block are 16 consecutive columns (gated: 8 gates and the 8 values
+// they gate): the epilogue then works in registers on whole 16-byte pieces.
+#include <algorithm>
+
+#include "oz2_layers.h"
+
+namespace {
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __bf16 v8b __attribute__((ext_vector_type(8)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) uint8_t lds8;
+typedef __attribute__((address_space(3))) v4s lds_v4s;
+
+constexpr int SB = 64;   // bytes of l in a stage
+
+// 16 bytes of operand
+template <class T>
+struct Frag;
+template <>
+struct Frag<__bf16> {
+  v8b v;
+};
+template <>
+struct Frag<_Float16> {
+  v8h v;
+};
+template <>
+struct Frag<float> {
+  v4f v;
+};
+
+__device__ __forceinline__ v4f mma(const Frag<__bf16>& a, const Frag<__bf16>& b, v4f c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ v4f mma(const Frag<_Float16>& a, const Frag<_Float16>& b, v4f c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, b.v, c, 0, 0, 0);
+}
+__device__ __forceinline__ v4f mma(const Frag<float>& a, const Frag<float>& b, v4f c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[e], b.v[e], c, 0, 0, 0);
+  return c;
+}
+
+// ------------------------------------------------------------ LDS layouts
+// Rows contiguous along l: [row][64 B], the row's four 16-byte pieces rotated so
+// that the pieces a read serves together (rows 0-3, 12-15 of one piece and 4-11 of the
+// next) lie in different banks.
+__device__ __forceinline__ int row_swz(int r) { return (-(r >> 2)) & 3; }
+
+// Rows contiguous along the tile's other dimension: [l][R entries], R = 128 or
+// 256, the 16-byte pieces of row l permuted so that the rows read together lie in
+// different banks: blocks of 16 columns (2 pieces of 16 bits, 4 of 32) by an
+// exclusive or with col_swz.
+template <class T>
+__device__ __forceinline__ int col_swz(int l) {
+  return sizeof(T) == 2 ? (l & 3) | ((l >> 3) & 1) << 2 : (l >> 2) & 3;
+}
+template <class T>
+__device__ __forceinline__ int col_piece(int l, int piece) {
+  return piece ^ (col_swz<T>(l) * (sizeof(T) == 2 ? 2 : 4));
+}
+
+// The fragment of block b (16 rows) of a tile of R rows at LDS address `base`.
+template <class T, bool ROWS, int R>
+struct Reader {
+  uint32_t at;   // lane's address within block 0
+  int sw;        // !ROWS: the lane's block permutation
+  __device__ __forceinline__ Reader(int lane) {
+    const int r = lane & 15, g = lane >> 4;
+    if (ROWS) {
+      at = (uint32_t)(r * SB + 16 * (g ^ row_swz(r)));
+      sw = 0;
+    } else if (sizeof(T) == 2) {
+      const int l = 8 * g + (r >> 2);   // and + 4 in the second read
+      sw = col_swz<T>(l);
+      at = (uint32_t)(l * R * 2 + 8 * (r & 3));
+    } else {
+      sw = col_swz<T>(4 * g);
+      at = (uint32_t)(4 * g * R * 4 + 4 * r);
+    }
+  }
+  __device__ __forceinline__ Frag<T> get(const uint8_t* base, int b) const {
+    Frag<T> f;
+    if constexpr (ROWS) {
+      f.v = *reinterpret_cast<const decltype(f.v)*>(base + at + b * 16 * SB);
+    } else if constexpr (sizeof(T) == 2) {
+      const uint8_t* p = base + at + ((b ^ sw) << 5);
+      typedef short v8s __attribute__((ext_vector_type(8)));
+      const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p));
+      const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + 4 * R * 2));
+      const v8s both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      f.v = __builtin_bit_cast(decltype(f.v), both);
+    } else {
+      const uint8_t* p = base + at + ((b ^ sw) << 6);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f.v[e] = *reinterpret_cast<const float*>(p + e * R * 4);
+    }
+    return f;
+  }
+};
+
+// ------------------------------------------------------------ rows of W
+// LDS row q of a tile of B in the forward product: column block q/64 of 64
+// columns; fragment block j = (q/16)%4, row r = q%16 of it becomes accumulator
+// e = r%4 of lane group g = r/4, which is to be column 16 g + 4 j + e; gated:
+// column 8 g + 4 (j%2) + e of the block's 32, gates in j < 2, values in j >= 2.
+// Returns the row of W and, in col, the column of y.
+__device__ __forceinline__ int dealt_row(int q, int tile0, int N, bool gated, int& col) {
+  const int j = (q >> 4) & 3, r = q & 15;
+  if (!gated) {
+    col = tile0 + (q & ~63) + 16 * (r >> 2) + 4 * j + (r & 3);
+    return col;
+  }
+  col = tile0 + ((q & ~63) >> 1) + 8 * (r >> 2) + 4 * (j & 1) + (r & 3);
+  return col + (j >> 1) * N;
+}
+
+// ------------------------------------------------------------ epilogue
+// W values of the lane's row: stores n <= valid of them at p.
+template <class T, int W>
+__device__ __forceinline__ void put(T* p, const float* v, int valid) {
+  constexpr int P = W < 16 / (int)sizeof(T) ? W : 16 / (int)sizeof(T);
+#pragma unroll
+  for (int c = 0; c < W; c += P) {
+    if (c >= valid) break;
+    Piece<T, P> o;
+#pragma unroll
+    for (int i = 0; i < P; ++i) o.v[i] = from_f<T>(v[c + i]);
+    store_piece(p + c, o, valid - c);
+  }
+}
+template <class T, int W>
+__device__ __forceinline__ void add(const T* p, float* v, int valid) {
+  constexpr int P = W < 16 / (int)sizeof(T) ? W : 16 / (int)sizeof(T);
+#pragma unroll
+  for (int c = 0; c < W; c += P) {
+    if (c >= valid) break;
+    const Piece<T, P> o = load_piece<T, P>(p + c, valid - c);
+#pragma unroll
+    for (int i = 0; i < P; ++i) v[c + i] += to_f(o.v[i]);
+  }
+}
+
+// One row's W consecutive columns of y from column col on (valid of them exist):
+// v the pre-activations, gated: u the values.  y may be res.
+template <class T, int W>
+__device__ __forceinline__ void finish(const Oz2Product& p, ll row, int col, int valid, float* v,
+                                       float* u) {
+  if (p.z) {
+    T* z = (T*)p.z + row * p.ldz + col;
+    put<T, W>(z, v, valid);
+    if (p.gated) put<T, W>(z + p.N, u, valid);
+  }
+  if (p.act != OZ2_ACT_NONE) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = act_f<T>(v[i], p.act);
+  }
+  if (p.gated) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] *= u[i];
+  }
+  if (p.res) add<T, W>((const T*)p.res + row * p.ldr + col, v, valid);
+  put<T, W>((T*)p.y + row * p.ldy + col, v, valid);
+}
+
+// The accumulators acc[j][i] of a wave whose first row is `row` and first LDS row
+// of B (column of D) `wn`, tile column tile0; rows end before `end`.
+template <class T, Oz2Side SIDE, int MI>
+__device__ __forceinline__ void epilogue(const Oz2Product& p, const v4f (&acc)[4][MI], int group, int row,
+                                         int end, int tile0, int wn, int lane, int split) {
+  const int r = lane & 15, g = lane >> 4;
+  if constexpr (SIDE == OZ2_FWD) {
+    const bool gated = p.gated != 0;
+    const int col = tile0 + (gated ? wn / 2 + 8 * g : wn + 16 * g);
+    const int valid = p.N - col;
+    if (valid <= 0) return;
+    float b[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) b[i] = 0.0f;
+    if (p.bias && p.splits == 1) {
+      const T* bp = (const T*)p.bias + group * p.stride_bias + col;
+      if (gated) {
+        add<T, 8>(bp, b, valid);
+        add<T, 8>(bp + p.N, b + 8, valid);
+      } else {
+        add<T, 16>(bp, b, valid);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int t = row + 16 * i + r;
+      if (t >= end) continue;
+      float v[16];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * j + e] = acc[j][i][e] + b[4 * j + e];
+      if (p.splits > 1) {
+        float* q = p.part + ((ll)split * p.M + t) * p.N2 + col;
+        if (gated) {
+          put<float, 8>(q, v, valid);
+          put<float, 8>(q + p.N, v + 8, valid);
+        } else {
+          put<float, 16>(q, v, valid);
+        }
+      } else if (gated) {
+        finish<T, 8>(p, t, col, valid, v, v + 8);
+      } else {
+        finish<T, 16>(p, t, col, valid, v, v);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int t = row + 16 * i + r;
+      if (t >= end) continue;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int col = tile0 + wn + 16 * j + 4 * g;
+        if (col >= p.N2) continue;
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = acc[j][i][e];
+        if (p.splits > 1)
+          put<float, 4>(p.part + ((ll)split * p.M + t) * p.N2 + col, v, p.N2 - col);
+        else
+          put<T, 4>((T*)p.y + (SIDE == OZ2_WGRAD ? group * p.strideB : 0) + t * p.ldy + col, v, p.N2 - col);
+      }
+    }
+  }
+}
+
+// rows [row, row + tile) below end of y (and z) are zeros: columns col .. col + n
+template <class T>
+__device__ __forceinline__ void zero_rows(const Oz2Product& p, int row, int end, int col, int n, int tile,
+                                          int threads) {
+  const int w = min(n, p.N - col);
+  for (int q = threadIdx.x; q < tile * n; q += threads) {
+    const int t = row + q / n, c = q % n;
+    if (t >= end || c >= w) continue;
+    ((T*)p.y)[t * p.ldy + col + c] = (T)0.0f;
+    if (p.z) {
+      ((T*)p.z)[t * p.ldz + col + c] = (T)0.0f;
+      if (p.gated) ((T*)p.z)[t * p.ldz + p.N + col + c] = (T)0.0f;
+    }
+  }
+}
+
+// ------------------------------------------------ 128 x 128 tiles
+// 256 threads = 4 waves, 64 x 64 outputs each; two stages in LDS, the next one in
+// registers under a stage's products.  Any size, any alignment.
+constexpr int TM = 128, NT = 256;
+
+struct Tile {
+  int group, row, end;   // rows of D
+  int col0;              // first column of y
+  int l0, l1;            // range of the sum
+  int split;
+};
+
+template <Oz2Side SIDE>
+__device__ __forceinline__ bool tile_of(const Oz2Product& p, int tile, int ncol, int rows_t, Tile& t) {
+  const int cols = p.gated ? tile / 2 : tile;
+  t.col0 = ((int)blockIdx.x % ncol) * cols;
+  const int rt = (int)blockIdx.x / ncol;
+  if (SIDE == OZ2_WGRAD) {
+    t.group = (int)blockIdx.z;
+    t.row = rt * tile;
+    t.end = p.M;
+    group_range(p.gr, t.group, t.l0, t.l1);
+  } else {
+    if (!group_tile(p.gr, tile, rt, t.group, t.row, t.end)) return false;
+    t.l0 = 0;
+    t.l1 = p.L;
+  }
+  t.split = 0;
+  if (p.splits > 1) {   // (one group) whole stages, as even as they go
+    t.split = (int)blockIdx.y;
+    const int st = 64;
+    const ll n = (t.l1 - t.l0 + st - 1) / st;
+    const int a = (int)(n * t.split / p.splits) * st, b = (int)(n * (t.split + 1) / p.splits) * st;
+    t.l1 = min(t.l1, t.l0 + b);
+    t.l0 += a;
+  }
+  return true;
+}
+
+// One thread's two 16-byte pieces of an operand's stage, by way of registers.
+template <class T, bool ROWS>
+struct Loader {
+  static constexpr int P = 16 / sizeof(T), KE = SB / sizeof(T);
+  const T* src[2];
+  int valid[2];          // ROWS: the row exists; else entries of the piece that exist
+  int l[2];              // ROWS: first l of the piece; else its l
+  uint32_t dst[2];
+  ll step;
+  __device__ __forceinline__ void init(const T* base, ll ld, int q, int u, int row, bool exists,
+                                       int nvalid) {
+    if (ROWS) {
+      const int c = q & 3;
+      src[u] = base + (ll)row * ld + c * P;
+      valid[u] = exists;
+      l[u] = c * P;
+      dst[u] = (uint32_t)((q >> 2) * SB + 16 * (c ^ row_swz(q >> 2)));
+      step = KE;
+    } else {
+      constexpr int PR = TM / P;   // pieces per l
+      const int k = q / PR, c = q % PR;
+      src[u] = base + k * ld + c * P;
+      valid[u] = nvalid - c * P;
+      l[u] = k;
+      dst[u] = (uint32_t)(k * TM * sizeof(T) + 16 * col_piece<T>(k, c));
+      step = KE * ld;
+    }
+  }
+  // `left`: entries of l from the stage's first on
+  __device__ __forceinline__ Piece<T, P> fetch(int u, int left) const {
+    const int n = ROWS ? (valid[u] ? left - l[u] : 0) : (l[u] < left ? valid[u] : 0);
+    return load_piece<T>(src[u], n);
+  }
+};
+
+template <class T, Oz2Side SIDE>
+__global__ void __launch_bounds__(NT, 2)
+k_product(Oz2Product p, int ncol) {
+  constexpr bool AR = SIDE != OZ2_WGRAD, BR = SIDE == OZ2_FWD;
+  constexpr int KE = SB / sizeof(T), OP = TM * SB;
+  __shared__ __attribute__((aligned(16))) uint8_t LB[2][2 * OP];
+  Tile t;
+  if (!tile_of<SIDE>(p, TM, ncol, 0, t)) return;
+  if (SIDE != OZ2_WGRAD && t.group < 0) {
+    zero_rows<T>(p, t.row, t.end, t.col0, p.gated ? TM / 2 : TM, TM, NT);
+    return;
+  }
+  const T* A = (const T*)p.A;
+  const T* B = (const T*)p.B;
+  if (SIDE == OZ2_WGRAD) {
+    A += t.l0 * p.lda;
+    B += t.l0 * p.ldb;
+  } else {
+    A += t.l0;
+    B += t.group * p.strideB + (BR ? (ll)t.l0 : t.l0 * p.ldb);
+  }
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wr = w >> 1, wc = w & 1;
+  Loader<T, AR> la;
+  Loader<T, BR> lb;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int q = tid + NT * u;
+    if (AR) {
+      const int row = t.row + (q >> 2);
+      la.init(A, p.lda, q, u, row, row < t.end, 0);
+    } else {
+      la.init(A + t.row, p.lda, q, u, 0, true, t.end - t.row);
+    }
+    if (BR) {
+      int col;
+      const int row = dealt_row(q >> 2, t.col0, p.N, p.gated != 0, col);
+      lb.init(B, p.ldb, q, u, row, col < p.N, 0);
+    } else {
+      lb.init(B + t.col0, p.ldb, q, u, 0, true, p.N2 - t.col0);
+    }
+  }
+  v4f acc[4][4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  const Reader<T, AR, TM> ra(lane);
+  const Reader<T, BR, TM> rb(lane);
+  const int len = t.l1 - t.l0, n = (len + KE - 1) / KE;
+  Piece<T, 16 / sizeof(T)> pa[2], pb[2];
+  auto fetch = [&](int it) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      pa[u] = la.fetch(u, len - it * KE);
+      pb[u] = lb.fetch(u, len - it * KE);
+      la.src[u] += la.step;
+      lb.src[u] += lb.step;
+    }
+  };
+  if (n > 0) fetch(0);
+  for (int it = 0; it < n; ++it) {
+    uint8_t* sa = LB[it & 1];
+    uint8_t* sb = sa + OP;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      __builtin_memcpy(__builtin_assume_aligned(sa + la.dst[u], 16), &pa[u], 16);
+      __builtin_memcpy(__builtin_assume_aligned(sb + lb.dst[u], 16), &pb[u], 16);
+    }
+    __syncthreads();
+    if (it + 1 < n) fetch(it + 1);
+    Frag<T> fa[4], fb[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) fa[i] = ra.get(sa, 4 * wr + i);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) fb[j] = rb.get(sb, 4 * wc + j);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[j][i] = mma(fb[j], fa[i], acc[j][i]);
+  }
+  epilogue<T, SIDE, 4>(p, acc, t.group, t.row + 64 * wr, t.end, t.col0, 64 * wc, lane, t.split);
+}
+
+template <class T>
+hipError_t launch_product(Oz2Side side, const Oz2Product& p, hipStream_t s) {
+  const int cols = p.gated && side == OZ2_FWD ? TM / 2 : TM, n = side == OZ2_FWD ? p.N : p.N2;
+  const int ncol = (n + cols - 1) / cols;
+  const ll rt = side == OZ2_WGRAD ? (p.M + TM - 1) / TM : oz2_row_tiles(p.gr, TM);
+  if (ncol == 0 || rt == 0) return hipSuccess;
+  if (rt * ncol >= (1ll << 31)) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)(rt * ncol), 1, side == OZ2_WGRAD ? p.gr.groups : 1);
+  if (side == OZ2_FWD)
+    hipLaunchKernelGGL((k_product<T, OZ2_FWD>), grid, dim3(NT), 0, s, p, ncol);
+  else if (side == OZ2_DGRAD)
+    hipLaunchKernelGGL((k_product<T, OZ2_DGRAD>), grid, dim3(NT), 0, s, p, ncol);
+  else
+    hipLaunchKernelGGL((k_product<T, OZ2_WGRAD>), grid, dim3(NT), 0, s, p, ncol);
+  return hipGetLastError();
+}
+
+// ------------------------------------------------ slope: dZ and its column sums
+// dZ = dY f'(Z).  A workgroup takes OZ2_SUM_ROWS rows of one group and 8 (fp32 4)
+// x 32 columns of n: 8 rows at a time, 32 threads a row; the column sums of its
+// rows leave as one partial row, summed in order by k_sums.  Memory-bound.
+template <class T>
+__global__ void __launch_bounds__(256)
+k_slope(Oz2Slope p) {
+  constexpr int P = 16 / sizeof(T);
+  __shared__ float red[8][32 * 2 * P];
+  int group, row, end;
+  const bool tail_out = !group_tile(p.gr, OZ2_SUM_ROWS, (int)blockIdx.x, group, row, end);
+  if (tail_out || group < 0) return;   // dZ outside the groups is never read
+  end = min(end, row + OZ2_SUM_ROWS);
+  const int c = ((int)blockIdx.y * 32 + (int)(threadIdx.x & 31)) * P, rr = threadIdx.x >> 5;
+  const int n2 = p.gated ? 2 * p.n : p.n, valid = p.n - c;
+  float sg[P], su[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) sg[i] = su[i] = 0.0f;
+  if (valid > 0) {
+    for (int t = row + rr; t < end; t += 8) {
+      const Piece<T, P> g = load_piece<T>((const T*)p.dy + t * p.lddy + c, valid);
+      Piece<T, P> a, u, o;
+      if (p.z) a = load_piece<T>((const T*)p.z + t * p.ldz + c, valid);
+      if (p.gated) u = load_piece<T>((const T*)p.z + t * p.ldz + p.n + c, valid);
+      float d[P];
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const float x = to_f(g.v[i]);
+        d[i] = p.act == OZ2_ACT_NONE ? x : x * act_d<T>(to_f(a.v[i]), p.act);
+        if (p.gated) {
+          d[i] *= to_f(u.v[i]);
+          const float e = x * act_f<T>(to_f(a.v[i]), p.act);
+          su[i] += e;
+          u.v[i] = from_f<T>(e);
+        }
+        sg[i] += d[i];
+        o.v[i] = from_f<T>(d[i]);
+      }
+      if (p.dz) {
+        T* q = (T*)p.dz + t * p.ldd;
+        store_piece(q + c, o, valid);
+        if (p.gated) store_piece(q + p.n + c, u, valid);
+        // the pad of the row is read as part of the last piece: zeros
+        if (valid <= P)
+          for (int e = n2; e < p.ldd; ++e) q[e] = (T)0.0f;
+      }
+    }
+  }
+  if (!p.db) return;
+  const int l = threadIdx.x & 31;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    red[rr][l * 2 * P + i] = sg[i];
+    red[rr][l * 2 * P + P + i] = su[i];
+  }
+  __syncthreads();
+  for (int q = threadIdx.x; q < 32 * 2 * P; q += 256) {
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) s += red[k][q];
+    const int piece = q / (2 * P), i = q % (2 * P);
+    const int col = ((int)blockIdx.y * 32 + piece) * P + i % P;
+    const bool up = i >= P;
+    if (col < p.n && (!up || p.gated)) p.part[(ll)blockIdx.x * n2 + (up ? p.n + col : col)] = s;
+  }
+}
+
+// db of group blockIdx.y: the partial rows of its row tiles, in order, four sums at a time
+template <class T>
+__global__ void __launch_bounds__(256)
+k_sums(Oz2Slope p) {
+  const int n2 = p.gated ? 2 * p.n : p.n, c = (int)(blockIdx.x * 256 + threadIdx.x);
+  const int g = (int)blockIdx.y;
+  int first = 0, count = 0;
+  if (!p.gr.offsets) {
+    count = (p.gr.rows + OZ2_SUM_ROWS - 1) / OZ2_SUM_ROWS;
+  } else {
+    for (int i = 0; i <= g; ++i) {
+      int s, e;
+      group_range(p.gr, i, s, e);
+      const int k = (e - s + OZ2_SUM_ROWS - 1) / OZ2_SUM_ROWS;
+      if (i < g) first += k;
+      else count = k;
+    }
+  }
+  if (c >= n2) return;
+  const float* q = p.part + (ll)first * n2 + c;
+  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  int k = 0;
+  for (; k + 4 <= count; k += 4)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) s[u] += q[(ll)(k + u) * n2];
+  for (; k < count; ++k) s[0] += q[(ll)k * n2];
+  ((T*)p.db)[g * p.stride_db + c] = from_f<T>((s[0] + s[1]) + (s[2] + s[3]));
+}
+
+template <class T>
+hipError_t launch_slope(const Oz2Slope& p, hipStream_t s) {
+  constexpr int P = 16 / sizeof(T);
+  const ll rt = oz2_row_tiles(p.gr, OZ2_SUM_ROWS);
+  const int cb = (p.n + 32 * P - 1) / (32 * P);
+  if (rt > 0 && cb > 0) {
+    hipLaunchKernelGGL(k_slope<T>, dim3((unsigned)rt, (unsigned)cb), dim3(256), 0, s, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const int n2 = p.gated ? 2 * p.n : p.n;
+  if (p.db && n2 > 0) {
+    hipLaunchKernelGGL(k_sums<T>, dim3((unsigned)((n2 + 255) / 256), (unsigned)p.gr.groups), dim3(256), 0,
+                       s, p);
+    return hipGetLastError();
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t oz2_launch_product(int dtype, Oz2Side side, const Oz2Product& p, hipStream_t s) {
+  if (dtype == OZ2_F32) return launch_product<float>(side, p, s);
+  if (dtype == OZ2_F16) return launch_product<_Float16>(side, p, s);
+  return launch_product<__bf16>(side, p, s);
+}
+
+hipError_t oz2_launch_slope(int dtype, const Oz2Slope& p, hipStream_t s) {
+  if (dtype == OZ2_F32) return launch_slope<float>(p, s);
+  if (dtype == OZ2_F16) return launch_slope<_Float16>(p, s);
+  return launch_slope<__bf16>(p, s);
+}

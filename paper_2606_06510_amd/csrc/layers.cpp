@@ -1,0 +1,414 @@
+// Host side of the layer operators (include/ozaki2/layers.h): argument checks,
+// workspace layout, launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "../../include/ozaki2.h"
+#include "oz2_layers.h"
+
+namespace {
+
+constexpr ll kMaxRows = 1ll << 30, kMaxWidth = 1ll << 24, kMaxLd = 1ll << 40, kMaxElems = 1ll << 40;
+
+size_t element(int dtype) { return dtype == OZ2_F32 ? 4 : 2; }
+size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+
+// `count` matrices of rows x cols elements
+struct Mat {
+  const void* p;
+  ll rows, cols, ld;
+  int count;
+  ll stride;
+  bool empty() const { return !p || rows <= 0 || cols <= 0 || count <= 0; }
+  size_t span(size_t e) const { return (size_t)((count - 1) * stride + (rows - 1) * ld + cols) * e; }
+};
+
+Mat mat(const void* p, ll rows, ll cols, ll ld, int count = 1, ll stride = 0) {
+  return Mat{p, rows, cols, ld, count, stride};
+}
+
+// an operand that is needed: there, aligned to its elements, leading dimension
+// and stride in range
+bool good(const Mat& m, size_t e, bool output = false) {
+  if (m.rows <= 0 || m.cols <= 0 || m.count <= 0) return true;
+  if (!m.p || (uintptr_t)m.p % e) return false;
+  if (m.ld < m.cols || m.ld > kMaxLd) return false;
+  if (m.count == 1) return true;
+  if (m.stride < 0 || m.stride > kMaxLd) return false;
+  return !output || m.stride >= (m.rows - 1) * m.ld + m.cols;
+}
+
+// no element in both.  Matrices of one leading dimension may lie side by side
+// (column ranges of one buffer).
+bool disjoint(const Mat& a, const Mat& b, size_t e) {
+  if (a.empty() || b.empty()) return true;
+  const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p;
+  if (a0 + a.span(e) <= b0 || b0 + b.span(e) <= a0) return true;
+  if (a.count > 1 || b.count > 1 || a.ld != b.ld) return false;
+  const ll pitch = a.ld * (ll)e;
+  ll d = ((ll)b0 - (ll)a0) % pitch;
+  if (d < 0) d += pitch;
+  return d >= a.cols * (ll)e && d + b.cols * (ll)e <= pitch;
+}
+bool disjoint_bytes(const Mat& a, size_t e, const void* p, size_t bytes) {
+  if (a.empty() || !p || !bytes) return true;
+  const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)p;
+  return a0 + a.span(e) <= b0 || b0 + bytes <= a0;
+}
+
+int hip_status(hipError_t e) { return e == hipSuccess ? OZ2_OK : OZ2_E_DEVICE; }
+
+bool sizes_ok(int dtype, int act, ll rows, ll groups, ll out, ll in, int gated) {
+  if (dtype < OZ2_F32 || dtype > OZ2_BF16 || act < OZ2_ACT_NONE || act > OZ2_ACT_SILU) return false;
+  if (rows < 0 || out < 0 || in < 0 || rows > kMaxRows || out > kMaxWidth || in > kMaxWidth) return false;
+  if (groups < 1 || groups > OZ2_MAX_EXPERTS) return false;
+  const ll n2 = gated ? 2 * out : out;
+  return rows * n2 < kMaxElems && rows * in < kMaxElems && (double)n2 * in * groups < (double)kMaxElems;
+}
+
+// pitch of dZ in the workspace: whole 64-byte pieces
+ll slope_pitch(ll n2, size_t e) {
+  const ll per = 64 / (ll)e;
+  return (n2 + per - 1) / per * per;
+}
+
+struct BackwardLayout {
+  size_t dz, sums, total;
+};
+BackwardLayout backward_layout(int dtype, int act, int gated, const Oz2Groups& gr, ll out) {
+  const size_t e = element(dtype);
+  const ll n2 = gated ? 2 * out : out;
+  BackwardLayout L{};
+  size_t o = 0;
+  L.dz = o;
+  if (act != OZ2_ACT_NONE || gated) o = align256(o + (size_t)gr.rows * slope_pitch(n2, e) * e);
+  L.sums = o;
+  o = align256(o + (size_t)oz2_row_tiles(gr, OZ2_SUM_ROWS) * n2 * 4);
+  L.total = o;
+  return L;
+}
+
+int check_workspace(const void* ws, size_t bytes, size_t need) {
+  if (!need) return OZ2_OK;
+  return ws && (uintptr_t)ws % 256 == 0 && bytes >= need ? OZ2_OK : OZ2_E_WORKSPACE;
+}
+
+size_t forward_bytes(int, int, const Oz2Groups&, ll, ll) { return 0; }
+
+int forward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, const Mat& x, const Mat& w,
+            const Mat& bias, const Mat& res, const Mat& y, const Mat& z, void* ws, size_t ws_bytes,
+            hipStream_t s) {
+  const size_t e = element(dtype);
+  if (gr.rows == 0 || out == 0) return OZ2_OK;
+  if (in > 0 && (!good(x, e) || !good(w, e))) return OZ2_E_INVALID;
+  if ((bias.p && !good(bias, e)) || (res.p && !good(res, e)) || !good(y, e, true) ||
+      (z.p && !good(z, e, true)))
+    return OZ2_E_INVALID;
+  const bool in_place = res.p == y.p && res.ld == y.ld;
+  const Mat* outs[2] = {&y, &z};
+  for (const Mat* o : outs) {
+    if (in > 0 && (!disjoint(*o, x, e) || !disjoint(*o, w, e))) return OZ2_E_INVALID;
+    if (!disjoint(*o, bias, e)) return OZ2_E_INVALID;
+    if (!(o == &y && in_place) && !disjoint(*o, res, e)) return OZ2_E_INVALID;
+    if (gr.offsets && !disjoint_bytes(*o, e, gr.offsets, 4 * (size_t)(gr.groups + 1))) return OZ2_E_INVALID;
+  }
+  if (!disjoint(y, z, e)) return OZ2_E_INVALID;
+  const size_t need = forward_bytes(dtype, gated, gr, out, in);
+  int st = check_workspace(ws, ws_bytes, need);
+  if (st != OZ2_OK) return st;
+  for (const Mat* m : {&x, &w, &bias, &res, &y, &z})
+    if (!disjoint_bytes(*m, e, ws, need)) return OZ2_E_INVALID;
+  if ((st = oz2_device_ok()) != OZ2_OK) return st;
+  Oz2Product p{};
+  p.A = x.p;
+  p.B = w.p;
+  p.lda = x.ld;
+  p.ldb = w.ld;
+  p.M = gr.rows;
+  p.N2 = (int)(gated ? 2 * out : out);
+  p.L = (int)in;
+  p.gr = gr;
+  p.strideB = w.stride;
+  p.bias = bias.p;
+  p.stride_bias = bias.stride;
+  p.res = res.p;
+  p.ldr = res.ld;
+  p.y = const_cast<void*>(y.p);
+  p.ldy = y.ld;
+  p.z = const_cast<void*>(z.p);
+  p.ldz = z.ld;
+  p.N = (int)out;
+  p.act = act;
+  p.gated = gated ? 1 : 0;
+  p.splits = 1;
+  return hip_status(oz2_launch_product(dtype, OZ2_FWD, p, s));
+}
+
+int backward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, const Mat& dy, const Mat& x,
+             const Mat& w, const Mat& z, const Mat& dx, const Mat& dw, const Mat& db, void* ws,
+             size_t ws_bytes, hipStream_t s) {
+  const size_t e = element(dtype);
+  const ll n2 = gated ? 2 * out : out;
+  const bool sloped = act != OZ2_ACT_NONE || gated;
+  const bool want_dx = dx.p && gr.rows > 0 && in > 0, want_dw = dw.p && n2 > 0 && in > 0,
+             want_db = db.p && n2 > 0;
+  if (!want_dx && !want_dw && !want_db) return OZ2_OK;
+  const bool sums = gr.rows > 0 && out > 0;   // anything to sum
+  if (sums && (!good(dy, e) || (sloped && !good(z, e)))) return OZ2_E_INVALID;
+  if ((want_dx && (!good(dx, e, true) || (sums && !good(w, e)))) ||
+      (want_dw && (!good(dw, e, true) || (sums && !good(x, e)))) || (want_db && !good(db, e, true)))
+    return OZ2_E_INVALID;
+  const Mat* ins[4] = {&dy, sloped ? &z : nullptr, want_dx ? &w : nullptr, want_dw ? &x : nullptr};
+  const Mat* outs[3] = {want_dx ? &dx : nullptr, want_dw ? &dw : nullptr, want_db ? &db : nullptr};
+  for (int i = 0; i < 3; ++i) {
+    if (!outs[i]) continue;
+    for (const Mat* m : ins)
+      if (m && sums && !disjoint(*outs[i], *m, e)) return OZ2_E_INVALID;
+    for (int j = 0; j < i; ++j)
+      if (outs[j] && !disjoint(*outs[i], *outs[j], e)) return OZ2_E_INVALID;
+    if (gr.offsets && !disjoint_bytes(*outs[i], e, gr.offsets, 4 * (size_t)(gr.groups + 1)))
+      return OZ2_E_INVALID;
+  }
+  const BackwardLayout L = backward_layout(dtype, act, gated, gr, out);
+  int st = check_workspace(ws, ws_bytes, L.total);
+  if (st != OZ2_OK) return st;
+  for (const Mat* m : ins)
+    if (m && sums && !disjoint_bytes(*m, e, ws, L.total)) return OZ2_E_INVALID;
+  for (const Mat* m : outs)
+    if (m && !disjoint_bytes(*m, e, ws, L.total)) return OZ2_E_INVALID;
+  if ((st = oz2_device_ok()) != OZ2_OK) return st;
+  uint8_t* base = (uint8_t*)ws;
+  hipError_t err = hipSuccess;
+  const bool want_dz = sloped && (want_dx || want_dw);
+  if (want_dz || want_db) {
+    Oz2Slope q{};
+    q.dy = dy.p;
+    q.lddy = dy.ld;
+    q.z = sloped ? z.p : nullptr;
+    q.ldz = z.ld;
+    q.dz = want_dz ? base + L.dz : nullptr;
+    q.ldd = slope_pitch(n2, e);
+    q.n = (int)out;
+    q.act = act;
+    q.gated = gated ? 1 : 0;
+    q.gr = gr;
+    q.db = want_db ? const_cast<void*>(db.p) : nullptr;
+    q.stride_db = db.stride;
+    q.part = (float*)(base + L.sums);
+    if ((err = oz2_launch_slope(dtype, q, s)) != hipSuccess) return hip_status(err);
+  }
+  Oz2Product p{};
+  p.A = sloped ? base + L.dz : dy.p;
+  p.lda = sloped ? slope_pitch(n2, e) : dy.ld;
+  p.gr = gr;
+  p.splits = 1;
+  if (want_dx) {
+    Oz2Product d = p;
+    d.B = w.p;
+    d.ldb = w.ld;
+    d.strideB = w.stride;
+    d.M = gr.rows;
+    d.N2 = d.N = (int)in;
+    d.L = (int)n2;
+    d.y = const_cast<void*>(dx.p);
+    d.ldy = dx.ld;
+    if ((err = oz2_launch_product(dtype, OZ2_DGRAD, d, s)) != hipSuccess) return hip_status(err);
+  }
+  if (want_dw) {
+    Oz2Product d = p;
+    d.B = x.p;
+    d.ldb = x.ld;
+    d.M = (int)n2;
+    d.N2 = d.N = (int)in;
+    d.L = gr.rows;
+    d.y = const_cast<void*>(dw.p);
+    d.ldy = dw.ld;
+    d.strideB = dw.stride;
+    if ((err = oz2_launch_product(dtype, OZ2_WGRAD, d, s)) != hipSuccess) return hip_status(err);
+  }
+  return OZ2_OK;
+}
+
+bool tokens_ok(int dtype, int tokens, int top_k, int width) {
+  return dtype >= OZ2_F32 && dtype <= OZ2_BF16 && tokens >= 0 && top_k >= 1 && top_k <= OZ2_MAX_TOPK &&
+         width >= 0 && width <= kMaxWidth && (ll)tokens * top_k <= kMaxRows &&
+         (ll)tokens * top_k * width < kMaxElems;
+}
+bool int_ok(const void* p) { return p && (uintptr_t)p % 4 == 0; }
+
+}  // namespace
+
+extern "C" {
+
+size_t ozaki2_linear_workspace_bytes(int dtype, int gated, int rows, int out, int in) {
+  if (!sizes_ok(dtype, OZ2_ACT_NONE, rows, 1, out, in, gated)) return 0;
+  return forward_bytes(dtype, gated, Oz2Groups{nullptr, 1, rows}, out, in);
+}
+
+int ozaki2_linear(int dtype, int activation, int gated, int rows, int out, int in, const void* x, ll ldx,
+                  const void* w, ll ldw, const void* bias, const void* residual, ll ldr, void* y, ll ldy,
+                  void* z, ll ldz, void* workspace, size_t ws_bytes, void* stream) {
+  if (!sizes_ok(dtype, activation, rows, 1, out, in, gated)) return OZ2_E_INVALID;
+  const ll n2 = gated ? 2ll * out : out;
+  return forward(dtype, activation, gated, Oz2Groups{nullptr, 1, rows}, out, in, mat(x, rows, in, ldx),
+                 mat(w, n2, in, ldw), mat(bias, 1, n2, n2), mat(residual, rows, out, ldr),
+                 mat(y, rows, out, ldy), mat(z, rows, n2, ldz), workspace, ws_bytes, (hipStream_t)stream);
+}
+
+size_t ozaki2_grouped_linear_workspace_bytes(int dtype, int gated, int rows, int groups, int out, int in) {
+  if (!sizes_ok(dtype, OZ2_ACT_NONE, rows, groups, out, in, gated)) return 0;
+  static const int any = 0;
+  return forward_bytes(dtype, gated, Oz2Groups{&any, groups, rows}, out, in);
+}
+
+int ozaki2_grouped_linear(int dtype, int activation, int gated, int rows, int groups, int out, int in,
+                          const int* offsets, const void* x, ll ldx, const void* w, ll ldw, ll stride_w,
+                          const void* bias, ll stride_bias, void* y, ll ldy, void* z, ll ldz,
+                          void* workspace, size_t ws_bytes, void* stream) {
+  if (!sizes_ok(dtype, activation, rows, groups, out, in, gated) || !int_ok(offsets)) return OZ2_E_INVALID;
+  const ll n2 = gated ? 2ll * out : out;
+  return forward(dtype, activation, gated, Oz2Groups{offsets, groups, rows}, out, in,
+                 mat(x, rows, in, ldx), mat(w, n2, in, ldw, groups, stride_w),
+                 mat(bias, 1, n2, n2, groups, stride_bias), Mat{}, mat(y, rows, out, ldy),
+                 mat(z, rows, n2, ldz), workspace, ws_bytes, (hipStream_t)stream);
+}
+
+size_t ozaki2_linear_backward_workspace_bytes(int dtype, int activation, int gated, int rows, int out,
+                                              int in) {
+  if (!sizes_ok(dtype, activation, rows, 1, out, in, gated)) return 0;
+  return backward_layout(dtype, activation, gated, Oz2Groups{nullptr, 1, rows}, out).total;
+}
+
+int ozaki2_linear_backward(int dtype, int activation, int gated, int rows, int out, int in, const void* dy,
+                           ll lddy, const void* x, ll ldx, const void* w, ll ldw, const void* z, ll ldz,
+                           void* dx, ll lddx, void* dw, ll lddw, void* dbias, void* workspace,
+                           size_t ws_bytes, void* stream) {
+  if (!sizes_ok(dtype, activation, rows, 1, out, in, gated)) return OZ2_E_INVALID;
+  const ll n2 = gated ? 2ll * out : out;
+  return backward(dtype, activation, gated, Oz2Groups{nullptr, 1, rows}, out, in, mat(dy, rows, out, lddy),
+                  mat(x, rows, in, ldx), mat(w, n2, in, ldw), mat(z, rows, n2, ldz),
+                  mat(dx, rows, in, lddx), mat(dw, n2, in, lddw), mat(dbias, 1, n2, n2), workspace,
+                  ws_bytes, (hipStream_t)stream);
+}
+
+size_t ozaki2_grouped_linear_backward_workspace_bytes(int dtype, int activation, int gated, int rows,
+                                                      int groups, int out, int in) {
+  if (!sizes_ok(dtype, activation, rows, groups, out, in, gated)) return 0;
+  static const int any = 0;
+  return backward_layout(dtype, activation, gated, Oz2Groups{&any, groups, rows}, out).total;
+}
+
+int ozaki2_grouped_linear_backward(int dtype, int activation, int gated, int rows, int groups, int out,
+                                   int in, const int* offsets, const void* dy, ll lddy, const void* x,
+                                   ll ldx, const void* w, ll ldw, ll stride_w, const void* z, ll ldz,
+                                   void* dx, ll lddx, void* dw, ll lddw, ll stride_dw, void* dbias,
+                                   ll stride_dbias, void* workspace, size_t ws_bytes, void* stream) {
+  if (!sizes_ok(dtype, activation, rows, groups, out, in, gated) || !int_ok(offsets)) return OZ2_E_INVALID;
+  const ll n2 = gated ? 2ll * out : out;
+  return backward(dtype, activation, gated, Oz2Groups{offsets, groups, rows}, out, in,
+                  mat(dy, rows, out, lddy), mat(x, rows, in, ldx), mat(w, n2, in, ldw, groups, stride_w),
+                  mat(z, rows, n2, ldz), mat(dx, rows, in, lddx), mat(dw, n2, in, lddw, groups, stride_dw),
+                  mat(dbias, 1, n2, n2, groups, stride_dbias), workspace, ws_bytes, (hipStream_t)stream);
+}
+
+size_t ozaki2_expert_sort_workspace_bytes(int tokens, int top_k, int num_experts) {
+  if (!tokens_ok(OZ2_F32, tokens, top_k, 0) || num_experts < 1 || num_experts > OZ2_MAX_EXPERTS) return 0;
+  const int nb = oz2_sort_blocks((ll)tokens * top_k);
+  return nb > 1 ? align256((size_t)nb * (num_experts + 1) * 4) : 0;
+}
+
+int ozaki2_expert_sort(int tokens, int top_k, int num_experts, const void* experts, int wide_ids,
+                       ll ldexperts, int* offsets, int* rows, int* slots, void* workspace, size_t ws_bytes,
+                       void* stream) {
+  if (!tokens_ok(OZ2_F32, tokens, top_k, 0) || num_experts < 1 || num_experts > OZ2_MAX_EXPERTS)
+    return OZ2_E_INVALID;
+  const size_t ie = wide_ids ? 8 : 4;
+  const Mat ids = mat(experts, tokens, top_k, ldexperts);
+  const ll pairs = (ll)tokens * top_k;
+  const Mat o = mat(offsets, 1, num_experts + 1, num_experts + 1), r = mat(rows, 1, pairs, pairs),
+            sl = mat(slots, 1, pairs, pairs);
+  if (!good(ids, ie) || !good(o, 4) || !good(r, 4) || !good(sl, 4)) return OZ2_E_INVALID;
+  if (!disjoint(o, r, 4) || !disjoint(o, sl, 4) || !disjoint(r, sl, 4)) return OZ2_E_INVALID;
+  for (const Mat* m : {&o, &r, &sl})
+    if (!ids.empty() && !disjoint_bytes(*m, 4, ids.p, ids.span(ie))) return OZ2_E_INVALID;
+  const size_t need = ozaki2_expert_sort_workspace_bytes(tokens, top_k, num_experts);
+  int st = check_workspace(workspace, ws_bytes, need);
+  if (st != OZ2_OK) return st;
+  if ((st = oz2_device_ok()) != OZ2_OK) return st;
+  return hip_status(oz2_launch_sort(tokens, top_k, num_experts, experts, wide_ids != 0, ldexperts, offsets,
+                                    rows, slots, (int*)workspace, (hipStream_t)stream));
+}
+
+int ozaki2_expert_gather(int dtype, int tokens, int top_k, int width, const void* x, ll ldx,
+                         const int* slots, const int* kept, const float* weights, void* xs, ll ldxs,
+                         void* stream) {
+  if (!tokens_ok(dtype, tokens, top_k, width)) return OZ2_E_INVALID;
+  if (tokens == 0 || width == 0) return OZ2_OK;
+  const size_t e = element(dtype);
+  const ll pairs = (ll)tokens * top_k;
+  const Mat mx = mat(x, tokens, width, ldx), mo = mat(xs, pairs, width, ldxs);
+  if (!good(mx, e) || !good(mo, e, true) || !int_ok(slots) || !int_ok(kept) ||
+      (weights && !int_ok(weights)) || !disjoint(mx, mo, e))
+    return OZ2_E_INVALID;
+  if (!disjoint_bytes(mo, e, slots, 4 * pairs) || !disjoint_bytes(mo, e, kept, 4) ||
+      !disjoint_bytes(mo, e, weights, weights ? 4 * pairs : 0))
+    return OZ2_E_INVALID;
+  const int st = oz2_device_ok();
+  if (st != OZ2_OK) return st;
+  return hip_status(oz2_launch_gather(dtype, Oz2Tokens{tokens, top_k, width, slots, kept, weights}, x, ldx,
+                                      xs, ldxs, (hipStream_t)stream));
+}
+
+int ozaki2_expert_combine(int dtype, int tokens, int top_k, int width, const void* ys, ll ldys,
+                          const int* slots, const int* kept, const float* weights, const void* residual,
+                          ll ldr, void* y, ll ldy, void* stream) {
+  if (!tokens_ok(dtype, tokens, top_k, width)) return OZ2_E_INVALID;
+  if (tokens == 0 || width == 0) return OZ2_OK;
+  const size_t e = element(dtype);
+  const ll pairs = (ll)tokens * top_k;
+  const Mat mi = mat(ys, pairs, width, ldys), mr = mat(residual, tokens, width, ldr),
+            mo = mat(y, tokens, width, ldy);
+  if (!good(mi, e) || !good(mo, e, true) || (residual && !good(mr, e)) || !int_ok(slots) || !int_ok(kept) ||
+      (weights && !int_ok(weights)) || !disjoint(mi, mo, e))
+    return OZ2_E_INVALID;
+  if (residual && !(residual == y && ldr == ldy) && !disjoint(mr, mo, e)) return OZ2_E_INVALID;
+  if (!disjoint_bytes(mo, e, slots, 4 * pairs) || !disjoint_bytes(mo, e, kept, 4) ||
+      !disjoint_bytes(mo, e, weights, weights ? 4 * pairs : 0))
+    return OZ2_E_INVALID;
+  const int st = oz2_device_ok();
+  if (st != OZ2_OK) return st;
+  return hip_status(oz2_launch_combine(dtype, Oz2Tokens{tokens, top_k, width, slots, kept, weights}, ys,
+                                       ldys, residual, ldr, y, ldy, (hipStream_t)stream));
+}
+
+int ozaki2_expert_combine_backward(int dtype, int tokens, int top_k, int width, const void* dy, ll lddy,
+                                   const void* ys, ll ldys, const int* slots, const int* kept,
+                                   const float* weights, void* dys, ll lddys, float* dweights,
+                                   void* stream) {
+  if (!tokens_ok(dtype, tokens, top_k, width)) return OZ2_E_INVALID;
+  if (tokens == 0 || (!dys && !dweights) || (width == 0 && !dweights)) return OZ2_OK;
+  const size_t e = element(dtype);
+  const ll pairs = (ll)tokens * top_k;
+  const Mat md = mat(dy, tokens, width, lddy), mi = mat(dweights ? ys : nullptr, pairs, width, ldys),
+            mo = mat(dys, pairs, width, lddys);
+  if (!good(md, e) || (dweights && (!good(mi, e) || !int_ok(dweights))) || (dys && !good(mo, e, true)) ||
+      !int_ok(slots) || !int_ok(kept) || !int_ok(weights))
+    return OZ2_E_INVALID;
+  if (!disjoint(md, mo, e) || !disjoint(mi, mo, e)) return OZ2_E_INVALID;
+  const Mat mw = mat(dweights, 1, pairs, pairs);
+  for (const void* p : {(const void*)slots, (const void*)weights})
+    if (!disjoint_bytes(mo, e, p, 4 * pairs) || !disjoint_bytes(mw, 4, p, 4 * pairs)) return OZ2_E_INVALID;
+  if (!disjoint_bytes(mo, e, kept, 4) || !disjoint_bytes(mw, 4, kept, 4) ||
+      !disjoint_bytes(mo, e, dweights, dweights ? 4 * pairs : 0) ||
+      !disjoint_bytes(md, e, dweights, dweights ? 4 * pairs : 0) ||
+      !disjoint_bytes(mi, e, dweights, dweights ? 4 * pairs : 0))
+    return OZ2_E_INVALID;
+  const int st = oz2_device_ok();
+  if (st != OZ2_OK) return st;
+  return hip_status(oz2_launch_combine_backward(dtype,
+                                                Oz2Tokens{tokens, top_k, width, slots, kept, weights}, dy,
+                                                lddy, ys, ldys, dys, lddys, dweights, (hipStream_t)stream));
+}
+
+}  // extern "C"

@@ -131,6 +131,8 @@ struct Oz2Layout {
 // compute units of the current device (queried once per process, thread-safe;
 // 256 if the query fails)
 int oz2_device_cus();
+// OZ2_OK if the current device is a gfx950 (cached per device), else the error
+int oz2_device_ok();
 
 // The internal workspace buffers held on the current device, the current one
 // first (a diagnostic for tests; not part of the public ABI): at most max of

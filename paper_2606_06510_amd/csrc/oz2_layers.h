@@ -1,0 +1,249 @@
+// Definitions shared by the host code and the kernels of the layer operators
+// (include/ozaki2/layers.h): element types, activations, 16-byte pieces of rows,
+// the groups of rows, and the launchers.  Not part of the public ABI.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/ozaki2/layers.h"
+
+typedef long long ll;
+
+int oz2_device_cus();   // as in oz2_internal.h
+int oz2_device_ok();
+
+// Groups of rows: group g is rows [offsets[g], offsets[g+1]) of `rows`, clamped
+// so that whatever the array holds, no row index leaves [0, rows].
+// offsets null: one group of all rows.
+struct Oz2Groups {
+  const int* offsets;
+  int groups;
+  int rows;
+};
+
+// D[i][j] = sum over l < L of A(i, l) B(j, l), i < M, j < N2.
+enum Oz2Side {
+  OZ2_FWD,     // A = X, B = W: both with l contiguous; epilogue
+  OZ2_DGRAD,   // A = dZ (l contiguous), B = W (j contiguous)
+  OZ2_WGRAD    // A = dZ, B = X: i and j contiguous
+};
+
+struct Oz2Product {
+  const void *A, *B;
+  ll lda, ldb;           // elements between rows of A and B as they lie in memory
+  int M, N2, L;          // WGRAD: L = all rows, its groups give each product its own range
+  Oz2Groups gr;          // FWD, DGRAD: groups of rows i; WGRAD: of l
+  ll strideB;            // FWD, DGRAD: elements between the groups' B; WGRAD: between their D
+  const void* bias;
+  ll stride_bias;
+  const void* res;
+  ll ldr;
+  void* y;               // D, or f(..) of it in FWD: N columns
+  ll ldy;
+  void* z;
+  ll ldz;
+  int N;                 // columns of y (N2, gated N2 / 2)
+  int act, gated;
+  float* part;           // splits > 1: [split][M][N2] partial sums
+  int splits;
+};
+
+#ifdef __HIPCC__
+namespace {
+
+template <class T>
+__device__ __forceinline__ float to_f(T v) {
+  return (float)v;
+}
+template <class T>
+__device__ __forceinline__ T from_f(float v) {
+  return (T)v;   // to nearest even; fp16 overflows to infinity
+}
+
+// N elements that move as one piece, from and to any element-aligned address
+// (gfx950 serves unaligned 16-byte accesses in one instruction)
+template <class T, int N>
+struct Piece {
+  T v[N];
+};
+template <class T, int N = 16 / (int)sizeof(T)>
+__device__ __forceinline__ Piece<T, N> load_piece(const T* p, int valid) {
+  Piece<T, N> r;
+  if (valid >= N) {
+    __builtin_memcpy(&r, p, sizeof(r));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.v[i] = i < valid ? p[i] : (T)0.0f;
+  }
+  return r;
+}
+template <class T, int N>
+__device__ __forceinline__ void store_piece(T* p, const Piece<T, N>& r, int valid) {
+  if (valid >= N) {
+    __builtin_memcpy(p, &r, sizeof(r));
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < valid) p[i] = r.v[i];
+  }
+}
+
+// f(x) and f'(x).  16-bit results take the hardware's exponential (2^-21
+// relative at worst, where the result keeps 2^-11); fp32 ones the library's.
+template <class T>
+__device__ __forceinline__ float exp_for(float x) {
+  return sizeof(T) == 4 ? expf(x) : __expf(x);
+}
+// 1 / (1 + e^-x): 0 and 1 at the ends (e^-x may be infinite)
+template <class T>
+__device__ __forceinline__ float sigmoid(float x) {
+  return sizeof(T) == 4 ? 1.0f / (1.0f + expf(-x)) : __builtin_amdgcn_rcpf(1.0f + __expf(-x));
+}
+
+constexpr float kHalfRoot = 0.70710678118654752f;      // 1 / sqrt 2
+constexpr float kGauss = 0.39894228040143268f;         // 1 / sqrt(2 pi)
+constexpr float kTanh = 1.5957691216057308f;           // 2 sqrt(2 / pi)
+
+template <class T>
+__device__ __forceinline__ float act_f(float x, int act) {
+  switch (act) {
+    case OZ2_ACT_RELU:
+      return x < 0.0f ? 0.0f : x;          // NaN stays
+    case OZ2_ACT_GELU:
+      return 0.5f * x * erfcf(-x * kHalfRoot);
+    case OZ2_ACT_GELU_TANH:                // 0.5 (1 + tanh(q)) = sigmoid(2 q)
+      return x * sigmoid<T>(kTanh * (x + 0.044715f * x * x * x));
+    case OZ2_ACT_SILU:
+      return x * sigmoid<T>(x);
+    default:
+      return x;
+  }
+}
+
+// Where the bell-shaped factor of the second term has underflowed the term is 0,
+// whatever the powers of x beside it.
+template <class T>
+__device__ __forceinline__ float act_d(float x, int act) {
+  switch (act) {
+    case OZ2_ACT_RELU:
+      return x > 0.0f ? 1.0f : (x <= 0.0f ? 0.0f : x);
+    case OZ2_ACT_GELU: {
+      const float s = 0.5f * erfcf(-x * kHalfRoot), b = exp_for<T>(-0.5f * x * x);
+      return b == 0.0f ? s : s + x * kGauss * b;
+    }
+    case OZ2_ACT_GELU_TANH: {
+      const float s = sigmoid<T>(kTanh * (x + 0.044715f * x * x * x)), b = s * (1.0f - s);
+      return b == 0.0f ? s : s + x * b * kTanh * (1.0f + 0.134145f * x * x);
+    }
+    case OZ2_ACT_SILU: {
+      const float s = sigmoid<T>(x), b = s * (1.0f - s);
+      return b == 0.0f ? s : s + x * b;
+    }
+    default:
+      return 1.0f;
+  }
+}
+
+__device__ __forceinline__ int group_start(const Oz2Groups& g, int i) {
+  return min(max(g.offsets[i], 0), g.rows);
+}
+// rows [start, end) of group i
+__device__ __forceinline__ void group_range(const Oz2Groups& g, int i, int& start, int& end) {
+  if (!g.offsets) {
+    start = 0;
+    end = g.rows;
+    return;
+  }
+  start = group_start(g, i);
+  end = max(start, group_start(g, i + 1));
+}
+
+// Tile t of the row tiles (of `tile` rows) of all groups in turn: its group and
+// rows [row, end).  After them come the tiles of the rows from the last offset
+// on: group -1.  False: no such tile.  Every lane of the wave calls it; the
+// result is uniform.
+__device__ __forceinline__ bool group_tile(const Oz2Groups& g, int tile, int t, int& group, int& row,
+                                           int& end) {
+  if (!g.offsets) {
+    group = 0;
+    row = t * tile;
+    end = g.rows;
+    return row < end;
+  }
+  const int lane = threadIdx.x & 63;
+  int before = 0;
+  for (int g0 = 0; g0 < g.groups; g0 += 64) {
+    const int i = g0 + lane;
+    int s = 0, e = 0;
+    if (i < g.groups) group_range(g, i, s, e);
+    const int mine = (e - s + tile - 1) / tile;
+    int sum = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int up = __shfl_up(sum, d);
+      if (lane >= d) sum += up;
+    }
+    const unsigned long long hit = __ballot(before + sum > t);
+    if (hit) {
+      const int l = __ffsll((long long)hit) - 1;
+      group = __builtin_amdgcn_readfirstlane(g0 + l);
+      const int first = __shfl(before + sum - mine, l);
+      row = __builtin_amdgcn_readfirstlane(__shfl(s, l) + (t - first) * tile);
+      end = __builtin_amdgcn_readfirstlane(__shfl(e, l));
+      return true;
+    }
+    before += __shfl(sum, 63);
+  }
+  const int tail = group_start(g, g.groups);
+  group = -1;
+  row = __builtin_amdgcn_readfirstlane(tail + (t - before) * tile);
+  end = g.rows;
+  return row < end;
+}
+
+}  // namespace
+#endif
+
+// most row tiles of `tile` rows that groups of `rows` rows in all can make, with
+// those of the rows outside
+inline ll oz2_row_tiles(const Oz2Groups& g, int tile) {
+  return g.offsets ? (ll)g.rows / tile + g.groups + 1 : ((ll)g.rows + tile - 1) / tile;
+}
+
+// ---------------------------------------------------------------- launchers
+hipError_t oz2_launch_product(int dtype, Oz2Side side, const Oz2Product& p, hipStream_t s);
+// dZ (pitch ldd, a multiple of 64 bytes; entries beyond n2 zero) from dY and Z,
+// or nothing of it where dz is null; column sums of dZ into db where not null,
+// by way of part ([row tile][n2])
+struct Oz2Slope {
+  const void* dy;
+  ll lddy;
+  const void* z;
+  ll ldz;
+  void* dz;
+  ll ldd;
+  int n, act, gated;
+  Oz2Groups gr;
+  void* db;
+  ll stride_db;
+  float* part;
+};
+#define OZ2_SUM_ROWS 128   // rows per partial column sum
+hipError_t oz2_launch_slope(int dtype, const Oz2Slope& p, hipStream_t s);
+
+struct Oz2Tokens {
+  int tokens, top_k, width;
+  const int* slots;
+  const int* kept;
+  const float* weights;
+};
+hipError_t oz2_launch_sort(int tokens, int top_k, int E, const void* ids, bool wide, ll ld, int* offsets,
+                           int* rows, int* slots, int* counts, hipStream_t s);
+int oz2_sort_blocks(ll pairs);
+hipError_t oz2_launch_gather(int dtype, const Oz2Tokens& t, const void* x, ll ldx, void* xs, ll ldxs,
+                             hipStream_t s);
+hipError_t oz2_launch_combine(int dtype, const Oz2Tokens& t, const void* ys, ll ldys, const void* res,
+                              ll ldr, void* y, ll ldy, hipStream_t s);
+hipError_t oz2_launch_combine_backward(int dtype, const Oz2Tokens& t, const void* dy, ll lddy,
+                                       const void* ys, ll ldys, void* dys, ll lddys, float* dw,
+                                       hipStream_t s);

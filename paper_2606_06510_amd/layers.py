@@ -1,0 +1,407 @@
+"""Feed-forward layers of language models on the matrix cores (include/ozaki2/layers.h):
+dense products with bias, activation and residual in the epilogue, tokens
+in the order of their experts and back, the experts' products, and the gradients.
+
+Argument checks and marshalling only; every step runs in the library's gfx950
+kernels.  Matrices are row-major 2-D device tensors, one token per row: rows may
+be any number of elements apart, the elements of a row are adjacent.  All of a
+call's matrices have one dtype (float32, float16 or bfloat16) and one device.
+Outputs and workspaces that are not given are allocated on the stream of the call
+(``stream``, else torch's current one).
+"""
+from __future__ import annotations
+
+from typing import NamedTuple
+
+from . import _lib
+
+ACTIVATIONS = {"none": _lib.OZ2_ACT_NONE, "relu": _lib.OZ2_ACT_RELU, "gelu": _lib.OZ2_ACT_GELU,
+               "gelu_tanh": _lib.OZ2_ACT_GELU_TANH, "silu": _lib.OZ2_ACT_SILU}
+
+
+class ExpertOrder(NamedTuple):
+    """Token-expert pairs in the order of their experts (int32 device tensors).
+
+    offsets [E + 1]: expert e has places offsets[e] .. offsets[e + 1] - 1, and
+    offsets[E] pairs are kept; rows [tokens * top_k]: the pair (token * top_k +
+    choice) at each place, dropped ones last; slots [tokens, top_k]: the place
+    of each pair."""
+    offsets: "torch.Tensor"   # noqa: F821
+    rows: "torch.Tensor"      # noqa: F821
+    slots: "torch.Tensor"     # noqa: F821
+
+
+_codes = None
+
+
+def _dtype(name, t):
+    global _codes
+    import torch
+    if _codes is None:
+        _codes = {torch.float32: _lib.OZ2_F32, torch.float16: _lib.OZ2_F16,
+                  torch.bfloat16: _lib.OZ2_BF16}
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
+    try:
+        return _codes[t.dtype]
+    except KeyError:
+        raise ValueError(f"{name}: expected float32, float16 or bfloat16, got {t.dtype}") from None
+
+
+def _act(activation):
+    try:
+        return ACTIVATIONS[activation]
+    except (KeyError, TypeError):
+        raise ValueError(f"activation: expected one of {', '.join(ACTIVATIONS)}, "
+                         f"got {activation!r}") from None
+
+
+def _device(name, t):
+    if t.device.type != "cuda":
+        raise ValueError(f"{name}: expected a tensor on a CUDA device, got one on {t.device}")
+    return t.device
+
+
+def _tensor(name, t, like, shape, dtype=None):
+    """The C ABI sees pointers and sizes only: what does not match is refused here."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.dtype != (dtype or like.dtype):
+        raise ValueError(f"{name}: expected dtype {dtype or like.dtype}, got {t.dtype}")
+    if t.device != like.device:
+        raise ValueError(f"{name}: expected a tensor on {like.device}, got one on {t.device}")
+
+
+def _ld(name, t):
+    """Distance of the rows of a 2-D tensor whose rows are contiguous (a dimension
+    of size 1 carries no stride)."""
+    rows, cols = t.shape[-2:]
+    if cols > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be adjacent (stride 1)")
+    if rows <= 1:
+        return max(cols, 1)
+    ld = t.stride(-2)
+    if ld < cols:
+        raise ValueError(f"{name}: rows overlap (stride {ld} for rows of {cols})")
+    return max(ld, 1)
+
+
+def _matrix(name, t, like, shape):
+    _tensor(name, t, like, shape)
+    return _ld(name, t)
+
+
+def _stack(name, t, like, shape):
+    """Leading dimension and distance of the matrices of a 3-D tensor."""
+    _tensor(name, t, like, shape)
+    return _ld(name, t), t.stride(0) if shape[0] > 1 else 0
+
+
+def _dense(name, t, like, shape, dtype):
+    _tensor(name, t, like, shape, dtype)
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor")
+
+
+def _vectors(name, t, like, shape):
+    """Distance of the vectors (rows) of a 1-D or 2-D tensor."""
+    _tensor(name, t, like, shape)
+    if shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the elements must be adjacent (stride 1)")
+    return t.stride(0) if len(shape) == 2 and shape[0] > 1 else 0
+
+
+def _dim2(name, t, n=2):
+    if t.dim() != n:
+        raise ValueError(f"{name}: expected {n} dimensions, got shape {tuple(t.shape)}")
+    return t.shape
+
+
+def _launch(device, stream, call):
+    """call(stream handle) with ``device`` and the stream current, so that what
+    it allocates belongs to the stream that uses it."""
+    import torch
+    index = device.index
+    if stream is None:
+        if index is None or index == torch.cuda.current_device():
+            return call(torch.cuda.current_stream().cuda_stream)
+        with torch.cuda.device(device):
+            return call(torch.cuda.current_stream().cuda_stream)
+    if isinstance(stream, int):
+        stream = (torch.cuda.ExternalStream(stream, device=device) if stream
+                  else torch.cuda.default_stream(device))
+    if stream.device != device:
+        raise ValueError(f"stream: on {stream.device}, the tensors on {device}")
+    with torch.cuda.stream(stream):
+        return call(stream.cuda_stream)
+
+
+def _workspace(workspace, need, device):
+    if workspace is None:
+        if not need:
+            return None, 0
+        import torch
+        return torch.empty(need, dtype=torch.uint8, device=device), need
+    if workspace.device != device:
+        raise ValueError("workspace: on another device")
+    # the library checks its size
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+# ------------------------------------------------------------------ dense
+
+def linear(x, w, bias=None, residual=None, activation="none", gated=False,
+           save_preactivation=False, out=None, workspace=None, stream=None):
+    """f(x w^T + bias) + residual for x [T, in], w [out, in], bias [out] and
+    residual [T, out]; f is ``activation``.
+
+    gated: w has 2 out rows and bias 2 out entries, gates first, and the result
+    is f(gates) * values + residual.  save_preactivation: returns (y, z) with z =
+    x w^T + bias, rounded, as linear_backward takes it.  out may be residual
+    itself."""
+    code, act, dev = _dtype("x", x), _act(activation), _device("x", x)
+    T, K = _dim2("x", x)
+    n2 = _dim2("w", w)[0]
+    if gated and n2 % 2:
+        raise ValueError(f"w: a gated layer has an even number of rows, got {n2}")
+    N = n2 // 2 if gated else n2
+    ldx, ldw = _ld("x", x), _matrix("w", w, x, (n2, K))
+    if bias is not None:
+        _vectors("bias", bias, x, (n2,))
+    ldr = _matrix("residual", residual, x, (T, N)) if residual is not None else 0
+    if out is not None:
+        _matrix("out", out, x, (T, N))
+    need = _lib.ozaki2_linear_workspace_bytes(code, gated, T, N, K)
+
+    def call(s):
+        y = x.new_empty((T, N)) if out is None else out
+        z = x.new_empty((T, n2)) if save_preactivation else None
+        ws, nb = _workspace(workspace, need, dev)
+        _lib.ozaki2_linear(code, act, gated, T, N, K, x, ldx, w, ldw, bias, residual, ldr, y,
+                           _ld("out", y), z, n2, ws, nb, s)
+        return (y, z) if save_preactivation else y
+    return _launch(dev, stream, call)
+
+
+def linear_backward(dy, x, w, preactivation=None, activation="none", gated=False, need_dx=True,
+                    need_dw=True, need_dbias=True, dx=None, dw=None, dbias=None, workspace=None,
+                    stream=None):
+    """(dx, dw, dbias) of ``linear`` from dy [T, out] and the pre-activation
+    it saved (none without activation and gates); None for what is not needed.
+    The residual's gradient is dy itself.  dx, dw, dbias: outputs to write into."""
+    code, act, dev = _dtype("dy", dy), _act(activation), _device("dy", dy)
+    T, N = _dim2("dy", dy)
+    n2 = 2 * N if gated else N
+    K = _dim2("x", x)[1]
+    lddy, ldx, ldw = _ld("dy", dy), _matrix("x", x, dy, (T, K)), _matrix("w", w, dy, (n2, K))
+    z, ldz = _preactivation(preactivation, act, gated, dy, (T, n2))
+    for name, t, shape in (("dx", dx, (T, K)), ("dw", dw, (n2, K))):
+        if t is not None:
+            _matrix(name, t, dy, shape)
+    if dbias is not None:
+        _vectors("dbias", dbias, dy, (n2,))
+    need = _lib.ozaki2_linear_backward_workspace_bytes(code, act, gated, T, N, K)
+
+    def call(s):
+        gx = dy.new_empty((T, K)) if need_dx and dx is None else dx
+        gw = dy.new_empty((n2, K)) if need_dw and dw is None else dw
+        gb = dy.new_empty((n2,)) if need_dbias and dbias is None else dbias
+        ws, nb = _workspace(workspace, need, dev)
+        _lib.ozaki2_linear_backward(code, act, gated, T, N, K, dy, lddy, x, ldx, w, ldw, z, ldz,
+                                    gx, _ld("dx", gx) if gx is not None else 0,
+                                    gw, _ld("dw", gw) if gw is not None else 0, gb, ws, nb, s)
+        return gx, gw, gb
+    return _launch(dev, stream, call)
+
+
+def _preactivation(z, act, gated, like, shape):
+    if act == _lib.OZ2_ACT_NONE and not gated:
+        return None, 0
+    if z is None:
+        raise ValueError("preactivation: needed for the slope of the activation "
+                         "(save_preactivation of the forward call)")
+    return z, _matrix("preactivation", z, like, shape)
+
+
+# ---------------------------------------------------------------- experts
+
+def _offsets(offsets, groups, like):
+    import torch
+    _dense("offsets", offsets, like, (groups + 1,), torch.int32)
+
+
+def grouped_linear(x, w, offsets, bias=None, activation="none", gated=False,
+                   save_preactivation=False, out=None, workspace=None, stream=None):
+    """``linear`` of a group of layers: rows offsets[g] .. offsets[g + 1] - 1 of x
+    [S, in] through w[g] ([G, out, in], gated 2 out) and bias[g].  offsets is an int32
+    device tensor [G + 1]; the host never reads it.  Rows from offsets[G] on are zeros."""
+    code, act, dev = _dtype("x", x), _act(activation), _device("x", x)
+    S, K = _dim2("x", x)
+    G, n2 = _dim2("w", w, 3)[:2]
+    if gated and n2 % 2:
+        raise ValueError(f"w: a gated layer has an even number of rows, got {n2}")
+    N = n2 // 2 if gated else n2
+    ldx = _ld("x", x)
+    ldw, sw = _stack("w", w, x, (G, n2, K))
+    _offsets(offsets, G, x)
+    sb = _vectors("bias", bias, x, (G, n2)) if bias is not None else 0
+    if out is not None:
+        _matrix("out", out, x, (S, N))
+    need = _lib.ozaki2_grouped_linear_workspace_bytes(code, gated, S, G, N, K)
+
+    def call(s):
+        y = x.new_empty((S, N)) if out is None else out
+        z = x.new_empty((S, n2)) if save_preactivation else None
+        ws, nb = _workspace(workspace, need, dev)
+        _lib.ozaki2_grouped_linear(code, act, gated, S, G, N, K, offsets, x, ldx, w, ldw, sw, bias,
+                                   sb, y, _ld("out", y), z, n2, ws, nb, s)
+        return (y, z) if save_preactivation else y
+    return _launch(dev, stream, call)
+
+
+def grouped_linear_backward(dy, x, w, offsets, preactivation=None, activation="none", gated=False,
+                            need_dx=True, need_dw=True, need_dbias=True, dx=None, dw=None,
+                            dbias=None, workspace=None, stream=None):
+    """(dx, dw, dbias) of ``grouped_linear``: zeros in the rows from offsets[G] on
+    and for groups without rows."""
+    code, act, dev = _dtype("dy", dy), _act(activation), _device("dy", dy)
+    S, N = _dim2("dy", dy)
+    n2 = 2 * N if gated else N
+    K = _dim2("x", x)[1]
+    G = _dim2("w", w, 3)[0]
+    lddy, ldx = _ld("dy", dy), _matrix("x", x, dy, (S, K))
+    ldw, sw = _stack("w", w, dy, (G, n2, K))
+    _offsets(offsets, G, dy)
+    z, ldz = _preactivation(preactivation, act, gated, dy, (S, n2))
+    if dx is not None:
+        _matrix("dx", dx, dy, (S, K))
+    if dw is not None:
+        _stack("dw", dw, dy, (G, n2, K))
+    if dbias is not None:
+        _vectors("dbias", dbias, dy, (G, n2))
+    need = _lib.ozaki2_grouped_linear_backward_workspace_bytes(code, act, gated, S, G, N, K)
+
+    def call(s):
+        gx = dy.new_empty((S, K)) if need_dx and dx is None else dx
+        gw = dy.new_empty((G, n2, K)) if need_dw and dw is None else dw
+        gb = dy.new_empty((G, n2)) if need_dbias and dbias is None else dbias
+        ws, nb = _workspace(workspace, need, dev)
+        _lib.ozaki2_grouped_linear_backward(
+            code, act, gated, S, G, N, K, offsets, dy, lddy, x, ldx, w, ldw, sw, z, ldz,
+            gx, _ld("dx", gx) if gx is not None else 0,
+            gw, _ld("dw", gw) if gw is not None else 0, gw.stride(0) if gw is not None else 0,
+            gb, gb.stride(0) if gb is not None else 0, ws, nb, s)
+        return gx, gw, gb
+    return _launch(dev, stream, call)
+
+
+def expert_sort(experts, num_experts, workspace=None, stream=None):
+    """The ExpertOrder of experts [tokens, top_k] (int32 or int64): stable; a
+    value outside [0, num_experts) drops its pair."""
+    import torch
+    if not isinstance(experts, torch.Tensor):
+        raise TypeError(f"experts: expected a torch tensor, got {type(experts).__name__}")
+    if experts.dtype not in (torch.int32, torch.int64):
+        raise ValueError(f"experts: expected int32 or int64, got {experts.dtype}")
+    dev = _device("experts", experts)
+    T, k = _dim2("experts", experts)
+    ld = _ld("experts", experts)
+    if num_experts < 1 or num_experts > _lib.OZ2_MAX_EXPERTS:
+        raise ValueError(f"num_experts: expected 1 to {_lib.OZ2_MAX_EXPERTS}, got {num_experts}")
+    need = _lib.ozaki2_expert_sort_workspace_bytes(T, k, num_experts)
+
+    def call(s):
+        kw = dict(dtype=torch.int32, device=dev)
+        o = ExpertOrder(torch.empty(num_experts + 1, **kw), torch.empty(T * k, **kw),
+                        torch.empty((T, k), **kw))
+        ws, nb = _workspace(workspace, need, dev)
+        _lib.ozaki2_expert_sort(T, k, num_experts, experts, experts.dtype == torch.int64, ld,
+                                o.offsets, o.rows, o.slots, ws, nb, s)
+        return o
+    return _launch(dev, stream, call)
+
+
+def _order(order, like, tokens=None):
+    """(slots, pointer to the number of pairs kept, T, k)"""
+    import torch
+    offsets, _, slots = order
+    T, k = _dim2("order.slots", slots)
+    if tokens is not None and T != tokens:
+        raise ValueError(f"order.slots: expected {tokens} tokens, got {T}")
+    _dense("order.slots", slots, like, (T, k), torch.int32)
+    n, = _dim2("order.offsets", offsets, 1)
+    if n < 2:
+        raise ValueError("order.offsets: expected at least 2 entries")
+    _dense("order.offsets", offsets, like, (n,), torch.int32)
+    return slots, offsets.data_ptr() + 4 * (n - 1), T, k
+
+
+def _weights(weights, like, shape):
+    import torch
+    _dense("weights", weights, like, shape, torch.float32)
+    return weights
+
+
+def expert_gather(x, order, weights=None, out=None, stream=None):
+    """x[t] at the places of its pairs: [tokens * top_k, width], zeros for dropped
+    pairs; with weights (float32 [tokens, top_k]), times the pair's weight."""
+    code, dev = _dtype("x", x), _device("x", x)
+    T0, width = _dim2("x", x)
+    slots, kept, T, k = _order(order, x, T0)
+    ldx = _ld("x", x)
+    if weights is not None:
+        _weights(weights, x, (T, k))
+    if out is not None:
+        _matrix("out", out, x, (T * k, width))
+
+    def call(s):
+        xs = x.new_empty((T * k, width)) if out is None else out
+        _lib.ozaki2_expert_gather(code, T, k, width, x, ldx, slots, kept, weights, xs,
+                                  _ld("out", xs), s)
+        return xs
+    return _launch(dev, stream, call)
+
+
+def expert_combine(ys, order, weights=None, residual=None, out=None, stream=None):
+    """residual[t] + the sum over a token's pairs of weight * ys[place]: [tokens,
+    width].  Dropped pairs are left out.  Without weights it is the gradient of
+    expert_gather.  out may be residual itself."""
+    code, dev = _dtype("ys", ys), _device("ys", ys)
+    S, width = _dim2("ys", ys)
+    slots, kept, T, k = _order(order, ys)
+    ldys = _matrix("ys", ys, ys, (T * k, width))
+    if weights is not None:
+        _weights(weights, ys, (T, k))
+    ldr = _matrix("residual", residual, ys, (T, width)) if residual is not None else 0
+    if out is not None:
+        _matrix("out", out, ys, (T, width))
+
+    def call(s):
+        y = ys.new_empty((T, width)) if out is None else out
+        _lib.ozaki2_expert_combine(code, T, k, width, ys, ldys, slots, kept, weights, residual,
+                                   ldr, y, _ld("out", y), s)
+        return y
+    return _launch(dev, stream, call)
+
+
+def expert_combine_backward(dy, ys, order, weights, need_dys=True, need_dweights=True,
+                            stream=None):
+    """(dys, dweights) of ``expert_combine`` from dy [tokens, width]; zeros for
+    dropped pairs, None for what is not needed.  The residual's gradient is dy."""
+    import torch
+    code, dev = _dtype("dy", dy), _device("dy", dy)
+    T0, width = _dim2("dy", dy)
+    slots, kept, T, k = _order(order, dy, T0)
+    lddy, ldys = _ld("dy", dy), _matrix("ys", ys, dy, (T * k, width))
+    _weights(weights, dy, (T, k))
+
+    def call(s):
+        dys = dy.new_empty((T * k, width)) if need_dys else None
+        dw = torch.empty((T, k), dtype=torch.float32, device=dev) if need_dweights else None
+        _lib.ozaki2_expert_combine_backward(code, T, k, width, dy, lddy, ys, ldys, slots, kept,
+                                            weights, dys, max(width, 1), dw, s)
+        return dys, dw
+    return _launch(dev, stream, call)
