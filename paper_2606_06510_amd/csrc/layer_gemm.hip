@@ -119,6 +119,83 @@ struct Reader {
   }
 };
 
+// ------------------------------------------------------------ direct loads
+// A wave's load of 1 KiB of a stage straight into LDS (lane L's 16 bytes to m0 + 16 L).
+// Lanes whose offset is at or beyond kRecords read zeros: that is how rows, columns
+// and ends of the sum that do not exist become zeros without a branch.
+constexpr uint32_t kRecords = 0x80000000u, kNowhere = 0x80000000u;
+typedef int v4i __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ void bar() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+__device__ __forceinline__ const uint8_t* uniform(const void* p) {
+  const uint64_t a = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)a);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+  return (const uint8_t*)((uint64_t)hi << 32 | lo);
+}
+
+// (one wait state between writing m0 and the load that reads it)
+__device__ __forceinline__ void load_lds(const uint8_t* base, uint32_t voff, uint32_t m0) {
+  const uint64_t a = (uint64_t)base;
+  const v4i rsrc = {(int)(uint32_t)a, (int)(uint32_t)(a >> 32), (int)kRecords, 0x00027000};
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff),
+               "s"(rsrc), "s"(m0)
+               : "memory");
+}
+
+// One operand's stages: a wave's share is the 1 KiB blocks w, w + W, .. of the R / 16
+// blocks of a stage, W waves.
+template <class T, bool ROWS, int R, int W>
+struct Stream {
+  static constexpr int N = R / 16 / W, KE = SB / sizeof(T), P = 16 / sizeof(T);
+  const uint8_t* base;   // uniform
+  ll step;
+  uint32_t vo[N];
+  int l[N];              // the lane's first l of the stage
+  // src: the tile's first row (ROWS) or first l (else, at its first column) ; row(q)
+  // gives the offset in rows from src of LDS row q, or -1; cols: columns from there on
+  template <class F>
+  __device__ __forceinline__ void init(const T* src, ll ld, int w, int lane, F row, int cols) {
+    base = uniform(src);
+    if (ROWS) {
+      step = SB;
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        const int q = (w + W * u) * 16 + (lane >> 2), c = (lane & 3) ^ row_swz(q), at = row(q);
+        l[u] = c * P;
+        vo[u] = at < 0 ? kNowhere : (uint32_t)(at * ld * (ll)sizeof(T)) + 16u * c;
+      }
+    } else {
+      constexpr int PR = R / P;   // pieces per l
+      step = KE * ld * (ll)sizeof(T);
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        const int q = (w + W * u) * 64 + lane;
+        l[u] = q / PR;
+        const int c = col_piece<T>(l[u], q % PR);
+        vo[u] = c * P >= cols ? kNowhere : (uint32_t)(l[u] * ld * (ll)sizeof(T)) + 16u * c;
+      }
+    }
+  }
+  // the next stage, of which `left` entries of l exist, to LDS at `at` (+ the wave's blocks)
+  __device__ __forceinline__ void issue(uint32_t at, int left) {
+#pragma unroll
+    for (int u = 0; u < N; ++u)
+      load_lds(base, left >= KE || l[u] < left ? vo[u] : kNowhere, at + 1024u * W * u);
+    base += step;
+  }
+};
+
 // ------------------------------------------------------------ rows of W
 // LDS row q of a tile of B in the forward product: column block q/64 of 64
 // columns; fragment block j = (q/16)%4, row r = q%16 of it becomes accumulator
@@ -266,10 +343,8 @@ __device__ __forceinline__ void zero_rows(const Oz2Product& p, int row, int end,
   }
 }
 
-// ------------------------------------------------ 128 x 128 tiles
-// 256 threads = 4 waves, 64 x 64 outputs each; two stages in LDS, the next one in
-// registers under a stage's products.  Any size, any alignment.
-constexpr int TM = 128, NT = 256;
+// ------------------------------------------------ tiles
+constexpr int TM = 128, NT = 256;   // of the small tiles
 
 struct Tile {
   int group, row, end;   // rows of D
@@ -304,6 +379,114 @@ __device__ __forceinline__ bool tile_of(const Oz2Product& p, int tile, int ncol,
   }
   return true;
 }
+
+// Where the operands' tiles start
+template <class T, Oz2Side SIDE>
+__device__ __forceinline__ void origins(const Oz2Product& p, const Tile& t, const T*& A, const T*& B) {
+  A = (const T*)p.A;
+  B = (const T*)p.B;
+  if (SIDE == OZ2_WGRAD) {
+    A += t.l0 * p.lda;
+    B += t.l0 * p.ldb;
+  } else {
+    A += t.l0;
+    B += t.group * p.strideB + (SIDE == OZ2_FWD ? (ll)t.l0 : t.l0 * p.ldb);
+  }
+}
+
+// ------------------------------------------------ 256 x 256 tiles (16 bits)
+// 8 waves, 2 per SIMD, 128 x 64 outputs each; a ring of four 32 KiB stages, three in
+// flight.  The two waves of a SIMD run a phase apart: one reads fragments and issues
+// loads while the other's 32 products run.
+constexpr int BT = 256, BNT = 512, BNB = 4, BOP = BT * SB, BST = 2 * BOP;
+
+// this wave's share of stage s has landed (four loads a stage, returning in
+// order; issued up to stage min(s + 2, n - 1))
+__device__ __forceinline__ void big_wait(int s, int n) {
+  if (s >= n) return;
+  if (s + 2 < n) wait_vm<8>();
+  else if (s + 1 < n) wait_vm<4>();
+  else wait_vm<0>();
+}
+
+template <class T, Oz2Side SIDE>
+__global__ void __launch_bounds__(BNT, 1)
+k_product256(Oz2Product p, int ncol) {
+  constexpr bool AR = SIDE != OZ2_WGRAD, BR = SIDE == OZ2_FWD;
+  constexpr int KE = SB / sizeof(T);
+  __shared__ __attribute__((aligned(16))) uint8_t LB[BNB * BST];
+  Tile t;
+  if (!tile_of<SIDE>(p, BT, ncol, 0, t)) return;
+  if (SIDE != OZ2_WGRAD && t.group < 0) {
+    zero_rows<T>(p, t.row, t.end, t.col0, p.gated ? BT / 2 : BT, BT, BNT);
+    return;
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds8*)LB;
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = w >> 2;
+  const T *A, *B;
+  origins<T, SIDE>(p, t, A, B);
+  Stream<T, AR, BT, 8> sa;
+  Stream<T, BR, BT, 8> sb;
+  if (AR)
+    sa.init(A + t.row * p.lda, p.lda, w, lane, [&](int q) { return t.row + q < t.end ? q : -1; }, 0);
+  else
+    sa.init(A + t.row, p.lda, w, lane, [](int) { return 0; }, t.end - t.row);
+  if (BR) {
+    // rows of W counted from the tile's first column on
+    sb.init(B + t.col0 * p.ldb, p.ldb, w, lane, [&](int q) {
+      int col;
+      const int row = dealt_row(q, t.col0, p.N, p.gated != 0, col);
+      return col < p.N ? row - t.col0 : -1;
+    }, 0);
+  } else {
+    sb.init(B + t.col0, p.ldb, w, lane, [](int) { return 0; }, p.N2 - t.col0);
+  }
+  const int len = t.l1 - t.l0, n = (len + KE - 1) / KE;
+  auto issue = [&](int it) {
+    const uint32_t at = lds0 + (it & (BNB - 1)) * BST + 1024u * w;
+    sa.issue(at, len - it * KE);
+    sb.issue(at + BOP, len - it * KE);
+  };
+#pragma unroll
+  for (int it = 0; it < BNB - 1; ++it)
+    if (it < n) issue(it);
+  big_wait(0, n);
+  bar();
+  if (g) bar();
+  const int wr = w >> 2, wc = w & 3;
+  const Reader<T, AR, BT> ra(lane);
+  const Reader<T, BR, BT> rb(lane);
+  v4f acc[4][8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int it = 0; it < n; ++it) {
+    if (it + 3 < n) issue(it + 3);
+    const uint8_t* st = LB + (it & (BNB - 1)) * BST;
+    Frag<T> fa[8], fb[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) fb[j] = rb.get(st + BOP, 4 * wc + j);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) fa[i] = ra.get(st, 8 * wr + i);
+    wait_lds();
+    if (g) big_wait(it + 1, n);
+    bar();
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j][i] = mma(fb[j], fa[i], acc[j][i]);
+    if (!g) big_wait(it + 1, n);
+    bar();
+  }
+  if (!g) bar();
+  epilogue<T, SIDE, 8>(p, acc, t.group, t.row + 128 * wr, t.end, t.col0, 64 * wc, lane, t.split);
+}
+
+// ------------------------------------------------ 128 x 128 tiles, by way of registers
+// 256 threads = 4 waves, 64 x 64 outputs each; two stages in LDS, the next one in
+// registers under a stage's products.  Any size, any alignment.
 
 // One thread's two 16-byte pieces of an operand's stage, by way of registers.
 template <class T, bool ROWS>
@@ -352,15 +535,8 @@ k_product(Oz2Product p, int ncol) {
     zero_rows<T>(p, t.row, t.end, t.col0, p.gated ? TM / 2 : TM, TM, NT);
     return;
   }
-  const T* A = (const T*)p.A;
-  const T* B = (const T*)p.B;
-  if (SIDE == OZ2_WGRAD) {
-    A += t.l0 * p.lda;
-    B += t.l0 * p.ldb;
-  } else {
-    A += t.l0;
-    B += t.group * p.strideB + (BR ? (ll)t.l0 : t.l0 * p.ldb);
-  }
+  const T *A, *B;
+  origins<T, SIDE>(p, t, A, B);
   const int tid = threadIdx.x, lane = tid & 63;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wr = w >> 1, wc = w & 1;
   Loader<T, AR> la;
@@ -424,8 +600,43 @@ k_product(Oz2Product p, int ncol) {
   epilogue<T, SIDE, 4>(p, acc, t.group, t.row + 64 * wr, t.end, t.col0, 64 * wc, lane, t.split);
 }
 
+// Direct loads take rows on 16-byte boundaries, whole pieces, and offsets within a
+// stage's rows below kRecords.
+template <class T>
+bool direct_side(const void* x, ll ld, bool rows, ll extent, int tile) {
+  constexpr int P = 16 / sizeof(T);
+  return (uintptr_t)x % 16 == 0 && ld % P == 0 && extent % P == 0 &&
+         ld * (ll)sizeof(T) * (rows ? tile : SB / (ll)sizeof(T)) < (ll)kRecords - 65536;
+}
+template <class T>
+bool direct(Oz2Side side, const Oz2Product& p, int tile) {
+  constexpr int P = 16 / sizeof(T);
+  if (p.strideB % P && side != OZ2_WGRAD) return false;
+  // (gated: rows of W from a tile's gates to its values lie within N rows)
+  const ll wrows = p.gated && side == OZ2_FWD ? (ll)p.N + tile : tile;
+  const ll acols = side == OZ2_WGRAD ? p.M : p.L;
+  return direct_side<T>(p.A, p.lda, side != OZ2_WGRAD, p.padded ? 0 : acols, tile) &&
+         direct_side<T>(p.B, p.ldb, side == OZ2_FWD, side == OZ2_FWD ? p.L : p.N2, (int)wrows);
+}
+
 template <class T>
 hipError_t launch_product(Oz2Side side, const Oz2Product& p, hipStream_t s) {
+  if constexpr (sizeof(T) == 2) {
+    if (direct<T>(side, p, BT)) {
+      const int cols = p.gated && side == OZ2_FWD ? BT / 2 : BT, n = side == OZ2_FWD ? p.N : p.N2;
+      const int ncol = (n + cols - 1) / cols;
+      const ll rt = side == OZ2_WGRAD ? (p.M + BT - 1) / BT : oz2_row_tiles(p.gr, BT);
+      if (ncol == 0 || rt == 0) return hipSuccess;
+      const dim3 grid((unsigned)(rt * ncol), 1, side == OZ2_WGRAD ? p.gr.groups : 1);
+      if (side == OZ2_FWD)
+        hipLaunchKernelGGL((k_product256<T, OZ2_FWD>), grid, dim3(BNT), 0, s, p, ncol);
+      else if (side == OZ2_DGRAD)
+        hipLaunchKernelGGL((k_product256<T, OZ2_DGRAD>), grid, dim3(BNT), 0, s, p, ncol);
+      else
+        hipLaunchKernelGGL((k_product256<T, OZ2_WGRAD>), grid, dim3(BNT), 0, s, p, ncol);
+      return hipGetLastError();
+    }
+  }
   const int cols = p.gated && side == OZ2_FWD ? TM / 2 : TM, n = side == OZ2_FWD ? p.N : p.N2;
   const int ncol = (n + cols - 1) / cols;
   const ll rt = side == OZ2_WGRAD ? (p.M + TM - 1) / TM : oz2_row_tiles(p.gr, TM);

@@ -201,6 +201,7 @@ int backward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, 
   Oz2Product p{};
   p.A = sloped ? base + L.dz : dy.p;
   p.lda = sloped ? slope_pitch(n2, e) : dy.ld;
+  p.padded = sloped;
   p.gr = gr;
   p.splits = 1;
   if (want_dx) {

@@ -44,6 +44,7 @@ struct Oz2Product {
   ll ldz;
   int N;                 // columns of y (N2, gated N2 / 2)
   int act, gated;
+  bool padded;           // A's rows go on, in zeros, to a multiple of 16 bytes
   float* part;           // splits > 1: [split][M][N2] partial sums
   int splits;
 };
