@@ -13,14 +13,16 @@
 // its 16 lanes read 4 l x 16 columns and each receives one column) or as four
 // words (32 bits).
 //
-// The instruction's first operand is B, so that a lane's accumulators are
-// consecutive columns j of one row i of D.  Where B's rows are contiguous along l
-// (forward) the loader also deals them out so that the lane's 16 accumulators of
-// a 64-column block are 16 consecutive columns (gated: 8 gates and the 8 values
-// they gate): the epilogue then works in registers on whole 16-byte pieces.
+// The instruction's first operand is B, so that a lane's accumulators are four
+// consecutive columns j of one row i of D.  They leave by way of LDS, a few rows of a
+// wave's outputs at a time, so that the epilogue is a short loop over whole 16-byte
+// pieces of rows (unrolled over the accumulators it was 330 KB of code, run once a
+// tile: 30 us of instruction fetches).
 #include <algorithm>
 
 #include "oz2_layers.h"
+
+#pragma clang fp contract(fast)
 
 namespace {
 
@@ -59,6 +61,22 @@ __device__ __forceinline__ v4f mma(const Frag<float>& a, const Frag<float>& b, v
 #pragma unroll
   for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[e], b.v[e], c, 0, 0, 0);
   return c;
+}
+
+// The same with the accumulators in the accumulation registers for good: the compiler
+// moves them to and fro where they take all of that half of the register file.  It
+// sees no matrix instruction here, so the wait states before a result is read are
+// the caller's (acc_settle).
+__device__ __forceinline__ void mma_acc(const Frag<__bf16>& a, const Frag<__bf16>& b, v4f& c) {
+  asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a.v), "v"(b.v));
+}
+__device__ __forceinline__ void mma_acc(const Frag<_Float16>& a, const Frag<_Float16>& b, v4f& c) {
+  asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a.v), "v"(b.v));
+}
+__device__ __forceinline__ void acc_settle() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // ------------------------------------------------------------ LDS layouts
@@ -187,143 +205,181 @@ struct Stream {
       }
     }
   }
-  // the next stage, of which `left` entries of l exist, to LDS at `at` (+ the wave's blocks)
-  __device__ __forceinline__ void issue(uint32_t at, int left) {
-#pragma unroll
-    for (int u = 0; u < N; ++u)
-      load_lds(base, left >= KE || l[u] < left ? vo[u] : kNowhere, at + 1024u * W * u);
-    base += step;
+  // block u of the next stage, of which `left` entries of l exist, to LDS at `at` (the
+  // stage + the wave's first block); the last one moves on to the stage after it
+  __device__ __forceinline__ void issue(int u, uint32_t at, int left) {
+    load_lds(base, l[u] < left ? vo[u] : kNowhere, at + 1024u * W * u);
+    if (u == N - 1) base += step;
   }
 };
 
 // ------------------------------------------------------------ rows of W
-// LDS row q of a tile of B in the forward product: column block q/64 of 64
-// columns; fragment block j = (q/16)%4, row r = q%16 of it becomes accumulator
-// e = r%4 of lane group g = r/4, which is to be column 16 g + 4 j + e; gated:
-// column 8 g + 4 (j%2) + e of the block's 32, gates in j < 2, values in j >= 2.
-// Returns the row of W and, in col, the column of y.
-__device__ __forceinline__ int dealt_row(int q, int tile0, int N, bool gated, int& col) {
-  const int j = (q >> 4) & 3, r = q & 15;
-  if (!gated) {
-    col = tile0 + (q & ~63) + 16 * (r >> 2) + 4 * j + (r & 3);
-    return col;
+// LDS row q of a gated layer's tile of W: in blocks of 64, 32 gates and the 32 values
+// they gate.  Its row of W, and in col its column of y.
+__device__ __forceinline__ int w_row(int q, int tile0, int N, bool gated, int& col) {
+  if (!gated) return col = tile0 + q;
+  col = tile0 + (q >> 6) * 32 + (q & 31);
+  return col + ((q >> 5) & 1) * N;
+}
+
+// ------------------------------------------------ tiles
+constexpr int TM = 128, NT = 256;   // of the small tiles
+
+struct Tile {
+  int group, row, end;   // rows of D; group -1: rows of no group
+  int col0;              // first column of y
+  int l0, l1;            // range of the sum
+  int split;
+};
+
+template <Oz2Side SIDE>
+__device__ __forceinline__ bool tile_of(const Oz2Product& p, int tile, int ncol, Tile& t) {
+  const int cols = p.gated ? tile / 2 : tile;
+  const ll b = blockIdx.x;
+  int r, c;
+  t.split = 0;
+  if (SIDE == OZ2_WGRAD) {
+    const int nrow = (p.M + tile - 1) / tile;
+    const ll q = xcd_order(b, (ll)nrow * ncol);
+    if (q < 0) return false;
+    banded(q, nrow, ncol, r, c);
+    t.group = (int)blockIdx.z;
+    t.row = r * tile;
+    t.end = p.M;
+    group_range(p.gr, t.group, t.l0, t.l1);
+  } else {
+    const int nrow = group_tiles(p.gr, tile);
+    const ll n = (ll)nrow * ncol, q = xcd_order(b, n);
+    t.l0 = 0;
+    t.l1 = p.L;
+    if (q >= 0) {
+      banded(q, nrow, ncol, r, c);
+      group_tile(p.gr, tile, r, t.group, t.row, t.end);
+    } else {   // the rows outside the groups
+      const ll k = b - (n + 7) / 8 * 8;
+      if (k < 0 || !p.gr.offsets) return false;
+      c = (int)(k % ncol);
+      t.group = -1;
+      const ll row = group_start(p.gr, p.gr.groups) + k / ncol * tile;
+      if (row >= p.gr.rows) return false;
+      t.row = (int)row;
+      t.end = p.gr.rows;
+    }
   }
-  col = tile0 + ((q & ~63) >> 1) + 8 * (r >> 2) + 4 * (j & 1) + (r & 3);
-  return col + (j >> 1) * N;
+  t.col0 = c * cols;
+  return true;
 }
 
 // ------------------------------------------------------------ epilogue
-// W values of the lane's row: stores n <= valid of them at p.
 template <class T, int W>
-__device__ __forceinline__ void put(T* p, const float* v, int valid) {
-  constexpr int P = W < 16 / (int)sizeof(T) ? W : 16 / (int)sizeof(T);
+__device__ __forceinline__ void activate(float (&v)[W], int act) {
+  if (act == OZ2_ACT_RELU) {
 #pragma unroll
-  for (int c = 0; c < W; c += P) {
-    if (c >= valid) break;
-    Piece<T, P> o;
+    for (int i = 0; i < W; ++i) v[i] = act_f<T>(v[i], OZ2_ACT_RELU);
+  } else if (act == OZ2_ACT_GELU) {
 #pragma unroll
-    for (int i = 0; i < P; ++i) o.v[i] = from_f<T>(v[c + i]);
-    store_piece(p + c, o, valid - c);
+    for (int i = 0; i < W; ++i) v[i] = act_f<T>(v[i], OZ2_ACT_GELU);
+  } else if (act == OZ2_ACT_GELU_TANH) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = act_f<T>(v[i], OZ2_ACT_GELU_TANH);
+  } else if (act == OZ2_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = act_f<T>(v[i], OZ2_ACT_SILU);
   }
 }
 template <class T, int W>
-__device__ __forceinline__ void add(const T* p, float* v, int valid) {
-  constexpr int P = W < 16 / (int)sizeof(T) ? W : 16 / (int)sizeof(T);
+__device__ __forceinline__ void add_to(float (&v)[W], const T* p, int valid) {
+  const Piece<T, W> o = load_piece<T, W>(p, valid);
 #pragma unroll
-  for (int c = 0; c < W; c += P) {
-    if (c >= valid) break;
-    const Piece<T, P> o = load_piece<T, P>(p + c, valid - c);
+  for (int i = 0; i < W; ++i) v[i] += to_f(o.v[i]);
+}
+template <class T, int W>
+__device__ __forceinline__ void put(T* p, const float (&v)[W], int valid) {
+  Piece<T, W> o;
 #pragma unroll
-    for (int i = 0; i < P; ++i) v[c + i] += to_f(o.v[i]);
-  }
+  for (int i = 0; i < W; ++i) o.v[i] = from_f<T>(v[i]);
+  store_piece(p, o, valid);
 }
 
-// One row's W consecutive columns of y from column col on (valid of them exist):
-// v the pre-activations, gated: u the values.  y may be res.
+// W consecutive columns of one row of y from column col on (valid of them exist): v the
+// pre-activations, gated: u the values.  y may be res.
 template <class T, int W>
-__device__ __forceinline__ void finish(const Oz2Product& p, ll row, int col, int valid, float* v,
-                                       float* u) {
+__device__ __forceinline__ void finish(const Oz2Product& p, ll row, int col, int valid, float (&v)[W],
+                                       float (&u)[W]) {
   if (p.z) {
     T* z = (T*)p.z + row * p.ldz + col;
     put<T, W>(z, v, valid);
     if (p.gated) put<T, W>(z + p.N, u, valid);
   }
-  if (p.act != OZ2_ACT_NONE) {
-#pragma unroll
-    for (int i = 0; i < W; ++i) v[i] = act_f<T>(v[i], p.act);
-  }
+  activate<T, W>(v, p.act);
   if (p.gated) {
 #pragma unroll
     for (int i = 0; i < W; ++i) v[i] *= u[i];
   }
-  if (p.res) add<T, W>((const T*)p.res + row * p.ldr + col, v, valid);
+  if (p.res) add_to<T, W>(v, (const T*)p.res + row * p.ldr + col, valid);
   put<T, W>((T*)p.y + row * p.ldy + col, v, valid);
 }
 
-// The accumulators acc[j][i] of a wave whose first row is `row` and first LDS row
-// of B (column of D) `wn`, tile column tile0; rows end before `end`.
-template <class T, Oz2Side SIDE, int MI>
-__device__ __forceinline__ void epilogue(const Oz2Product& p, const v4f (&acc)[4][MI], int group, int row,
-                                         int end, int tile0, int wn, int lane, int split) {
-  const int r = lane & 15, g = lane >> 4;
-  if constexpr (SIDE == OZ2_FWD) {
-    const bool gated = p.gated != 0;
-    const int col = tile0 + (gated ? wn / 2 + 8 * g : wn + 16 * g);
-    const int valid = p.N - col;
-    if (valid <= 0) return;
-    float b[16];
+// Accumulators acc[j][i] of a wave: 16 MI rows from `row` on (they end before `end`),
+// LDS rows wn .. wn + 64 NB - 1 of B.  PI blocks of 16 rows at a time go through the
+// wave's own part of LDS, lw: 16 PI rows of 64 NB + 4 floats.
+template <class T, Oz2Side SIDE, int MI, int NB, int PI>
+__device__ __forceinline__ void epilogue(const Oz2Product& p, const v4f (&acc)[4 * NB][MI], float* lw,
+                                         const Tile& t, int row, int wn, int lane) {
+  constexpr int W = 16 / sizeof(T), PITCH = 64 * NB + 4;
+  const bool gated = SIDE == OZ2_FWD && p.gated;
+  const int lpr = gated ? 32 * NB / W : 64 * NB / W;   // lanes a row
+  const int lr = lane / lpr, c = lane % lpr * W;
+  const int col = t.col0 + (gated ? wn / 2 : wn) + c;
+  const int at = gated ? (c >> 5) * 64 + (c & 31) : c;   // of the (gate's) columns in lw
+  const int valid = (SIDE == OZ2_FWD ? p.N : p.N2) - col;
+  float b[W], bu[W];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) b[i] = 0.0f;
-    if (p.bias && p.splits == 1) {
-      const T* bp = (const T*)p.bias + group * p.stride_bias + col;
-      if (gated) {
-        add<T, 8>(bp, b, valid);
-        add<T, 8>(bp + p.N, b + 8, valid);
-      } else {
-        add<T, 16>(bp, b, valid);
+  for (int i = 0; i < W; ++i) b[i] = bu[i] = 0.0f;
+  if (SIDE == OZ2_FWD && p.bias && p.splits == 1 && valid > 0) {
+    const T* bp = (const T*)p.bias + t.group * p.stride_bias + col;
+    add_to<T, W>(b, bp, valid);
+    if (gated) add_to<T, W>(bu, bp + p.N, valid);
+  }
+#pragma clang loop unroll(disable)
+  for (int ps = 0; ps < MI / PI; ++ps) {
+#pragma unroll
+    for (int k = 0; k < MI / PI; ++k)
+      if (k == ps) {
+#pragma unroll
+        for (int i = 0; i < PI; ++i)
+#pragma unroll
+          for (int j = 0; j < 4 * NB; ++j)
+            *reinterpret_cast<v4f*>(lw + (16 * i + (lane & 15)) * PITCH + 16 * j + 4 * (lane >> 4)) =
+                acc[j][k * PI + i];
       }
-    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const int rows = min(16 * PI, t.end - row - 16 * PI * ps);
+    if (valid > 0) {
+#pragma clang loop unroll(disable)
+      for (int r = lr; r < rows; r += 64 / lpr) {
+        const ll tr = row + 16 * PI * ps + r;
+        const float* q = lw + r * PITCH + at;
+        float v[W], u[W];
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const int t = row + 16 * i + r;
-      if (t >= end) continue;
-      float v[16];
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[4 * j + e] = acc[j][i][e] + b[4 * j + e];
-      if (p.splits > 1) {
-        float* q = p.part + ((ll)split * p.M + t) * p.N2 + col;
-        if (gated) {
-          put<float, 8>(q, v, valid);
-          put<float, 8>(q + p.N, v + 8, valid);
-        } else {
-          put<float, 16>(q, v, valid);
+        for (int i = 0; i < W; ++i) {
+          v[i] = q[i] + b[i];
+          u[i] = gated ? q[32 + i] + bu[i] : 0.0f;
         }
-      } else if (gated) {
-        finish<T, 8>(p, t, col, valid, v, v + 8);
-      } else {
-        finish<T, 16>(p, t, col, valid, v, v);
+        if (p.splits > 1) {
+          float* d = p.part + ((ll)t.split * p.M + tr) * p.N2 + col;
+          put<float, W>(d, v, valid);
+          if (gated) put<float, W>(d + p.N, u, valid);
+        } else if (SIDE == OZ2_FWD) {
+          finish<T, W>(p, tr, col, valid, v, u);
+        } else {
+          put<T, W>((T*)p.y + (SIDE == OZ2_WGRAD ? t.group * p.strideB : 0) + tr * p.ldy + col, v, valid);
+        }
       }
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const int t = row + 16 * i + r;
-      if (t >= end) continue;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int col = tile0 + wn + 16 * j + 4 * g;
-        if (col >= p.N2) continue;
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[j][i][e];
-        if (p.splits > 1)
-          put<float, 4>(p.part + ((ll)split * p.M + t) * p.N2 + col, v, p.N2 - col);
-        else
-          put<T, 4>((T*)p.y + (SIDE == OZ2_WGRAD ? group * p.strideB : 0) + t * p.ldy + col, v, p.N2 - col);
-      }
-    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -343,43 +399,6 @@ __device__ __forceinline__ void zero_rows(const Oz2Product& p, int row, int end,
   }
 }
 
-// ------------------------------------------------ tiles
-constexpr int TM = 128, NT = 256;   // of the small tiles
-
-struct Tile {
-  int group, row, end;   // rows of D
-  int col0;              // first column of y
-  int l0, l1;            // range of the sum
-  int split;
-};
-
-template <Oz2Side SIDE>
-__device__ __forceinline__ bool tile_of(const Oz2Product& p, int tile, int ncol, int rows_t, Tile& t) {
-  const int cols = p.gated ? tile / 2 : tile;
-  t.col0 = ((int)blockIdx.x % ncol) * cols;
-  const int rt = (int)blockIdx.x / ncol;
-  if (SIDE == OZ2_WGRAD) {
-    t.group = (int)blockIdx.z;
-    t.row = rt * tile;
-    t.end = p.M;
-    group_range(p.gr, t.group, t.l0, t.l1);
-  } else {
-    if (!group_tile(p.gr, tile, rt, t.group, t.row, t.end)) return false;
-    t.l0 = 0;
-    t.l1 = p.L;
-  }
-  t.split = 0;
-  if (p.splits > 1) {   // (one group) whole stages, as even as they go
-    t.split = (int)blockIdx.y;
-    const int st = 64;
-    const ll n = (t.l1 - t.l0 + st - 1) / st;
-    const int a = (int)(n * t.split / p.splits) * st, b = (int)(n * (t.split + 1) / p.splits) * st;
-    t.l1 = min(t.l1, t.l0 + b);
-    t.l0 += a;
-  }
-  return true;
-}
-
 // Where the operands' tiles start
 template <class T, Oz2Side SIDE>
 __device__ __forceinline__ void origins(const Oz2Product& p, const Tile& t, const T*& A, const T*& B) {
@@ -395,19 +414,12 @@ __device__ __forceinline__ void origins(const Oz2Product& p, const Tile& t, cons
 }
 
 // ------------------------------------------------ 256 x 256 tiles (16 bits)
-// 8 waves, 2 per SIMD, 128 x 64 outputs each; a ring of four 32 KiB stages, three in
-// flight.  The two waves of a SIMD run a phase apart: one reads fragments and issues
-// loads while the other's 32 products run.
-constexpr int BT = 256, BNT = 512, BNB = 4, BOP = BT * SB, BST = 2 * BOP;
-
-// this wave's share of stage s has landed (four loads a stage, returning in
-// order; issued up to stage min(s + 2, n - 1))
-__device__ __forceinline__ void big_wait(int s, int n) {
-  if (s >= n) return;
-  if (s + 2 < n) wait_vm<8>();
-  else if (s + 1 < n) wait_vm<4>();
-  else wait_vm<0>();
-}
+// 4 waves, one per SIMD, 128 x 128 outputs each: 16 fragment reads feed 64
+// products.  A ring of four 32 KiB stages.  While stage `it` is multiplied, its
+// successor's fragments are read into the other set of registers and the loads of
+// stage it + 4 go out into the place of `it` (whose fragments every wave holds),
+// spread over the products; one barrier a stage.
+constexpr int BT = 256, BNT = 256, BNB = 4, BOP = BT * SB, BST = 2 * BOP;
 
 template <class T, Oz2Side SIDE>
 __global__ void __launch_bounds__(BNT, 1)
@@ -416,18 +428,18 @@ k_product256(Oz2Product p, int ncol) {
   constexpr int KE = SB / sizeof(T);
   __shared__ __attribute__((aligned(16))) uint8_t LB[BNB * BST];
   Tile t;
-  if (!tile_of<SIDE>(p, BT, ncol, 0, t)) return;
+  if (!tile_of<SIDE>(p, BT, ncol, t)) return;
   if (SIDE != OZ2_WGRAD && t.group < 0) {
     zero_rows<T>(p, t.row, t.end, t.col0, p.gated ? BT / 2 : BT, BT, BNT);
     return;
   }
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds8*)LB;
   const int lane = threadIdx.x & 63;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = w >> 2;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const T *A, *B;
   origins<T, SIDE>(p, t, A, B);
-  Stream<T, AR, BT, 8> sa;
-  Stream<T, BR, BT, 8> sb;
+  Stream<T, AR, BT, 4> sa;
+  Stream<T, BR, BT, 4> sb;
   if (AR)
     sa.init(A + t.row * p.lda, p.lda, w, lane, [&](int q) { return t.row + q < t.end ? q : -1; }, 0);
   else
@@ -436,52 +448,73 @@ k_product256(Oz2Product p, int ncol) {
     // rows of W counted from the tile's first column on
     sb.init(B + t.col0 * p.ldb, p.ldb, w, lane, [&](int q) {
       int col;
-      const int row = dealt_row(q, t.col0, p.N, p.gated != 0, col);
+      const int row = w_row(q, t.col0, p.N, p.gated != 0, col);
       return col < p.N ? row - t.col0 : -1;
     }, 0);
   } else {
     sb.init(B + t.col0, p.ldb, w, lane, [](int) { return 0; }, p.N2 - t.col0);
   }
   const int len = t.l1 - t.l0, n = (len + KE - 1) / KE;
-  auto issue = [&](int it) {
+  auto issue = [&](int u, int it) {   // u < 8: the eight loads of a wave's share
     const uint32_t at = lds0 + (it & (BNB - 1)) * BST + 1024u * w;
-    sa.issue(at, len - it * KE);
-    sb.issue(at + BOP, len - it * KE);
+    if (u < 4)
+      sa.issue(u, at, len - it * KE);
+    else
+      sb.issue(u - 4, at + BOP, len - it * KE);
   };
+  // Stages beyond the last one are loaded too, as zeros (nothing is read for them), so
+  // that the loop has no other ends: it runs over an even number of stages.
 #pragma unroll
-  for (int it = 0; it < BNB - 1; ++it)
-    if (it < n) issue(it);
-  big_wait(0, n);
-  bar();
-  if (g) bar();
-  const int wr = w >> 2, wc = w & 3;
+  for (int it = 0; it < BNB; ++it)
+#pragma unroll
+    for (int u = 0; u < 8; ++u) issue(u, it);
+  const int wr = w >> 1, wc = w & 1;
   const Reader<T, AR, BT> ra(lane);
   const Reader<T, BR, BT> rb(lane);
-  v4f acc[4][8];
+  v4f acc[8][8];
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
+  for (int j = 0; j < 8; ++j)
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int it = 0; it < n; ++it) {
-    if (it + 3 < n) issue(it + 3);
-    const uint8_t* st = LB + (it & (BNB - 1)) * BST;
-    Frag<T> fa[8], fb[4];
+  Frag<T> fa[2][8], fb[2][8];
+  wait_vm<24>();
+  bar();
 #pragma unroll
-    for (int j = 0; j < 4; ++j) fb[j] = rb.get(st + BOP, 4 * wc + j);
+  for (int j = 0; j < 8; ++j) fb[0][j] = rb.get(LB + BOP, 8 * wc + j);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) fa[i] = ra.get(st, 8 * wr + i);
-    wait_lds();
-    if (g) big_wait(it + 1, n);
-    bar();
+  for (int i = 0; i < 8; ++i) fa[0][i] = ra.get(LB, 8 * wr + i);
+  for (int it0 = 0; it0 < n; it0 += 2) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int S = 0; S < 2; ++S) {
+      const int it = it0 + S;
+      // this wave's share of stage it + 1 has landed, and all waves hold stage it's
+      // fragments
+      wait_lds();
+      wait_vm<16>();
+      bar();
+      const uint8_t* st = LB + ((it + 1) & (BNB - 1)) * BST;
+      // a read or a load between two products, never more: the next product is issued
+      // before the matrix unit has done with the last
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[j][i] = mma(fb[j], fa[i], acc[j][i]);
-    if (!g) big_wait(it + 1, n);
-    bar();
+      for (int m = 0; m < 64; ++m) {
+        mma_acc(fb[S][m & 7], fa[S][m >> 3], acc[m & 7][m >> 3]);
+        if (m % 3 == 0 && m < 48) {
+          const int k = m / 3;
+          if (k < 8)
+            fb[1 - S][k] = rb.get(st + BOP, 8 * wc + k);
+          else
+            fa[1 - S][k - 8] = ra.get(st, 8 * wr + k - 8);
+        }
+        if (m % 8 == 4) issue(m / 8, it + 4);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
   }
-  if (!g) bar();
-  epilogue<T, SIDE, 8>(p, acc, t.group, t.row + 128 * wr, t.end, t.col0, 64 * wc, lane, t.split);
+  wait_vm<0>();
+  acc_settle();
+  __syncthreads();
+  epilogue<T, SIDE, 8, 2, 2>(p, acc, reinterpret_cast<float*>(LB) + w * 32 * 132, t, t.row + 128 * wr,
+                             128 * wc, lane);
 }
 
 // ------------------------------------------------ 128 x 128 tiles, by way of registers
@@ -530,7 +563,7 @@ k_product(Oz2Product p, int ncol) {
   constexpr int KE = SB / sizeof(T), OP = TM * SB;
   __shared__ __attribute__((aligned(16))) uint8_t LB[2][2 * OP];
   Tile t;
-  if (!tile_of<SIDE>(p, TM, ncol, 0, t)) return;
+  if (!tile_of<SIDE>(p, TM, ncol, t)) return;
   if (SIDE != OZ2_WGRAD && t.group < 0) {
     zero_rows<T>(p, t.row, t.end, t.col0, p.gated ? TM / 2 : TM, TM, NT);
     return;
@@ -552,7 +585,7 @@ k_product(Oz2Product p, int ncol) {
     }
     if (BR) {
       int col;
-      const int row = dealt_row(q >> 2, t.col0, p.N, p.gated != 0, col);
+      const int row = w_row(q >> 2, t.col0, p.N, p.gated != 0, col);
       lb.init(B, p.ldb, q, u, row, col < p.N, 0);
     } else {
       lb.init(B + t.col0, p.ldb, q, u, 0, true, p.N2 - t.col0);
@@ -597,7 +630,9 @@ k_product(Oz2Product p, int ncol) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[j][i] = mma(fb[j], fa[i], acc[j][i]);
   }
-  epilogue<T, SIDE, 4>(p, acc, t.group, t.row + 64 * wr, t.end, t.col0, 64 * wc, lane, t.split);
+  __syncthreads();
+  epilogue<T, SIDE, 4, 1, 1>(p, acc, reinterpret_cast<float*>(LB) + w * 16 * 68, t, t.row + 64 * wr, 64 * wc,
+                             lane);
 }
 
 // Direct loads take rows on 16-byte boundaries, whole pieces, and offsets within a
@@ -619,37 +654,38 @@ bool direct(Oz2Side side, const Oz2Product& p, int tile) {
          direct_side<T>(p.B, p.ldb, side == OZ2_FWD, side == OZ2_FWD ? p.L : p.N2, (int)wrows);
 }
 
+#define OZ2_SIDES(kern, grid, threads)                                                  \
+  do {                                                                                  \
+    if (side == OZ2_FWD)                                                                \
+      hipLaunchKernelGGL((kern<T, OZ2_FWD>), grid, dim3(threads), 0, s, p, ncol);       \
+    else if (side == OZ2_DGRAD)                                                         \
+      hipLaunchKernelGGL((kern<T, OZ2_DGRAD>), grid, dim3(threads), 0, s, p, ncol);     \
+    else                                                                                \
+      hipLaunchKernelGGL((kern<T, OZ2_WGRAD>), grid, dim3(threads), 0, s, p, ncol);     \
+    return hipGetLastError();                                                           \
+  } while (0)
+
+// columns of tiles and the grid of a product in `tile` x `tile` tiles
+dim3 tile_grid(Oz2Side side, const Oz2Product& p, int tile, int& ncol) {
+  const int cols = p.gated && side == OZ2_FWD ? tile / 2 : tile, n = side == OZ2_FWD ? p.N : p.N2;
+  ncol = (n + cols - 1) / cols;
+  if (side == OZ2_WGRAD)
+    return dim3((unsigned)(((ll)((p.M + tile - 1) / tile) * ncol + 7) / 8 * 8), 1, p.gr.groups);
+  return dim3((unsigned)oz2_tile_blocks(p.gr, tile, ncol));
+}
+
 template <class T>
 hipError_t launch_product(Oz2Side side, const Oz2Product& p, hipStream_t s) {
+  int ncol;
+  if (p.M == 0 || p.N2 == 0) return hipSuccess;
   if constexpr (sizeof(T) == 2) {
     if (direct<T>(side, p, BT)) {
-      const int cols = p.gated && side == OZ2_FWD ? BT / 2 : BT, n = side == OZ2_FWD ? p.N : p.N2;
-      const int ncol = (n + cols - 1) / cols;
-      const ll rt = side == OZ2_WGRAD ? (p.M + BT - 1) / BT : oz2_row_tiles(p.gr, BT);
-      if (ncol == 0 || rt == 0) return hipSuccess;
-      const dim3 grid((unsigned)(rt * ncol), 1, side == OZ2_WGRAD ? p.gr.groups : 1);
-      if (side == OZ2_FWD)
-        hipLaunchKernelGGL((k_product256<T, OZ2_FWD>), grid, dim3(BNT), 0, s, p, ncol);
-      else if (side == OZ2_DGRAD)
-        hipLaunchKernelGGL((k_product256<T, OZ2_DGRAD>), grid, dim3(BNT), 0, s, p, ncol);
-      else
-        hipLaunchKernelGGL((k_product256<T, OZ2_WGRAD>), grid, dim3(BNT), 0, s, p, ncol);
-      return hipGetLastError();
+      const dim3 grid = tile_grid(side, p, BT, ncol);
+      OZ2_SIDES(k_product256, grid, BNT);
     }
   }
-  const int cols = p.gated && side == OZ2_FWD ? TM / 2 : TM, n = side == OZ2_FWD ? p.N : p.N2;
-  const int ncol = (n + cols - 1) / cols;
-  const ll rt = side == OZ2_WGRAD ? (p.M + TM - 1) / TM : oz2_row_tiles(p.gr, TM);
-  if (ncol == 0 || rt == 0) return hipSuccess;
-  if (rt * ncol >= (1ll << 31)) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)(rt * ncol), 1, side == OZ2_WGRAD ? p.gr.groups : 1);
-  if (side == OZ2_FWD)
-    hipLaunchKernelGGL((k_product<T, OZ2_FWD>), grid, dim3(NT), 0, s, p, ncol);
-  else if (side == OZ2_DGRAD)
-    hipLaunchKernelGGL((k_product<T, OZ2_DGRAD>), grid, dim3(NT), 0, s, p, ncol);
-  else
-    hipLaunchKernelGGL((k_product<T, OZ2_WGRAD>), grid, dim3(NT), 0, s, p, ncol);
-  return hipGetLastError();
+  const dim3 grid = tile_grid(side, p, TM, ncol);
+  OZ2_SIDES(k_product, grid, NT);
 }
 
 // ------------------------------------------------ slope: dZ and its column sums
@@ -661,9 +697,9 @@ __global__ void __launch_bounds__(256)
 k_slope(Oz2Slope p) {
   constexpr int P = 16 / sizeof(T);
   __shared__ float red[8][32 * 2 * P];
+  if ((int)blockIdx.x >= group_tiles(p.gr, OZ2_SUM_ROWS)) return;
   int group, row, end;
-  const bool tail_out = !group_tile(p.gr, OZ2_SUM_ROWS, (int)blockIdx.x, group, row, end);
-  if (tail_out || group < 0) return;   // dZ outside the groups is never read
+  group_tile(p.gr, OZ2_SUM_ROWS, (int)blockIdx.x, group, row, end);
   end = min(end, row + OZ2_SUM_ROWS);
   const int c = ((int)blockIdx.y * 32 + (int)(threadIdx.x & 31)) * P, rr = threadIdx.x >> 5;
   const int n2 = p.gated ? 2 * p.n : p.n, valid = p.n - c;

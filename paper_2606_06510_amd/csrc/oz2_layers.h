@@ -50,6 +50,8 @@ struct Oz2Product {
 };
 
 #ifdef __HIPCC__
+// products and sums of the epilogues may be fused; nothing here is compared bit for bit
+#pragma clang fp contract(fast)
 namespace {
 
 template <class T>
@@ -105,13 +107,31 @@ constexpr float kHalfRoot = 0.70710678118654752f;      // 1 / sqrt 2
 constexpr float kGauss = 0.39894228040143268f;         // 1 / sqrt(2 pi)
 constexpr float kTanh = 1.5957691216057308f;           // 2 sqrt(2 / pi)
 
+// Phi(x), the normal distribution, and in *bell e^(-x^2/2).  16 bits: Abramowitz and
+// Stegun's 7.1.26, erfc(q) = e^(-q^2) (a1 t + .. + a5 t^5), t = 1 / (1 + 0.3275911 q), q
+// >= 0, good to 1.5e-7, which shares its exponential with the slope and takes a
+// quarter of the library's erfc (the slope of 4096^2 bf16 entries: 58 us with that).
+template <class T>
+__device__ __forceinline__ float gauss_tail(float x, float* bell) {
+  if (sizeof(T) == 4) {
+    if (bell) *bell = expf(-0.5f * x * x);
+    return 0.5f * erfcf(-x * kHalfRoot);
+  }
+  const float q = fabsf(x) * kHalfRoot, e = __expf(-0.5f * x * x);
+  const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * q);
+  const float half = 0.5f * e * t *
+      (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+  if (bell) *bell = e;
+  return x > 0.0f ? 1.0f - half : half;
+}
+
 template <class T>
 __device__ __forceinline__ float act_f(float x, int act) {
   switch (act) {
     case OZ2_ACT_RELU:
       return x < 0.0f ? 0.0f : x;          // NaN stays
     case OZ2_ACT_GELU:
-      return 0.5f * x * erfcf(-x * kHalfRoot);
+      return x * gauss_tail<T>(x, nullptr);
     case OZ2_ACT_GELU_TANH:                // 0.5 (1 + tanh(q)) = sigmoid(2 q)
       return x * sigmoid<T>(kTanh * (x + 0.044715f * x * x * x));
     case OZ2_ACT_SILU:
@@ -129,7 +149,8 @@ __device__ __forceinline__ float act_d(float x, int act) {
     case OZ2_ACT_RELU:
       return x > 0.0f ? 1.0f : (x <= 0.0f ? 0.0f : x);
     case OZ2_ACT_GELU: {
-      const float s = 0.5f * erfcf(-x * kHalfRoot), b = exp_for<T>(-0.5f * x * x);
+      float b;
+      const float s = gauss_tail<T>(x, &b);
       return b == 0.0f ? s : s + x * kGauss * b;
     }
     case OZ2_ACT_GELU_TANH: {
@@ -159,18 +180,29 @@ __device__ __forceinline__ void group_range(const Oz2Groups& g, int i, int& star
   end = max(start, group_start(g, i + 1));
 }
 
-// Tile t of the row tiles (of `tile` rows) of all groups in turn: its group and
-// rows [row, end).  After them come the tiles of the rows from the last offset
-// on: group -1.  False: no such tile.  Every lane of the wave calls it; the
-// result is uniform.
-__device__ __forceinline__ bool group_tile(const Oz2Groups& g, int tile, int t, int& group, int& row,
-                                           int& end) {
-  if (!g.offsets) {
-    group = 0;
-    row = t * tile;
-    end = g.rows;
-    return row < end;
+// Row tiles of `tile` rows that the groups have.  Every lane of the wave calls it;
+// the result is uniform.
+__device__ __forceinline__ int group_tiles(const Oz2Groups& g, int tile) {
+  if (!g.offsets) return (int)(((ll)g.rows + tile - 1) / tile);
+  int n = 0;
+  for (int i = threadIdx.x & 63; i < g.groups; i += 64) {
+    int s, e;
+    group_range(g, i, s, e);
+    n += (e - s + tile - 1) / tile;
   }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d);
+  return __builtin_amdgcn_readfirstlane(n);
+}
+
+// Tile t < group_tiles() of the row tiles of all groups in turn: its group and
+// rows [row, end).  Likewise uniform.
+__device__ __forceinline__ void group_tile(const Oz2Groups& g, int tile, int t, int& group, int& row,
+                                           int& end) {
+  group = 0;
+  row = t * tile;
+  end = g.rows;
+  if (!g.offsets) return;
   const int lane = threadIdx.x & 63;
   int before = 0;
   for (int g0 = 0; g0 < g.groups; g0 += 64) {
@@ -191,15 +223,27 @@ __device__ __forceinline__ bool group_tile(const Oz2Groups& g, int tile, int t, 
       const int first = __shfl(before + sum - mine, l);
       row = __builtin_amdgcn_readfirstlane(__shfl(s, l) + (t - first) * tile);
       end = __builtin_amdgcn_readfirstlane(__shfl(e, l));
-      return true;
+      return;
     }
     before += __shfl(sum, 63);
   }
-  const int tail = group_start(g, g.groups);
-  group = -1;
-  row = __builtin_amdgcn_readfirstlane(tail + (t - before) * tile);
-  end = g.rows;
-  return row < end;
+}
+
+// Workgroup b's place in an order of n items in which each XCD (workgroups go
+// round-robin over the eight of them, each with an L2 of its own) has a contiguous
+// eighth.  -1 where it has none; items take 8 ceil(n / 8) workgroups.
+__device__ __forceinline__ ll xcd_order(ll b, ll n) {
+  const ll per = (n + 7) >> 3, p = (b & 7) * per + (b >> 3);
+  return (b >> 3) < per && p < n ? p : -1;
+}
+
+// Tile p of nrow x ncol tiles in bands of four rows of tiles, a band column by
+// column: 32 workgroups that run together (an XCD's) share 4 panels of A and 8 of B.
+__device__ __forceinline__ void banded(ll p, int nrow, int ncol, int& r, int& c) {
+  const ll band = p / (4ll * ncol);
+  const int in = (int)(p - band * 4 * ncol), h = min(4, nrow - (int)band * 4);
+  c = in / h;
+  r = (int)band * 4 + in - c * h;
 }
 
 }  // namespace
@@ -209,6 +253,10 @@ __device__ __forceinline__ bool group_tile(const Oz2Groups& g, int tile, int t, 
 // those of the rows outside
 inline ll oz2_row_tiles(const Oz2Groups& g, int tile) {
   return g.offsets ? (ll)g.rows / tile + g.groups + 1 : ((ll)g.rows + tile - 1) / tile;
+}
+// workgroups for them and ncol tiles across
+inline ll oz2_tile_blocks(const Oz2Groups& g, int tile, int ncol) {
+  return (oz2_row_tiles(g, tile) * ncol + 7) / 8 * 8 + 8;
 }
 
 // ---------------------------------------------------------------- launchers
