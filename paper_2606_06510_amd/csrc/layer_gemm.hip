@@ -4,10 +4,10 @@
 // contiguous along j) and of W (A = dZ contiguous along i, B = X along j), each
 // for one product or for groups of rows.
 //
-// A stage is 64 bytes of l (32 entries of 16 bits, 16 of 32) for all rows of the
-// workgroup's tiles, in LDS in the layout of its source, read as 16-byte
-// fragments: lane (r = L%16, g = L/16) of a block of 16 rows holds row r and l =
-// 8 g .. 8 g + 7 (16 bits) or 4 g .. 4 g + 3 (32 bits) of the stage, which is one
+// A step is 64 bytes of l (32 entries of 16 bits, 16 of 32), a stage one step or two,
+// for all rows of the workgroup's tiles, in LDS in the layout of its source, read as
+// 16-byte fragments: lane (r = L%16, g = L/16) of a block of 16 rows holds row r and
+// l = 8 g .. 8 g + 7 (16 bits) or 4 g .. 4 g + 3 (32 bits) of the step, which is one
 // 16x16x32 instruction or four 16x16x4 ones.  Rows contiguous along l give a
 // fragment as one read; the others through the transposing LDS read (16 bits:
 // its 16 lanes read 4 l x 16 columns and each receives one column) or as four
@@ -33,7 +33,7 @@ typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) uint8_t lds8;
 typedef __attribute__((address_space(3))) v4s lds_v4s;
 
-constexpr int SB = 64;   // bytes of l in a stage
+constexpr int SB = 64, SB2 = 128;   // bytes of l in a stage of the small and of the large tiles
 
 // 16 bytes of operand
 template <class T>
@@ -80,10 +80,13 @@ __device__ __forceinline__ void acc_settle() {
 }
 
 // ------------------------------------------------------------ LDS layouts
-// Rows contiguous along l: [row][64 B], the row's four 16-byte pieces rotated so
-// that the pieces a read serves together (rows 0-3, 12-15 of one piece and 4-11 of the
-// next) lie in different banks.
-__device__ __forceinline__ int row_swz(int r) { return (-(r >> 2)) & 3; }
+// Rows contiguous along l: [row][64 or 128 B], the row's 16-byte pieces permuted by
+// an exclusive or so that the pieces a read serves together (rows 0-3, 12-15 of one
+// piece and 4-11 of the next) lie in different banks.
+template <int BYTES>
+__device__ __forceinline__ int row_swz(int r) {
+  return BYTES == 64 ? (-(r >> 2)) & 3 : (r >> 1) & 7;
+}
 
 // Rows contiguous along the tile's other dimension: [l][R entries], R = 128 or
 // 256, the 16-byte pieces of row l permuted so that the rows read together lie in
@@ -98,15 +101,16 @@ __device__ __forceinline__ int col_piece(int l, int piece) {
   return piece ^ (col_swz<T>(l) * (sizeof(T) == 2 ? 2 : 4));
 }
 
-// The fragment of block b (16 rows) of a tile of R rows at LDS address `base`.
-template <class T, bool ROWS, int R>
+// The fragment of block b (16 rows) and step h of a stage of BYTES bytes of l of a tile
+// of R rows at LDS address `base`.
+template <class T, bool ROWS, int R, int BYTES>
 struct Reader {
   uint32_t at;   // lane's address within block 0
   int sw;        // !ROWS: the lane's block permutation
   __device__ __forceinline__ Reader(int lane) {
     const int r = lane & 15, g = lane >> 4;
     if (ROWS) {
-      at = (uint32_t)(r * SB + 16 * (g ^ row_swz(r)));
+      at = (uint32_t)(r * BYTES + 16 * (g ^ row_swz<BYTES>(r)));
       sw = 0;
     } else if (sizeof(T) == 2) {
       const int l = 8 * g + (r >> 2);   // and + 4 in the second read
@@ -117,12 +121,12 @@ struct Reader {
       at = (uint32_t)(4 * g * R * 4 + 4 * r);
     }
   }
-  __device__ __forceinline__ Frag<T> get(const uint8_t* base, int b) const {
+  __device__ __forceinline__ Frag<T> get(const uint8_t* base, int b, int h = 0) const {
     Frag<T> f;
     if constexpr (ROWS) {
-      f.v = *reinterpret_cast<const decltype(f.v)*>(base + at + b * 16 * SB);
+      f.v = *reinterpret_cast<const decltype(f.v)*>(base + (at ^ 64u * h) + b * 16 * BYTES);
     } else if constexpr (sizeof(T) == 2) {
-      const uint8_t* p = base + at + ((b ^ sw) << 5);
+      const uint8_t* p = base + at + ((b ^ sw) << 5) + h * 32 * R * 2;
       typedef short v8s __attribute__((ext_vector_type(8)));
       const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p));
       const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + 4 * R * 2));
@@ -171,11 +175,11 @@ __device__ __forceinline__ void load_lds(const uint8_t* base, uint32_t voff, uin
                : "memory");
 }
 
-// One operand's stages: a wave's share is the 1 KiB blocks w, w + W, .. of the R / 16
-// blocks of a stage, W waves.
-template <class T, bool ROWS, int R, int W>
+// One operand's stages: a wave's share is the 1 KiB blocks w, w + W, .. of a stage, W
+// waves.
+template <class T, bool ROWS, int R, int W, int BYTES>
 struct Stream {
-  static constexpr int N = R / 16 / W, KE = SB / sizeof(T), P = 16 / sizeof(T);
+  static constexpr int N = R * BYTES / 1024 / W, KE = BYTES / sizeof(T), P = 16 / sizeof(T);
   const uint8_t* base;   // uniform
   ll step;
   uint32_t vo[N];
@@ -186,10 +190,12 @@ struct Stream {
   __device__ __forceinline__ void init(const T* src, ll ld, int w, int lane, F row, int cols) {
     base = uniform(src);
     if (ROWS) {
-      step = SB;
+      constexpr int PR = BYTES / 16;   // pieces per row
+      step = BYTES;
 #pragma unroll
       for (int u = 0; u < N; ++u) {
-        const int q = (w + W * u) * 16 + (lane >> 2), c = (lane & 3) ^ row_swz(q), at = row(q);
+        const int q = (w + W * u) * (64 / PR) + lane / PR, at = row(q);
+        const int c = (lane % PR) ^ row_swz<BYTES>(q);
         l[u] = c * P;
         vo[u] = at < 0 ? kNowhere : (uint32_t)(at * ld * (ll)sizeof(T)) + 16u * c;
       }
@@ -287,60 +293,114 @@ __device__ __forceinline__ void activate(float (&v)[W], int act) {
     for (int i = 0; i < W; ++i) v[i] = act_f<T>(v[i], OZ2_ACT_SILU);
   }
 }
-template <class T, int W>
-__device__ __forceinline__ void add_to(float (&v)[W], const T* p, int valid) {
-  const Piece<T, W> o = load_piece<T, W>(p, valid);
-#pragma unroll
-  for (int i = 0; i < W; ++i) v[i] += to_f(o.v[i]);
-}
-template <class T, int W>
-__device__ __forceinline__ void put(T* p, const float (&v)[W], int valid) {
+
+// W entries at p, all of them there (ALL) or `valid`
+template <class T, int W, bool ALL>
+__device__ __forceinline__ void put(T* p, const float* v, int valid) {
   Piece<T, W> o;
 #pragma unroll
   for (int i = 0; i < W; ++i) o.v[i] = from_f<T>(v[i]);
-  store_piece(p, o, valid);
+  store_piece(p, o, ALL ? W : valid);
 }
-
-// W consecutive columns of one row of y from column col on (valid of them exist): v the
-// pre-activations, gated: u the values.  y may be res.
-template <class T, int W>
-__device__ __forceinline__ void finish(const Oz2Product& p, ll row, int col, int valid, float (&v)[W],
-                                       float (&u)[W]) {
-  if (p.z) {
-    T* z = (T*)p.z + row * p.ldz + col;
-    put<T, W>(z, v, valid);
-    if (p.gated) put<T, W>(z + p.N, u, valid);
-  }
-  activate<T, W>(v, p.act);
-  if (p.gated) {
+template <class T, int W, bool ALL>
+__device__ __forceinline__ void add_to(float* v, const T* p, int valid) {
+  const Piece<T, W> o = load_piece<T, W>(p, ALL ? W : valid);
 #pragma unroll
-    for (int i = 0; i < W; ++i) v[i] *= u[i];
-  }
-  if (p.res) add_to<T, W>(v, (const T*)p.res + row * p.ldr + col, valid);
-  put<T, W>((T*)p.y + row * p.ldy + col, v, valid);
+  for (int i = 0; i < W; ++i) v[i] += to_f(o.v[i]);
 }
 
-// Accumulators acc[j][i] of a wave: 16 MI rows from `row` on (they end before `end`),
+// `steps` rows of a lane from `row` on, STRIDE apart (those before `end`): W columns
+// from col on, read from lw (PITCH floats a row), U rows in flight.  y may be res.
+template <class T, Oz2Side SIDE, bool GATED, bool ALL, int W, int STRIDE, int STEPS, int PITCH>
+__device__ __forceinline__ void emit(const Oz2Product& p, const Tile& t, const float* lw, int row, int col,
+                                     int valid, const float* b, const float* bu) {
+  constexpr int U = STEPS < 4 ? STEPS : 4;
+#pragma clang loop unroll(disable)
+  for (int s = 0; s < STEPS; s += U) {
+    if (row + s * STRIDE >= t.end) return;
+    float v[U * W], u[GATED ? U * W : 1];
+    Piece<T, W> r[U];
+#pragma unroll
+    for (int q = 0; q < U; ++q) {
+      const int at = row + (s + q) * STRIDE;
+      if (SIDE == OZ2_FWD && p.res && at < t.end)
+        r[q] = load_piece<T, W>((const T*)p.res + at * p.ldr + col, ALL ? W : valid);
+#pragma unroll
+      for (int i = 0; i < W; i += 4) {
+        const v4f x = *reinterpret_cast<const v4f*>(lw + (s + q) * STRIDE * PITCH + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[q * W + i + e] = SIDE == OZ2_FWD ? x[e] + b[i + e] : x[e];
+        if (GATED) {
+          const v4f y = *reinterpret_cast<const v4f*>(lw + (s + q) * STRIDE * PITCH + 32 + i);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) u[q * W + i + e] = y[e] + bu[i + e];
+        }
+      }
+    }
+    if (p.splits > 1) {
+#pragma unroll
+      for (int q = 0; q < U; ++q) {
+        const int at = row + (s + q) * STRIDE;
+        if (at >= t.end) continue;
+        float* d = p.part + ((ll)t.split * p.M + at) * p.N2 + col;
+        put<float, W, ALL>(d, v + q * W, valid);
+        if (GATED) put<float, W, ALL>(d + p.N, u + q * W, valid);
+      }
+      continue;
+    }
+    if (SIDE == OZ2_FWD) {
+      if (p.z) {
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+          const int at = row + (s + q) * STRIDE;
+          if (at >= t.end) continue;
+          T* z = (T*)p.z + at * p.ldz + col;
+          put<T, W, ALL>(z, v + q * W, valid);
+          if (GATED) put<T, W, ALL>(z + p.N, u + q * W, valid);
+        }
+      }
+      activate<T, U * W>(v, p.act);
+      if (GATED) {
+#pragma unroll
+        for (int i = 0; i < U * W; ++i) v[i] *= u[i];
+      }
+      if (p.res) {
+#pragma unroll
+        for (int i = 0; i < U * W; ++i) v[i] += to_f(r[i / W].v[i % W]);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < U; ++q) {
+      const int at = row + (s + q) * STRIDE;
+      if (at >= t.end) continue;
+      put<T, W, ALL>((T*)p.y + (SIDE == OZ2_WGRAD ? t.group * p.strideB : 0) + at * p.ldy + col, v + q * W,
+                     valid);
+    }
+  }
+}
+
+// Accumulators acc[j][i] of a wave: 16 MI rows from `row` on (they end before t.end),
 // LDS rows wn .. wn + 64 NB - 1 of B.  PI blocks of 16 rows at a time go through the
 // wave's own part of LDS, lw: 16 PI rows of 64 NB + 4 floats.
-template <class T, Oz2Side SIDE, int MI, int NB, int PI>
-__device__ __forceinline__ void epilogue(const Oz2Product& p, const v4f (&acc)[4 * NB][MI], float* lw,
-                                         const Tile& t, int row, int wn, int lane) {
+template <class T, Oz2Side SIDE, bool GATED, int MI, int NB, int PI>
+__device__ __forceinline__ void epilogue_of(const Oz2Product& p, const v4f (&acc)[4 * NB][MI], float* lw,
+                                            const Tile& t, int row, int wn, int lane) {
   constexpr int W = 16 / sizeof(T), PITCH = 64 * NB + 4;
-  const bool gated = SIDE == OZ2_FWD && p.gated;
-  const int lpr = gated ? 32 * NB / W : 64 * NB / W;   // lanes a row
-  const int lr = lane / lpr, c = lane % lpr * W;
-  const int col = t.col0 + (gated ? wn / 2 : wn) + c;
-  const int at = gated ? (c >> 5) * 64 + (c & 31) : c;   // of the (gate's) columns in lw
+  constexpr int LPR = (GATED ? 32 : 64) * NB / W;   // lanes a row
+  constexpr int STRIDE = 64 / LPR, STEPS = 16 * PI / STRIDE;
+  const int lr = lane / LPR, c = lane % LPR * W;
+  const int col = t.col0 + (GATED ? wn / 2 : wn) + c;
+  const int at = GATED ? (c >> 5) * 64 + (c & 31) : c;   // of the (gate's) columns in lw
   const int valid = (SIDE == OZ2_FWD ? p.N : p.N2) - col;
   float b[W], bu[W];
 #pragma unroll
   for (int i = 0; i < W; ++i) b[i] = bu[i] = 0.0f;
   if (SIDE == OZ2_FWD && p.bias && p.splits == 1 && valid > 0) {
     const T* bp = (const T*)p.bias + t.group * p.stride_bias + col;
-    add_to<T, W>(b, bp, valid);
-    if (gated) add_to<T, W>(bu, bp + p.N, valid);
+    add_to<T, W, false>(b, bp, valid);
+    if (GATED) add_to<T, W, false>(bu, bp + p.N, valid);
   }
+  float* lq = lw + (lane & 15) * PITCH + 4 * (lane >> 4);
 #pragma clang loop unroll(disable)
   for (int ps = 0; ps < MI / PI; ++ps) {
 #pragma unroll
@@ -350,37 +410,28 @@ __device__ __forceinline__ void epilogue(const Oz2Product& p, const v4f (&acc)[4
         for (int i = 0; i < PI; ++i)
 #pragma unroll
           for (int j = 0; j < 4 * NB; ++j)
-            *reinterpret_cast<v4f*>(lw + (16 * i + (lane & 15)) * PITCH + 16 * j + 4 * (lane >> 4)) =
-                acc[j][k * PI + i];
+            *reinterpret_cast<v4f*>(lq + 16 * i * PITCH + 16 * j) = acc[j][k * PI + i];
       }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    const int rows = min(16 * PI, t.end - row - 16 * PI * ps);
-    if (valid > 0) {
-#pragma clang loop unroll(disable)
-      for (int r = lr; r < rows; r += 64 / lpr) {
-        const ll tr = row + 16 * PI * ps + r;
-        const float* q = lw + r * PITCH + at;
-        float v[W], u[W];
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-          v[i] = q[i] + b[i];
-          u[i] = gated ? q[32 + i] + bu[i] : 0.0f;
-        }
-        if (p.splits > 1) {
-          float* d = p.part + ((ll)t.split * p.M + tr) * p.N2 + col;
-          put<float, W>(d, v, valid);
-          if (gated) put<float, W>(d + p.N, u, valid);
-        } else if (SIDE == OZ2_FWD) {
-          finish<T, W>(p, tr, col, valid, v, u);
-        } else {
-          put<T, W>((T*)p.y + (SIDE == OZ2_WGRAD ? t.group * p.strideB : 0) + tr * p.ldy + col, v, valid);
-        }
-      }
-    }
+    const int r0 = row + 16 * PI * ps + lr;
+    const float* lr0 = lw + lr * PITCH + at;
+    if (valid >= W)
+      emit<T, SIDE, GATED, true, W, STRIDE, STEPS, PITCH>(p, t, lr0, r0, col, W, b, bu);
+    else if (valid > 0)
+      emit<T, SIDE, GATED, false, W, STRIDE, STEPS, PITCH>(p, t, lr0, r0, col, valid, b, bu);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
+}
+
+template <class T, Oz2Side SIDE, int MI, int NB, int PI>
+__device__ __forceinline__ void epilogue(const Oz2Product& p, const v4f (&acc)[4 * NB][MI], float* lw,
+                                         const Tile& t, int row, int wn, int lane) {
+  if (SIDE == OZ2_FWD && p.gated)
+    epilogue_of<T, SIDE, true, MI, NB, PI>(p, acc, lw, t, row, wn, lane);
+  else
+    epilogue_of<T, SIDE, false, MI, NB, PI>(p, acc, lw, t, row, wn, lane);
 }
 
 // rows [row, row + tile) below end of y (and z) are zeros: columns col .. col + n
@@ -414,19 +465,21 @@ __device__ __forceinline__ void origins(const Oz2Product& p, const Tile& t, cons
 }
 
 // ------------------------------------------------ 256 x 256 tiles (16 bits)
-// 4 waves, one per SIMD, 128 x 128 outputs each: 16 fragment reads feed 64
-// products.  A ring of four 32 KiB stages.  While stage `it` is multiplied, its
-// successor's fragments are read into the other set of registers and the loads of
-// stage it + 4 go out into the place of `it` (whose fragments every wave holds),
-// spread over the products; one barrier a stage.
-constexpr int BT = 256, BNT = 256, BNB = 4, BOP = BT * SB, BST = 2 * BOP;
+// 4 waves, one per SIMD, 128 x 128 outputs each: 16 fragment reads feed the 64 products
+// of a step.  Stages of two steps, 64 KiB (whole 128-byte lines of rows that are
+// contiguous along l; stages of half of that took 0.84 us a step against 0.65 of
+// operands that read whole lines anyway), two of them in LDS.  While a step is
+// multiplied, the next one's fragments are read into the other set of registers; once
+// every wave holds a stage's last fragments, the loads of the stage after the next go
+// out into its place.  One barrier a stage.
+constexpr int BT = 256, BNT = 256, BOP = BT * SB2, BST = 2 * BOP;
 
 template <class T, Oz2Side SIDE>
 __global__ void __launch_bounds__(BNT, 1)
 k_product256(Oz2Product p, int ncol) {
   constexpr bool AR = SIDE != OZ2_WGRAD, BR = SIDE == OZ2_FWD;
-  constexpr int KE = SB / sizeof(T);
-  __shared__ __attribute__((aligned(16))) uint8_t LB[BNB * BST];
+  constexpr int KE = SB2 / sizeof(T);
+  __shared__ __attribute__((aligned(16))) uint8_t LB[2 * BST];
   Tile t;
   if (!tile_of<SIDE>(p, BT, ncol, t)) return;
   if (SIDE != OZ2_WGRAD && t.group < 0) {
@@ -438,8 +491,8 @@ k_product256(Oz2Product p, int ncol) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const T *A, *B;
   origins<T, SIDE>(p, t, A, B);
-  Stream<T, AR, BT, 4> sa;
-  Stream<T, BR, BT, 4> sb;
+  Stream<T, AR, BT, 4, SB2> sa;
+  Stream<T, BR, BT, 4, SB2> sb;
   if (AR)
     sa.init(A + t.row * p.lda, p.lda, w, lane, [&](int q) { return t.row + q < t.end ? q : -1; }, 0);
   else
@@ -455,57 +508,54 @@ k_product256(Oz2Product p, int ncol) {
     sb.init(B + t.col0, p.ldb, w, lane, [](int) { return 0; }, p.N2 - t.col0);
   }
   const int len = t.l1 - t.l0, n = (len + KE - 1) / KE;
-  auto issue = [&](int u, int it) {   // u < 8: the eight loads of a wave's share
-    const uint32_t at = lds0 + (it & (BNB - 1)) * BST + 1024u * w;
-    if (u < 4)
-      sa.issue(u, at, len - it * KE);
+  auto issue = [&](int u, int it) {   // u < 16: the loads of a wave's share of stage it
+    const uint32_t at = lds0 + (it & 1) * BST + 1024u * w;
+    if (u & 1)
+      sa.issue(u >> 1, at, len - it * KE);
     else
-      sb.issue(u - 4, at + BOP, len - it * KE);
+      sb.issue(u >> 1, at + BOP, len - it * KE);
   };
-  // Stages beyond the last one are loaded too, as zeros (nothing is read for them), so
-  // that the loop has no other ends: it runs over an even number of stages.
+  // stages beyond the last one are loaded too, as zeros (nothing is read for them)
 #pragma unroll
-  for (int it = 0; it < BNB; ++it)
-#pragma unroll
-    for (int u = 0; u < 8; ++u) issue(u, it);
+  for (int u = 0; u < 32; ++u) issue(u & 15, u >> 4);
   const int wr = w >> 1, wc = w & 1;
-  const Reader<T, AR, BT> ra(lane);
-  const Reader<T, BR, BT> rb(lane);
+  const Reader<T, AR, BT, SB2> ra(lane);
+  const Reader<T, BR, BT, SB2> rb(lane);
   v4f acc[8][8];
 #pragma unroll
   for (int j = 0; j < 8; ++j)
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  Frag<T> fa[2][8], fb[2][8];
-  wait_vm<24>();
+  Frag<T> fa[2][8], fb[2][8];   // of the two steps of a stage
+  wait_vm<16>();
   bar();
 #pragma unroll
   for (int j = 0; j < 8; ++j) fb[0][j] = rb.get(LB + BOP, 8 * wc + j);
 #pragma unroll
   for (int i = 0; i < 8; ++i) fa[0][i] = ra.get(LB, 8 * wr + i);
-  for (int it0 = 0; it0 < n; it0 += 2) {
+  for (int it = 0; it < n; ++it) {
 #pragma unroll
-    for (int S = 0; S < 2; ++S) {
-      const int it = it0 + S;
-      // this wave's share of stage it + 1 has landed, and all waves hold stage it's
-      // fragments
+    for (int h = 0; h < 2; ++h) {
       wait_lds();
-      wait_vm<16>();
-      bar();
-      const uint8_t* st = LB + ((it + 1) & (BNB - 1)) * BST;
-      // a read or a load between two products, never more: the next product is issued
-      // before the matrix unit has done with the last
+      if (h) {
+        // all waves hold the last fragments of stage it, and stage it + 1 has landed
+        wait_vm<0>();
+        bar();
+      }
+      const uint8_t* st = LB + ((it + h) & 1) * BST;
+      // a read or a load between two products, hardly ever more: the next product is
+      // issued before the matrix unit has done with the last
 #pragma unroll
       for (int m = 0; m < 64; ++m) {
-        mma_acc(fb[S][m & 7], fa[S][m >> 3], acc[m & 7][m >> 3]);
+        mma_acc(fb[h][m & 7], fa[h][m >> 3], acc[m & 7][m >> 3]);
         if (m % 3 == 0 && m < 48) {
           const int k = m / 3;
           if (k < 8)
-            fb[1 - S][k] = rb.get(st + BOP, 8 * wc + k);
+            fb[1 - h][k] = rb.get(st + BOP, 8 * wc + k, 1 - h);
           else
-            fa[1 - S][k - 8] = ra.get(st, 8 * wr + k - 8);
+            fa[1 - h][k - 8] = ra.get(st, 8 * wr + k - 8, 1 - h);
         }
-        if (m % 8 == 4) issue(m / 8, it + 4);
+        if (h && m % 3 == 1 && m < 48) issue(m / 3, it + 2);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -537,7 +587,7 @@ struct Loader {
       src[u] = base + (ll)row * ld + c * P;
       valid[u] = exists;
       l[u] = c * P;
-      dst[u] = (uint32_t)((q >> 2) * SB + 16 * (c ^ row_swz(q >> 2)));
+      dst[u] = (uint32_t)((q >> 2) * SB + 16 * (c ^ row_swz<SB>(q >> 2)));
       step = KE;
     } else {
       constexpr int PR = TM / P;   // pieces per l
@@ -596,8 +646,8 @@ k_product(Oz2Product p, int ncol) {
   for (int j = 0; j < 4; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  const Reader<T, AR, TM> ra(lane);
-  const Reader<T, BR, TM> rb(lane);
+  const Reader<T, AR, TM, SB> ra(lane);
+  const Reader<T, BR, TM, SB> rb(lane);
   const int len = t.l1 - t.l0, n = (len + KE - 1) / KE;
   Piece<T, 16 / sizeof(T)> pa[2], pb[2];
   auto fetch = [&](int it) {
