@@ -4,7 +4,7 @@
 // contiguous along j) and of W (A = dZ contiguous along i, B = X along j), each
 // for one product or for groups of rows.
 //
-// A step is 64 bytes of l (32 entries of 16 bits, 16 of 32), a stage one step or two,
+// A step is 64 bytes of l (32 entries of 16 bits, 16 of 32), a stage two steps,
 // for all rows of the workgroup's tiles, in LDS in the layout of its source, read as
 // 16-byte fragments: lane (r = L%16, g = L/16) of a block of 16 rows holds row r and
 // l = 8 g .. 8 g + 7 (16 bits) or 4 g .. 4 g + 3 (32 bits) of the step, which is one
@@ -33,7 +33,7 @@ typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) uint8_t lds8;
 typedef __attribute__((address_space(3))) v4s lds_v4s;
 
-constexpr int SB = 64, SB2 = 128;   // bytes of l in a stage of the small and of the large tiles
+constexpr int SB2 = 128;   // bytes of l in a stage
 
 // 16 bytes of operand
 template <class T>
@@ -80,13 +80,10 @@ __device__ __forceinline__ void acc_settle() {
 }
 
 // ------------------------------------------------------------ LDS layouts
-// Rows contiguous along l: [row][64 or 128 B], the row's 16-byte pieces permuted by
-// an exclusive or so that the pieces a read serves together (rows 0-3, 12-15 of one
+// Rows contiguous along l: [row][128 B], the row's 16-byte pieces permuted by an
+// exclusive or so that the pieces a read serves together (rows 0-3, 12-15 of one
 // piece and 4-11 of the next) lie in different banks.
-template <int BYTES>
-__device__ __forceinline__ int row_swz(int r) {
-  return BYTES == 64 ? (-(r >> 2)) & 3 : (r >> 1) & 7;
-}
+__device__ __forceinline__ int row_swz(int r) { return (r >> 1) & 7; }
 
 // Rows contiguous along the tile's other dimension: [l][R entries], R = 128 or
 // 256, the 16-byte pieces of row l permuted so that the rows read together lie in
@@ -101,16 +98,15 @@ __device__ __forceinline__ int col_piece(int l, int piece) {
   return piece ^ (col_swz<T>(l) * (sizeof(T) == 2 ? 2 : 4));
 }
 
-// The fragment of block b (16 rows) and step h of a stage of BYTES bytes of l of a tile
-// of R rows at LDS address `base`.
-template <class T, bool ROWS, int R, int BYTES>
+// The fragment of block b (16 rows) and step h of a stage of a tile of R rows at LDS address `base`.
+template <class T, bool ROWS, int R>
 struct Reader {
   uint32_t at;   // lane's address within block 0
   int sw;        // !ROWS: the lane's block permutation
   __device__ __forceinline__ Reader(int lane) {
     const int r = lane & 15, g = lane >> 4;
     if (ROWS) {
-      at = (uint32_t)(r * BYTES + 16 * (g ^ row_swz<BYTES>(r)));
+      at = (uint32_t)(r * SB2 + 16 * (g ^ row_swz(r)));
       sw = 0;
     } else if (sizeof(T) == 2) {
       const int l = 8 * g + (r >> 2);   // and + 4 in the second read
@@ -124,16 +120,16 @@ struct Reader {
   __device__ __forceinline__ Frag<T> get(const uint8_t* base, int b, int h = 0) const {
     Frag<T> f;
     if constexpr (ROWS) {
-      f.v = *reinterpret_cast<const decltype(f.v)*>(base + (at ^ 64u * h) + b * 16 * BYTES);
+      f.v = *reinterpret_cast<const decltype(f.v)*>(base + (at ^ 64u * h) + b * 16 * SB2);
     } else if constexpr (sizeof(T) == 2) {
-      const uint8_t* p = base + at + ((b ^ sw) << 5) + h * 32 * R * 2;
+      const uint8_t* p = base + at + ((b ^ sw) << 5) + h * 64 * R;
       typedef short v8s __attribute__((ext_vector_type(8)));
       const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p));
       const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s*)(p + 4 * R * 2));
       const v8s both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       f.v = __builtin_bit_cast(decltype(f.v), both);
     } else {
-      const uint8_t* p = base + at + ((b ^ sw) << 6);
+      const uint8_t* p = base + at + ((b ^ sw) << 6) + h * 64 * R;
 #pragma unroll
       for (int e = 0; e < 4; ++e) f.v[e] = *reinterpret_cast<const float*>(p + e * R * 4);
     }
@@ -177,11 +173,12 @@ __device__ __forceinline__ void load_lds(const uint8_t* base, uint32_t voff, uin
 
 // One operand's stages: a wave's share is the 1 KiB blocks w, w + W, .. of a stage, W
 // waves.
-template <class T, bool ROWS, int R, int W, int BYTES>
+template <class T, bool ROWS, int R, int W>
 struct Stream {
-  static constexpr int N = R * BYTES / 1024 / W, KE = BYTES / sizeof(T), P = 16 / sizeof(T);
+  static constexpr int N = R * SB2 / 1024 / W, KE = SB2 / sizeof(T), P = 16 / sizeof(T);
   const uint8_t* base;   // uniform
   ll step;
+  ll alt;                // gated: from the gates' rows to the values', those of odd u
   uint32_t vo[N];
   int l[N];              // the lane's first l of the stage
   // src: the tile's first row (ROWS) or first l (else, at its first column) ; row(q)
@@ -189,13 +186,14 @@ struct Stream {
   template <class F>
   __device__ __forceinline__ void init(const T* src, ll ld, int w, int lane, F row, int cols) {
     base = uniform(src);
+    alt = 0;
     if (ROWS) {
-      constexpr int PR = BYTES / 16;   // pieces per row
-      step = BYTES;
+      constexpr int PR = SB2 / 16;   // pieces per row
+      step = SB2;
 #pragma unroll
       for (int u = 0; u < N; ++u) {
         const int q = (w + W * u) * (64 / PR) + lane / PR, at = row(q);
-        const int c = (lane % PR) ^ row_swz<BYTES>(q);
+        const int c = (lane % PR) ^ row_swz(q);
         l[u] = c * P;
         vo[u] = at < 0 ? kNowhere : (uint32_t)(at * ld * (ll)sizeof(T)) + 16u * c;
       }
@@ -214,18 +212,17 @@ struct Stream {
   // block u of the next stage, of which `left` entries of l exist, to LDS at `at` (the
   // stage + the wave's first block); the last one moves on to the stage after it
   __device__ __forceinline__ void issue(int u, uint32_t at, int left) {
-    load_lds(base, l[u] < left ? vo[u] : kNowhere, at + 1024u * W * u);
+    load_lds(ROWS && (u & 1) ? base + alt : base, l[u] < left ? vo[u] : kNowhere, at + 1024u * W * u);
     if (u == N - 1) base += step;
   }
 };
 
 // ------------------------------------------------------------ rows of W
-// LDS row q of a gated layer's tile of W: in blocks of 64, 32 gates and the 32 values
-// they gate.  Its row of W, and in col its column of y.
-__device__ __forceinline__ int w_row(int q, int tile0, int N, bool gated, int& col) {
-  if (!gated) return col = tile0 + q;
-  col = tile0 + (q >> 6) * 32 + (q & 31);
-  return col + ((q >> 5) & 1) * N;
+// The column of y (from the tile's first on) of LDS row q of a tile of W; gated: in
+// blocks of 64 rows, 32 gates and the 32 values they gate (8 rows a load, so a wave's
+// loads are of gates and of values in turn).
+__device__ __forceinline__ int w_col(int q, bool gated) {
+  return gated ? (q >> 6) * 32 + (q & 31) : q;
 }
 
 // ------------------------------------------------ tiles
@@ -273,6 +270,13 @@ __device__ __forceinline__ bool tile_of(const Oz2Product& p, int tile, int ncol,
     }
   }
   t.col0 = c * cols;
+  if (p.splits > 1) {   // (one group) whole stages, as even as they go
+    const int st = SB2 / (p.esize), n = (t.l1 - t.l0 + st - 1) / st;
+    t.split = (int)blockIdx.y;
+    const int a = (int)((ll)n * t.split / p.splits), e = (int)((ll)n * (t.split + 1) / p.splits);
+    t.l1 = min(t.l1, t.l0 + e * st);
+    t.l0 += a * st;
+  }
   return true;
 }
 
@@ -464,6 +468,25 @@ __device__ __forceinline__ void origins(const Oz2Product& p, const Tile& t, cons
   }
 }
 
+template <class T, Oz2Side SIDE, int R, class SA, class SBT>
+__device__ __forceinline__ void streams(const Oz2Product& p, const Tile& t, int w, int lane, SA& sa, SBT& sb) {
+  const T *A, *B;
+  origins<T, SIDE>(p, t, A, B);
+  if (SIDE != OZ2_WGRAD)
+    sa.init(A + t.row * p.lda, p.lda, w, lane, [&](int q) { return t.row + q < t.end ? q : -1; }, 0);
+  else
+    sa.init(A + t.row, p.lda, w, lane, [](int) { return 0; }, t.end - t.row);
+  if (SIDE == OZ2_FWD) {
+    sb.init(B + t.col0 * p.ldb, p.ldb, w, lane, [&](int q) {
+      const int c = w_col(q, p.gated != 0);
+      return t.col0 + c < p.N ? c : -1;
+    }, 0);
+    if (p.gated) sb.alt = p.N * p.ldb * (ll)sizeof(T);
+  } else {
+    sb.init(B + t.col0, p.ldb, w, lane, [](int) { return 0; }, p.N2 - t.col0);
+  }
+}
+
 // ------------------------------------------------ 256 x 256 tiles (16 bits)
 // 4 waves, one per SIMD, 128 x 128 outputs each: 16 fragment reads feed the 64 products
 // of a step.  Stages of two steps, 64 KiB (whole 128-byte lines of rows that are
@@ -489,24 +512,9 @@ k_product256(Oz2Product p, int ncol) {
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds8*)LB;
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const T *A, *B;
-  origins<T, SIDE>(p, t, A, B);
-  Stream<T, AR, BT, 4, SB2> sa;
-  Stream<T, BR, BT, 4, SB2> sb;
-  if (AR)
-    sa.init(A + t.row * p.lda, p.lda, w, lane, [&](int q) { return t.row + q < t.end ? q : -1; }, 0);
-  else
-    sa.init(A + t.row, p.lda, w, lane, [](int) { return 0; }, t.end - t.row);
-  if (BR) {
-    // rows of W counted from the tile's first column on
-    sb.init(B + t.col0 * p.ldb, p.ldb, w, lane, [&](int q) {
-      int col;
-      const int row = w_row(q, t.col0, p.N, p.gated != 0, col);
-      return col < p.N ? row - t.col0 : -1;
-    }, 0);
-  } else {
-    sb.init(B + t.col0, p.ldb, w, lane, [](int) { return 0; }, p.N2 - t.col0);
-  }
+  Stream<T, AR, BT, 4> sa;
+  Stream<T, BR, BT, 4> sb;
+  streams<T, SIDE, BT>(p, t, w, lane, sa, sb);
   const int len = t.l1 - t.l0, n = (len + KE - 1) / KE;
   auto issue = [&](int u, int it) {   // u < 16: the loads of a wave's share of stage it
     const uint32_t at = lds0 + (it & 1) * BST + 1024u * w;
@@ -519,8 +527,8 @@ k_product256(Oz2Product p, int ncol) {
 #pragma unroll
   for (int u = 0; u < 32; ++u) issue(u & 15, u >> 4);
   const int wr = w >> 1, wc = w & 1;
-  const Reader<T, AR, BT, SB2> ra(lane);
-  const Reader<T, BR, BT, SB2> rb(lane);
+  const Reader<T, AR, BT> ra(lane);
+  const Reader<T, BR, BT> rb(lane);
   v4f acc[8][8];
 #pragma unroll
   for (int j = 0; j < 8; ++j)
@@ -567,42 +575,124 @@ k_product256(Oz2Product p, int ncol) {
                              128 * wc, lane);
 }
 
-// ------------------------------------------------ 128 x 128 tiles, by way of registers
-// 256 threads = 4 waves, 64 x 64 outputs each; two stages in LDS, the next one in
-// registers under a stage's products.  Any size, any alignment.
+// ------------------------------------------------ 128 x 128 tiles
+// For products with few large tiles, and all of fp32.  4 waves, 64 x 64 outputs each;
+// two 32 KiB stages of 128 bytes of l, so that two workgroups of a CU cover each
+// other's waits.
+constexpr int DOP = TM * SB2, DST = 2 * DOP;
 
-// One thread's two 16-byte pieces of an operand's stage, by way of registers.
+template <class T, Oz2Side SIDE>
+__global__ void __launch_bounds__(NT, 2)
+k_product128(Oz2Product p, int ncol) {
+  constexpr bool AR = SIDE != OZ2_WGRAD, BR = SIDE == OZ2_FWD;
+  constexpr int KE = SB2 / sizeof(T);
+  __shared__ __attribute__((aligned(16))) uint8_t LB[2 * DST];
+  Tile t;
+  if (!tile_of<SIDE>(p, TM, ncol, t)) return;
+  if (SIDE != OZ2_WGRAD && t.group < 0) {
+    zero_rows<T>(p, t.row, t.end, t.col0, p.gated ? TM / 2 : TM, TM, NT);
+    return;
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds8*)LB;
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = w >> 1, wc = w & 1;
+  Stream<T, AR, TM, 4> sa;
+  Stream<T, BR, TM, 4> sb;
+  streams<T, SIDE, TM>(p, t, w, lane, sa, sb);
+  const int len = t.l1 - t.l0, n = (len + KE - 1) / KE;
+  auto issue = [&](int it) {
+    const uint32_t at = lds0 + (it & 1) * DST + 1024u * w;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) sa.issue(u, at, len - it * KE);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) sb.issue(u, at + DOP, len - it * KE);
+  };
+  issue(0);   // (stages beyond the last are loaded as zeros)
+  issue(1);
+  const Reader<T, AR, TM> ra(lane);
+  const Reader<T, BR, TM> rb(lane);
+  v4f acc[4][4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int it = 0; it < n; ++it) {
+    const uint8_t* st = LB + (it & 1) * DST;
+    Frag<T> fa[2][4], fb[2][4];
+    wait_vm<8>();
+    bar();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) fb[h][j] = rb.get(st + DOP, 4 * wc + j, h);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) fa[h][i] = ra.get(st, 4 * wr + i, h);
+    }
+    wait_lds();
+    bar();
+    issue(it + 2);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j][i] = mma(fb[h][j], fa[h][i], acc[j][i]);
+  }
+  wait_vm<0>();
+  __syncthreads();
+  epilogue<T, SIDE, 4, 1, 1>(p, acc, reinterpret_cast<float*>(LB) + w * 16 * 68, t, t.row + 64 * wr, 64 * wc,
+                             lane);
+}
+
+// ------------------------------------------------ 128 x 128 tiles, by way of registers
+// The same for operands that direct loads do not take: rows of any length from any
+// address.  A stage waits in LDS, the next two on their way in registers.
+
+// A thread's four 16-byte pieces of an operand's stage
 template <class T, bool ROWS>
 struct Loader {
-  static constexpr int P = 16 / sizeof(T), KE = SB / sizeof(T);
-  const T* src[2];
-  int valid[2];          // ROWS: the row exists; else entries of the piece that exist
-  int l[2];              // ROWS: first l of the piece; else its l
-  uint32_t dst[2];
+  static constexpr int P = 16 / sizeof(T), KE = SB2 / sizeof(T), N = 4;
+  typedef Piece<T, P> Set[N];
+  const T* src[N];
+  int valid[N];          // ROWS: the row exists; else entries of the piece that exist
+  int l[N];              // ROWS: first l of the piece; else its l
+  uint32_t dst[N];
   ll step;
-  __device__ __forceinline__ void init(const T* base, ll ld, int q, int u, int row, bool exists,
-                                       int nvalid) {
-    if (ROWS) {
-      const int c = q & 3;
-      src[u] = base + (ll)row * ld + c * P;
-      valid[u] = exists;
-      l[u] = c * P;
-      dst[u] = (uint32_t)((q >> 2) * SB + 16 * (c ^ row_swz<SB>(q >> 2)));
-      step = KE;
-    } else {
-      constexpr int PR = TM / P;   // pieces per l
-      const int k = q / PR, c = q % PR;
-      src[u] = base + k * ld + c * P;
-      valid[u] = nvalid - c * P;
-      l[u] = k;
-      dst[u] = (uint32_t)(k * TM * sizeof(T) + 16 * col_piece<T>(k, c));
-      step = KE * ld;
+  template <class F>
+  __device__ __forceinline__ void init(const T* base, ll ld, int tid, F row, int cols) {
+    step = ROWS ? KE : KE * ld;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int q = tid + NT * u;
+      if (ROWS) {
+        const int c = q & 7;
+        const ll at = row(q >> 3);
+        src[u] = base + at * ld + c * P;
+        valid[u] = at >= 0;
+        l[u] = c * P;
+        dst[u] = (uint32_t)((q >> 3) * SB2 + 16 * (c ^ row_swz(q >> 3)));
+      } else {
+        constexpr int PR = TM / P;   // pieces per l
+        l[u] = q / PR;
+        const int c = q % PR;
+        src[u] = base + l[u] * ld + c * P;
+        valid[u] = cols - c * P;
+        dst[u] = (uint32_t)(l[u] * TM * sizeof(T) + 16 * col_piece<T>(l[u], c));
+      }
     }
   }
-  // `left`: entries of l from the stage's first on
-  __device__ __forceinline__ Piece<T, P> fetch(int u, int left) const {
-    const int n = ROWS ? (valid[u] ? left - l[u] : 0) : (l[u] < left ? valid[u] : 0);
-    return load_piece<T>(src[u], n);
+  // the next stage, of which `left` entries of l exist
+  __device__ __forceinline__ void fetch(Set& s, int left) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int n = ROWS ? (valid[u] ? left - l[u] : 0) : (l[u] < left ? valid[u] : 0);
+      s[u] = load_piece<T>(src[u], n);
+      src[u] += step;
+    }
+  }
+  __device__ __forceinline__ void store(uint8_t* at, const Set& s) const {
+#pragma unroll
+    for (int u = 0; u < N; ++u) __builtin_memcpy(__builtin_assume_aligned(at + dst[u], 16), &s[u], 16);
   }
 };
 
@@ -610,8 +700,8 @@ template <class T, Oz2Side SIDE>
 __global__ void __launch_bounds__(NT, 2)
 k_product(Oz2Product p, int ncol) {
   constexpr bool AR = SIDE != OZ2_WGRAD, BR = SIDE == OZ2_FWD;
-  constexpr int KE = SB / sizeof(T), OP = TM * SB;
-  __shared__ __attribute__((aligned(16))) uint8_t LB[2][2 * OP];
+  constexpr int KE = SB2 / sizeof(T);
+  __shared__ __attribute__((aligned(16))) uint8_t LB[2 * DST];
   Tile t;
   if (!tile_of<SIDE>(p, TM, ncol, t)) return;
   if (SIDE != OZ2_WGRAD && t.group < 0) {
@@ -624,61 +714,55 @@ k_product(Oz2Product p, int ncol) {
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6), wr = w >> 1, wc = w & 1;
   Loader<T, AR> la;
   Loader<T, BR> lb;
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int q = tid + NT * u;
-    if (AR) {
-      const int row = t.row + (q >> 2);
-      la.init(A, p.lda, q, u, row, row < t.end, 0);
-    } else {
-      la.init(A + t.row, p.lda, q, u, 0, true, t.end - t.row);
-    }
-    if (BR) {
-      int col;
-      const int row = w_row(q >> 2, t.col0, p.N, p.gated != 0, col);
-      lb.init(B, p.ldb, q, u, row, col < p.N, 0);
-    } else {
-      lb.init(B + t.col0, p.ldb, q, u, 0, true, p.N2 - t.col0);
-    }
-  }
+  if (AR)
+    la.init(A, p.lda, tid, [&](int q) { return t.row + q < t.end ? (ll)t.row + q : -1ll; }, 0);
+  else
+    la.init(A + t.row, p.lda, tid, [](int) { return 0ll; }, t.end - t.row);
+  if (BR)
+    lb.init(B, p.ldb, tid, [&](int q) {
+      const int c = t.col0 + w_col(q, p.gated != 0);
+      return c < p.N ? (ll)c + (p.gated && (q & 32) ? p.N : 0) : -1ll;
+    }, 0);
+  else
+    lb.init(B + t.col0, p.ldb, tid, [](int) { return 0ll; }, p.N2 - t.col0);
   v4f acc[4][4];
 #pragma unroll
   for (int j = 0; j < 4; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  const Reader<T, AR, TM, SB> ra(lane);
-  const Reader<T, BR, TM, SB> rb(lane);
+  const Reader<T, AR, TM> ra(lane);
+  const Reader<T, BR, TM> rb(lane);
   const int len = t.l1 - t.l0, n = (len + KE - 1) / KE;
-  Piece<T, 16 / sizeof(T)> pa[2], pb[2];
-  auto fetch = [&](int it) {
+  typename Loader<T, AR>::Set pa[2];
+  typename Loader<T, BR>::Set pb[2];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    la.fetch(pa[u], len - u * KE);
+    lb.fetch(pb[u], len - u * KE);
+  }
+  // (an even number of stages: those beyond the last are zeros)
+  for (int it0 = 0; it0 < n; it0 += 2) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      pa[u] = la.fetch(u, len - it * KE);
-      pb[u] = lb.fetch(u, len - it * KE);
-      la.src[u] += la.step;
-      lb.src[u] += lb.step;
+      uint8_t* st = LB + u * DST;
+      la.store(st, pa[u]);
+      lb.store(st + DOP, pb[u]);
+      __syncthreads();
+      la.fetch(pa[u], len - (it0 + u + 2) * KE);
+      lb.fetch(pb[u], len - (it0 + u + 2) * KE);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        Frag<T> fa[4], fb[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) fb[j] = rb.get(st + DOP, 4 * wc + j, h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) fa[i] = ra.get(st, 4 * wr + i, h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[j][i] = mma(fb[j], fa[i], acc[j][i]);
+      }
     }
-  };
-  if (n > 0) fetch(0);
-  for (int it = 0; it < n; ++it) {
-    uint8_t* sa = LB[it & 1];
-    uint8_t* sb = sa + OP;
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      __builtin_memcpy(__builtin_assume_aligned(sa + la.dst[u], 16), &pa[u], 16);
-      __builtin_memcpy(__builtin_assume_aligned(sb + lb.dst[u], 16), &pb[u], 16);
-    }
-    __syncthreads();
-    if (it + 1 < n) fetch(it + 1);
-    Frag<T> fa[4], fb[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) fa[i] = ra.get(sa, 4 * wr + i);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) fb[j] = rb.get(sb, 4 * wc + j);
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[j][i] = mma(fb[j], fa[i], acc[j][i]);
   }
   __syncthreads();
   epilogue<T, SIDE, 4, 1, 1>(p, acc, reinterpret_cast<float*>(LB) + w * 16 * 68, t, t.row + 64 * wr, 64 * wc,
@@ -691,17 +775,15 @@ template <class T>
 bool direct_side(const void* x, ll ld, bool rows, ll extent, int tile) {
   constexpr int P = 16 / sizeof(T);
   return (uintptr_t)x % 16 == 0 && ld % P == 0 && extent % P == 0 &&
-         ld * (ll)sizeof(T) * (rows ? tile : SB / (ll)sizeof(T)) < (ll)kRecords - 65536;
+         ld * (rows ? (ll)sizeof(T) * tile : SB2) < (ll)kRecords - 65536;
 }
 template <class T>
 bool direct(Oz2Side side, const Oz2Product& p, int tile) {
   constexpr int P = 16 / sizeof(T);
   if (p.strideB % P && side != OZ2_WGRAD) return false;
-  // (gated: rows of W from a tile's gates to its values lie within N rows)
-  const ll wrows = p.gated && side == OZ2_FWD ? (ll)p.N + tile : tile;
   const ll acols = side == OZ2_WGRAD ? p.M : p.L;
   return direct_side<T>(p.A, p.lda, side != OZ2_WGRAD, p.padded ? 0 : acols, tile) &&
-         direct_side<T>(p.B, p.ldb, side == OZ2_FWD, side == OZ2_FWD ? p.L : p.N2, (int)wrows);
+         direct_side<T>(p.B, p.ldb, side == OZ2_FWD, side == OZ2_FWD ? p.L : p.N2, tile);
 }
 
 #define OZ2_SIDES(kern, grid, threads)                                                  \
@@ -724,18 +806,208 @@ dim3 tile_grid(Oz2Side side, const Oz2Product& p, int tile, int& ncol) {
   return dim3((unsigned)oz2_tile_blocks(p.gr, tile, ncol));
 }
 
+// The epilogue of W columns of one row from column col on (valid of them exist), v and
+// u the sums
+template <class T, int W>
+__device__ __forceinline__ void finish(const Oz2Product& p, int group, ll row, int col, int valid,
+                                       float (&v)[W], float (&u)[W]) {
+  if (p.bias) {
+    const T* b = (const T*)p.bias + group * p.stride_bias + col;
+    add_to<T, W, false>(v, b, valid);
+    if (p.gated) add_to<T, W, false>(u, b + p.N, valid);
+  }
+  if (p.z) {
+    T* z = (T*)p.z + row * p.ldz + col;
+    put<T, W, false>(z, v, valid);
+    if (p.gated) put<T, W, false>(z + p.N, u, valid);
+  }
+  activate<T, W>(v, p.act);
+  if (p.gated) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] *= u[i];
+  }
+  if (p.res) add_to<T, W, false>(v, (const T*)p.res + row * p.ldr + col, valid);
+  put<T, W, false>((T*)p.y + row * p.ldy + col, v, valid);
+}
+
+// The sum of a product's splits, in order, and the epilogue: 16 bytes of y a thread
 template <class T>
-hipError_t launch_product(Oz2Side side, const Oz2Product& p, hipStream_t s) {
+__global__ void __launch_bounds__(256)
+k_join(Oz2Product p) {
+  constexpr int W = 16 / sizeof(T);
+  const int pieces = (p.N + W - 1) / W;
+  const ll id = (ll)blockIdx.x * 256 + threadIdx.x, row = id / pieces;
+  if (row >= p.M) return;
+  const int col = (int)(id - row * pieces) * W, valid = p.N - col;
+  float v[W], u[W];
+#pragma unroll
+  for (int i = 0; i < W; ++i) v[i] = u[i] = 0.0f;
+  for (int s = 0; s < p.splits; ++s) {
+    const float* q = p.part + ((ll)s * p.M + row) * p.N2 + col;
+    add_to<float, W, false>(v, q, valid);
+    if (p.gated) add_to<float, W, false>(u, q + p.N, valid);
+  }
+  finish<T, W>(p, 0, row, col, valid, v, u);
+}
+
+// ------------------------------------------------ few rows: one read of W
+// y = f(x W^T ..) for groups of a few rows each (single tokens, decoding): the bytes of
+// W bound it.  A workgroup takes 16 columns of y of one group (gated: their gates and
+// values), its eight waves share out the 128-byte chunks of l and read their rows of
+// W straight into fragments, UN chunks in flight; 16 TB rows of x at a time are the
+// other operand.  The waves' sums meet in LDS and are added in order.
+constexpr int RNT = 512, RW = RNT / 64;
+
+template <class T, int TB, bool GATED>
+__global__ void __launch_bounds__(RNT)
+k_rows(Oz2Product p) {
+  constexpr int P = 16 / sizeof(T), KC = SB2 / sizeof(T), G = GATED ? 2 : 1;
+  constexpr int UN = TB == 1 && !GATED ? 8 : TB <= 2 ? 4 : 2;
+  __shared__ v4f red[RW][G * TB][64];
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n0 = (int)blockIdx.x * 16, group = (int)blockIdx.y;
+  if (group == p.gr.groups) {   // the rows of no group
+    for (int t = group_start(p.gr, group) + (tid >> 4); t < p.gr.rows; t += RNT / 16) {
+      const int c = n0 + (tid & 15);
+      if (c >= p.N) continue;
+      ((T*)p.y)[t * p.ldy + c] = (T)0.0f;
+      if (p.z) {
+        ((T*)p.z)[t * p.ldz + c] = (T)0.0f;
+        if (GATED) ((T*)p.z)[t * p.ldz + p.N + c] = (T)0.0f;
+      }
+    }
+    return;
+  }
+  int r0, r1;
+  group_range(p.gr, group, r0, r1);
+  // rows that do not exist are read as the last one: their results are not stored
+  const T* wp = (const T*)p.B + group * p.strideB + min(n0 + r, p.N - 1) * p.ldb + g * P;
+  const ll up = GATED ? p.N * p.ldb : 0;
+  const int nch = (p.L + KC - 1) / KC, full = p.L / KC;
+  for (int row = r0; row < r1; row += 16 * TB) {
+    const T* xp[TB];
+#pragma unroll
+    for (int b = 0; b < TB; ++b) xp[b] = (const T*)p.A + min(row + 16 * b + r, r1 - 1) * p.lda + g * P;
+    v4f acc[G][TB];
+#pragma unroll
+    for (int k = 0; k < G; ++k)
+#pragma unroll
+      for (int b = 0; b < TB; ++b) acc[k][b] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    typedef decltype(Frag<T>::v) V;
+    for (int c0 = w; c0 < full; c0 += RW * UN) {
+      Frag<T> wf[UN][2][G], xf[UN][2][TB];
+#pragma unroll
+      for (int q = 0; q < UN; ++q) {
+        // chunks beyond the last full one: the last again, with zeros for x
+        const bool on = c0 + RW * q < full;
+        const int k = min(c0 + RW * q, full - 1) * KC;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int e = 0; e < G; ++e) __builtin_memcpy(&wf[q][h][e].v, wp + e * up + k + 4 * h * P, 16);
+#pragma unroll
+          for (int b = 0; b < TB; ++b) {
+            if (on)
+              __builtin_memcpy(&xf[q][h][b].v, xp[b] + k + 4 * h * P, 16);
+            else
+              xf[q][h][b].v = V{};
+          }
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < UN; ++q)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < G; ++e)
+#pragma unroll
+            for (int b = 0; b < TB; ++b) acc[e][b] = mma(wf[q][h][e], xf[q][h][b], acc[e][b]);
+    }
+    if (nch > full && full % RW == w) {   // the last chunk, in part
+      const int k = full * KC;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int valid = p.L - k - (g + 4 * h) * P;
+        Frag<T> wf[G], xf[TB];
+#pragma unroll
+        for (int e = 0; e < G; ++e)
+          wf[e].v = __builtin_bit_cast(V, load_piece<T>(wp + e * up + k + 4 * h * P, valid));
+#pragma unroll
+        for (int b = 0; b < TB; ++b)
+          xf[b].v = __builtin_bit_cast(V, load_piece<T>(xp[b] + k + 4 * h * P, valid));
+#pragma unroll
+        for (int e = 0; e < G; ++e)
+#pragma unroll
+          for (int b = 0; b < TB; ++b) acc[e][b] = mma(wf[e], xf[b], acc[e][b]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < G; ++e)
+#pragma unroll
+      for (int b = 0; b < TB; ++b) red[w][e * TB + b][lane] = acc[e][b];
+    __syncthreads();
+    if (tid < TB * 64) {   // entry tid: accumulators of lane `lane` of block w
+      v4f s[2] = {v4f{0.0f, 0.0f, 0.0f, 0.0f}, v4f{0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+      for (int k = 0; k < RW; ++k)
+#pragma unroll
+        for (int e = 0; e < G; ++e) s[e] += red[k][e * TB + w][lane];
+      const int t = row + 16 * w + r, col = n0 + 4 * g, valid = p.N - col;
+      if (t < r1 && valid > 0) {
+        float v[4], u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[i] = s[0][i];
+          u[i] = s[1][i];
+        }
+        finish<T, 4>(p, group, t, col, valid, v, u);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+template <class T, bool GATED>
+hipError_t launch_rows(int blocks, const Oz2Product& p, hipStream_t s) {
+  const dim3 grid((unsigned)((p.N + 15) / 16), (unsigned)(p.gr.groups + (p.gr.offsets ? 1 : 0)));
+  if (blocks == 1)
+    hipLaunchKernelGGL((k_rows<T, 1, GATED>), grid, dim3(RNT), 0, s, p);
+  else if (blocks == 2)
+    hipLaunchKernelGGL((k_rows<T, 2, GATED>), grid, dim3(RNT), 0, s, p);
+  else
+    hipLaunchKernelGGL((k_rows<T, 4, GATED>), grid, dim3(RNT), 0, s, p);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t launch_tiles(Oz2Side side, bool big, const Oz2Product& p, hipStream_t s) {
   int ncol;
-  if (p.M == 0 || p.N2 == 0) return hipSuccess;
   if constexpr (sizeof(T) == 2) {
-    if (direct<T>(side, p, BT)) {
-      const dim3 grid = tile_grid(side, p, BT, ncol);
+    if (big && direct<T>(side, p, BT)) {
+      dim3 grid = tile_grid(side, p, BT, ncol);
+      grid.y = p.splits;
       OZ2_SIDES(k_product256, grid, BNT);
     }
   }
-  const dim3 grid = tile_grid(side, p, TM, ncol);
+  dim3 grid = tile_grid(side, p, TM, ncol);
+  grid.y = p.splits;
+  if (direct<T>(side, p, TM)) OZ2_SIDES(k_product128, grid, NT);
   OZ2_SIDES(k_product, grid, NT);
+}
+
+template <class T>
+hipError_t launch_product(Oz2Side side, const Oz2Plan& plan, Oz2Product p, hipStream_t s) {
+  if (p.M == 0 || p.N2 == 0) return hipSuccess;
+  p.esize = sizeof(T);
+  p.splits = plan.splits;
+  if (plan.rows) return p.gated ? launch_rows<T, true>(plan.rows, p, s) : launch_rows<T, false>(plan.rows, p, s);
+  const hipError_t e = launch_tiles<T>(side, plan.big, p, s);
+  if (e != hipSuccess || p.splits == 1) return e;
+  constexpr int W = 16 / sizeof(T);
+  const ll items = (ll)p.M * ((p.N + W - 1) / W);
+  hipLaunchKernelGGL(k_join<T>, dim3((unsigned)((items + 255) / 256)), dim3(256), 0, s, p);
+  return hipGetLastError();
 }
 
 // ------------------------------------------------ slope: dZ and its column sums
@@ -855,10 +1127,11 @@ hipError_t launch_slope(const Oz2Slope& p, hipStream_t s) {
 
 }  // namespace
 
-hipError_t oz2_launch_product(int dtype, Oz2Side side, const Oz2Product& p, hipStream_t s) {
-  if (dtype == OZ2_F32) return launch_product<float>(side, p, s);
-  if (dtype == OZ2_F16) return launch_product<_Float16>(side, p, s);
-  return launch_product<__bf16>(side, p, s);
+hipError_t oz2_launch_product(int dtype, Oz2Side side, const Oz2Plan& plan, const Oz2Product& p,
+                              hipStream_t s) {
+  if (dtype == OZ2_F32) return launch_product<float>(side, plan, p, s);
+  if (dtype == OZ2_F16) return launch_product<_Float16>(side, plan, p, s);
+  return launch_product<__bf16>(side, plan, p, s);
 }
 
 hipError_t oz2_launch_slope(int dtype, const Oz2Slope& p, hipStream_t s) {

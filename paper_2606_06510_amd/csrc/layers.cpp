@@ -3,13 +3,14 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "../../include/ozaki2.h"
 #include "oz2_layers.h"
 
 namespace {
 
-constexpr ll kMaxRows = 1ll << 30, kMaxWidth = 1ll << 24, kMaxLd = 1ll << 40, kMaxElems = 1ll << 40;
+constexpr ll kMaxRows = 1ll << 30, kMaxWidth = 1ll << 21, kMaxLd = 1ll << 40, kMaxElems = 1ll << 40;
 
 size_t element(int dtype) { return dtype == OZ2_F32 ? 4 : 2; }
 size_t align256(size_t x) { return (x + 255) / 256 * 256; }
@@ -73,10 +74,15 @@ ll slope_pitch(ll n2, size_t e) {
   return (n2 + per - 1) / per * per;
 }
 
+size_t partial_bytes(const Oz2Plan& pl, ll M, ll N2) {
+  return pl.splits > 1 ? align256((size_t)pl.splits * M * N2 * 4) : 0;
+}
+
 struct BackwardLayout {
-  size_t dz, sums, total;
+  size_t dz, sums, parts, total;
+  Oz2Plan dgrad, wgrad;
 };
-BackwardLayout backward_layout(int dtype, int act, int gated, const Oz2Groups& gr, ll out) {
+BackwardLayout backward_layout(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in) {
   const size_t e = element(dtype);
   const ll n2 = gated ? 2 * out : out;
   BackwardLayout L{};
@@ -85,6 +91,10 @@ BackwardLayout backward_layout(int dtype, int act, int gated, const Oz2Groups& g
   if (act != OZ2_ACT_NONE || gated) o = align256(o + (size_t)gr.rows * slope_pitch(n2, e) * e);
   L.sums = o;
   o = align256(o + (size_t)oz2_row_tiles(gr, OZ2_SUM_ROWS) * n2 * 4);
+  L.parts = o;   // of one product after the other
+  L.dgrad = oz2_plan(dtype, OZ2_DGRAD, gr.rows, in, n2, gr);
+  L.wgrad = oz2_plan(dtype, OZ2_WGRAD, n2, in, gr.rows, gr);
+  o += std::max(partial_bytes(L.dgrad, gr.rows, in), partial_bytes(L.wgrad, n2, in));
   L.total = o;
   return L;
 }
@@ -94,7 +104,10 @@ int check_workspace(const void* ws, size_t bytes, size_t need) {
   return ws && (uintptr_t)ws % 256 == 0 && bytes >= need ? OZ2_OK : OZ2_E_WORKSPACE;
 }
 
-size_t forward_bytes(int, int, const Oz2Groups&, ll, ll) { return 0; }
+size_t forward_bytes(int dtype, int gated, const Oz2Groups& gr, ll out, ll in) {
+  const ll n2 = gated ? 2 * out : out;
+  return partial_bytes(oz2_plan(dtype, OZ2_FWD, gr.rows, n2, in, gr), gr.rows, n2);
+}
 
 int forward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, const Mat& x, const Mat& w,
             const Mat& bias, const Mat& res, const Mat& y, const Mat& z, void* ws, size_t ws_bytes,
@@ -141,8 +154,8 @@ int forward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, c
   p.N = (int)out;
   p.act = act;
   p.gated = gated ? 1 : 0;
-  p.splits = 1;
-  return hip_status(oz2_launch_product(dtype, OZ2_FWD, p, s));
+  p.part = (float*)ws;
+  return hip_status(oz2_launch_product(dtype, OZ2_FWD, oz2_plan(dtype, OZ2_FWD, gr.rows, p.N2, in, gr), p, s));
 }
 
 int backward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, const Mat& dy, const Mat& x,
@@ -170,7 +183,7 @@ int backward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, 
     if (gr.offsets && !disjoint_bytes(*outs[i], e, gr.offsets, 4 * (size_t)(gr.groups + 1)))
       return OZ2_E_INVALID;
   }
-  const BackwardLayout L = backward_layout(dtype, act, gated, gr, out);
+  const BackwardLayout L = backward_layout(dtype, act, gated, gr, out, in);
   int st = check_workspace(ws, ws_bytes, L.total);
   if (st != OZ2_OK) return st;
   for (const Mat* m : ins)
@@ -203,7 +216,7 @@ int backward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, 
   p.lda = sloped ? slope_pitch(n2, e) : dy.ld;
   p.padded = sloped;
   p.gr = gr;
-  p.splits = 1;
+  p.part = (float*)(base + L.parts);
   if (want_dx) {
     Oz2Product d = p;
     d.B = w.p;
@@ -214,7 +227,7 @@ int backward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, 
     d.L = (int)n2;
     d.y = const_cast<void*>(dx.p);
     d.ldy = dx.ld;
-    if ((err = oz2_launch_product(dtype, OZ2_DGRAD, d, s)) != hipSuccess) return hip_status(err);
+    if ((err = oz2_launch_product(dtype, OZ2_DGRAD, L.dgrad, d, s)) != hipSuccess) return hip_status(err);
   }
   if (want_dw) {
     Oz2Product d = p;
@@ -226,7 +239,7 @@ int backward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, 
     d.y = const_cast<void*>(dw.p);
     d.ldy = dw.ld;
     d.strideB = dw.stride;
-    if ((err = oz2_launch_product(dtype, OZ2_WGRAD, d, s)) != hipSuccess) return hip_status(err);
+    if ((err = oz2_launch_product(dtype, OZ2_WGRAD, L.wgrad, d, s)) != hipSuccess) return hip_status(err);
   }
   return OZ2_OK;
 }
@@ -239,6 +252,54 @@ bool tokens_ok(int dtype, int tokens, int top_k, int width) {
 bool int_ok(const void* p) { return p && (uintptr_t)p % 4 == 0; }
 
 }  // namespace
+
+// The faster of the two tilings by a fit of measured times (us; L in stages of 128
+// bytes, CUs of a round):
+//   256 x 256: 6 a launch; a round of tiles 8 + 1.05 a stage, 1.65 on a full chip
+//   128 x 128: 5 a launch; workgroups alone on their CU 0.55 a stage (fp32 2.1); two a
+//              CU 3 + 1.1 (4.2) a stage a round
+//   a sum in s parts: 4 for the second launch, the parts written and read at 4 TB/s
+// for instance bf16 (256 / 128 tiles): 4096^3 120 / 153, 2048^2 x 4096 82 / 43 (two
+// parts 48), 1024^2 x 4096 79 / 37 (two 27, four 26), 512^2 x 4096 78 / 36 (four 18),
+// 1024^3 27 / 13 (two 17), 6144 x 4096 x 1024 67 / 61.
+// Groups: their sizes are not known here; even ones are assumed, and the sum stays
+// whole.  Few rows a group: see k_rows.
+Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr) {
+  const double cus = oz2_device_cus();
+  const bool wide = dtype == OZ2_F32;
+  if (side == OZ2_FWD) {
+    if (!gr.offsets && M <= 64) return Oz2Plan{M <= 16 ? 1 : M <= 32 ? 2 : 4, false, 1};
+    if (gr.offsets && M <= 8ll * gr.groups) return Oz2Plan{M <= 2ll * gr.groups ? 1 : 2, false, 1};
+  }
+  const double stages = std::max<double>(1.0, std::ceil((double)L * (wide ? 4 : 2) / 128.0 /
+                                                        (gr.offsets && side == OZ2_WGRAD ? gr.groups : 1)));
+  auto tiles = [&](double t) {
+    if (!gr.offsets) return std::ceil(M / t) * std::ceil(N2 / t);
+    if (side == OZ2_WGRAD) return std::ceil(M / t) * std::ceil(N2 / t) * gr.groups;
+    return std::ceil((double)M / gr.groups / t) * gr.groups * std::ceil(N2 / t);
+  };
+  Oz2Plan best{0, false, 1};
+  double t_best = 1e30;
+  if (!wide) {
+    const double n = tiles(256.0), load = std::min(1.0, n / cus);
+    best.big = true;
+    t_best = 6.0 + std::max(1.0, n <= 4.0 * cus ? std::ceil(n / cus) : n / cus) * (8.0 + stages * (1.05 + 0.6 * load));
+  }
+  const double n = tiles(128.0), alone = wide ? 2.1 : 0.55, full = wide ? 4.2 : 1.1;
+  const int most = gr.offsets ? 1 : (int)std::min(32.0, std::max(1.0, stages / 4.0));
+  for (int s = 1; s <= most; ++s) {
+    if (s > 1 && n * s > 2.0 * cus) break;
+    const double per = std::ceil(stages / s), wgs = n * s;
+    double t = wgs <= cus ? 5.0 + per * alone
+                          : 5.0 + (wgs <= 8.0 * cus ? std::ceil(wgs / (2.0 * cus)) : wgs / (2.0 * cus)) * (3.0 + per * full);
+    if (s > 1) t += 4.0 + s * (double)M * N2 * 8.0 / 4e6;
+    if (t < t_best) {
+      t_best = t;
+      best = Oz2Plan{0, false, s};
+    }
+  }
+  return best;
+}
 
 extern "C" {
 
@@ -278,7 +339,7 @@ int ozaki2_grouped_linear(int dtype, int activation, int gated, int rows, int gr
 size_t ozaki2_linear_backward_workspace_bytes(int dtype, int activation, int gated, int rows, int out,
                                               int in) {
   if (!sizes_ok(dtype, activation, rows, 1, out, in, gated)) return 0;
-  return backward_layout(dtype, activation, gated, Oz2Groups{nullptr, 1, rows}, out).total;
+  return backward_layout(dtype, activation, gated, Oz2Groups{nullptr, 1, rows}, out, in).total;
 }
 
 int ozaki2_linear_backward(int dtype, int activation, int gated, int rows, int out, int in, const void* dy,
@@ -297,7 +358,7 @@ size_t ozaki2_grouped_linear_backward_workspace_bytes(int dtype, int activation,
                                                       int groups, int out, int in) {
   if (!sizes_ok(dtype, activation, rows, groups, out, in, gated)) return 0;
   static const int any = 0;
-  return backward_layout(dtype, activation, gated, Oz2Groups{&any, groups, rows}, out).total;
+  return backward_layout(dtype, activation, gated, Oz2Groups{&any, groups, rows}, out, in).total;
 }
 
 int ozaki2_grouped_linear_backward(int dtype, int activation, int gated, int rows, int groups, int out,

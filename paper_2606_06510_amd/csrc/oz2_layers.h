@@ -46,8 +46,18 @@ struct Oz2Product {
   int act, gated;
   bool padded;           // A's rows go on, in zeros, to a multiple of 16 bytes
   float* part;           // splits > 1: [split][M][N2] partial sums
+  int splits, esize;     // (set by the launcher)
+};
+
+// How a product runs: `rows` > 0: the kernel of few rows, that many blocks of 16 at a
+// time (1, 2, 4; FWD); else 256 x 256 tiles (16 bits, and operands that direct loads
+// take) or 128 x 128 ones, the sum in how many parts, joined by a second launch.
+struct Oz2Plan {
+  int rows;
+  bool big;
   int splits;
 };
+Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr);
 
 #ifdef __HIPCC__
 // products and sums of the epilogues may be fused; nothing here is compared bit for bit
@@ -260,7 +270,8 @@ inline ll oz2_tile_blocks(const Oz2Groups& g, int tile, int ncol) {
 }
 
 // ---------------------------------------------------------------- launchers
-hipError_t oz2_launch_product(int dtype, Oz2Side side, const Oz2Product& p, hipStream_t s);
+hipError_t oz2_launch_product(int dtype, Oz2Side side, const Oz2Plan& plan, const Oz2Product& p,
+                              hipStream_t s);
 // dZ (pitch ldd, a multiple of 64 bytes; entries beyond n2 zero) from dY and Z,
 // or nothing of it where dz is null; column sums of dZ into db where not null,
 // by way of part ([row tile][n2])
