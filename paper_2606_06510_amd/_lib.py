@@ -170,9 +170,7 @@ def _status_string(st):
 
 
 def _ptr(x):
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or isinstance(x, int):
         return x
     if hasattr(x, "data_ptr"):
         return x.data_ptr()

@@ -14,11 +14,13 @@ namespace {
 // part, so "earlier" is: earlier workgroups (counted by a first launch), earlier
 // waves (counted in LDS), and earlier lanes (a ballot per bit of the key).
 constexpr int SORT_NT = 512, SORT_W = SORT_NT / 64;
+constexpr int SORT_KEYS = 4;                      // of a thread, kept in registers
+constexpr int SORT_CHUNK = SORT_NT * SORT_KEYS;   // pairs of a workgroup, or a multiple
 
 struct SortArgs {
   const void* ids;
   ll ld;
-  int k, E, pairs, chunk;   // chunk: pairs per workgroup, a multiple of SORT_NT
+  int k, E, pairs, chunk;   // chunk: pairs per workgroup, a multiple of SORT_CHUNK
   bool wide;
 };
 
@@ -44,36 +46,53 @@ __global__ void __launch_bounds__(SORT_NT)
 k_sort_place(SortArgs a, const int* __restrict__ counts, int* __restrict__ offsets,
              int* __restrict__ rows, int* __restrict__ slots) {
   __shared__ int at[SORT_W][OZ2_MAX_EXPERTS + 1];   // counts, then next place, of each wave and key
-  __shared__ int tot[OZ2_MAX_EXPERTS + 1];
+  __shared__ int tot[OZ2_MAX_EXPERTS + 1], before[OZ2_MAX_EXPERTS + 1];
   __shared__ int wsum[SORT_W];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, K = a.E + 1;
-  for (int i = tid; i < SORT_W * K; i += SORT_NT) at[i / K][i % K] = 0;
-  __syncthreads();
   const int part = a.chunk / SORT_W, p0 = blockIdx.x * a.chunk + w * part;
   const int p1 = min(a.pairs, p0 + part);
-  for (int p = p0 + lane; p < p1; p += 64) atomicAdd(&at[w][key_of(a, p)], 1);
-  __syncthreads();
-  // pairs of each key in all, and in earlier workgroups
-  for (int e = tid; e < K; e += SORT_NT) {
-    int all = 0, before = 0;
-    if (gridDim.x == 1) {
+  // the wave's first SORT_KEYS steps' keys (all, unless there are a great many pairs)
+  int keys[SORT_KEYS];
 #pragma unroll
-      for (int v = 0; v < SORT_W; ++v) all += at[v][e];
-    } else {
-      for (int b = 0; b < (int)gridDim.x; ++b) {
+  for (int i = 0; i < SORT_KEYS; ++i) {
+    const int p = p0 + 64 * i + lane;
+    keys[i] = p < p1 ? key_of(a, p) : -1;
+  }
+  for (int e = tid; e < K; e += SORT_NT) {
+    tot[e] = before[e] = 0;
+#pragma unroll
+    for (int v = 0; v < SORT_W; ++v) at[v][e] = 0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < SORT_KEYS; ++i)
+    if (keys[i] >= 0) atomicAdd(&at[w][keys[i]], 1);
+  for (int p = p0 + 64 * SORT_KEYS + lane; p < p1; p += 64) atomicAdd(&at[w][key_of(a, p)], 1);
+  // pairs of each key in all, and in earlier workgroups: every eighth one a wave's
+  if (gridDim.x > 1) {
+    for (int e = lane; e < K; e += 64) {
+      int all = 0, early = 0;
+#pragma unroll 4
+      for (int b = w; b < (int)gridDim.x; b += SORT_W) {
         const int c = counts[(ll)b * K + e];
         all += c;
-        before += b < (int)blockIdx.x ? c : 0;
+        early += b < (int)blockIdx.x ? c : 0;
       }
+      atomicAdd(&tot[e], all);
+      atomicAdd(&before[e], early);
     }
-    tot[e] = all;
+  }
+  __syncthreads();
+  for (int e = tid; e < K; e += SORT_NT) {
     // exclusive over the waves, from the earlier workgroups' pairs on
+    int n = before[e];
 #pragma unroll
     for (int v = 0; v < SORT_W; ++v) {
       const int c = at[v][e];
-      at[v][e] = before;
-      before += c;
+      at[v][e] = n;
+      n += c;
     }
+    if (gridDim.x == 1) tot[e] = n;
   }
   __syncthreads();
   // exclusive sums of tot: each thread `per` consecutive keys
@@ -104,10 +123,8 @@ k_sort_place(SortArgs a, const int* __restrict__ counts, int* __restrict__ offse
   }
   __syncthreads();
   const int bits = 32 - __clz(a.E);   // of keys 0..E
-  for (int q = p0; q < p1; q += 64) {
-    const int p = q + lane;
-    const bool live = p < p1;
-    const int key = live ? key_of(a, p) : 0;
+  auto place = [&](int p, int key) {  // key < 0: no pair
+    const bool live = key >= 0;
     unsigned long long same = __ballot(live);
     for (int b = 0; b < bits; ++b) {
       const bool one = (key >> b) & 1;
@@ -116,14 +133,19 @@ k_sort_place(SortArgs a, const int* __restrict__ counts, int* __restrict__ offse
     }
     const int rank = __popcll(same & ((1ull << lane) - 1));
     if (live) {
-      const int place = tot[key] + at[w][key] + rank;
-      rows[place] = p;
-      slots[p] = place;
+      const int to = tot[key] + at[w][key] + rank;
+      rows[to] = p;
+      slots[p] = to;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     if (live && rank == 0) at[w][key] += __popcll(same);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  }
+  };
+#pragma unroll
+  for (int i = 0; i < SORT_KEYS; ++i)
+    if (p0 + 64 * i < p1) place(p0 + 64 * i + lane, keys[i]);
+  for (int q = p0 + 64 * SORT_KEYS; q < p1; q += 64)
+    place(q + lane, q + lane < p1 ? key_of(a, q + lane) : -1);
 }
 
 // ---------------------------------------------------------------- rows
@@ -162,7 +184,7 @@ k_gather(Oz2Tokens a, const T* __restrict__ x, ll ldx, T* __restrict__ xs, ll ld
 #pragma unroll
         for (int i = 0; i < P; ++i) o.v[i] = from_f<T>(f * to_f(v.v[i]));
       }
-      store_piece(xs + s * ldxs + (ll)c * P, o, valid);
+      store_stream(xs + s * ldxs + (ll)c * P, o, valid);
     }
   }
 }
@@ -210,7 +232,7 @@ k_combine(Oz2Tokens a, const T* __restrict__ ys, ll ldys, const T* res, ll ldr, 
     Piece<T, P> o;
 #pragma unroll
     for (int i = 0; i < P; ++i) o.v[i] = from_f<T>(sum[i]);
-    store_piece(y + t * ldy + (ll)c * P, o, valid);
+    store_stream(y + t * ldy + (ll)c * P, o, valid);
   }
 }
 
@@ -261,7 +283,7 @@ k_combine_backward(Oz2Tokens a, const T* __restrict__ dy, ll lddy, const T* __re
           Piece<T, P> o;
 #pragma unroll
           for (int i = 0; i < P; ++i) o.v[i] = from_f<T>(on ? f[u] * to_f(g.v[i]) : 0.0f);
-          store_piece(dys + s[u] * lddys + (ll)c * P, o, valid);
+          store_stream(dys + s[u] * lddys + (ll)c * P, o, valid);
         }
       }
     }
@@ -313,17 +335,18 @@ int lanes_per_row(int pieces) { return pieces <= 8 ? 8 : pieces <= 16 ? 16 : pie
     else { auto* f = kern<T, 64>; __VA_ARGS__; }                 \
   } while (0)
 
-// workgroups of the sort: one where its own loop is shorter than a second launch
+// workgroups of the sort: one where its own loop is shorter than a second launch, at
+// most 256 (each adds up the counts of all)
 int oz2_sort_blocks(ll pairs) {
-  if (pairs <= 4096) return 1;
-  return (int)std::min<ll>(128, (pairs + 2047) / 2048);
+  if (pairs <= 2 * SORT_CHUNK) return 1;
+  return (int)std::min<ll>(256, (pairs + SORT_CHUNK - 1) / SORT_CHUNK);
 }
 
 hipError_t oz2_launch_sort(int tokens, int top_k, int E, const void* ids, bool wide, ll ld, int* offsets,
                            int* rows, int* slots, int* counts, hipStream_t s) {
   const ll pairs = (ll)tokens * top_k;
   int nb = oz2_sort_blocks(pairs);
-  const ll chunk = std::max<ll>(1, ((pairs + nb - 1) / nb + SORT_NT - 1) / SORT_NT) * SORT_NT;
+  const ll chunk = std::max<ll>(1, ((pairs + nb - 1) / nb + SORT_CHUNK - 1) / SORT_CHUNK) * SORT_CHUNK;
   nb = std::max(1, (int)((pairs + chunk - 1) / chunk));
   SortArgs a{ids, ld, top_k, E, (int)pairs, (int)chunk, wide};
   if (nb > 1) {

@@ -304,7 +304,7 @@ __device__ __forceinline__ void put(T* p, const float* v, int valid) {
   Piece<T, W> o;
 #pragma unroll
   for (int i = 0; i < W; ++i) o.v[i] = from_f<T>(v[i]);
-  store_piece(p, o, ALL ? W : valid);
+  store_stream(p, o, ALL ? W : valid);
 }
 template <class T, int W, bool ALL>
 __device__ __forceinline__ void add_to(float* v, const T* p, int valid) {
@@ -783,7 +783,7 @@ bool direct(Oz2Side side, const Oz2Product& p, int tile) {
   if (p.strideB % P && side != OZ2_WGRAD) return false;
   const ll acols = side == OZ2_WGRAD ? p.M : p.L;
   return direct_side<T>(p.A, p.lda, side != OZ2_WGRAD, p.padded ? 0 : acols, tile) &&
-         direct_side<T>(p.B, p.ldb, side == OZ2_FWD, side == OZ2_FWD ? p.L : p.N2, tile);
+         direct_side<T>(p.B, p.ldb, side == OZ2_FWD, p.paddedB ? 0 : side == OZ2_FWD ? p.L : p.N2, tile);
 }
 
 #define OZ2_SIDES(kern, grid, threads)                                                  \
@@ -980,6 +980,64 @@ hipError_t launch_rows(int blocks, const Oz2Product& p, hipStream_t s) {
   return hipGetLastError();
 }
 
+// ------------------------------------------------ operands in whole lines
+// Rows that are not whole 16-byte pieces, copied to rows of whole 128-byte lines with
+// zeros at their ends, for the direct loads: 16-bit rows from any address take 2.6 us
+// a stage of 128 x 128 tiles, direct loads 0.55.  64 lanes a row, both operands.
+struct Rows {
+  const void* src;
+  ll ld, stride;     // elements between rows, and between matrices of `per` rows
+  ll rows;
+  int per, cols;
+  void* dst;
+  ll pitch;
+};
+
+template <class T>
+__global__ void __launch_bounds__(256)
+k_pack(Rows a, Rows b) {
+  constexpr int P = 16 / sizeof(T);
+  ll row = (ll)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const bool second = row >= a.rows;
+  if (second) row -= a.rows;
+  const Rows& m = second ? b : a;
+  if (row >= m.rows) return;
+  const ll k = row / m.per;
+  const T* src = (const T*)m.src + k * m.stride + (row - k * m.per) * m.ld;
+  T* dst = (T*)m.dst + row * m.pitch;
+  for (int c = (threadIdx.x & 63) * P; c < m.pitch; c += 64 * P)
+    store_piece(dst + c, load_piece<T>(src + c, m.cols - c), P);
+}
+
+template <class T>
+hipError_t pack(Oz2Side side, const Oz2Plan& plan, Oz2Product& p, hipStream_t s) {
+  Rows r[2] = {};
+  const int groups = p.gr.offsets ? p.gr.groups : 1;
+  T* at = (T*)p.packed;
+  if (plan.pack & 1) {
+    const int cols = side == OZ2_WGRAD ? p.M : p.L, rows = side == OZ2_WGRAD ? p.L : p.M;
+    r[0] = Rows{p.A, p.lda, 0, rows, std::max(rows, 1), cols, at, (ll)(oz2_packed_pitch(cols, sizeof(T)))};
+    p.A = at;
+    p.lda = r[0].pitch;
+    at += rows * r[0].pitch;
+    p.padded = true;
+  }
+  if (plan.pack & 2) {
+    const int cols = side == OZ2_FWD ? p.L : p.N2;
+    const int per = side == OZ2_FWD ? p.N2 : p.L, count = side == OZ2_WGRAD ? 1 : groups;
+    Rows& q = r[1];
+    q = Rows{p.B, p.ldb, p.strideB, (ll)per * count, std::max(per, 1), cols, at, oz2_packed_pitch(cols, sizeof(T))};
+    p.B = at;
+    p.ldb = q.pitch;
+    if (side != OZ2_WGRAD) p.strideB = per * q.pitch;
+    p.paddedB = true;
+  }
+  const ll rows = r[0].rows + r[1].rows;
+  if (rows == 0) return hipSuccess;
+  hipLaunchKernelGGL(k_pack<T>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, r[0], r[1]);
+  return hipGetLastError();
+}
+
 template <class T>
 hipError_t launch_tiles(Oz2Side side, bool big, const Oz2Product& p, hipStream_t s) {
   int ncol;
@@ -1002,7 +1060,9 @@ hipError_t launch_product(Oz2Side side, const Oz2Plan& plan, Oz2Product p, hipSt
   p.esize = sizeof(T);
   p.splits = plan.splits;
   if (plan.rows) return p.gated ? launch_rows<T, true>(plan.rows, p, s) : launch_rows<T, false>(plan.rows, p, s);
-  const hipError_t e = launch_tiles<T>(side, plan.big, p, s);
+  hipError_t e = plan.pack ? pack<T>(side, plan, p, s) : hipSuccess;
+  if (e != hipSuccess) return e;
+  e = launch_tiles<T>(side, plan.big, p, s);
   if (e != hipSuccess || p.splits == 1) return e;
   constexpr int W = 16 / sizeof(T);
   const ll items = (ll)p.M * ((p.N + W - 1) / W);
@@ -1011,50 +1071,69 @@ hipError_t launch_product(Oz2Side side, const Oz2Plan& plan, Oz2Product p, hipSt
 }
 
 // ------------------------------------------------ slope: dZ and its column sums
-// dZ = dY f'(Z).  A workgroup takes OZ2_SUM_ROWS rows of one group and 8 (fp32 4)
-// x 32 columns of n: 8 rows at a time, 32 threads a row; the column sums of its
-// rows leave as one partial row, summed in order by k_sums.  Memory-bound.
-template <class T>
+// dZ = dY f'(Z).  A workgroup takes p.sum_rows rows of one group and 32 pieces of 16
+// bytes of n, 8 rows at a time; the column sums of its rows leave as one partial row,
+// added up in order by k_sums.  Bound by memory: dY and Z read and dZ written once.
+template <class T, int ACT, bool GATED>
 __global__ void __launch_bounds__(256)
 k_slope(Oz2Slope p) {
-  constexpr int P = 16 / sizeof(T);
+  constexpr int P = 16 / sizeof(T), U = 2;
+  constexpr bool SLOPED = GATED || ACT != OZ2_ACT_NONE;
   __shared__ float red[8][32 * 2 * P];
-  if ((int)blockIdx.x >= group_tiles(p.gr, OZ2_SUM_ROWS)) return;
+  if ((int)blockIdx.x >= group_tiles(p.gr, p.sum_rows)) return;
   int group, row, end;
-  group_tile(p.gr, OZ2_SUM_ROWS, (int)blockIdx.x, group, row, end);
-  end = min(end, row + OZ2_SUM_ROWS);
+  group_tile(p.gr, p.sum_rows, (int)blockIdx.x, group, row, end);
+  end = min(end, row + p.sum_rows);
   const int c = ((int)blockIdx.y * 32 + (int)(threadIdx.x & 31)) * P, rr = threadIdx.x >> 5;
-  const int n2 = p.gated ? 2 * p.n : p.n, valid = p.n - c;
+  const int n2 = GATED ? 2 * p.n : p.n, valid = p.n - c;
   float sg[P], su[P];
 #pragma unroll
   for (int i = 0; i < P; ++i) sg[i] = su[i] = 0.0f;
   if (valid > 0) {
-    for (int t = row + rr; t < end; t += 8) {
-      const Piece<T, P> g = load_piece<T>((const T*)p.dy + t * p.lddy + c, valid);
-      Piece<T, P> a, u, o;
-      if (p.z) a = load_piece<T>((const T*)p.z + t * p.ldz + c, valid);
-      if (p.gated) u = load_piece<T>((const T*)p.z + t * p.ldz + p.n + c, valid);
-      float d[P];
+#pragma clang loop unroll(disable)
+    for (int t0 = row + rr; t0 < end; t0 += 8 * U) {
+      Piece<T, P> g[U], a[U], u[U];
 #pragma unroll
-      for (int i = 0; i < P; ++i) {
-        const float x = to_f(g.v[i]);
-        d[i] = p.act == OZ2_ACT_NONE ? x : x * act_d<T>(to_f(a.v[i]), p.act);
-        if (p.gated) {
-          d[i] *= to_f(u.v[i]);
-          const float e = x * act_f<T>(to_f(a.v[i]), p.act);
-          su[i] += e;
-          u.v[i] = from_f<T>(e);
-        }
-        sg[i] += d[i];
-        o.v[i] = from_f<T>(d[i]);
+      for (int q = 0; q < U; ++q) {
+        const ll t = min(t0 + 8 * q, end - 1);
+        g[q] = load_piece<T>((const T*)p.dy + t * p.lddy + c, valid);
+        if (SLOPED) a[q] = load_piece<T>((const T*)p.z + t * p.ldz + c, valid);
+        if (GATED) u[q] = load_piece<T>((const T*)p.z + t * p.ldz + p.n + c, valid);
       }
-      if (p.dz) {
-        T* q = (T*)p.dz + t * p.ldd;
-        store_piece(q + c, o, valid);
-        if (p.gated) store_piece(q + p.n + c, u, valid);
-        // the pad of the row is read as part of the last piece: zeros
-        if (valid <= P)
-          for (int e = n2; e < p.ldd; ++e) q[e] = (T)0.0f;
+      float d[U * P], e[U * P];
+#pragma unroll
+      for (int i = 0; i < U * P; ++i) d[i] = t0 + 8 * (i / P) < end ? to_f(g[i / P].v[i % P]) : 0.0f;
+      if (GATED) {
+#pragma unroll
+        for (int i = 0; i < U * P; ++i) e[i] = d[i] * act_f<T>(to_f(a[i / P].v[i % P]), ACT);
+#pragma unroll
+        for (int i = 0; i < U * P; ++i) {
+          su[i % P] += e[i];
+          d[i] *= to_f(u[i / P].v[i % P]);
+          u[i / P].v[i % P] = from_f<T>(e[i]);
+        }
+      }
+      if (ACT != OZ2_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < U * P; ++i) d[i] *= act_d<T>(to_f(a[i / P].v[i % P]), ACT);
+      }
+#pragma unroll
+      for (int i = 0; i < U * P; ++i) {
+        // (rows past the end: d is 0, but 0 times a slope of NaN is not)
+        if (t0 + 8 * (i / P) < end) sg[i % P] += d[i];
+        g[i / P].v[i % P] = from_f<T>(d[i]);
+      }
+      if (SLOPED && p.dz) {
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+          if (t0 + 8 * q >= end) continue;
+          T* z = (T*)p.dz + (t0 + 8 * q) * p.ldd;
+          store_stream(z + c, g[q], valid);
+          if (GATED) store_stream(z + p.n + c, u[q], valid);
+          // the pad of the row is read as part of the last piece: zeros
+          if (valid <= P)
+            for (int k = n2; k < p.ldd; ++k) z[k] = (T)0.0f;
+        }
       }
     }
   }
@@ -1073,52 +1152,84 @@ k_slope(Oz2Slope p) {
     const int piece = q / (2 * P), i = q % (2 * P);
     const int col = ((int)blockIdx.y * 32 + piece) * P + i % P;
     const bool up = i >= P;
-    if (col < p.n && (!up || p.gated)) p.part[(ll)blockIdx.x * n2 + (up ? p.n + col : col)] = s;
+    if (col < p.n && (!up || GATED)) p.part[(ll)blockIdx.x * n2 + (up ? p.n + col : col)] = s;
   }
 }
 
-// db of group blockIdx.y: the partial rows of its row tiles, in order, four sums at a time
+// db of group blockIdx.y, 32 columns a workgroup: the partial rows of the group's row
+// tiles in eight runs, each in order, then the runs in order
 template <class T>
 __global__ void __launch_bounds__(256)
 k_sums(Oz2Slope p) {
-  const int n2 = p.gated ? 2 * p.n : p.n, c = (int)(blockIdx.x * 256 + threadIdx.x);
-  const int g = (int)blockIdx.y;
-  int first = 0, count = 0;
+  __shared__ float red[8][32];
+  const int n2 = p.gated ? 2 * p.n : p.n, l = threadIdx.x & 31, run = threadIdx.x >> 5;
+  const int c = (int)blockIdx.x * 32 + l, g = (int)blockIdx.y;
+  int first = 0, count;
   if (!p.gr.offsets) {
-    count = (p.gr.rows + OZ2_SUM_ROWS - 1) / OZ2_SUM_ROWS;
+    count = (int)(((ll)p.gr.rows + p.sum_rows - 1) / p.sum_rows);
   } else {
-    for (int i = 0; i <= g; ++i) {
-      int s, e;
+    int s, e;
+    const int lane = threadIdx.x & 63;
+    for (int i = lane; i < g; i += 64) {
       group_range(p.gr, i, s, e);
-      const int k = (e - s + OZ2_SUM_ROWS - 1) / OZ2_SUM_ROWS;
-      if (i < g) first += k;
-      else count = k;
+      first += (e - s + p.sum_rows - 1) / p.sum_rows;
     }
-  }
-  if (c >= n2) return;
-  const float* q = p.part + (ll)first * n2 + c;
-  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  int k = 0;
-  for (; k + 4 <= count; k += 4)
 #pragma unroll
-    for (int u = 0; u < 4; ++u) s[u] += q[(ll)(k + u) * n2];
-  for (; k < count; ++k) s[0] += q[(ll)k * n2];
-  ((T*)p.db)[g * p.stride_db + c] = from_f<T>((s[0] + s[1]) + (s[2] + s[3]));
+    for (int d = 1; d < 64; d <<= 1) first += __shfl_xor(first, d);
+    group_range(p.gr, g, s, e);
+    count = (e - s + p.sum_rows - 1) / p.sum_rows;
+  }
+  const int per = (count + 7) / 8, k0 = run * per, k1 = min(count, k0 + per);
+  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (c < n2) {
+    const float* q = p.part + (ll)first * n2 + c;
+    int k = k0;
+    for (; k + 4 <= k1; k += 4)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) s[u] += q[(ll)(k + u) * n2];
+    for (; k < k1; ++k) s[0] += q[(ll)k * n2];
+  }
+  red[run][l] = (s[0] + s[1]) + (s[2] + s[3]);
+  __syncthreads();
+  if (run == 0 && c < n2) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += red[k][l];
+    ((T*)p.db)[g * p.stride_db + c] = from_f<T>(sum);
+  }
 }
 
 template <class T>
-hipError_t launch_slope(const Oz2Slope& p, hipStream_t s) {
+hipError_t launch_slope(Oz2Slope p, hipStream_t s) {
   constexpr int P = 16 / sizeof(T);
-  const ll rt = oz2_row_tiles(p.gr, OZ2_SUM_ROWS);
   const int cb = (p.n + 32 * P - 1) / (32 * P);
+  // long workgroups where there are enough of them: a workgroup's start (its place among
+  // the groups) takes as long as 16 rows
+  p.sum_rows = OZ2_SUM_ROWS;
+  while (p.sum_rows < 128 && (ll)p.gr.rows / p.sum_rows * cb > 8ll * oz2_device_cus()) p.sum_rows *= 2;
+  const ll rt = oz2_row_tiles(p.gr, p.sum_rows);
   if (rt > 0 && cb > 0) {
-    hipLaunchKernelGGL(k_slope<T>, dim3((unsigned)rt, (unsigned)cb), dim3(256), 0, s, p);
+    const dim3 grid((unsigned)rt, (unsigned)cb);
+#define OZ2_SLOPE(ACT)                                                          \
+  case ACT:                                                                     \
+    if (p.gated)                                                                \
+      hipLaunchKernelGGL((k_slope<T, ACT, true>), grid, dim3(256), 0, s, p);    \
+    else                                                                        \
+      hipLaunchKernelGGL((k_slope<T, ACT, false>), grid, dim3(256), 0, s, p);   \
+    break
+    switch (p.act) {
+      OZ2_SLOPE(OZ2_ACT_NONE);
+      OZ2_SLOPE(OZ2_ACT_RELU);
+      OZ2_SLOPE(OZ2_ACT_GELU);
+      OZ2_SLOPE(OZ2_ACT_GELU_TANH);
+      OZ2_SLOPE(OZ2_ACT_SILU);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   const int n2 = p.gated ? 2 * p.n : p.n;
   if (p.db && n2 > 0) {
-    hipLaunchKernelGGL(k_sums<T>, dim3((unsigned)((n2 + 255) / 256), (unsigned)p.gr.groups), dim3(256), 0,
+    hipLaunchKernelGGL(k_sums<T>, dim3((unsigned)((n2 + 31) / 32), (unsigned)p.gr.groups), dim3(256), 0,
                        s, p);
     return hipGetLastError();
   }

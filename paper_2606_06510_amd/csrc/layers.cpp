@@ -74,8 +74,12 @@ ll slope_pitch(ll n2, size_t e) {
   return (n2 + per - 1) / per * per;
 }
 
-size_t partial_bytes(const Oz2Plan& pl, ll M, ll N2) {
+// the parts of a split sum, then the packed operands
+size_t part_bytes(const Oz2Plan& pl, ll M, ll N2) {
   return pl.splits > 1 ? align256((size_t)pl.splits * M * N2 * 4) : 0;
+}
+size_t product_bytes(const Oz2Plan& pl, ll M, ll N2) {
+  return part_bytes(pl, M, N2) + align256(pl.packed_bytes);
 }
 
 struct BackwardLayout {
@@ -92,9 +96,10 @@ BackwardLayout backward_layout(int dtype, int act, int gated, const Oz2Groups& g
   L.sums = o;
   o = align256(o + (size_t)oz2_row_tiles(gr, OZ2_SUM_ROWS) * n2 * 4);
   L.parts = o;   // of one product after the other
-  L.dgrad = oz2_plan(dtype, OZ2_DGRAD, gr.rows, in, n2, gr);
-  L.wgrad = oz2_plan(dtype, OZ2_WGRAD, n2, in, gr.rows, gr);
-  o += std::max(partial_bytes(L.dgrad, gr.rows, in), partial_bytes(L.wgrad, n2, in));
+  const bool sloped = act != OZ2_ACT_NONE || gated;
+  L.dgrad = oz2_plan(dtype, OZ2_DGRAD, gr.rows, in, n2, gr, sloped);
+  L.wgrad = oz2_plan(dtype, OZ2_WGRAD, n2, in, gr.rows, gr, sloped);
+  o += std::max(product_bytes(L.dgrad, gr.rows, in), product_bytes(L.wgrad, n2, in));
   L.total = o;
   return L;
 }
@@ -106,7 +111,7 @@ int check_workspace(const void* ws, size_t bytes, size_t need) {
 
 size_t forward_bytes(int dtype, int gated, const Oz2Groups& gr, ll out, ll in) {
   const ll n2 = gated ? 2 * out : out;
-  return partial_bytes(oz2_plan(dtype, OZ2_FWD, gr.rows, n2, in, gr), gr.rows, n2);
+  return product_bytes(oz2_plan(dtype, OZ2_FWD, gr.rows, n2, in, gr), gr.rows, n2);
 }
 
 int forward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, const Mat& x, const Mat& w,
@@ -154,8 +159,10 @@ int forward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, c
   p.N = (int)out;
   p.act = act;
   p.gated = gated ? 1 : 0;
+  const Oz2Plan plan = oz2_plan(dtype, OZ2_FWD, gr.rows, p.N2, in, gr);
   p.part = (float*)ws;
-  return hip_status(oz2_launch_product(dtype, OZ2_FWD, oz2_plan(dtype, OZ2_FWD, gr.rows, p.N2, in, gr), p, s));
+  p.packed = (uint8_t*)ws + part_bytes(plan, p.M, p.N2);
+  return hip_status(oz2_launch_product(dtype, OZ2_FWD, plan, p, s));
 }
 
 int backward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, const Mat& dy, const Mat& x,
@@ -227,6 +234,7 @@ int backward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, 
     d.L = (int)n2;
     d.y = const_cast<void*>(dx.p);
     d.ldy = dx.ld;
+    d.packed = base + L.parts + part_bytes(L.dgrad, d.M, d.N2);
     if ((err = oz2_launch_product(dtype, OZ2_DGRAD, L.dgrad, d, s)) != hipSuccess) return hip_status(err);
   }
   if (want_dw) {
@@ -238,6 +246,7 @@ int backward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, 
     d.L = gr.rows;
     d.y = const_cast<void*>(dw.p);
     d.ldy = dw.ld;
+    d.packed = base + L.parts + part_bytes(L.wgrad, d.M, d.N2);
     d.strideB = dw.stride;
     if ((err = oz2_launch_product(dtype, OZ2_WGRAD, L.wgrad, d, s)) != hipSuccess) return hip_status(err);
   }
@@ -259,43 +268,62 @@ bool int_ok(const void* p) { return p && (uintptr_t)p % 4 == 0; }
 //   128 x 128: 5 a launch; workgroups alone on their CU 0.55 a stage (fp32 2.1); two a
 //              CU 3 + 1.1 (4.2) a stage a round
 //   a sum in s parts: 4 for the second launch, the parts written and read at 4 TB/s
+//   operands whose rows are not whole 16-byte pieces: copied first (4, and 4 TB/s), or
+//   128 x 128 tiles by way of registers, 2.6 (4.0 two a CU; fp32 1 more) a stage
 // for instance bf16 (256 / 128 tiles): 4096^3 120 / 153, 2048^2 x 4096 82 / 43 (two
 // parts 48), 1024^2 x 4096 79 / 37 (two 27, four 26), 512^2 x 4096 78 / 36 (four 18),
 // 1024^3 27 / 13 (two 17), 6144 x 4096 x 1024 67 / 61.
 // Groups: their sizes are not known here; even ones are assumed, and the sum stays
 // whole.  Few rows a group: see k_rows.
-Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr) {
+Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr, bool padded) {
   const double cus = oz2_device_cus();
   const bool wide = dtype == OZ2_F32;
   if (side == OZ2_FWD) {
-    if (!gr.offsets && M <= 64) return Oz2Plan{M <= 16 ? 1 : M <= 32 ? 2 : 4, false, 1};
-    if (gr.offsets && M <= 8ll * gr.groups) return Oz2Plan{M <= 2ll * gr.groups ? 1 : 2, false, 1};
+    if (!gr.offsets && M <= 64) return Oz2Plan{M <= 16 ? 1 : M <= 32 ? 2 : 4, false, 1, 0, 0};
+    if (gr.offsets && M <= 8ll * gr.groups) return Oz2Plan{M <= 2ll * gr.groups ? 1 : 2, false, 1, 0, 0};
   }
-  const double stages = std::max<double>(1.0, std::ceil((double)L * (wide ? 4 : 2) / 128.0 /
-                                                        (gr.offsets && side == OZ2_WGRAD ? gr.groups : 1)));
+  const ll e = wide ? 4 : 2, groups = gr.offsets ? gr.groups : 1;
+  const double stages = std::max<double>(1.0, std::ceil((double)L * e / 128.0 /
+                                                        (side == OZ2_WGRAD ? groups : 1)));
+  // rows of A and B as they lie in memory
+  const ll wa = side == OZ2_WGRAD ? M : L, wb = side == OZ2_FWD ? L : N2;
+  const ll ra = side == OZ2_WGRAD ? L : M, rb = side == OZ2_FWD ? groups * N2 : side == OZ2_DGRAD ? groups * L : L;
+  const int odd = (!padded && wa * e % 16 ? 1 : 0) | (wb * e % 16 ? 2 : 0);
+  const size_t packed = (odd & 1 ? (size_t)ra * oz2_packed_pitch(wa, e) * e : 0) +
+                        (odd & 2 ? (size_t)rb * oz2_packed_pitch(wb, e) * e : 0);
   auto tiles = [&](double t) {
     if (!gr.offsets) return std::ceil(M / t) * std::ceil(N2 / t);
     if (side == OZ2_WGRAD) return std::ceil(M / t) * std::ceil(N2 / t) * gr.groups;
     return std::ceil((double)M / gr.groups / t) * gr.groups * std::ceil(N2 / t);
   };
-  Oz2Plan best{0, false, 1};
+  Oz2Plan best{0, false, 1, 0, 0};
   double t_best = 1e30;
-  if (!wide) {
-    const double n = tiles(256.0), load = std::min(1.0, n / cus);
-    best.big = true;
-    t_best = 6.0 + std::max(1.0, n <= 4.0 * cus ? std::ceil(n / cus) : n / cus) * (8.0 + stages * (1.05 + 0.6 * load));
-  }
-  const double n = tiles(128.0), alone = wide ? 2.1 : 0.55, full = wide ? 4.2 : 1.1;
+  const double n = tiles(128.0), big = tiles(256.0);
   const int most = gr.offsets ? 1 : (int)std::min(32.0, std::max(1.0, stages / 4.0));
-  for (int s = 1; s <= most; ++s) {
-    if (s > 1 && n * s > 2.0 * cus) break;
-    const double per = std::ceil(stages / s), wgs = n * s;
-    double t = wgs <= cus ? 5.0 + per * alone
-                          : 5.0 + (wgs <= 8.0 * cus ? std::ceil(wgs / (2.0 * cus)) : wgs / (2.0 * cus)) * (3.0 + per * full);
-    if (s > 1) t += 4.0 + s * (double)M * N2 * 8.0 / 4e6;
-    if (t < t_best) {
-      t_best = t;
-      best = Oz2Plan{0, false, s};
+  for (int pack = 0; pack <= (odd ? 1 : 0); ++pack) {
+    const double first = pack ? 4.0 + (double)packed / 2e6 : 0.0;
+    const bool slow = odd && !pack;
+    if (!wide && !slow) {
+      const double load = std::min(1.0, big / cus);
+      const double t = first + 6.0 + std::max(1.0, big <= 4.0 * cus ? std::ceil(big / cus) : big / cus) *
+                                         (8.0 + stages * (1.05 + 0.6 * load));
+      if (t < t_best) {
+        t_best = t;
+        best = Oz2Plan{0, true, 1, pack ? odd : 0, pack ? packed : 0};
+      }
+    }
+    const double alone = wide ? 2.1 + slow : slow ? 2.6 : 0.55, full = wide ? 4.2 + slow : slow ? 4.0 : 1.1;
+    for (int s = 1; s <= most; ++s) {
+      if (s > 1 && n * s > 2.0 * cus) break;
+      const double per = std::ceil(stages / s), wgs = n * s;
+      double t = wgs <= cus ? 5.0 + per * alone
+                            : 5.0 + (wgs <= 8.0 * cus ? std::ceil(wgs / (2.0 * cus)) : wgs / (2.0 * cus)) *
+                                        (3.0 + per * full);
+      if (s > 1) t += 4.0 + s * (double)M * N2 * 8.0 / 4e6;
+      if ((t += first) < t_best) {
+        t_best = t;
+        best = Oz2Plan{0, false, s, pack ? odd : 0, pack ? packed : 0};
+      }
     }
   }
   return best;

@@ -11,6 +11,7 @@ Outputs and workspaces that are not given are allocated on the stream of the cal
 """
 from __future__ import annotations
 
+from functools import lru_cache
 from typing import NamedTuple
 
 from . import _lib
@@ -31,21 +32,37 @@ class ExpertOrder(NamedTuple):
     slots: "torch.Tensor"     # noqa: F821
 
 
-_codes = None
+_torch = None
+_codes = {}
+
+# bytes of workspace, functions of types and sizes alone
+_linear_bytes = lru_cache(4096)(lambda *a: _lib.ozaki2_linear_workspace_bytes(*a))
+_linear_backward_bytes = lru_cache(4096)(
+    lambda *a: _lib.ozaki2_linear_backward_workspace_bytes(*a))
+_grouped_bytes = lru_cache(4096)(lambda *a: _lib.ozaki2_grouped_linear_workspace_bytes(*a))
+_grouped_backward_bytes = lru_cache(4096)(
+    lambda *a: _lib.ozaki2_grouped_linear_backward_workspace_bytes(*a))
+_sort_bytes = lru_cache(4096)(lambda *a: _lib.ozaki2_expert_sort_workspace_bytes(*a))
+
+
+def _init():
+    """torch is imported by the first call, as everywhere in this package"""
+    global _torch
+    import torch
+    _codes.update({torch.float32: _lib.OZ2_F32, torch.float16: _lib.OZ2_F16,
+                   torch.bfloat16: _lib.OZ2_BF16})
+    _torch = torch
 
 
 def _dtype(name, t):
-    global _codes
-    import torch
-    if _codes is None:
-        _codes = {torch.float32: _lib.OZ2_F32, torch.float16: _lib.OZ2_F16,
-                  torch.bfloat16: _lib.OZ2_BF16}
-    if not isinstance(t, torch.Tensor):
+    if _torch is None:
+        _init()
+    if not isinstance(t, _torch.Tensor):
         raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
-    try:
-        return _codes[t.dtype]
-    except KeyError:
-        raise ValueError(f"{name}: expected float32, float16 or bfloat16, got {t.dtype}") from None
+    code = _codes.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name}: expected float32, float16 or bfloat16, got {t.dtype}")
+    return code
 
 
 def _act(activation):
@@ -57,28 +74,30 @@ def _act(activation):
 
 
 def _device(name, t):
-    if t.device.type != "cuda":
-        raise ValueError(f"{name}: expected a tensor on a CUDA device, got one on {t.device}")
-    return t.device
+    dev = t.device
+    if dev.type != "cuda":
+        raise ValueError(f"{name}: expected a tensor on a CUDA device, got one on {dev}")
+    return dev
 
 
 def _tensor(name, t, like, shape, dtype=None):
     """The C ABI sees pointers and sizes only: what does not match is refused here."""
-    import torch
-    if not isinstance(t, torch.Tensor):
+    if not isinstance(t, _torch.Tensor):
         raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
     if t.shape != shape:
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.dtype != (dtype or like.dtype):
+    if t.dtype is not (dtype or like.dtype):
         raise ValueError(f"{name}: expected dtype {dtype or like.dtype}, got {t.dtype}")
     if t.device != like.device:
         raise ValueError(f"{name}: expected a tensor on {like.device}, got one on {t.device}")
 
 
 def _ld(name, t):
-    """Distance of the rows of a 2-D tensor whose rows are contiguous (a dimension
-    of size 1 carries no stride)."""
+    """Distance of the rows of a tensor whose rows are contiguous (a dimension of
+    size 1 carries no stride)."""
     rows, cols = t.shape[-2:]
+    if t.is_contiguous():
+        return cols or 1
     if cols > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}: the elements of a row must be adjacent (stride 1)")
     if rows <= 1:
@@ -114,41 +133,45 @@ def _vectors(name, t, like, shape):
     return t.stride(0) if len(shape) == 2 and shape[0] > 1 else 0
 
 
-def _dim2(name, t, n=2):
-    if t.dim() != n:
-        raise ValueError(f"{name}: expected {n} dimensions, got shape {tuple(t.shape)}")
-    return t.shape
+def _p(t):
+    return None if t is None else t.data_ptr()
 
 
 def _launch(device, stream, call):
     """call(stream handle) with ``device`` and the stream current, so that what
     it allocates belongs to the stream that uses it."""
-    import torch
-    index = device.index
+    cuda = _torch.cuda
     if stream is None:
-        if index is None or index == torch.cuda.current_device():
-            return call(torch.cuda.current_stream().cuda_stream)
-        with torch.cuda.device(device):
-            return call(torch.cuda.current_stream().cuda_stream)
+        if device.index == cuda.current_device():
+            return call(cuda.current_stream().cuda_stream)
+        with cuda.device(device):
+            return call(cuda.current_stream().cuda_stream)
     if isinstance(stream, int):
-        stream = (torch.cuda.ExternalStream(stream, device=device) if stream
-                  else torch.cuda.default_stream(device))
+        stream = (cuda.ExternalStream(stream, device=device) if stream
+                  else cuda.default_stream(device))
     if stream.device != device:
         raise ValueError(f"stream: on {stream.device}, the tensors on {device}")
-    with torch.cuda.stream(stream):
+    with cuda.stream(stream):
         return call(stream.cuda_stream)
 
 
 def _workspace(workspace, need, device):
+    """(tensor, its pointer, its bytes)"""
     if workspace is None:
         if not need:
-            return None, 0
-        import torch
-        return torch.empty(need, dtype=torch.uint8, device=device), need
+            return None, None, 0
+        workspace = _torch.empty(need, dtype=_torch.uint8, device=device)
+        return workspace, workspace.data_ptr(), need
     if workspace.device != device:
         raise ValueError("workspace: on another device")
     # the library checks its size
-    return workspace, workspace.numel() * workspace.element_size()
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _dim2(name, t, n=2):
+    if t.dim() != n:
+        raise ValueError(f"{name}: expected {n} dimensions, got shape {tuple(t.shape)}")
+    return t.shape
 
 
 # ------------------------------------------------------------------ dense
@@ -164,7 +187,7 @@ def linear(x, w, bias=None, residual=None, activation="none", gated=False,
     itself."""
     code, act, dev = _dtype("x", x), _act(activation), _device("x", x)
     T, K = _dim2("x", x)
-    n2 = _dim2("w", w)[0]
+    n2, _ = _dim2("w", w)
     if gated and n2 % 2:
         raise ValueError(f"w: a gated layer has an even number of rows, got {n2}")
     N = n2 // 2 if gated else n2
@@ -172,16 +195,15 @@ def linear(x, w, bias=None, residual=None, activation="none", gated=False,
     if bias is not None:
         _vectors("bias", bias, x, (n2,))
     ldr = _matrix("residual", residual, x, (T, N)) if residual is not None else 0
-    if out is not None:
-        _matrix("out", out, x, (T, N))
-    need = _lib.ozaki2_linear_workspace_bytes(code, gated, T, N, K)
+    ldy = _matrix("out", out, x, (T, N)) if out is not None else N
+    need = _linear_bytes(code, gated, T, N, K)
 
     def call(s):
         y = x.new_empty((T, N)) if out is None else out
         z = x.new_empty((T, n2)) if save_preactivation else None
-        ws, nb = _workspace(workspace, need, dev)
-        _lib.ozaki2_linear(code, act, gated, T, N, K, x, ldx, w, ldw, bias, residual, ldr, y,
-                           _ld("out", y), z, n2, ws, nb, s)
+        keep, ws, nb = _workspace(workspace, need, dev)
+        _lib.ozaki2_linear(code, act, gated, T, N, K, x.data_ptr(), ldx, w.data_ptr(), ldw, _p(bias),
+                           _p(residual), ldr, y.data_ptr(), ldy, _p(z), n2, ws, nb, s)
         return (y, z) if save_preactivation else y
     return _launch(dev, stream, call)
 
@@ -203,16 +225,18 @@ def linear_backward(dy, x, w, preactivation=None, activation="none", gated=False
             _matrix(name, t, dy, shape)
     if dbias is not None:
         _vectors("dbias", dbias, dy, (n2,))
-    need = _lib.ozaki2_linear_backward_workspace_bytes(code, act, gated, T, N, K)
+    need = _linear_backward_bytes(code, act, gated, T, N, K)
 
     def call(s):
         gx = dy.new_empty((T, K)) if need_dx and dx is None else dx
         gw = dy.new_empty((n2, K)) if need_dw and dw is None else dw
         gb = dy.new_empty((n2,)) if need_dbias and dbias is None else dbias
-        ws, nb = _workspace(workspace, need, dev)
-        _lib.ozaki2_linear_backward(code, act, gated, T, N, K, dy, lddy, x, ldx, w, ldw, z, ldz,
-                                    gx, _ld("dx", gx) if gx is not None else 0,
-                                    gw, _ld("dw", gw) if gw is not None else 0, gb, ws, nb, s)
+        keep, ws, nb = _workspace(workspace, need, dev)
+        _lib.ozaki2_linear_backward(code, act, gated, T, N, K, dy.data_ptr(), lddy, x.data_ptr(),
+                                    ldx, w.data_ptr(), ldw, _p(z), ldz,
+                                    _p(gx), _ld("dx", gx) if gx is not None else 0,
+                                    _p(gw), _ld("dw", gw) if gw is not None else 0, _p(gb), ws, nb,
+                                    s)
         return gx, gw, gb
     return _launch(dev, stream, call)
 
@@ -229,8 +253,7 @@ def _preactivation(z, act, gated, like, shape):
 # ---------------------------------------------------------------- experts
 
 def _offsets(offsets, groups, like):
-    import torch
-    _dense("offsets", offsets, like, (groups + 1,), torch.int32)
+    _dense("offsets", offsets, like, (groups + 1,), _torch.int32)
 
 
 def grouped_linear(x, w, offsets, bias=None, activation="none", gated=False,
@@ -248,16 +271,16 @@ def grouped_linear(x, w, offsets, bias=None, activation="none", gated=False,
     ldw, sw = _stack("w", w, x, (G, n2, K))
     _offsets(offsets, G, x)
     sb = _vectors("bias", bias, x, (G, n2)) if bias is not None else 0
-    if out is not None:
-        _matrix("out", out, x, (S, N))
-    need = _lib.ozaki2_grouped_linear_workspace_bytes(code, gated, S, G, N, K)
+    ldy = _matrix("out", out, x, (S, N)) if out is not None else N
+    need = _grouped_bytes(code, gated, S, G, N, K)
 
     def call(s):
         y = x.new_empty((S, N)) if out is None else out
         z = x.new_empty((S, n2)) if save_preactivation else None
-        ws, nb = _workspace(workspace, need, dev)
-        _lib.ozaki2_grouped_linear(code, act, gated, S, G, N, K, offsets, x, ldx, w, ldw, sw, bias,
-                                   sb, y, _ld("out", y), z, n2, ws, nb, s)
+        keep, ws, nb = _workspace(workspace, need, dev)
+        _lib.ozaki2_grouped_linear(code, act, gated, S, G, N, K, offsets.data_ptr(), x.data_ptr(),
+                                   ldx, w.data_ptr(), ldw, sw, _p(bias), sb, y.data_ptr(), ldy,
+                                   _p(z), n2, ws, nb, s)
         return (y, z) if save_preactivation else y
     return _launch(dev, stream, call)
 
@@ -282,18 +305,19 @@ def grouped_linear_backward(dy, x, w, offsets, preactivation=None, activation="n
         _stack("dw", dw, dy, (G, n2, K))
     if dbias is not None:
         _vectors("dbias", dbias, dy, (G, n2))
-    need = _lib.ozaki2_grouped_linear_backward_workspace_bytes(code, act, gated, S, G, N, K)
+    need = _grouped_backward_bytes(code, act, gated, S, G, N, K)
 
     def call(s):
         gx = dy.new_empty((S, K)) if need_dx and dx is None else dx
         gw = dy.new_empty((G, n2, K)) if need_dw and dw is None else dw
         gb = dy.new_empty((G, n2)) if need_dbias and dbias is None else dbias
-        ws, nb = _workspace(workspace, need, dev)
+        keep, ws, nb = _workspace(workspace, need, dev)
         _lib.ozaki2_grouped_linear_backward(
-            code, act, gated, S, G, N, K, offsets, dy, lddy, x, ldx, w, ldw, sw, z, ldz,
-            gx, _ld("dx", gx) if gx is not None else 0,
-            gw, _ld("dw", gw) if gw is not None else 0, gw.stride(0) if gw is not None else 0,
-            gb, gb.stride(0) if gb is not None else 0, ws, nb, s)
+            code, act, gated, S, G, N, K, offsets.data_ptr(), dy.data_ptr(), lddy, x.data_ptr(),
+            ldx, w.data_ptr(), ldw, sw, _p(z), ldz,
+            _p(gx), _ld("dx", gx) if gx is not None else 0,
+            _p(gw), _ld("dw", gw) if gw is not None else 0, gw.stride(0) if gw is not None else 0,
+            _p(gb), gb.stride(0) if gb is not None else 0, ws, nb, s)
         return gx, gw, gb
     return _launch(dev, stream, call)
 
@@ -301,7 +325,9 @@ def grouped_linear_backward(dy, x, w, offsets, preactivation=None, activation="n
 def expert_sort(experts, num_experts, workspace=None, stream=None):
     """The ExpertOrder of experts [tokens, top_k] (int32 or int64): stable; a
     value outside [0, num_experts) drops its pair."""
-    import torch
+    if _torch is None:
+        _init()
+    torch = _torch
     if not isinstance(experts, torch.Tensor):
         raise TypeError(f"experts: expected a torch tensor, got {type(experts).__name__}")
     if experts.dtype not in (torch.int32, torch.int64):
@@ -311,37 +337,36 @@ def expert_sort(experts, num_experts, workspace=None, stream=None):
     ld = _ld("experts", experts)
     if num_experts < 1 or num_experts > _lib.OZ2_MAX_EXPERTS:
         raise ValueError(f"num_experts: expected 1 to {_lib.OZ2_MAX_EXPERTS}, got {num_experts}")
-    need = _lib.ozaki2_expert_sort_workspace_bytes(T, k, num_experts)
+    need = _sort_bytes(T, k, num_experts)
 
     def call(s):
         kw = dict(dtype=torch.int32, device=dev)
         o = ExpertOrder(torch.empty(num_experts + 1, **kw), torch.empty(T * k, **kw),
                         torch.empty((T, k), **kw))
-        ws, nb = _workspace(workspace, need, dev)
-        _lib.ozaki2_expert_sort(T, k, num_experts, experts, experts.dtype == torch.int64, ld,
-                                o.offsets, o.rows, o.slots, ws, nb, s)
+        keep, ws, nb = _workspace(workspace, need, dev)
+        _lib.ozaki2_expert_sort(T, k, num_experts, experts.data_ptr(),
+                                experts.dtype is torch.int64, ld, o.offsets.data_ptr(),
+                                o.rows.data_ptr(), o.slots.data_ptr(), ws, nb, s)
         return o
     return _launch(dev, stream, call)
 
 
 def _order(order, like, tokens=None):
-    """(slots, pointer to the number of pairs kept, T, k)"""
-    import torch
+    """(pointers to the slots and to the number of pairs kept, T, k)"""
     offsets, _, slots = order
     T, k = _dim2("order.slots", slots)
     if tokens is not None and T != tokens:
         raise ValueError(f"order.slots: expected {tokens} tokens, got {T}")
-    _dense("order.slots", slots, like, (T, k), torch.int32)
+    _dense("order.slots", slots, like, (T, k), _torch.int32)
     n, = _dim2("order.offsets", offsets, 1)
     if n < 2:
         raise ValueError("order.offsets: expected at least 2 entries")
-    _dense("order.offsets", offsets, like, (n,), torch.int32)
-    return slots, offsets.data_ptr() + 4 * (n - 1), T, k
+    _dense("order.offsets", offsets, like, (n,), _torch.int32)
+    return slots.data_ptr(), offsets.data_ptr() + 4 * (n - 1), T, k
 
 
 def _weights(weights, like, shape):
-    import torch
-    _dense("weights", weights, like, shape, torch.float32)
+    _dense("weights", weights, like, shape, _torch.float32)
     return weights
 
 
@@ -354,13 +379,12 @@ def expert_gather(x, order, weights=None, out=None, stream=None):
     ldx = _ld("x", x)
     if weights is not None:
         _weights(weights, x, (T, k))
-    if out is not None:
-        _matrix("out", out, x, (T * k, width))
+    ldo = _matrix("out", out, x, (T * k, width)) if out is not None else max(width, 1)
 
     def call(s):
         xs = x.new_empty((T * k, width)) if out is None else out
-        _lib.ozaki2_expert_gather(code, T, k, width, x, ldx, slots, kept, weights, xs,
-                                  _ld("out", xs), s)
+        _lib.ozaki2_expert_gather(code, T, k, width, x.data_ptr(), ldx, slots, kept, _p(weights),
+                                  xs.data_ptr(), ldo, s)
         return xs
     return _launch(dev, stream, call)
 
@@ -376,13 +400,12 @@ def expert_combine(ys, order, weights=None, residual=None, out=None, stream=None
     if weights is not None:
         _weights(weights, ys, (T, k))
     ldr = _matrix("residual", residual, ys, (T, width)) if residual is not None else 0
-    if out is not None:
-        _matrix("out", out, ys, (T, width))
+    ldo = _matrix("out", out, ys, (T, width)) if out is not None else max(width, 1)
 
     def call(s):
         y = ys.new_empty((T, width)) if out is None else out
-        _lib.ozaki2_expert_combine(code, T, k, width, ys, ldys, slots, kept, weights, residual,
-                                   ldr, y, _ld("out", y), s)
+        _lib.ozaki2_expert_combine(code, T, k, width, ys.data_ptr(), ldys, slots, kept, _p(weights),
+                                   _p(residual), ldr, y.data_ptr(), ldo, s)
         return y
     return _launch(dev, stream, call)
 
@@ -391,7 +414,6 @@ def expert_combine_backward(dy, ys, order, weights, need_dys=True, need_dweights
                             stream=None):
     """(dys, dweights) of ``expert_combine`` from dy [tokens, width]; zeros for
     dropped pairs, None for what is not needed.  The residual's gradient is dy."""
-    import torch
     code, dev = _dtype("dy", dy), _device("dy", dy)
     T0, width = _dim2("dy", dy)
     slots, kept, T, k = _order(order, dy, T0)
@@ -400,8 +422,9 @@ def expert_combine_backward(dy, ys, order, weights, need_dys=True, need_dweights
 
     def call(s):
         dys = dy.new_empty((T * k, width)) if need_dys else None
-        dw = torch.empty((T, k), dtype=torch.float32, device=dev) if need_dweights else None
-        _lib.ozaki2_expert_combine_backward(code, T, k, width, dy, lddy, ys, ldys, slots, kept,
-                                            weights, dys, max(width, 1), dw, s)
+        dw = _torch.empty((T, k), dtype=_torch.float32, device=dev) if need_dweights else None
+        _lib.ozaki2_expert_combine_backward(code, T, k, width, dy.data_ptr(), lddy, ys.data_ptr(),
+                                            ldys, slots, kept, weights.data_ptr(), _p(dys),
+                                            max(width, 1), _p(dw), s)
         return dys, dw
     return _launch(dev, stream, call)
