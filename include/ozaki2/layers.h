@@ -23,7 +23,9 @@
  * outputs that overlap an input or another output; OZ2_E_WORKSPACE for a
  * workspace that is smaller than the _workspace_bytes function says or not
  * 256-byte aligned).  A workspace of 0 bytes may be null.  Sizes of zero are
- * allowed: an empty sum is zero.
+ * allowed: an empty sum is zero.  Limits: rows and token-expert pairs up to 2^30,
+ * in and out up to 2^21, and matrices (all groups' weights together) below 2^40
+ * elements.
  * Results do not depend on timing: no atomics decide the order of a sum.
  * Infinities and NaN follow from the formulas in 32-bit arithmetic.
  */

@@ -149,42 +149,40 @@ k_sort_place(SortArgs a, const int* __restrict__ counts, int* __restrict__ offse
 }
 
 // ---------------------------------------------------------------- rows
-// LPR lanes walk the 16-byte pieces of one token's row; a token's row is read
-// once and meets all of its places.  All rows may start at any element.
-template <int LPR>
-__device__ __forceinline__ bool token_of(int tokens, int& t, int& lane) {
-  const ll id = (ll)blockIdx.x * 256 + threadIdx.x;
-  t = (int)min(id / LPR, (ll)tokens);
-  lane = (int)(id % LPR);
-  return t < tokens;
-}
+// LPR lanes walk the 16-byte pieces of one token's row; a token's row is read once and
+// meets all of its places.  All rows may start at any element.  Grids are bounded: a
+// workgroup goes on to the tokens a grid further.
+constexpr ll ROW_BLOCKS = 1 << 20;
+#define OZ2_TOKENS(t, lane)                                                                     \
+  const int lane = (int)(threadIdx.x % LPR);                                                    \
+  for (ll t = ((ll)blockIdx.x * 256 + threadIdx.x) / LPR; t < a.tokens; t += (ll)gridDim.x * 256 / LPR)
 
 template <class T, int LPR>
 __global__ void __launch_bounds__(256)
 k_gather(Oz2Tokens a, const T* __restrict__ x, ll ldx, T* __restrict__ xs, ll ldxs) {
   constexpr int P = 16 / sizeof(T);
-  int t, lane;
-  if (!token_of<LPR>(a.tokens, t, lane)) return;
   const int pairs = a.tokens * a.top_k, kept = min(*a.kept, pairs);
   const int pieces = (a.width + P - 1) / P;
-  const int* sl = a.slots + (ll)t * a.top_k;
-  const float* wt = a.weights ? a.weights + (ll)t * a.top_k : nullptr;
-  for (int c = lane + LPR * (int)blockIdx.y; c < pieces; c += LPR * (int)gridDim.y) {
-    const int valid = a.width - c * P;
-    const Piece<T, P> v = load_piece<T>(x + t * ldx + (ll)c * P, valid);
-    for (int j = 0; j < a.top_k; ++j) {
-      const int s = sl[j];
-      if (s < 0 || s >= pairs) continue;
-      Piece<T, P> o = v;
-      if (s >= kept) {
+  OZ2_TOKENS(t, lane) {
+    const int* sl = a.slots + t * a.top_k;
+    const float* wt = a.weights ? a.weights + t * a.top_k : nullptr;
+    for (int c = lane + LPR * (int)blockIdx.y; c < pieces; c += LPR * (int)gridDim.y) {
+      const int valid = a.width - c * P;
+      const Piece<T, P> v = load_piece<T>(x + t * ldx + (ll)c * P, valid);
+      for (int j = 0; j < a.top_k; ++j) {
+        const int s = sl[j];
+        if (s < 0 || s >= pairs) continue;
+        Piece<T, P> o = v;
+        if (s >= kept) {
 #pragma unroll
-        for (int i = 0; i < P; ++i) o.v[i] = (T)0.0f;
-      } else if (wt) {
-        const float f = wt[j];
+          for (int i = 0; i < P; ++i) o.v[i] = (T)0.0f;
+        } else if (wt) {
+          const float f = wt[j];
 #pragma unroll
-        for (int i = 0; i < P; ++i) o.v[i] = from_f<T>(f * to_f(v.v[i]));
+          for (int i = 0; i < P; ++i) o.v[i] = from_f<T>(f * to_f(v.v[i]));
+        }
+        store_stream(xs + s * ldxs + (ll)c * P, o, valid);
       }
-      store_stream(xs + s * ldxs + (ll)c * P, o, valid);
     }
   }
 }
@@ -193,46 +191,46 @@ template <class T, int LPR>
 __global__ void __launch_bounds__(256)
 k_combine(Oz2Tokens a, const T* __restrict__ ys, ll ldys, const T* res, ll ldr, T* y, ll ldy) {
   constexpr int P = 16 / sizeof(T), UN = 4;
-  int t, lane;
-  if (!token_of<LPR>(a.tokens, t, lane)) return;
   const int kept = min(*a.kept, a.tokens * a.top_k);
   const int pieces = (a.width + P - 1) / P;
-  const int* sl = a.slots + (ll)t * a.top_k;
-  const float* wt = a.weights ? a.weights + (ll)t * a.top_k : nullptr;
-  for (int c = lane + LPR * (int)blockIdx.y; c < pieces; c += LPR * (int)gridDim.y) {
-    const int valid = a.width - c * P;
-    float sum[P];
-    if (res) {
-      const Piece<T, P> r = load_piece<T>(res + t * ldr + (ll)c * P, valid);
+  OZ2_TOKENS(t, lane) {
+    const int* sl = a.slots + t * a.top_k;
+    const float* wt = a.weights ? a.weights + t * a.top_k : nullptr;
+    for (int c = lane + LPR * (int)blockIdx.y; c < pieces; c += LPR * (int)gridDim.y) {
+      const int valid = a.width - c * P;
+      float sum[P];
+      if (res) {
+        const Piece<T, P> r = load_piece<T>(res + t * ldr + (ll)c * P, valid);
 #pragma unroll
-      for (int i = 0; i < P; ++i) sum[i] = to_f(r.v[i]);
-    } else {
+        for (int i = 0; i < P; ++i) sum[i] = to_f(r.v[i]);
+      } else {
 #pragma unroll
-      for (int i = 0; i < P; ++i) sum[i] = 0.0f;
-    }
-    for (int j0 = 0; j0 < a.top_k; j0 += UN) {   // UN rows in flight
-      Piece<T, P> v[UN];
-      float f[UN];
-      bool on[UN];
-#pragma unroll
-      for (int u = 0; u < UN; ++u) {
-        const int j = j0 + u;
-        const int s = j < a.top_k ? sl[j] : -1;
-        on[u] = s >= 0 && s < kept;
-        f[u] = on[u] && wt ? wt[j] : 1.0f;
-        if (on[u]) v[u] = load_piece<T>(ys + s * ldys + (ll)c * P, valid);
+        for (int i = 0; i < P; ++i) sum[i] = 0.0f;
       }
+      for (int j0 = 0; j0 < a.top_k; j0 += UN) {   // UN rows in flight
+        Piece<T, P> v[UN];
+        float f[UN];
+        bool on[UN];
 #pragma unroll
-      for (int u = 0; u < UN; ++u)
-        if (on[u]) {
-#pragma unroll
-          for (int i = 0; i < P; ++i) sum[i] += f[u] * to_f(v[u].v[i]);
+        for (int u = 0; u < UN; ++u) {
+          const int j = j0 + u;
+          const int s = j < a.top_k ? sl[j] : -1;
+          on[u] = s >= 0 && s < kept;
+          f[u] = on[u] && wt ? wt[j] : 1.0f;
+          if (on[u]) v[u] = load_piece<T>(ys + s * ldys + (ll)c * P, valid);
         }
-    }
-    Piece<T, P> o;
 #pragma unroll
-    for (int i = 0; i < P; ++i) o.v[i] = from_f<T>(sum[i]);
-    store_stream(y + t * ldy + (ll)c * P, o, valid);
+        for (int u = 0; u < UN; ++u)
+          if (on[u]) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) sum[i] += f[u] * to_f(v[u].v[i]);
+          }
+      }
+      Piece<T, P> o;
+#pragma unroll
+      for (int i = 0; i < P; ++i) o.v[i] = from_f<T>(sum[i]);
+      store_stream(y + t * ldy + (ll)c * P, o, valid);
+    }
   }
 }
 
@@ -244,75 +242,74 @@ k_combine_backward(Oz2Tokens a, const T* __restrict__ dy, ll lddy, const T* __re
                    T* __restrict__ dys, ll lddys, float* __restrict__ dw) {
   constexpr int P = 16 / sizeof(T), UN = 4;
   __shared__ float red[4][UN];
-  int t, lane;
-  const bool live = token_of<LPR>(a.tokens, t, lane);
-  if (LPR <= 64 && !live) return;   // LPR = 256: one token per workgroup, all live
   const int pairs = a.tokens * a.top_k, kept = min(*a.kept, pairs);
   const int pieces = (a.width + P - 1) / P;
-  const int* sl = a.slots + (ll)t * a.top_k;
-  const float* wt = a.weights + (ll)t * a.top_k;
-  for (int j0 = 0; j0 < a.top_k; j0 += UN) {
-    int s[UN];
-    float f[UN], dot[UN];
-#pragma unroll
-    for (int u = 0; u < UN; ++u) {
-      const int j = j0 + u;
-      s[u] = j < a.top_k ? sl[j] : -1;
-      if (s[u] >= pairs) s[u] = -1;
-      f[u] = s[u] >= 0 && s[u] < kept ? wt[j] : 0.0f;
-      dot[u] = 0.0f;
-    }
-    for (int c = lane; c < pieces; c += LPR) {
-      const int valid = a.width - c * P;
-      const Piece<T, P> g = load_piece<T>(dy + t * lddy + (ll)c * P, valid);
-      Piece<T, P> v[UN];
-      if (dw) {
-#pragma unroll
-        for (int u = 0; u < UN; ++u)
-          if (s[u] >= 0 && s[u] < kept) v[u] = load_piece<T>(ys + s[u] * ldys + (ll)c * P, valid);
-      }
+  OZ2_TOKENS(t, lane) {   // (LPR = 256: one token a workgroup, so its barriers are met by all)
+    const int* sl = a.slots + t * a.top_k;
+    const float* wt = a.weights + t * a.top_k;
+    for (int j0 = 0; j0 < a.top_k; j0 += UN) {
+      int s[UN];
+      float f[UN], dot[UN];
 #pragma unroll
       for (int u = 0; u < UN; ++u) {
-        if (s[u] < 0) continue;
-        const bool on = s[u] < kept;
-        if (dw && on) {
+        const int j = j0 + u;
+        s[u] = j < a.top_k ? sl[j] : -1;
+        if (s[u] >= pairs) s[u] = -1;
+        f[u] = s[u] >= 0 && s[u] < kept ? wt[j] : 0.0f;
+        dot[u] = 0.0f;
+      }
+      for (int c = lane; c < pieces; c += LPR) {
+        const int valid = a.width - c * P;
+        const Piece<T, P> g = load_piece<T>(dy + t * lddy + (ll)c * P, valid);
+        Piece<T, P> v[UN];
+        if (dw) {
 #pragma unroll
-          for (int i = 0; i < P; ++i) dot[u] += to_f(g.v[i]) * to_f(v[u].v[i]);
+          for (int u = 0; u < UN; ++u)
+            if (s[u] >= 0 && s[u] < kept) v[u] = load_piece<T>(ys + s[u] * ldys + (ll)c * P, valid);
         }
-        if (dys) {
-          Piece<T, P> o;
 #pragma unroll
-          for (int i = 0; i < P; ++i) o.v[i] = from_f<T>(on ? f[u] * to_f(g.v[i]) : 0.0f);
-          store_stream(dys + s[u] * lddys + (ll)c * P, o, valid);
+        for (int u = 0; u < UN; ++u) {
+          if (s[u] < 0) continue;
+          const bool on = s[u] < kept;
+          if (dw && on) {
+#pragma unroll
+            for (int i = 0; i < P; ++i) dot[u] += to_f(g.v[i]) * to_f(v[u].v[i]);
+          }
+          if (dys) {
+            Piece<T, P> o;
+#pragma unroll
+            for (int i = 0; i < P; ++i) o.v[i] = from_f<T>(on ? f[u] * to_f(g.v[i]) : 0.0f);
+            store_stream(dys + s[u] * lddys + (ll)c * P, o, valid);
+          }
         }
       }
-    }
-    if (!dw) continue;
-#pragma unroll
-    for (int u = 0; u < UN; ++u)
-#pragma unroll
-      for (int d = 1; d < (LPR < 64 ? LPR : 64); d <<= 1) dot[u] += __shfl_xor(dot[u], d);
-    if (LPR > 64) {
-      if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-        for (int u = 0; u < UN; ++u) red[threadIdx.x >> 6][u] = dot[u];
-      }
-      __syncthreads();
-#pragma unroll
-      for (int u = 0; u < UN; ++u) dot[u] = (red[0][u] + red[1][u]) + (red[2][u] + red[3][u]);
-      __syncthreads();
-    }
-    if (lane == 0) {
+      if (!dw) continue;
 #pragma unroll
       for (int u = 0; u < UN; ++u)
-        if (j0 + u < a.top_k) dw[(ll)t * a.top_k + j0 + u] = dot[u];
+#pragma unroll
+        for (int d = 1; d < (LPR < 64 ? LPR : 64); d <<= 1) dot[u] += __shfl_xor(dot[u], d);
+      if (LPR > 64) {
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+          for (int u = 0; u < UN; ++u) red[threadIdx.x >> 6][u] = dot[u];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < UN; ++u) dot[u] = (red[0][u] + red[1][u]) + (red[2][u] + red[3][u]);
+        __syncthreads();
+      }
+      if (lane == 0) {
+#pragma unroll
+        for (int u = 0; u < UN; ++u)
+          if (j0 + u < a.top_k) dw[t * a.top_k + j0 + u] = dot[u];
+      }
     }
   }
 }
 
 // workgroups over the tokens, and over pieces of long rows until the chip is full
 dim3 row_grid(int tokens, int lpr, int pieces) {
-  const ll bx = ((ll)tokens * lpr + 255) / 256;
+  const ll bx = std::min(ROW_BLOCKS, ((ll)tokens * lpr + 255) / 256);
   const int want = (int)std::max<ll>(1, 2 * oz2_device_cus() / bx);
   return dim3((unsigned)bx, (unsigned)std::min(want, (pieces + lpr - 1) / lpr));
 }
@@ -386,11 +383,12 @@ hipError_t oz2_launch_combine_backward(int dtype, const Oz2Tokens& t, const void
   OZ2_TYPE(dtype, {
     const int pieces = (t.width + 16 / (int)sizeof(T) - 1) / (16 / (int)sizeof(T));
     if (pieces > 128) {
-      hipLaunchKernelGGL((k_combine_backward<T, 256>), dim3(t.tokens), dim3(256), 0, s, t, (const T*)dy,
+      hipLaunchKernelGGL((k_combine_backward<T, 256>), dim3((unsigned)std::min<ll>(t.tokens, ROW_BLOCKS)), dim3(256), 0, s,
+                         t, (const T*)dy,
                          lddy, (const T*)ys, ldys, (T*)dys, lddys, dw);
     } else {
       const int lpr = lanes_per_row(pieces);
-      const unsigned bx = (unsigned)(((ll)t.tokens * lpr + 255) / 256);
+      const unsigned bx = (unsigned)std::min(ROW_BLOCKS, ((ll)t.tokens * lpr + 255) / 256);
       OZ2_LANES(lpr, k_combine_backward, hipLaunchKernelGGL(f, dim3(bx), dim3(256), 0, s, t, (const T*)dy,
                                                             lddy, (const T*)ys, ldys, (T*)dys, lddys, dw));
     }

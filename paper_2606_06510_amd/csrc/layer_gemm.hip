@@ -862,7 +862,7 @@ template <class T, int TB, bool GATED>
 __global__ void __launch_bounds__(RNT)
 k_rows(Oz2Product p) {
   constexpr int P = 16 / sizeof(T), KC = SB2 / sizeof(T), G = GATED ? 2 : 1;
-  constexpr int UN = TB == 1 && !GATED ? 8 : TB <= 2 ? 4 : 2;
+  constexpr int UN = TB == 1 && !GATED ? 8 : 4;
   __shared__ v4f red[RW][G * TB][64];
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 15, g = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -973,10 +973,8 @@ hipError_t launch_rows(int blocks, const Oz2Product& p, hipStream_t s) {
   const dim3 grid((unsigned)((p.N + 15) / 16), (unsigned)(p.gr.groups + (p.gr.offsets ? 1 : 0)));
   if (blocks == 1)
     hipLaunchKernelGGL((k_rows<T, 1, GATED>), grid, dim3(RNT), 0, s, p);
-  else if (blocks == 2)
-    hipLaunchKernelGGL((k_rows<T, 2, GATED>), grid, dim3(RNT), 0, s, p);
   else
-    hipLaunchKernelGGL((k_rows<T, 4, GATED>), grid, dim3(RNT), 0, s, p);
+    hipLaunchKernelGGL((k_rows<T, 2, GATED>), grid, dim3(RNT), 0, s, p);
   return hipGetLastError();
 }
 
@@ -997,16 +995,15 @@ template <class T>
 __global__ void __launch_bounds__(256)
 k_pack(Rows a, Rows b) {
   constexpr int P = 16 / sizeof(T);
-  ll row = (ll)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const bool second = row >= a.rows;
-  if (second) row -= a.rows;
-  const Rows& m = second ? b : a;
-  if (row >= m.rows) return;
-  const ll k = row / m.per;
-  const T* src = (const T*)m.src + k * m.stride + (row - k * m.per) * m.ld;
-  T* dst = (T*)m.dst + row * m.pitch;
-  for (int c = (threadIdx.x & 63) * P; c < m.pitch; c += 64 * P)
-    store_piece(dst + c, load_piece<T>(src + c, m.cols - c), P);
+  for (ll row = (ll)blockIdx.x * 4 + (threadIdx.x >> 6); row < a.rows + b.rows; row += (ll)gridDim.x * 4) {
+    const bool second = row >= a.rows;
+    const Rows& m = second ? b : a;
+    const ll r = second ? row - a.rows : row, k = r / m.per;
+    const T* src = (const T*)m.src + k * m.stride + (r - k * m.per) * m.ld;
+    T* dst = (T*)m.dst + r * m.pitch;
+    for (int c = (threadIdx.x & 63) * P; c < m.pitch; c += 64 * P)
+      store_piece(dst + c, load_piece<T>(src + c, m.cols - c), P);
+  }
 }
 
 template <class T>
@@ -1034,7 +1031,8 @@ hipError_t pack(Oz2Side side, const Oz2Plan& plan, Oz2Product& p, hipStream_t s)
   }
   const ll rows = r[0].rows + r[1].rows;
   if (rows == 0) return hipSuccess;
-  hipLaunchKernelGGL(k_pack<T>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, r[0], r[1]);
+  hipLaunchKernelGGL(k_pack<T>, dim3((unsigned)std::min<ll>(1 << 20, (rows + 3) / 4)), dim3(256), 0, s, r[0],
+                     r[1]);
   return hipGetLastError();
 }
 
@@ -1080,11 +1078,13 @@ k_slope(Oz2Slope p) {
   constexpr int P = 16 / sizeof(T), U = 2;
   constexpr bool SLOPED = GATED || ACT != OZ2_ACT_NONE;
   __shared__ float red[8][32 * 2 * P];
-  if ((int)blockIdx.x >= group_tiles(p.gr, p.sum_rows)) return;
+  // a row's pieces in a row of workgroups: whole rows are read at a time
+  const int cb = (p.n + 32 * P - 1) / (32 * P), tile = (int)(blockIdx.x / cb), cc = (int)blockIdx.x - tile * cb;
+  if (tile >= group_tiles(p.gr, p.sum_rows)) return;
   int group, row, end;
-  group_tile(p.gr, p.sum_rows, (int)blockIdx.x, group, row, end);
+  group_tile(p.gr, p.sum_rows, tile, group, row, end);
   end = min(end, row + p.sum_rows);
-  const int c = ((int)blockIdx.y * 32 + (int)(threadIdx.x & 31)) * P, rr = threadIdx.x >> 5;
+  const int c = (cc * 32 + (int)(threadIdx.x & 31)) * P, rr = threadIdx.x >> 5;
   const int n2 = GATED ? 2 * p.n : p.n, valid = p.n - c;
   float sg[P], su[P];
 #pragma unroll
@@ -1150,9 +1150,9 @@ k_slope(Oz2Slope p) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) s += red[k][q];
     const int piece = q / (2 * P), i = q % (2 * P);
-    const int col = ((int)blockIdx.y * 32 + piece) * P + i % P;
+    const int col = (cc * 32 + piece) * P + i % P;
     const bool up = i >= P;
-    if (col < p.n && (!up || GATED)) p.part[(ll)blockIdx.x * n2 + (up ? p.n + col : col)] = s;
+    if (col < p.n && (!up || GATED)) p.part[(ll)tile * n2 + (up ? p.n + col : col)] = s;
   }
 }
 
@@ -1209,7 +1209,7 @@ hipError_t launch_slope(Oz2Slope p, hipStream_t s) {
   while (p.sum_rows < 128 && (ll)p.gr.rows / p.sum_rows * cb > 8ll * oz2_device_cus()) p.sum_rows *= 2;
   const ll rt = oz2_row_tiles(p.gr, p.sum_rows);
   if (rt > 0 && cb > 0) {
-    const dim3 grid((unsigned)rt, (unsigned)cb);
+    const dim3 grid((unsigned)(rt * cb));
 #define OZ2_SLOPE(ACT)                                                          \
   case ACT:                                                                     \
     if (p.gated)                                                                \

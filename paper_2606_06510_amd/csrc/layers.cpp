@@ -274,12 +274,15 @@ bool int_ok(const void* p) { return p && (uintptr_t)p % 4 == 0; }
 // parts 48), 1024^2 x 4096 79 / 37 (two 27, four 26), 512^2 x 4096 78 / 36 (four 18),
 // 1024^3 27 / 13 (two 17), 6144 x 4096 x 1024 67 / 61.
 // Groups: their sizes are not known here; even ones are assumed, and the sum stays
-// whole.  Few rows a group: see k_rows.
+// whole.
+// Few rows (on average, of groups): k_rows, one read of W; its reads of x for every 16
+// columns pass the time of tiles beyond 32 rows (4096^2 bf16, rows / 128-row tiles: 32
+// rows 13.9 / 18.9, 64 rows 21.3 / 18.9; gated 11008 x 4096, 64 rows 70 / 38).
 Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr, bool padded) {
   const double cus = oz2_device_cus();
   const bool wide = dtype == OZ2_F32;
   if (side == OZ2_FWD) {
-    if (!gr.offsets && M <= 64) return Oz2Plan{M <= 16 ? 1 : M <= 32 ? 2 : 4, false, 1, 0, 0};
+    if (!gr.offsets && M <= 32) return Oz2Plan{M <= 16 ? 1 : 2, false, 1, 0, 0};
     if (gr.offsets && M <= 8ll * gr.groups) return Oz2Plan{M <= 2ll * gr.groups ? 1 : 2, false, 1, 0, 0};
   }
   const ll e = wide ? 4 : 2, groups = gr.offsets ? gr.groups : 1;

@@ -51,7 +51,7 @@ struct Oz2Product {
 };
 
 // How a product runs: `rows` > 0: the kernel of few rows, that many blocks of 16 at a
-// time (1, 2, 4; FWD); else 256 x 256 tiles (16 bits, and operands that direct loads
+// time (1 or 2; FWD); else 256 x 256 tiles (16 bits, and operands that direct loads
 // take) or 128 x 128 ones, the sum in how many parts, joined by a second launch.
 struct Oz2Plan {
   int rows;
