@@ -85,17 +85,19 @@ __device__ __forceinline__ void acc_settle() {
 // piece and 4-11 of the next) lie in different banks.
 __device__ __forceinline__ int row_swz(int r) { return (r >> 1) & 7; }
 
-// Rows contiguous along the tile's other dimension: [l][R entries], R = 128 or
-// 256, the 16-byte pieces of row l permuted so that the rows read together lie in
-// different banks: blocks of 16 columns (2 pieces of 16 bits, 4 of 32) by an
-// exclusive or with col_swz.
-template <class T>
+// Rows contiguous along the tile's other dimension: [l][R entries], the 16-byte pieces
+// of row l permuted so that the rows read together lie in different banks: blocks of
+// 16 columns (2 pieces of 16 bits, 4 of 32) by an exclusive or with col_swz, less than
+// the R / 16 blocks of a row.
+template <class T, int R>
 __device__ __forceinline__ int col_swz(int l) {
-  return sizeof(T) == 2 ? (l & 3) | ((l >> 3) & 1) << 2 : (l >> 2) & 3;
+  if (sizeof(T) == 4) return (l >> 2) & 3;
+  return R == 64 ? (l & 3) ^ ((l >> 3) & 1) : (l & 3) | ((l >> 3) & 1) << 2;
 }
-template <class T>
+template <class T, int R>
 __device__ __forceinline__ int col_piece(int l, int piece) {
-  return piece ^ (col_swz<T>(l) * (sizeof(T) == 2 ? 2 : 4));
+  static_assert(R % 64 == 0 && (sizeof(T) == 4 || R == 64 || R >= 128), "col_swz");
+  return piece ^ (col_swz<T, R>(l) * (sizeof(T) == 2 ? 2 : 4));
 }
 
 // The fragment of block b (16 rows) and step h of a stage of a tile of R rows at LDS address `base`.
@@ -110,10 +112,10 @@ struct Reader {
       sw = 0;
     } else if (sizeof(T) == 2) {
       const int l = 8 * g + (r >> 2);   // and + 4 in the second read
-      sw = col_swz<T>(l);
+      sw = col_swz<T, R>(l);
       at = (uint32_t)(l * R * 2 + 8 * (r & 3));
     } else {
-      sw = col_swz<T>(4 * g);
+      sw = col_swz<T, R>(4 * g);
       at = (uint32_t)(4 * g * R * 4 + 4 * r);
     }
   }
@@ -204,7 +206,7 @@ struct Stream {
       for (int u = 0; u < N; ++u) {
         const int q = (w + W * u) * 64 + lane;
         l[u] = q / PR;
-        const int c = col_piece<T>(l[u], q % PR);
+        const int c = col_piece<T, R>(l[u], q % PR);
         vo[u] = c * P >= cols ? kNowhere : (uint32_t)(l[u] * ld * (ll)sizeof(T)) + 16u * c;
       }
     }
@@ -226,7 +228,7 @@ __device__ __forceinline__ int w_col(int q, bool gated) {
 }
 
 // ------------------------------------------------ tiles
-constexpr int TM = 128, NT = 256;   // of the small tiles
+constexpr int TM = 128, NT = 256;   // of the smaller tiles; threads of all
 
 struct Tile {
   int group, row, end;   // rows of D; group -1: rows of no group
@@ -495,10 +497,10 @@ __device__ __forceinline__ void streams(const Oz2Product& p, const Tile& t, int 
 // multiplied, the next one's fragments are read into the other set of registers; once
 // every wave holds a stage's last fragments, the loads of the stage after the next go
 // out into its place.  One barrier a stage.
-constexpr int BT = 256, BNT = 256, BOP = BT * SB2, BST = 2 * BOP;
+constexpr int BT = 256, BOP = BT * SB2, BST = 2 * BOP;
 
 template <class T, Oz2Side SIDE>
-__global__ void __launch_bounds__(BNT, 1)
+__global__ void __launch_bounds__(NT, 1)
 k_product256(Oz2Product p, int ncol) {
   constexpr bool AR = SIDE != OZ2_WGRAD, BR = SIDE == OZ2_FWD;
   constexpr int KE = SB2 / sizeof(T);
@@ -506,7 +508,7 @@ k_product256(Oz2Product p, int ncol) {
   Tile t;
   if (!tile_of<SIDE>(p, BT, ncol, t)) return;
   if (SIDE != OZ2_WGRAD && t.group < 0) {
-    zero_rows<T>(p, t.row, t.end, t.col0, p.gated ? BT / 2 : BT, BT, BNT);
+    zero_rows<T>(p, t.row, t.end, t.col0, p.gated ? BT / 2 : BT, BT, NT);
     return;
   }
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds8*)LB;
@@ -575,58 +577,59 @@ k_product256(Oz2Product p, int ncol) {
                              128 * wc, lane);
 }
 
-// ------------------------------------------------ 128 x 128 tiles
-// For products with few large tiles, and all of fp32.  4 waves, 64 x 64 outputs each;
-// two 32 KiB stages of 128 bytes of l, so that two workgroups of a CU cover each
-// other's waits.
-constexpr int DOP = TM * SB2, DST = 2 * DOP;
-
-template <class T, Oz2Side SIDE>
-__global__ void __launch_bounds__(NT, 2)
+// ------------------------------------------------ 128 x 128 and 64 x 64 tiles
+// For products with few large tiles, and all of fp32.  4 waves, 64 x 64 (16 x 64)
+// outputs each; two stages of 128 bytes of l, 32 (16) KiB each, so that two (four)
+// workgroups of a CU cover each other's waits.
+template <class T, Oz2Side SIDE, int TILE>
+__global__ void __launch_bounds__(NT, TILE == 128 ? 2 : 4)
 k_product128(Oz2Product p, int ncol) {
   constexpr bool AR = SIDE != OZ2_WGRAD, BR = SIDE == OZ2_FWD;
-  constexpr int KE = SB2 / sizeof(T);
-  __shared__ __attribute__((aligned(16))) uint8_t LB[2 * DST];
+  constexpr int KE = SB2 / sizeof(T), OP = TILE * SB2, ST = 2 * OP, MI = TILE == 128 ? 4 : 1;
+  constexpr int EP = 4 * 16 * 68 * 4;   // of the epilogue
+  __shared__ __attribute__((aligned(16))) uint8_t LB[2 * ST > EP ? 2 * ST : EP];
   Tile t;
-  if (!tile_of<SIDE>(p, TM, ncol, t)) return;
+  if (!tile_of<SIDE>(p, TILE, ncol, t)) return;
   if (SIDE != OZ2_WGRAD && t.group < 0) {
-    zero_rows<T>(p, t.row, t.end, t.col0, p.gated ? TM / 2 : TM, TM, NT);
+    zero_rows<T>(p, t.row, t.end, t.col0, p.gated ? TILE / 2 : TILE, TILE, NT);
     return;
   }
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds8*)LB;
   const int lane = threadIdx.x & 63;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = w >> 1, wc = w & 1;
-  Stream<T, AR, TM, 4> sa;
-  Stream<T, BR, TM, 4> sb;
-  streams<T, SIDE, TM>(p, t, w, lane, sa, sb);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = TILE == 128 ? w >> 1 : w, wc = TILE == 128 ? w & 1 : 0;
+  Stream<T, AR, TILE, 4> sa;
+  Stream<T, BR, TILE, 4> sb;
+  streams<T, SIDE, TILE>(p, t, w, lane, sa, sb);
+  constexpr int N = Stream<T, AR, TILE, 4>::N;
   const int len = t.l1 - t.l0, n = (len + KE - 1) / KE;
   auto issue = [&](int it) {
-    const uint32_t at = lds0 + (it & 1) * DST + 1024u * w;
+    const uint32_t at = lds0 + (it & 1) * ST + 1024u * w;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) sa.issue(u, at, len - it * KE);
+    for (int u = 0; u < N; ++u) sa.issue(u, at, len - it * KE);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) sb.issue(u, at + DOP, len - it * KE);
+    for (int u = 0; u < N; ++u) sb.issue(u, at + OP, len - it * KE);
   };
   issue(0);   // (stages beyond the last are loaded as zeros)
   issue(1);
-  const Reader<T, AR, TM> ra(lane);
-  const Reader<T, BR, TM> rb(lane);
-  v4f acc[4][4];
+  const Reader<T, AR, TILE> ra(lane);
+  const Reader<T, BR, TILE> rb(lane);
+  v4f acc[4][MI];
 #pragma unroll
   for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0; i < MI; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
   for (int it = 0; it < n; ++it) {
-    const uint8_t* st = LB + (it & 1) * DST;
-    Frag<T> fa[2][4], fb[2][4];
-    wait_vm<8>();
+    const uint8_t* st = LB + (it & 1) * ST;
+    Frag<T> fa[2][MI], fb[2][4];
+    wait_vm<2 * N>();
     bar();
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) fb[h][j] = rb.get(st + DOP, 4 * wc + j, h);
+      for (int j = 0; j < 4; ++j) fb[h][j] = rb.get(st + OP, 4 * wc + j, h);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) fa[h][i] = ra.get(st, 4 * wr + i, h);
+      for (int i = 0; i < MI; ++i) fa[h][i] = ra.get(st, MI * wr + i, h);
     }
     wait_lds();
     bar();
@@ -634,19 +637,21 @@ k_product128(Oz2Product p, int ncol) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[j][i] = mma(fb[h][j], fa[h][i], acc[j][i]);
   }
   wait_vm<0>();
   __syncthreads();
-  epilogue<T, SIDE, 4, 1, 1>(p, acc, reinterpret_cast<float*>(LB) + w * 16 * 68, t, t.row + 64 * wr, 64 * wc,
-                             lane);
+  epilogue<T, SIDE, MI, 1, 1>(p, acc, reinterpret_cast<float*>(LB) + w * 16 * 68, t, t.row + 16 * MI * wr,
+                              64 * wc, lane);
 }
 
 // ------------------------------------------------ 128 x 128 tiles, by way of registers
 // The same for operands that direct loads do not take: rows of any length from any
 // address.  A stage waits in LDS, the next two on their way in registers.
+
+constexpr int DOP = TM * SB2, DST = 2 * DOP;
 
 // A thread's four 16-byte pieces of an operand's stage
 template <class T, bool ROWS>
@@ -677,7 +682,7 @@ struct Loader {
         const int c = q % PR;
         src[u] = base + l[u] * ld + c * P;
         valid[u] = cols - c * P;
-        dst[u] = (uint32_t)(l[u] * TM * sizeof(T) + 16 * col_piece<T>(l[u], c));
+        dst[u] = (uint32_t)(l[u] * TM * sizeof(T) + 16 * col_piece<T, TM>(l[u], c));
       }
     }
   }
@@ -786,14 +791,14 @@ bool direct(Oz2Side side, const Oz2Product& p, int tile) {
          direct_side<T>(p.B, p.ldb, side == OZ2_FWD, p.paddedB ? 0 : side == OZ2_FWD ? p.L : p.N2, tile);
 }
 
-#define OZ2_SIDES(kern, grid, threads)                                                  \
+#define OZ2_SIDES(kern, ...)                                                            \
   do {                                                                                  \
     if (side == OZ2_FWD)                                                                \
-      hipLaunchKernelGGL((kern<T, OZ2_FWD>), grid, dim3(threads), 0, s, p, ncol);       \
+      hipLaunchKernelGGL((kern<T, OZ2_FWD __VA_ARGS__>), grid, dim3(NT), 0, s, p, ncol);   \
     else if (side == OZ2_DGRAD)                                                         \
-      hipLaunchKernelGGL((kern<T, OZ2_DGRAD>), grid, dim3(threads), 0, s, p, ncol);     \
+      hipLaunchKernelGGL((kern<T, OZ2_DGRAD __VA_ARGS__>), grid, dim3(NT), 0, s, p, ncol); \
     else                                                                                \
-      hipLaunchKernelGGL((kern<T, OZ2_WGRAD>), grid, dim3(threads), 0, s, p, ncol);     \
+      hipLaunchKernelGGL((kern<T, OZ2_WGRAD __VA_ARGS__>), grid, dim3(NT), 0, s, p, ncol); \
     return hipGetLastError();                                                           \
   } while (0)
 
@@ -1037,19 +1042,18 @@ hipError_t pack(Oz2Side side, const Oz2Plan& plan, Oz2Product& p, hipStream_t s)
 }
 
 template <class T>
-hipError_t launch_tiles(Oz2Side side, bool big, const Oz2Product& p, hipStream_t s) {
+hipError_t launch_tiles(Oz2Side side, int tile, const Oz2Product& p, hipStream_t s) {
   int ncol;
-  if constexpr (sizeof(T) == 2) {
-    if (big && direct<T>(side, p, BT)) {
-      dim3 grid = tile_grid(side, p, BT, ncol);
-      grid.y = p.splits;
-      OZ2_SIDES(k_product256, grid, BNT);
-    }
-  }
-  dim3 grid = tile_grid(side, p, TM, ncol);
+  // (operands that direct loads do not take: 128 x 128 whatever the plan)
+  if (!direct<T>(side, p, tile)) tile = 0;
+  dim3 grid = tile_grid(side, p, tile ? tile : TM, ncol);
   grid.y = p.splits;
-  if (direct<T>(side, p, TM)) OZ2_SIDES(k_product128, grid, NT);
-  OZ2_SIDES(k_product, grid, NT);
+  if constexpr (sizeof(T) == 2) {
+    if (tile == BT) OZ2_SIDES(k_product256);
+  }
+  if (tile == 128) OZ2_SIDES(k_product128, , 128);
+  if (tile == 64) OZ2_SIDES(k_product128, , 64);
+  OZ2_SIDES(k_product);
 }
 
 template <class T>
@@ -1060,7 +1064,7 @@ hipError_t launch_product(Oz2Side side, const Oz2Plan& plan, Oz2Product p, hipSt
   if (plan.rows) return p.gated ? launch_rows<T, true>(plan.rows, p, s) : launch_rows<T, false>(plan.rows, p, s);
   hipError_t e = plan.pack ? pack<T>(side, plan, p, s) : hipSuccess;
   if (e != hipSuccess) return e;
-  e = launch_tiles<T>(side, plan.big, p, s);
+  e = launch_tiles<T>(side, plan.tile, p, s);
   if (e != hipSuccess || p.splits == 1) return e;
   constexpr int W = 16 / sizeof(T);
   const ll items = (ll)p.M * ((p.N + W - 1) / W);

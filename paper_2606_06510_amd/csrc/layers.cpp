@@ -262,29 +262,32 @@ bool int_ok(const void* p) { return p && (uintptr_t)p % 4 == 0; }
 
 }  // namespace
 
-// The faster of the two tilings by a fit of measured times (us; L in stages of 128
-// bytes, CUs of a round):
+// The fastest of the tilings by a fit of measured times (us; L in stages of 128 bytes,
+// k workgroups on a CU):
 //   256 x 256: 6 a launch; a round of tiles 8 + 1.05 a stage, 1.65 on a full chip
-//   128 x 128: 5 a launch; workgroups alone on their CU 0.55 a stage (fp32 2.1); two a
-//              CU 3 + 1.1 (4.2) a stage a round
+//   128 x 128: 5 a launch; k = 1: 0.55 a stage (fp32 2.1); k = 2: 3 + 1.1 (4.2) a stage a
+//              round
+//   64 x 64:   3.5 a launch; 0.28 (0.67) a stage, from k = 2 to 4 0.21 k (0.61 k), and 2 a
+//              round
 //   a sum in s parts: 4 for the second launch, the parts written and read at 4 TB/s
 //   operands whose rows are not whole 16-byte pieces: copied first (4, and 4 TB/s), or
 //   128 x 128 tiles by way of registers, 2.6 (4.0 two a CU; fp32 1 more) a stage
-// for instance bf16 (256 / 128 tiles): 4096^3 120 / 153, 2048^2 x 4096 82 / 43 (two
-// parts 48), 1024^2 x 4096 79 / 37 (two 27, four 26), 512^2 x 4096 78 / 36 (four 18),
-// 1024^3 27 / 13 (two 17), 6144 x 4096 x 1024 67 / 61.
-// Groups: their sizes are not known here; even ones are assumed, and the sum stays
-// whole.
-// Few rows (on average, of groups): k_rows, one read of W; its reads of x for every 16
-// columns pass the time of tiles beyond 32 rows (4096^2 bf16, rows / 128-row tiles: 32
-// rows 13.9 / 18.9, 64 rows 21.3 / 18.9; gated 11008 x 4096, 64 rows 70 / 38).
+// for instance bf16 (256 / 128 / 64): 4096^3 120 / 153 / -, 2048^2 x 4096 82 / 42 / 53,
+// 1024^3 27 / 13 / 7.2, 1024^2 x 4096 79 / 36 (two parts 26) / 22, 512^2 x 1024 - / 12.5 /
+// 6.6, 128^2 x 8192 145 / 65 (eight 18) / 31 (eight 12), 6144 x 4096 x 1024 67 / 61 / -;
+// fp32 (128 / 64): 1024^3 71 (eight 36) / 25, 1500 x 1200 x 776 58 (two 41) / 34, 2048^2 x
+// 1024 80 / 83.
+//   few rows (k_rows): 2, W at 5.6 TB/s, and for each row 0.05 and 0.003 a megabyte of W
+//   (the workgroups' reads of x); bf16 (k_rows / tiles): 4096^2, 1 row 7.5 / 12, 16 rows
+//   10.4 / 13, 32 rows 13.9 / 13.6; gated 11008 x 4096, 1 row 34 / 30, 16 rows 39 / 29.
+//   Tiles read W at no more than 6.2 TB/s.
+// Groups: their sizes are not known here; even ones that end half a tile early are
+// assumed, and the sum stays whole.  At most 8 rows a group on average: k_rows.
 Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr, bool padded) {
   const double cus = oz2_device_cus();
   const bool wide = dtype == OZ2_F32;
-  if (side == OZ2_FWD) {
-    if (!gr.offsets && M <= 32) return Oz2Plan{M <= 16 ? 1 : 2, false, 1, 0, 0};
-    if (gr.offsets && M <= 8ll * gr.groups) return Oz2Plan{M <= 2ll * gr.groups ? 1 : 2, false, 1, 0, 0};
-  }
+  if (side == OZ2_FWD && gr.offsets && M <= 8ll * gr.groups)
+    return Oz2Plan{M <= 2ll * gr.groups ? 1 : 2, 0, 1, 0, 0};
   const ll e = wide ? 4 : 2, groups = gr.offsets ? gr.groups : 1;
   const double stages = std::max<double>(1.0, std::ceil((double)L * e / 128.0 /
                                                         (side == OZ2_WGRAD ? groups : 1)));
@@ -297,35 +300,43 @@ Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr
   auto tiles = [&](double t) {
     if (!gr.offsets) return std::ceil(M / t) * std::ceil(N2 / t);
     if (side == OZ2_WGRAD) return std::ceil(M / t) * std::ceil(N2 / t) * gr.groups;
-    return std::ceil((double)M / gr.groups / t) * gr.groups * std::ceil(N2 / t);
+    // (a group ends half a tile early on average)
+    return std::max(1.0, (double)M / gr.groups / t + 0.5) * gr.groups * std::ceil(N2 / t);
   };
-  Oz2Plan best{0, false, 1, 0, 0};
+  Oz2Plan best{0, 128, 1, 0, 0};
   double t_best = 1e30;
-  const double n = tiles(128.0), big = tiles(256.0);
+  const double mb = (double)groups * (side == OZ2_WGRAD ? M : L) * N2 * e / 1e6;   // of W (or dW)
+  if (side == OZ2_FWD && !gr.offsets && M <= 32) {
+    best = Oz2Plan{M <= 16 ? 1 : 2, 0, 1, 0, 0};
+    t_best = 2.0 + mb / 5.6 + (double)M * (0.05 + 0.003 * mb);
+  }
+  const double big = tiles(256.0);
   const int most = gr.offsets ? 1 : (int)std::min(32.0, std::max(1.0, stages / 4.0));
   for (int pack = 0; pack <= (odd ? 1 : 0); ++pack) {
     const double first = pack ? 4.0 + (double)packed / 2e6 : 0.0;
     const bool slow = odd && !pack;
+    auto take = [&](double t, int tile, int splits) {
+      t = std::max(t, 3.5 + mb / 6.2) + first + (splits > 1 ? 4.0 + splits * (double)M * N2 * 8.0 / 4e6 : 0.0);
+      if (t >= t_best) return;
+      t_best = t;
+      best = Oz2Plan{0, tile, splits, pack ? odd : 0, pack ? packed : 0};
+    };
     if (!wide && !slow) {
       const double load = std::min(1.0, big / cus);
-      const double t = first + 6.0 + std::max(1.0, big <= 4.0 * cus ? std::ceil(big / cus) : big / cus) *
-                                         (8.0 + stages * (1.05 + 0.6 * load));
-      if (t < t_best) {
-        t_best = t;
-        best = Oz2Plan{0, true, 1, pack ? odd : 0, pack ? packed : 0};
-      }
+      take(6.0 + std::max(1.0, big <= 4.0 * cus ? std::ceil(big / cus) : big / cus) *
+                     (8.0 + stages * (1.05 + 0.6 * load)), 256, 1);
     }
     const double alone = wide ? 2.1 + slow : slow ? 2.6 : 0.55, full = wide ? 4.2 + slow : slow ? 4.0 : 1.1;
     for (int s = 1; s <= most; ++s) {
-      if (s > 1 && n * s > 2.0 * cus) break;
-      const double per = std::ceil(stages / s), wgs = n * s;
-      double t = wgs <= cus ? 5.0 + per * alone
-                            : 5.0 + (wgs <= 8.0 * cus ? std::ceil(wgs / (2.0 * cus)) : wgs / (2.0 * cus)) *
-                                        (3.0 + per * full);
-      if (s > 1) t += 4.0 + s * (double)M * N2 * 8.0 / 4e6;
-      if ((t += first) < t_best) {
-        t_best = t;
-        best = Oz2Plan{0, false, s, pack ? odd : 0, pack ? packed : 0};
+      const double per = std::ceil(stages / s), w128 = tiles(128.0) * s, w64 = tiles(64.0) * s;
+      if (s == 1 || w128 <= 2.0 * cus)
+        take(w128 <= cus ? 5.0 + per * alone
+                         : 5.0 + (w128 <= 8.0 * cus ? std::ceil(w128 / (2.0 * cus)) : w128 / (2.0 * cus)) *
+                                     (3.0 + per * full), 128, s);
+      if (!slow && (s == 1 || w64 <= 4.0 * cus)) {
+        const double k = std::min(4.0, std::ceil(w64 / cus)), rounds = std::max(1.0, w64 / (4.0 * cus));
+        take(3.5 + rounds * (per * (wide ? std::max(0.67, 0.61 * k) : std::max(0.28, 0.21 * k)) +
+                             (rounds > 1.0 ? 2.0 : 0.0)), 64, s);
       }
     }
   }

@@ -51,11 +51,11 @@ struct Oz2Product {
 };
 
 // How a product runs: `rows` > 0: the kernel of few rows, that many blocks of 16 at a
-// time (1 or 2; FWD); else 256 x 256 tiles (16 bits, and operands that direct loads
-// take) or 128 x 128 ones, the sum in how many parts, joined by a second launch.
+// time (1 or 2; FWD); else tiles of 256 (16 bits), 128 or 64 rows and columns, the sum in
+// how many parts, joined by a second launch.
 struct Oz2Plan {
   int rows;
-  bool big;
+  int tile;
   int splits;
   int pack;              // 1: A, 2: B is first copied into rows of whole lines
   size_t packed_bytes;

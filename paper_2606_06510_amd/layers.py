@@ -82,22 +82,27 @@ def _device(name, t):
 
 def _tensor(name, t, like, shape, dtype=None):
     """The C ABI sees pointers and sizes only: what does not match is refused here."""
+    try:
+        if (t.shape == shape and t.dtype is (dtype or like.dtype) and t.device == like.device
+                and isinstance(t, _torch.Tensor)):
+            return
+    except AttributeError:
+        pass
     if not isinstance(t, _torch.Tensor):
         raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}")
     if t.shape != shape:
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
     if t.dtype is not (dtype or like.dtype):
         raise ValueError(f"{name}: expected dtype {dtype or like.dtype}, got {t.dtype}")
-    if t.device != like.device:
-        raise ValueError(f"{name}: expected a tensor on {like.device}, got one on {t.device}")
+    raise ValueError(f"{name}: expected a tensor on {like.device}, got one on {t.device}")
 
 
 def _ld(name, t):
     """Distance of the rows of a tensor whose rows are contiguous (a dimension of
     size 1 carries no stride)."""
-    rows, cols = t.shape[-2:]
     if t.is_contiguous():
-        return cols or 1
+        return t.shape[-1] or 1
+    rows, cols = t.shape[-2:]
     if cols > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}: the elements of a row must be adjacent (stride 1)")
     if rows <= 1:
@@ -128,9 +133,18 @@ def _dense(name, t, like, shape, dtype):
 def _vectors(name, t, like, shape):
     """Distance of the vectors (rows) of a 1-D or 2-D tensor."""
     _tensor(name, t, like, shape)
+    if t.is_contiguous():
+        return shape[-1]
     if shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}: the elements must be adjacent (stride 1)")
     return t.stride(0) if len(shape) == 2 and shape[0] > 1 else 0
+
+
+def _call(name, *args):
+    """A library entry point with pointers and handles as integers already"""
+    status = getattr(_lib.load(), name)(*args)
+    if status:
+        raise _lib.Ozaki2Error(name, status)
 
 
 def _p(t):
@@ -202,7 +216,7 @@ def linear(x, w, bias=None, residual=None, activation="none", gated=False,
         y = x.new_empty((T, N)) if out is None else out
         z = x.new_empty((T, n2)) if save_preactivation else None
         keep, ws, nb = _workspace(workspace, need, dev)
-        _lib.ozaki2_linear(code, act, gated, T, N, K, x.data_ptr(), ldx, w.data_ptr(), ldw, _p(bias),
+        _call("ozaki2_linear", code, act, gated, T, N, K, x.data_ptr(), ldx, w.data_ptr(), ldw, _p(bias),
                            _p(residual), ldr, y.data_ptr(), ldy, _p(z), n2, ws, nb, s)
         return (y, z) if save_preactivation else y
     return _launch(dev, stream, call)
@@ -232,7 +246,7 @@ def linear_backward(dy, x, w, preactivation=None, activation="none", gated=False
         gw = dy.new_empty((n2, K)) if need_dw and dw is None else dw
         gb = dy.new_empty((n2,)) if need_dbias and dbias is None else dbias
         keep, ws, nb = _workspace(workspace, need, dev)
-        _lib.ozaki2_linear_backward(code, act, gated, T, N, K, dy.data_ptr(), lddy, x.data_ptr(),
+        _call("ozaki2_linear_backward", code, act, gated, T, N, K, dy.data_ptr(), lddy, x.data_ptr(),
                                     ldx, w.data_ptr(), ldw, _p(z), ldz,
                                     _p(gx), _ld("dx", gx) if gx is not None else 0,
                                     _p(gw), _ld("dw", gw) if gw is not None else 0, _p(gb), ws, nb,
@@ -278,7 +292,7 @@ def grouped_linear(x, w, offsets, bias=None, activation="none", gated=False,
         y = x.new_empty((S, N)) if out is None else out
         z = x.new_empty((S, n2)) if save_preactivation else None
         keep, ws, nb = _workspace(workspace, need, dev)
-        _lib.ozaki2_grouped_linear(code, act, gated, S, G, N, K, offsets.data_ptr(), x.data_ptr(),
+        _call("ozaki2_grouped_linear", code, act, gated, S, G, N, K, offsets.data_ptr(), x.data_ptr(),
                                    ldx, w.data_ptr(), ldw, sw, _p(bias), sb, y.data_ptr(), ldy,
                                    _p(z), n2, ws, nb, s)
         return (y, z) if save_preactivation else y
@@ -312,8 +326,7 @@ def grouped_linear_backward(dy, x, w, offsets, preactivation=None, activation="n
         gw = dy.new_empty((G, n2, K)) if need_dw and dw is None else dw
         gb = dy.new_empty((G, n2)) if need_dbias and dbias is None else dbias
         keep, ws, nb = _workspace(workspace, need, dev)
-        _lib.ozaki2_grouped_linear_backward(
-            code, act, gated, S, G, N, K, offsets.data_ptr(), dy.data_ptr(), lddy, x.data_ptr(),
+        _call("ozaki2_grouped_linear_backward", code, act, gated, S, G, N, K, offsets.data_ptr(), dy.data_ptr(), lddy, x.data_ptr(),
             ldx, w.data_ptr(), ldw, sw, _p(z), ldz,
             _p(gx), _ld("dx", gx) if gx is not None else 0,
             _p(gw), _ld("dw", gw) if gw is not None else 0, gw.stride(0) if gw is not None else 0,
@@ -344,7 +357,7 @@ def expert_sort(experts, num_experts, workspace=None, stream=None):
         o = ExpertOrder(torch.empty(num_experts + 1, **kw), torch.empty(T * k, **kw),
                         torch.empty((T, k), **kw))
         keep, ws, nb = _workspace(workspace, need, dev)
-        _lib.ozaki2_expert_sort(T, k, num_experts, experts.data_ptr(),
+        _call("ozaki2_expert_sort", T, k, num_experts, experts.data_ptr(),
                                 experts.dtype is torch.int64, ld, o.offsets.data_ptr(),
                                 o.rows.data_ptr(), o.slots.data_ptr(), ws, nb, s)
         return o
@@ -383,7 +396,7 @@ def expert_gather(x, order, weights=None, out=None, stream=None):
 
     def call(s):
         xs = x.new_empty((T * k, width)) if out is None else out
-        _lib.ozaki2_expert_gather(code, T, k, width, x.data_ptr(), ldx, slots, kept, _p(weights),
+        _call("ozaki2_expert_gather", code, T, k, width, x.data_ptr(), ldx, slots, kept, _p(weights),
                                   xs.data_ptr(), ldo, s)
         return xs
     return _launch(dev, stream, call)
@@ -404,7 +417,7 @@ def expert_combine(ys, order, weights=None, residual=None, out=None, stream=None
 
     def call(s):
         y = ys.new_empty((T, width)) if out is None else out
-        _lib.ozaki2_expert_combine(code, T, k, width, ys.data_ptr(), ldys, slots, kept, _p(weights),
+        _call("ozaki2_expert_combine", code, T, k, width, ys.data_ptr(), ldys, slots, kept, _p(weights),
                                    _p(residual), ldr, y.data_ptr(), ldo, s)
         return y
     return _launch(dev, stream, call)
@@ -423,7 +436,7 @@ def expert_combine_backward(dy, ys, order, weights, need_dys=True, need_dweights
     def call(s):
         dys = dy.new_empty((T * k, width)) if need_dys else None
         dw = _torch.empty((T, k), dtype=_torch.float32, device=dev) if need_dweights else None
-        _lib.ozaki2_expert_combine_backward(code, T, k, width, dy.data_ptr(), lddy, ys.data_ptr(),
+        _call("ozaki2_expert_combine_backward", code, T, k, width, dy.data_ptr(), lddy, ys.data_ptr(),
                                             ldys, slots, kept, weights.data_ptr(), _p(dys),
                                             max(width, 1), _p(dw), s)
         return dys, dw
