@@ -1100,9 +1100,9 @@ k_slope(Oz2Slope p) {
 #pragma unroll
       for (int q = 0; q < U; ++q) {
         const ll t = min(t0 + 8 * q, end - 1);
-        g[q] = load_piece<T>((const T*)p.dy + t * p.lddy + c, valid);
-        if (SLOPED) a[q] = load_piece<T>((const T*)p.z + t * p.ldz + c, valid);
-        if (GATED) u[q] = load_piece<T>((const T*)p.z + t * p.ldz + p.n + c, valid);
+        g[q] = load_stream<T>((const T*)p.dy + t * p.lddy + c, valid);
+        if (SLOPED) a[q] = load_stream<T>((const T*)p.z + t * p.ldz + c, valid);
+        if (GATED) u[q] = load_stream<T>((const T*)p.z + t * p.ldz + p.n + c, valid);
       }
       float d[U * P], e[U * P];
 #pragma unroll

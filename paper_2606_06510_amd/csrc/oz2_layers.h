@@ -120,6 +120,15 @@ __device__ __forceinline__ void store_stream(T* p, const Piece<T, N>& r, int val
   }
   store_piece(p, r, valid);
 }
+// A piece that nobody reads again soon, past the caches likewise (the slope of 16384 x 2048
+// entries 62 -> 54 us)
+template <class T, int N = 16 / (int)sizeof(T)>
+__device__ __forceinline__ Piece<T, N> load_stream(const T* p, int valid) {
+  typedef uint32_t u4 __attribute__((ext_vector_type(4), aligned(2)));
+  if (valid >= N)
+    return __builtin_bit_cast(Piece<T, N>, __builtin_nontemporal_load(reinterpret_cast<const u4*>(p)));
+  return load_piece<T, N>(p, valid);
+}
 
 // f(x) and f'(x).  16-bit results take the hardware's exponential (2^-21
 // relative at worst, where the result keeps 2^-11); fp32 ones the library's.
