@@ -33,6 +33,7 @@ class ExpertOrder(NamedTuple):
 
 
 _torch = None
+_raw_stream = None
 _codes = {}
 
 # bytes of workspace, functions of types and sizes alone
@@ -47,8 +48,11 @@ _sort_bytes = lru_cache(4096)(lambda *a: _lib.ozaki2_expert_sort_workspace_bytes
 
 def _init():
     """torch is imported by the first call, as everywhere in this package"""
-    global _torch
+    global _torch, _raw_stream
     import torch
+    # the handle alone, where torch offers it (a Stream object takes 2.5 us to make)
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                          lambda index: torch.cuda.current_stream(index).cuda_stream)
     _codes.update({torch.float32: _lib.OZ2_F32, torch.float16: _lib.OZ2_F16,
                    torch.bfloat16: _lib.OZ2_BF16})
     _torch = torch
@@ -157,9 +161,9 @@ def _launch(device, stream, call):
     cuda = _torch.cuda
     if stream is None:
         if device.index == cuda.current_device():
-            return call(cuda.current_stream().cuda_stream)
+            return call(_raw_stream(device.index))
         with cuda.device(device):
-            return call(cuda.current_stream().cuda_stream)
+            return call(_raw_stream(device.index))
     if isinstance(stream, int):
         stream = (cuda.ExternalStream(stream, device=device) if stream
                   else cuda.default_stream(device))
