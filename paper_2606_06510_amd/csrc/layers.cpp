@@ -345,6 +345,16 @@ Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr
 
 extern "C" {
 
+void oz2_plan_of(int dtype, int side, ll M, ll N2, ll L, int rows, int groups, int padded, int* out) {
+  static const int any = 0;
+  const Oz2Plan p = oz2_plan(dtype, (Oz2Side)side, M, N2, L,
+                             Oz2Groups{groups ? &any : nullptr, groups ? groups : 1, rows}, padded != 0);
+  out[0] = p.rows;
+  out[1] = p.tile;
+  out[2] = p.splits;
+  out[3] = p.pack;
+}
+
 size_t ozaki2_linear_workspace_bytes(int dtype, int gated, int rows, int out, int in) {
   if (!sizes_ok(dtype, OZ2_ACT_NONE, rows, 1, out, in, gated)) return 0;
   return forward_bytes(dtype, gated, Oz2Groups{nullptr, 1, rows}, out, in);

@@ -64,6 +64,10 @@ inline ll oz2_packed_pitch(ll cols, size_t e) { return (cols * (ll)e + 127) / 12
 // padded: as in Oz2Product
 Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr,
                  bool padded = false);
+// the plan of a product (side 0, 1, 2; groups 0: one product) as rows, tile, splits and
+// pack: a diagnostic for tests, not part of the public ABI
+extern "C" void oz2_plan_of(int dtype, int side, ll M, ll N2, ll L, int rows, int groups, int padded,
+                            int* out);
 
 #ifdef __HIPCC__
 // products and sums of the epilogues may be fused; nothing here is compared bit for bit

@@ -220,8 +220,8 @@ def linear(x, w, bias=None, residual=None, activation="none", gated=False,
         y = x.new_empty((T, N)) if out is None else out
         z = x.new_empty((T, n2)) if save_preactivation else None
         keep, ws, nb = _workspace(workspace, need, dev)
-        _call("ozaki2_linear", code, act, gated, T, N, K, x.data_ptr(), ldx, w.data_ptr(), ldw, _p(bias),
-                           _p(residual), ldr, y.data_ptr(), ldy, _p(z), n2, ws, nb, s)
+        _call("ozaki2_linear", code, act, gated, T, N, K, x.data_ptr(), ldx, w.data_ptr(), ldw,
+              _p(bias), _p(residual), ldr, y.data_ptr(), ldy, _p(z), n2, ws, nb, s)
         return (y, z) if save_preactivation else y
     return _launch(dev, stream, call)
 
@@ -250,11 +250,10 @@ def linear_backward(dy, x, w, preactivation=None, activation="none", gated=False
         gw = dy.new_empty((n2, K)) if need_dw and dw is None else dw
         gb = dy.new_empty((n2,)) if need_dbias and dbias is None else dbias
         keep, ws, nb = _workspace(workspace, need, dev)
-        _call("ozaki2_linear_backward", code, act, gated, T, N, K, dy.data_ptr(), lddy, x.data_ptr(),
-                                    ldx, w.data_ptr(), ldw, _p(z), ldz,
-                                    _p(gx), _ld("dx", gx) if gx is not None else 0,
-                                    _p(gw), _ld("dw", gw) if gw is not None else 0, _p(gb), ws, nb,
-                                    s)
+        _call("ozaki2_linear_backward", code, act, gated, T, N, K, dy.data_ptr(), lddy,
+              x.data_ptr(), ldx, w.data_ptr(), ldw, _p(z), ldz, _p(gx),
+              _ld("dx", gx) if gx is not None else 0, _p(gw),
+              _ld("dw", gw) if gw is not None else 0, _p(gb), ws, nb, s)
         return gx, gw, gb
     return _launch(dev, stream, call)
 
@@ -296,9 +295,9 @@ def grouped_linear(x, w, offsets, bias=None, activation="none", gated=False,
         y = x.new_empty((S, N)) if out is None else out
         z = x.new_empty((S, n2)) if save_preactivation else None
         keep, ws, nb = _workspace(workspace, need, dev)
-        _call("ozaki2_grouped_linear", code, act, gated, S, G, N, K, offsets.data_ptr(), x.data_ptr(),
-                                   ldx, w.data_ptr(), ldw, sw, _p(bias), sb, y.data_ptr(), ldy,
-                                   _p(z), n2, ws, nb, s)
+        _call("ozaki2_grouped_linear", code, act, gated, S, G, N, K, offsets.data_ptr(),
+              x.data_ptr(), ldx, w.data_ptr(), ldw, sw, _p(bias), sb, y.data_ptr(), ldy, _p(z), n2,
+              ws, nb, s)
         return (y, z) if save_preactivation else y
     return _launch(dev, stream, call)
 
@@ -330,11 +329,11 @@ def grouped_linear_backward(dy, x, w, offsets, preactivation=None, activation="n
         gw = dy.new_empty((G, n2, K)) if need_dw and dw is None else dw
         gb = dy.new_empty((G, n2)) if need_dbias and dbias is None else dbias
         keep, ws, nb = _workspace(workspace, need, dev)
-        _call("ozaki2_grouped_linear_backward", code, act, gated, S, G, N, K, offsets.data_ptr(), dy.data_ptr(), lddy, x.data_ptr(),
-            ldx, w.data_ptr(), ldw, sw, _p(z), ldz,
-            _p(gx), _ld("dx", gx) if gx is not None else 0,
-            _p(gw), _ld("dw", gw) if gw is not None else 0, gw.stride(0) if gw is not None else 0,
-            _p(gb), gb.stride(0) if gb is not None else 0, ws, nb, s)
+        _call("ozaki2_grouped_linear_backward", code, act, gated, S, G, N, K, offsets.data_ptr(),
+              dy.data_ptr(), lddy, x.data_ptr(), ldx, w.data_ptr(), ldw, sw, _p(z), ldz, _p(gx),
+              _ld("dx", gx) if gx is not None else 0, _p(gw),
+              _ld("dw", gw) if gw is not None else 0, gw.stride(0) if gw is not None else 0, _p(gb),
+              gb.stride(0) if gb is not None else 0, ws, nb, s)
         return gx, gw, gb
     return _launch(dev, stream, call)
 
@@ -362,8 +361,8 @@ def expert_sort(experts, num_experts, workspace=None, stream=None):
                         torch.empty((T, k), **kw))
         keep, ws, nb = _workspace(workspace, need, dev)
         _call("ozaki2_expert_sort", T, k, num_experts, experts.data_ptr(),
-                                experts.dtype is torch.int64, ld, o.offsets.data_ptr(),
-                                o.rows.data_ptr(), o.slots.data_ptr(), ws, nb, s)
+              experts.dtype is torch.int64, ld, o.offsets.data_ptr(), o.rows.data_ptr(),
+              o.slots.data_ptr(), ws, nb, s)
         return o
     return _launch(dev, stream, call)
 
@@ -400,8 +399,8 @@ def expert_gather(x, order, weights=None, out=None, stream=None):
 
     def call(s):
         xs = x.new_empty((T * k, width)) if out is None else out
-        _call("ozaki2_expert_gather", code, T, k, width, x.data_ptr(), ldx, slots, kept, _p(weights),
-                                  xs.data_ptr(), ldo, s)
+        _call("ozaki2_expert_gather", code, T, k, width, x.data_ptr(), ldx, slots, kept,
+              _p(weights), xs.data_ptr(), ldo, s)
         return xs
     return _launch(dev, stream, call)
 
@@ -421,8 +420,8 @@ def expert_combine(ys, order, weights=None, residual=None, out=None, stream=None
 
     def call(s):
         y = ys.new_empty((T, width)) if out is None else out
-        _call("ozaki2_expert_combine", code, T, k, width, ys.data_ptr(), ldys, slots, kept, _p(weights),
-                                   _p(residual), ldr, y.data_ptr(), ldo, s)
+        _call("ozaki2_expert_combine", code, T, k, width, ys.data_ptr(), ldys, slots, kept,
+              _p(weights), _p(residual), ldr, y.data_ptr(), ldo, s)
         return y
     return _launch(dev, stream, call)
 
@@ -440,8 +439,8 @@ def expert_combine_backward(dy, ys, order, weights, need_dys=True, need_dweights
     def call(s):
         dys = dy.new_empty((T * k, width)) if need_dys else None
         dw = _torch.empty((T, k), dtype=_torch.float32, device=dev) if need_dweights else None
-        _call("ozaki2_expert_combine_backward", code, T, k, width, dy.data_ptr(), lddy, ys.data_ptr(),
-                                            ldys, slots, kept, weights.data_ptr(), _p(dys),
-                                            max(width, 1), _p(dw), s)
+        _call("ozaki2_expert_combine_backward", code, T, k, width, dy.data_ptr(), lddy,
+              ys.data_ptr(), ldys, slots, kept, weights.data_ptr(), _p(dys), max(width, 1), _p(dw),
+              s)
         return dys, dw
     return _launch(dev, stream, call)

@@ -18,8 +18,34 @@ ACTS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
 EACT = 2.0 ** -20
 
 
+ON_GPU = False   # 64-bit references of large sizes: torch's fp64 on the GPU
+
+
 def d(t):
-    return None if t is None else t.detach().cpu().double()
+    if t is None:
+        return None
+    return t.detach().double() if ON_GPU else t.detach().cpu().double()
+
+
+def plan(dtype, side, M, N2, L, rows, groups=0, padded=False):
+    """How the library runs a product: (few-row blocks, tile, splits, operands copied).
+    side: 0 forward, 1 gradient of x, 2 of w."""
+    import ctypes
+
+    import paper_2606_06510_amd as oz
+    f = oz.load().oz2_plan_of
+    ll, i = ctypes.c_longlong, ctypes.c_int
+    f.argtypes, f.restype = [i, i, ll, ll, ll, i, i, i, ctypes.POINTER(i)], None
+    out = (i * 4)()
+    f({"fp32": 0, "fp16": 1, "bf16": 2}[dtype], side, M, N2, L, rows, groups, padded, out)
+    return tuple(out)
+
+
+def plans(T, K, N, dtype, gated, sloped, groups=0):
+    """The three products of a layer"""
+    n2 = 2 * N if gated else N
+    return (plan(dtype, 0, T, n2, K, T, groups), plan(dtype, 1, T, K, n2, T, groups, sloped),
+            plan(dtype, 2, n2, K, T, T, groups, sloped))
 
 
 def act(z, name):

@@ -140,6 +140,28 @@ def test_rows_strides(pad, shift, dtype):
     check_rows(*rows_case(6, 2, 5, 2000, dtype, pad=pad, shift=shift))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_offsets_past_32_bits(dtype):
+    """rows so far apart that the last tokens' and places' begin past 2^32 bytes"""
+    T, k, width = 150, 2, 40
+    step = (1 << 24) // (2 if dtype == "bf16" else 4) + 8
+    c, order, kept, slots = rows_case(T, k, 5, width, dtype)
+    buf = torch.empty((T * k, step), dtype=lu.DTYPES[dtype], device=device())
+    for name, at in (("x", 0), ("ys", 64), ("dy", 128), ("r", 192)):
+        rows = c[name].shape[0]
+        buf[:rows, at:at + width] = c[name]
+        c[name] = buf[:rows, at:at + width]
+    check_rows(c, order, kept, slots)
+    ids = buf[:, 256:264].view(torch.int32)[:T, :k]
+    ids.copy_(ids_of(T, k, 5, seed=7, drop=0.1, wide=False))
+    o = oz().expert_sort(ids, 5)
+    offsets, rows, slots = lu.order(ids, 5)
+    assert o.offsets.tolist() == offsets and o.rows.tolist() == rows
+    c, order, kept, slots = rows_case(T, k, 5, width, dtype, seed=3)
+    xs = oz().expert_gather(c["x"], order, out=buf[:, :width])
+    assert torch.equal(xs, oz().expert_gather(c["x"], order))
+
+
 @pytest.mark.parametrize("dtype", list(lu.DTYPES))
 def test_rows_outputs_given(dtype):
     """in place of the residual, and into column ranges of wider buffers"""
