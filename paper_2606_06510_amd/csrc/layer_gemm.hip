@@ -497,14 +497,14 @@ __device__ __forceinline__ void streams(const Oz2Product& p, const Tile& t, int 
 // multiplied, the next one's fragments are read into the other set of registers; once
 // every wave holds a stage's last fragments, the loads of the stage after the next go
 // out into its place.  One barrier a stage.
-constexpr int BT = 256, BOP = BT * SB2, BST = 2 * BOP;
+constexpr int BT = 256, BOP = BT * SB2;
 
 template <class T, Oz2Side SIDE>
 __global__ void __launch_bounds__(NT, 1)
 k_product256(Oz2Product p, int ncol) {
   constexpr bool AR = SIDE != OZ2_WGRAD, BR = SIDE == OZ2_FWD;
   constexpr int KE = SB2 / sizeof(T);
-  __shared__ __attribute__((aligned(16))) uint8_t LB[2 * BST];
+  __shared__ __attribute__((aligned(16))) uint8_t LB[5 * BOP];   // 2 stages of A, 3 of B
   Tile t;
   if (!tile_of<SIDE>(p, BT, ncol, t)) return;
   if (SIDE != OZ2_WGRAD && t.group < 0) {
@@ -518,16 +518,18 @@ k_product256(Oz2Product p, int ncol) {
   Stream<T, BR, BT, 4> sb;
   streams<T, SIDE, BT>(p, t, w, lane, sa, sb);
   const int len = t.l1 - t.l0, n = (len + KE - 1) / KE;
-  auto issue = [&](int u, int it) {   // u < 16: the loads of a wave's share of stage it
-    const uint32_t at = lds0 + (it & 1) * BST + 1024u * w;
-    if (u & 1)
-      sa.issue(u >> 1, at, len - it * KE);
-    else
-      sb.issue(u >> 1, at + BOP, len - it * KE);
-  };
+  // the wave's share of stage it of A, and of B into place `at`
+  auto issue_a = [&](int u, int it) { sa.issue(u, lds0 + (it & 1) * BOP + 1024u * w, len - it * KE); };
+  auto issue_b = [&](int u, int it, int at) { sb.issue(u, lds0 + 2 * BOP + at + 1024u * w, len - it * KE); };
   // stages beyond the last one are loaded too, as zeros (nothing is read for them)
 #pragma unroll
-  for (int u = 0; u < 32; ++u) issue(u & 15, u >> 4);
+  for (int u = 0; u < 8; ++u) issue_a(u, 0);
+#pragma unroll
+  for (int u = 0; u < 16; ++u) issue_b(u & 7, u >> 3, (u >> 3) * BOP);
+#pragma unroll
+  for (int u = 0; u < 8; ++u) issue_a(u, 1);
+#pragma unroll
+  for (int u = 0; u < 8; ++u) issue_b(u, 2, 2 * BOP);
   const int wr = w >> 1, wc = w & 1;
   const Reader<T, AR, BT> ra(lane);
   const Reader<T, BR, BT> rb(lane);
@@ -537,22 +539,24 @@ k_product256(Oz2Product p, int ncol) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) acc[j][i] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
   Frag<T> fa[2][8], fb[2][8];   // of the two steps of a stage
-  wait_vm<16>();
+  wait_vm<24>();
   bar();
 #pragma unroll
-  for (int j = 0; j < 8; ++j) fb[0][j] = rb.get(LB + BOP, 8 * wc + j);
+  for (int j = 0; j < 8; ++j) fb[0][j] = rb.get(LB + 2 * BOP, 8 * wc + j);
 #pragma unroll
   for (int i = 0; i < 8; ++i) fa[0][i] = ra.get(LB, 8 * wr + i);
+  int at = 0;   // of B's stage it
   for (int it = 0; it < n; ++it) {
+    const int next = at == 2 * BOP ? 0 : at + BOP;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       wait_lds();
       if (h) {
         // all waves hold the last fragments of stage it, and stage it + 1 has landed
-        wait_vm<0>();
+        wait_vm<8>();
         bar();
       }
-      const uint8_t* st = LB + ((it + h) & 1) * BST;
+      const uint8_t *ta = LB + ((it + h) & 1) * BOP, *tb = LB + 2 * BOP + (h ? next : at);
       // a read or a load between two products, hardly ever more: the next product is
       // issued before the matrix unit has done with the last
 #pragma unroll
@@ -561,14 +565,20 @@ k_product256(Oz2Product p, int ncol) {
         if (m % 3 == 0 && m < 48) {
           const int k = m / 3;
           if (k < 8)
-            fb[1 - h][k] = rb.get(st + BOP, 8 * wc + k, 1 - h);
+            fb[1 - h][k] = rb.get(tb, 8 * wc + k, 1 - h);
           else
-            fa[1 - h][k - 8] = ra.get(st, 8 * wr + k - 8, 1 - h);
+            fa[1 - h][k - 8] = ra.get(ta, 8 * wr + k - 8, 1 - h);
         }
-        if (h && m % 3 == 1 && m < 48) issue(m / 3, it + 2);
+        if (h && m % 3 == 1 && m < 48) {
+          if (m < 24)
+            issue_a(m / 3, it + 2);
+          else
+            issue_b(m / 3 - 8, it + 3, at);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
+    at = next;
   }
   wait_vm<0>();
   acc_settle();
