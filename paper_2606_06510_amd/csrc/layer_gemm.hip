@@ -258,8 +258,13 @@ __device__ __forceinline__ bool tile_of(const Oz2Product& p, int tile, int ncol,
     t.l0 = 0;
     t.l1 = p.L;
     if (q >= 0) {
-      banded(q, nrow, ncol, r, c);
-      group_tile(p.gr, tile, r, t.group, t.row, t.end);
+      // in bands of one group's tiles
+      const int any = (int)(q / ncol);
+      int first;
+      group_tile(p.gr, tile, any, t.group, first, t.row, t.end);
+      const int start = t.row - (any - first) * tile;
+      banded(q - (ll)first * ncol, (t.end - start + tile - 1) / tile, ncol, r, c);
+      t.row = start + r * tile;
     } else {   // the rows outside the groups
       const ll k = b - (n + 7) / 8 * 8;
       if (k < 0 || !p.gr.offsets) return false;
@@ -1095,8 +1100,8 @@ k_slope(Oz2Slope p) {
   // a row's pieces in a row of workgroups: whole rows are read at a time
   const int cb = (p.n + 32 * P - 1) / (32 * P), tile = (int)(blockIdx.x / cb), cc = (int)blockIdx.x - tile * cb;
   if (tile >= group_tiles(p.gr, p.sum_rows)) return;
-  int group, row, end;
-  group_tile(p.gr, p.sum_rows, tile, group, row, end);
+  int group, first, row, end;
+  group_tile(p.gr, p.sum_rows, tile, group, first, row, end);
   end = min(end, row + p.sum_rows);
   const int c = (cc * 32 + (int)(threadIdx.x & 31)) * P, rr = threadIdx.x >> 5;
   const int n2 = GATED ? 2 * p.n : p.n, valid = p.n - c;

@@ -238,11 +238,11 @@ __device__ __forceinline__ int group_tiles(const Oz2Groups& g, int tile) {
   return __builtin_amdgcn_readfirstlane(n);
 }
 
-// Tile t < group_tiles() of the row tiles of all groups in turn: its group and
-// rows [row, end).  Likewise uniform.
-__device__ __forceinline__ void group_tile(const Oz2Groups& g, int tile, int t, int& group, int& row,
-                                           int& end) {
-  group = 0;
+// Tile t < group_tiles() of the row tiles of all groups in turn: its group, that group's
+// first tile, and its rows [row, end).  Likewise uniform.
+__device__ __forceinline__ void group_tile(const Oz2Groups& g, int tile, int t, int& group, int& first,
+                                           int& row, int& end) {
+  group = first = 0;
   row = t * tile;
   end = g.rows;
   if (!g.offsets) return;
@@ -263,7 +263,7 @@ __device__ __forceinline__ void group_tile(const Oz2Groups& g, int tile, int t, 
     if (hit) {
       const int l = __ffsll((long long)hit) - 1;
       group = __builtin_amdgcn_readfirstlane(g0 + l);
-      const int first = __shfl(before + sum - mine, l);
+      first = __builtin_amdgcn_readfirstlane(__shfl(before + sum - mine, l));
       row = __builtin_amdgcn_readfirstlane(__shfl(s, l) + (t - first) * tile);
       end = __builtin_amdgcn_readfirstlane(__shfl(e, l));
       return;
@@ -280,13 +280,14 @@ __device__ __forceinline__ ll xcd_order(ll b, ll n) {
   return (b >> 3) < per && p < n ? p : -1;
 }
 
-// Tile p of nrow x ncol tiles in bands of four rows of tiles, a band column by
-// column: 32 workgroups that run together (an XCD's) share 4 panels of A and 8 of B.
+// Tile p of nrow x ncol tiles in bands of four rows of tiles, the last of up to seven, a
+// band column by column: 32 workgroups that run together (an XCD's) share 4 to 7 panels
+// of A and 8 to 5 of B.
 __device__ __forceinline__ void banded(ll p, int nrow, int ncol, int& r, int& c) {
-  const ll band = p / (4ll * ncol);
-  const int in = (int)(p - band * 4 * ncol), h = min(4, nrow - (int)band * 4);
+  const int last = max(nrow / 4 - 1, 0), band = (int)min(p / (4ll * ncol), (ll)last);
+  const int in = (int)(p - band * 4ll * ncol), h = band == last ? nrow - 4 * band : 4;
   c = in / h;
-  r = (int)band * 4 + in - c * h;
+  r = band * 4 + in - c * h;
 }
 
 }  // namespace
