@@ -164,23 +164,33 @@ __device__ __forceinline__ const uint8_t* uniform(const void* p) {
   return (const uint8_t*)((uint64_t)hi << 32 | lo);
 }
 
-// (one wait state between writing m0 and the load that reads it)
+// (one wait state between writing m0 and the load that reads it); BYTES: 16, or 4 a lane
+template <int BYTES>
 __device__ __forceinline__ void load_lds(const uint8_t* base, uint32_t voff, uint32_t m0) {
   const uint64_t a = (uint64_t)base;
   const v4i rsrc = {(int)(uint32_t)a, (int)(uint32_t)(a >> 32), (int)kRecords, 0x00027000};
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff),
-               "s"(rsrc), "s"(m0)
-               : "memory");
+  if constexpr (BYTES == 16)
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(voff),
+                 "s"(rsrc), "s"(m0)
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(voff),
+                 "s"(rsrc), "s"(m0)
+                 : "memory");
 }
 
-// One operand's stages: a wave's share is the 1 KiB blocks w, w + W, .. of a stage, W
-// waves.
-template <class T, bool ROWS, int R, int W>
+// One operand's stages: a wave's share is the blocks w, w + W, .. of a stage, each 64
+// pieces of PB bytes, W waves.  16 bytes a piece; 4 for fp32 rows that start anywhere or
+// end within 16 bytes: four times the loads, 15% more time a stage, which is less than a
+// copy to whole lines first where the product is small (333 x 1001 x 555 15.5 us against
+// 19.3; 2047 x 2047 x 2048 168 against 151).
+template <class T, bool ROWS, int R, int W, int PB = 16>
 struct Stream {
-  static constexpr int N = R * SB2 / 1024 / W, KE = SB2 / sizeof(T), P = 16 / sizeof(T);
+  static constexpr int BLOCK = 64 * PB, N = R * SB2 / BLOCK / W, KE = SB2 / sizeof(T), P = 16 / sizeof(T);
+  static constexpr int Q = 16 / PB, E = PB / sizeof(T);   // pieces of 16 bytes; entries of one
   const uint8_t* base;   // uniform
   ll step;
-  ll alt;                // gated: from the gates' rows to the values', those of odd u
+  ll alt;                // gated: from the gates' rows to the values' (32 rows in turn)
   uint32_t vo[N];
   int l[N];              // the lane's first l of the stage
   // src: the tile's first row (ROWS) or first l (else, at its first column) ; row(q)
@@ -189,32 +199,33 @@ struct Stream {
   __device__ __forceinline__ void init(const T* src, ll ld, int w, int lane, F row, int cols) {
     base = uniform(src);
     alt = 0;
+    const int part = lane % Q * E;   // the lane's entries of 16 bytes start here
     if (ROWS) {
-      constexpr int PR = SB2 / 16;   // pieces per row
+      constexpr int PR = SB2 / 16;   // 16 bytes of a row
       step = SB2;
 #pragma unroll
       for (int u = 0; u < N; ++u) {
-        const int q = (w + W * u) * (64 / PR) + lane / PR, at = row(q);
-        const int c = (lane % PR) ^ row_swz(q);
-        l[u] = c * P;
-        vo[u] = at < 0 ? kNowhere : (uint32_t)(at * ld * (ll)sizeof(T)) + 16u * c;
+        const int q16 = (w + W * u) * (64 / Q) + lane / Q, q = q16 / PR, at = row(q);
+        l[u] = ((q16 % PR) ^ row_swz(q)) * P + part;
+        vo[u] = at < 0 ? kNowhere : (uint32_t)((at * ld + l[u]) * (ll)sizeof(T));
       }
     } else {
-      constexpr int PR = R / P;   // pieces per l
+      constexpr int PR = R / P;   // 16 bytes of an l
       step = KE * ld * (ll)sizeof(T);
 #pragma unroll
       for (int u = 0; u < N; ++u) {
-        const int q = (w + W * u) * 64 + lane;
-        l[u] = q / PR;
-        const int c = col_piece<T, R>(l[u], q % PR);
-        vo[u] = c * P >= cols ? kNowhere : (uint32_t)(l[u] * ld * (ll)sizeof(T)) + 16u * c;
+        const int q16 = (w + W * u) * (64 / Q) + lane / Q;
+        l[u] = q16 / PR;
+        const int c = col_piece<T, R>(l[u], q16 % PR) * P + part;
+        vo[u] = c >= cols ? kNowhere : (uint32_t)((l[u] * ld + c) * (ll)sizeof(T));
       }
     }
   }
   // block u of the next stage, of which `left` entries of l exist, to LDS at `at` (the
   // stage + the wave's first block); the last one moves on to the stage after it
   __device__ __forceinline__ void issue(int u, uint32_t at, int left) {
-    load_lds(ROWS && (u & 1) ? base + alt : base, l[u] < left ? vo[u] : kNowhere, at + 1024u * W * u);
+    const bool other = ROWS && W * BLOCK * u / SB2 & 32;
+    load_lds<PB>(other ? base + alt : base, l[u] < left ? vo[u] : kNowhere, at + (uint32_t)BLOCK * W * u);
     if (u == N - 1) base += step;
   }
 };
@@ -596,7 +607,7 @@ k_product256(Oz2Product p, int ncol) {
 // For products with few large tiles, and all of fp32.  4 waves, 64 x 64 (16 x 64)
 // outputs each; two stages of 128 bytes of l, 32 (16) KiB each, so that two (four)
 // workgroups of a CU cover each other's waits.
-template <class T, Oz2Side SIDE, int TILE>
+template <class T, Oz2Side SIDE, int TILE, int PB>
 __global__ void __launch_bounds__(NT, TILE == 128 ? 2 : 4)
 k_product128(Oz2Product p, int ncol) {
   constexpr bool AR = SIDE != OZ2_WGRAD, BR = SIDE == OZ2_FWD;
@@ -613,13 +624,13 @@ k_product128(Oz2Product p, int ncol) {
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = TILE == 128 ? w >> 1 : w, wc = TILE == 128 ? w & 1 : 0;
-  Stream<T, AR, TILE, 4> sa;
-  Stream<T, BR, TILE, 4> sb;
+  Stream<T, AR, TILE, 4, PB> sa;
+  Stream<T, BR, TILE, 4, PB> sb;
   streams<T, SIDE, TILE>(p, t, w, lane, sa, sb);
-  constexpr int N = Stream<T, AR, TILE, 4>::N;
+  constexpr int N = Stream<T, AR, TILE, 4, PB>::N;
   const int len = t.l1 - t.l0, n = (len + KE - 1) / KE;
   auto issue = [&](int it) {
-    const uint32_t at = lds0 + (it & 1) * ST + 1024u * w;
+    const uint32_t at = lds0 + (it & 1) * ST + 64u * PB * w;
 #pragma unroll
     for (int u = 0; u < N; ++u) sa.issue(u, at, len - it * KE);
 #pragma unroll
@@ -789,21 +800,24 @@ k_product(Oz2Product p, int ncol) {
                              lane);
 }
 
-// Direct loads take rows on 16-byte boundaries, whole pieces, and offsets within a
-// stage's rows below kRecords.
+// The pieces in which direct loads can take an operand: 16 bytes where its rows start
+// and end on them, 4 bytes of fp32, else (or where offsets within a stage's rows pass
+// kRecords) none, 0.
 template <class T>
-bool direct_side(const void* x, ll ld, bool rows, ll extent, int tile) {
+int direct_side(const void* x, ll ld, bool rows, ll extent, int tile) {
   constexpr int P = 16 / sizeof(T);
-  return (uintptr_t)x % 16 == 0 && ld % P == 0 && extent % P == 0 &&
-         ld * (rows ? (ll)sizeof(T) * tile : SB2) < (ll)kRecords - 65536;
+  if (ld * (rows ? (ll)sizeof(T) * tile : SB2) >= (ll)kRecords - 65536) return 0;
+  if ((uintptr_t)x % 16 == 0 && ld % P == 0 && extent % P == 0) return 16;
+  return sizeof(T) == 4 ? 4 : 0;
 }
 template <class T>
-bool direct(Oz2Side side, const Oz2Product& p, int tile) {
+int direct(Oz2Side side, const Oz2Product& p, int tile) {
   constexpr int P = 16 / sizeof(T);
-  if (p.strideB % P && side != OZ2_WGRAD) return false;
   const ll acols = side == OZ2_WGRAD ? p.M : p.L;
-  return direct_side<T>(p.A, p.lda, side != OZ2_WGRAD, p.padded ? 0 : acols, tile) &&
-         direct_side<T>(p.B, p.ldb, side == OZ2_FWD, p.paddedB ? 0 : side == OZ2_FWD ? p.L : p.N2, tile);
+  const int a = direct_side<T>(p.A, p.lda, side != OZ2_WGRAD, p.padded ? 0 : acols, tile);
+  const int b = direct_side<T>(p.B, p.ldb, side == OZ2_FWD, p.paddedB ? 0 : side == OZ2_FWD ? p.L : p.N2, tile);
+  const int group = side == OZ2_WGRAD || p.strideB % P == 0 ? 16 : sizeof(T) == 4 ? 4 : 0;
+  return std::min(std::min(a, b), group);
 }
 
 #define OZ2_SIDES(kern, ...)                                                            \
@@ -1060,14 +1074,19 @@ template <class T>
 hipError_t launch_tiles(Oz2Side side, int tile, const Oz2Product& p, hipStream_t s) {
   int ncol;
   // (operands that direct loads do not take: 128 x 128 whatever the plan)
-  if (!direct<T>(side, p, tile)) tile = 0;
+  const int pieces = direct<T>(side, p, tile);
+  if (!pieces) tile = 0;
   dim3 grid = tile_grid(side, p, tile ? tile : TM, ncol);
   grid.y = p.splits;
   if constexpr (sizeof(T) == 2) {
     if (tile == BT) OZ2_SIDES(k_product256);
   }
-  if (tile == 128) OZ2_SIDES(k_product128, , 128);
-  if (tile == 64) OZ2_SIDES(k_product128, , 64);
+  if constexpr (sizeof(T) == 4) {
+    if (tile == 128 && pieces == 4) OZ2_SIDES(k_product128, , 128, 4);
+    if (tile == 64 && pieces == 4) OZ2_SIDES(k_product128, , 64, 4);
+  }
+  if (tile == 128) OZ2_SIDES(k_product128, , 128, 16);
+  if (tile == 64) OZ2_SIDES(k_product128, , 64, 16);
   OZ2_SIDES(k_product);
 }
 

@@ -271,7 +271,8 @@ bool int_ok(const void* p) { return p && (uintptr_t)p % 4 == 0; }
 //              round
 //   a sum in s parts: 4 for the second launch, the parts written and read at 4 TB/s
 //   operands whose rows are not whole 16-byte pieces: copied first (4, and 4 TB/s), or
-//   128 x 128 tiles by way of registers, 2.6 (4.0 two a CU; fp32 1 more) a stage
+//   fp32 in pieces of 4 bytes, 15% more a stage, 16 bits in 128 x 128 tiles by way of
+//   registers, 2.6 (4.0 two a CU) a stage
 // for instance bf16 (256 / 128 / 64): 4096^3 120 / 153 / -, 2048^2 x 4096 82 / 42 / 53,
 // 1024^3 27 / 13 / 7.2, 1024^2 x 4096 79 / 36 (two parts 26) / 22, 512^2 x 1024 - / 12.5 /
 // 6.6, 128^2 x 8192 145 / 65 (eight 18) / 31 (eight 12), 6144 x 4096 x 1024 67 / 61 / -;
@@ -326,16 +327,17 @@ Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr
       take(6.0 + std::max(1.0, big <= 4.0 * cus ? std::ceil(big / cus) : big / cus) *
                      (8.0 + stages * (1.05 + 0.6 * load)), 256, 1);
     }
-    const double alone = wide ? 2.1 + slow : slow ? 2.6 : 0.55, full = wide ? 4.2 + slow : slow ? 4.0 : 1.1;
+    const double f = slow ? 1.15 : 1.0, alone = wide ? 2.1 * f : slow ? 2.6 : 0.55;
+    const double full = wide ? 4.2 * f : slow ? 4.0 : 1.1;
     for (int s = 1; s <= most; ++s) {
       const double per = std::ceil(stages / s), w128 = tiles(128.0) * s, w64 = tiles(64.0) * s;
       if (s == 1 || w128 <= 2.0 * cus)
         take(w128 <= cus ? 5.0 + per * alone
                          : 5.0 + (w128 <= 8.0 * cus ? std::ceil(w128 / (2.0 * cus)) : w128 / (2.0 * cus)) *
                                      (3.0 + per * full), 128, s);
-      if (!slow && (s == 1 || w64 <= 4.0 * cus)) {
+      if ((wide || !slow) && (s == 1 || w64 <= 4.0 * cus)) {
         const double k = std::min(4.0, std::ceil(w64 / cus)), rounds = std::max(1.0, w64 / (4.0 * cus));
-        take(3.5 + rounds * (per * (wide ? std::max(0.67, 0.61 * k) : std::max(0.28, 0.21 * k)) +
+        take(3.5 + rounds * (per * (wide ? f * std::max(0.67, 0.61 * k) : std::max(0.28, 0.21 * k)) +
                              (rounds > 1.0 ? 2.0 : 0.0)), 64, s);
       }
     }
