@@ -299,7 +299,7 @@ Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr
   const size_t packed = (odd & 1 ? (size_t)ra * oz2_packed_pitch(wa, e) * e : 0) +
                         (odd & 2 ? (size_t)rb * oz2_packed_pitch(wb, e) * e : 0);
   auto tiles = [&](double t) {
-    if (!gr.offsets) return std::ceil(M / t) * std::ceil(N2 / t);
+    if (!gr.offsets) return std::ceil(std::ceil(M / t) * std::ceil(N2 / t) / 8.0) * 8.0;   // (as launched)
     if (side == OZ2_WGRAD) return std::ceil(M / t) * std::ceil(N2 / t) * gr.groups;
     // (a group ends half a tile early on average)
     return std::max(1.0, (double)M / gr.groups / t + 0.5) * gr.groups * std::ceil(N2 / t);

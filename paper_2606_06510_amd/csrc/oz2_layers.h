@@ -298,9 +298,10 @@ __device__ __forceinline__ void banded(ll p, int nrow, int ncol, int& r, int& c)
 inline ll oz2_row_tiles(const Oz2Groups& g, int tile) {
   return g.offsets ? (ll)g.rows / tile + g.groups + 1 : ((ll)g.rows + tile - 1) / tile;
 }
-// workgroups for them and ncol tiles across
+// workgroups for them and ncol tiles across: a multiple of eight in the groups' order,
+// then those of the rows outside
 inline ll oz2_tile_blocks(const Oz2Groups& g, int tile, int ncol) {
-  return (oz2_row_tiles(g, tile) * ncol + 7) / 8 * 8 + 8;
+  return (oz2_row_tiles(g, tile) * ncol + 7) / 8 * 8 + (g.offsets ? 8 : 0);
 }
 
 // ---------------------------------------------------------------- launchers
