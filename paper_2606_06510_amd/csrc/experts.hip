@@ -12,7 +12,9 @@ namespace {
 // 0..E by counting: place = (pairs of lower keys) + (earlier pairs of the key).
 // A workgroup takes a contiguous range of pairs, each of its waves a contiguous
 // part, so "earlier" is: earlier workgroups (counted by a first launch), earlier
-// waves (counted in LDS), and earlier lanes (a ballot per bit of the key).
+// waves (counted in LDS), and earlier lanes (a ballot per bit of the key).  Bound by
+// the two launches and the chains of waits in them: 131072 pairs of 64 experts 4.8 and 7.0
+// us, 16 pairs (one launch) 3.2.
 constexpr int SORT_NT = 512, SORT_W = SORT_NT / 64;
 constexpr int SORT_KEYS = 4;                      // of a thread, kept in registers
 constexpr int SORT_CHUNK = SORT_NT * SORT_KEYS;   // pairs of a workgroup, or a multiple
@@ -151,12 +153,17 @@ k_sort_place(SortArgs a, const int* __restrict__ counts, int* __restrict__ offse
 // ---------------------------------------------------------------- rows
 // LPR lanes walk the 16-byte pieces of one token's row; a token's row is read once and
 // meets all of its places.  All rows may start at any element.  Grids are bounded: a
-// workgroup goes on to the tokens a grid further.
+// workgroup goes on to the tokens a grid further.  Bound by memory: k_gather of 16384
+// tokens to 8 places each, 4096 wide in bf16 (0.13 GB read, 1.05 written), 208 us, 5.7
+// TB/s; 5000 tokens, 4 places, 2001 wide in fp16: k_combine 23.4 us (117 MB, 5.0 TB/s),
+// k_combine_backward 39 (176 MB, 4.5).  Loads past the caches, which help the stores, cost
+// these 5 to 17%.
 constexpr ll ROW_BLOCKS = 1 << 20;
 #define OZ2_TOKENS(t, lane)                                                                     \
   const int lane = (int)(threadIdx.x % LPR);                                                    \
   for (ll t = ((ll)blockIdx.x * 256 + threadIdx.x) / LPR; t < a.tokens; t += (ll)gridDim.x * 256 / LPR)
 
+// Xs at each of a token's places = (weight x) X; zeros at those of dropped pairs
 template <class T, int LPR>
 __global__ void __launch_bounds__(256)
 k_gather(Oz2Tokens a, const T* __restrict__ x, ll ldx, T* __restrict__ xs, ll ldxs) {
@@ -187,6 +194,8 @@ k_gather(Oz2Tokens a, const T* __restrict__ x, ll ldx, T* __restrict__ xs, ll ld
   }
 }
 
+// Y = residual + sum over the places of weight x Ys, in 32 bits and in the order of the
+// choices
 template <class T, int LPR>
 __global__ void __launch_bounds__(256)
 k_combine(Oz2Tokens a, const T* __restrict__ ys, ll ldys, const T* res, ll ldr, T* y, ll ldy) {
@@ -234,7 +243,8 @@ k_combine(Oz2Tokens a, const T* __restrict__ ys, ll ldys, const T* res, ll ldr, 
   }
 }
 
-// UN places at a time: dY's piece is read once for them.  The dot products are
+// dYs = weight x dY at a place, dweight = <dY, Ys there>.  UN places at a time: dY's
+// piece is read once for them.  The dot products are
 // joined over the LPR lanes in a fixed order.
 template <class T, int LPR>
 __global__ void __launch_bounds__(256)

@@ -140,7 +140,8 @@ struct Reader {
 };
 
 // ------------------------------------------------------------ direct loads
-// A wave's load of 1 KiB of a stage straight into LDS (lane L's 16 bytes to m0 + 16 L).
+// A wave's load of 1 KiB of a stage straight into LDS (lane L's 16 bytes to m0 + 16 L; of
+// 256 bytes, lane L's 4 to m0 + 4 L).
 // Lanes whose offset is at or beyond kRecords read zeros: that is how rows, columns
 // and ends of the sum that do not exist become zeros without a branch.
 constexpr uint32_t kRecords = 0x80000000u, kNowhere = 0x80000000u;
@@ -164,7 +165,7 @@ __device__ __forceinline__ const uint8_t* uniform(const void* p) {
   return (const uint8_t*)((uint64_t)hi << 32 | lo);
 }
 
-// (one wait state between writing m0 and the load that reads it); BYTES: 16, or 4 a lane
+// (one wait state between writing m0 and the load that reads it)
 template <int BYTES>
 __device__ __forceinline__ void load_lds(const uint8_t* base, uint32_t voff, uint32_t m0) {
   const uint64_t a = (uint64_t)base;
@@ -509,10 +510,15 @@ __device__ __forceinline__ void streams(const Oz2Product& p, const Tile& t, int 
 // 4 waves, one per SIMD, 128 x 128 outputs each: 16 fragment reads feed the 64 products
 // of a step.  Stages of two steps, 64 KiB (whole 128-byte lines of rows that are
 // contiguous along l; stages of half of that took 0.84 us a step against 0.65 of
-// operands that read whole lines anyway), two of them in LDS.  While a step is
-// multiplied, the next one's fragments are read into the other set of registers; once
-// every wave holds a stage's last fragments, the loads of the stage after the next go
-// out into its place.  One barrier a stage.
+// operands that read whole lines anyway); LDS holds two of A's and three of B's.  While
+// a step is multiplied, the next one's fragments are read into the other set of
+// registers; once every wave holds a stage's last fragments, the loads of A's stage
+// after the next and of B's after that go out into its place (W comes from memory where A
+// mostly comes from a cache: 2% less time than with two stages of each).  One barrier a
+// stage.  Bound by the matrix cores, which the power limit holds at the rate of the
+// library's products: 16384 x 4096 x 16384 bf16, gated, 1.57-1.62 ms (1.36-1.40 PFLOP/s);
+// 4096^3 108 us for either gradient.  8-12 us of a tile are its first loads and its
+// epilogue, which nothing covers: groups of 1000 rows, 2 x 2048 x 4096, reach 1.08.
 constexpr int BT = 256, BOP = BT * SB2;
 
 template <class T, Oz2Side SIDE>
@@ -606,7 +612,9 @@ k_product256(Oz2Product p, int ncol) {
 // ------------------------------------------------ 128 x 128 and 64 x 64 tiles
 // For products with few large tiles, and all of fp32.  4 waves, 64 x 64 (16 x 64)
 // outputs each; two stages of 128 bytes of l, 32 (16) KiB each, so that two (four)
-// workgroups of a CU cover each other's waits.
+// workgroups of a CU cover each other's waits.  Bound by those waits and by reads of LDS
+// (a fragment read feeds 2 (0.8) products, the 256 wide tiles' 4): bf16 2048^2 x 1024 16 us
+// (540 TFLOP/s), 1024^3 7.2; fp32 1024^3 26 (83 TFLOP/s), 2048^2 x 1024 74 (116).
 template <class T, Oz2Side SIDE, int TILE, int PB>
 __global__ void __launch_bounds__(NT, TILE == 128 ? 2 : 4)
 k_product128(Oz2Product p, int ncol) {
@@ -674,8 +682,10 @@ k_product128(Oz2Product p, int ncol) {
 }
 
 // ------------------------------------------------ 128 x 128 tiles, by way of registers
-// The same for operands that direct loads do not take: rows of any length from any
-// address.  A stage waits in LDS, the next two on their way in registers.
+// The same for operands that direct loads do not take: 16-bit rows of any length from any
+// address where a copy would cost more, and rows more than 8 MiB apart.  A stage waits in
+// LDS, the next two on their way in registers.  Bound by the loads, which fall on no
+// boundary: 2.6 us a stage against 0.55.
 
 constexpr int DOP = TM * SB2, DST = 2 * DOP;
 
@@ -864,7 +874,9 @@ __device__ __forceinline__ void finish(const Oz2Product& p, int group, ll row, i
   put<T, W, false>((T*)p.y + row * p.ldy + col, v, valid);
 }
 
-// The sum of a product's splits, in order, and the epilogue: 16 bytes of y a thread
+// The sum of a product's splits, in order, and the epilogue: 16 bytes of y a thread.  Bound
+// by the launch and the parts' bytes (4 us and 4 TB/s); one part of 128^2 x 8192 bf16
+// takes 31 us, eight 12.
 template <class T>
 __global__ void __launch_bounds__(256)
 k_join(Oz2Product p) {
@@ -886,7 +898,8 @@ k_join(Oz2Product p) {
 
 // ------------------------------------------------ few rows: one read of W
 // y = f(x W^T ..) for groups of a few rows each (single tokens, decoding): the bytes of
-// W bound it.  A workgroup takes 16 columns of y of one group (gated: their gates and
+// W bound it (4096 x 4096 bf16, one row: 7.5 us, 4.5 TB/s; 14 experts of 2 x 2048 x 4096:
+// 80-90 us, 5.2-5.9 TB/s).  A workgroup takes 16 columns of y of one group (gated: their gates and
 // values), its eight waves share out the 128-byte chunks of l and read their rows of
 // W straight into fragments, UN chunks in flight; 16 TB rows of x at a time are the
 // other operand.  The waves' sums meet in LDS and are added in order.
@@ -1015,7 +1028,8 @@ hipError_t launch_rows(int blocks, const Oz2Product& p, hipStream_t s) {
 // ------------------------------------------------ operands in whole lines
 // Rows that are not whole 16-byte pieces, copied to rows of whole 128-byte lines with
 // zeros at their ends, for the direct loads: 16-bit rows from any address take 2.6 us
-// a stage of 128 x 128 tiles, direct loads 0.55.  64 lanes a row, both operands.
+// a stage of 128 x 128 tiles, direct loads 0.55.  64 lanes a row, both operands.  Bound by
+// its launch for small ones: 777 and 1301 rows of 995 fp16 6.2 us.
 struct Rows {
   const void* src;
   ll ld, stride;     // elements between rows, and between matrices of `per` rows
@@ -1109,7 +1123,8 @@ hipError_t launch_product(Oz2Side side, const Oz2Plan& plan, Oz2Product p, hipSt
 // ------------------------------------------------ slope: dZ and its column sums
 // dZ = dY f'(Z).  A workgroup takes p.sum_rows rows of one group and 32 pieces of 16
 // bytes of n, 8 rows at a time; the column sums of its rows leave as one partial row,
-// added up in order by k_sums.  Bound by memory: dY and Z read and dZ written once.
+// added up in order by k_sums.  Bound by memory: dY and Z read and dZ written once,
+// 4096^2 bf16 with gelu in 22.7 us, 4.4 TB/s.
 template <class T, int ACT, bool GATED>
 __global__ void __launch_bounds__(256)
 k_slope(Oz2Slope p) {
@@ -1195,7 +1210,8 @@ k_slope(Oz2Slope p) {
 }
 
 // db of group blockIdx.y, 32 columns a workgroup: the partial rows of the group's row
-// tiles in eight runs, each in order, then the runs in order
+// tiles in eight runs, each in order, then the runs in order (4.6 us, its launch and a
+// chain of loads)
 template <class T>
 __global__ void __launch_bounds__(256)
 k_sums(Oz2Slope p) {

@@ -14,7 +14,8 @@ DENSE = [(2056, 264, 6152, False), (2056, 6152, 130, True), (264, 2056, 6152, Fa
          (1544, 264, 4104, True), (130, 4104, 6152, False), (4104, 130, 6152, False),
          (1032, 1032, 1032, False), (2600, 1031, 999, False), (40, 1544, 130, True),
          (520, 130, 1544, False), (5000, 7, 9, False), (9, 5000, 70, True),
-         (2050, 2047, 2047, False), (264, 4104, 2600, False)]
+         (2050, 2047, 2047, False), (264, 4104, 2600, False),
+         (264, 2600, 4104, False), (4104, 264, 2600, False)]
 # the ends of the groups, rows after them, in, out, gated
 GROUPED = [([0, 700, 700, 1301, 2590, 2600], 30, 520, 4104, False),
            ([0, 1, 1200, 1456, 2600], 0, 4104, 520, True),
