@@ -613,8 +613,8 @@ k_product256(Oz2Product p, int ncol) {
 // For products with few large tiles, and all of fp32.  4 waves, 64 x 64 (16 x 64)
 // outputs each; two stages of 128 bytes of l, 32 (16) KiB each, so that two (four)
 // workgroups of a CU cover each other's waits.  Bound by those waits and by reads of LDS
-// (a fragment read feeds 2 (0.8) products, the 256 wide tiles' 4): bf16 2048^2 x 1024 16 us
-// (540 TFLOP/s), 1024^3 7.2; fp32 1024^3 26 (83 TFLOP/s), 2048^2 x 1024 74 (116).
+// (a fragment read feeds 2 (0.8) products, the 256 wide tiles' 4): bf16 2048 x 1024 x
+// 2048 16 us (540 TFLOP/s), 1024^3 7.2; fp32 1024^3 26 (83), 2048 x 1024 x 2048 74 (116).
 template <class T, Oz2Side SIDE, int TILE, int PB>
 __global__ void __launch_bounds__(NT, TILE == 128 ? 2 : 4)
 k_product128(Oz2Product p, int ncol) {
