@@ -946,13 +946,19 @@ k_rows(Oz2Product p) {
       Frag<T> wf[UN][2][G], xf[UN][2][TB];
 #pragma unroll
       for (int q = 0; q < UN; ++q) {
-        // chunks beyond the last full one: the last again, with zeros for x
+        // chunks beyond the last full one: zeros for both (zeros times an infinity of W
+        // would be a NaN)
         const bool on = c0 + RW * q < full;
-        const int k = min(c0 + RW * q, full - 1) * KC;
+        const int k = (c0 + RW * q) * KC;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
-          for (int e = 0; e < G; ++e) __builtin_memcpy(&wf[q][h][e].v, wp + e * up + k + 4 * h * P, 16);
+          for (int e = 0; e < G; ++e) {
+            if (on)
+              __builtin_memcpy(&wf[q][h][e].v, wp + e * up + k + 4 * h * P, 16);
+            else
+              wf[q][h][e].v = V{};
+          }
 #pragma unroll
           for (int b = 0; b < TB; ++b) {
             if (on)

@@ -160,6 +160,30 @@ def test_linear_infinities_and_nan(dtype):
 
 
 @pytest.mark.parametrize("dtype", list(lu.DTYPES))
+def test_linear_infinite_weights(dtype):
+    """an infinite weight times positive inputs is an infinite output, in whichever part
+    of the sum it lies: nothing beyond the sum's end meets it"""
+    lines = {torch.float32: 32, torch.float16: 64, torch.bfloat16: 64}[lu.DTYPES[dtype]]
+    for T in (1, 20, 70, 300):
+        for K in (8, lines, 3 * lines, 9 * lines, 33 * lines + 8, 70 * lines):
+            c = case(T, K, 24, dtype, False, seed=13)
+            x = c["x"].abs() + 0.5
+            for n, k in enumerate((0, K // 2, (K - 1) // lines * lines, K - 1)):
+                c["w"][2 * n, k] = float("inf")
+                c["w"][2 * n + 1, k] = -float("inf")
+            for gated in (False, True):
+                y = oz().linear(x, c["w"], gated=gated)
+                z = torch.full((T, 24), float("inf"), device=device())
+                z[:, 1::2] = -z[:, 1::2]
+                if gated:   # gates 0 .. 7 are infinite, the values they meet finite
+                    u = x.float() @ c["w"][12:].float().t()
+                    assert torch.equal(y[:, :8].float(), (z[:, :8] * u[:, :8].sign()))
+                else:
+                    assert torch.equal(y[:, :8].float(), z[:, :8])
+                assert bool(torch.isfinite(y[:, 8:]).all())
+
+
+@pytest.mark.parametrize("dtype", list(lu.DTYPES))
 @pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu", "relu"])
 def test_activations_at_large_arguments(act, dtype):
     """far out the functions are x or 0 and the slopes 1 or 0, without overflow
