@@ -58,6 +58,10 @@ bool disjoint_bytes(const Mat& a, size_t e, const void* p, size_t bytes) {
   return a0 + a.span(e) <= b0 || b0 + bytes <= a0;
 }
 
+bool offsets_apart(const Oz2Groups& gr, const void* ws, size_t bytes) {
+  return !gr.offsets || disjoint_bytes(mat(gr.offsets, 1, gr.groups + 1, gr.groups + 1), 4, ws, bytes);
+}
+
 int hip_status(hipError_t e) { return e == hipSuccess ? OZ2_OK : OZ2_E_DEVICE; }
 
 bool sizes_ok(int dtype, int act, ll rows, ll groups, ll out, ll in, int gated) {
@@ -137,6 +141,7 @@ int forward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, c
   if (st != OZ2_OK) return st;
   for (const Mat* m : {&x, &w, &bias, &res, &y, &z})
     if (!disjoint_bytes(*m, e, ws, need)) return OZ2_E_INVALID;
+  if (!offsets_apart(gr, ws, need)) return OZ2_E_INVALID;
   if ((st = oz2_device_ok()) != OZ2_OK) return st;
   Oz2Product p{};
   p.A = x.p;
@@ -197,6 +202,7 @@ int backward(int dtype, int act, int gated, const Oz2Groups& gr, ll out, ll in, 
     if (m && sums && !disjoint_bytes(*m, e, ws, L.total)) return OZ2_E_INVALID;
   for (const Mat* m : outs)
     if (m && !disjoint_bytes(*m, e, ws, L.total)) return OZ2_E_INVALID;
+  if (!offsets_apart(gr, ws, L.total)) return OZ2_E_INVALID;
   if ((st = oz2_device_ok()) != OZ2_OK) return st;
   uint8_t* base = (uint8_t*)ws;
   hipError_t err = hipSuccess;
@@ -451,6 +457,9 @@ int ozaki2_expert_sort(int tokens, int top_k, int num_experts, const void* exper
   const size_t need = ozaki2_expert_sort_workspace_bytes(tokens, top_k, num_experts);
   int st = check_workspace(workspace, ws_bytes, need);
   if (st != OZ2_OK) return st;
+  for (const Mat* m : {&o, &r, &sl})
+    if (!disjoint_bytes(*m, 4, workspace, need)) return OZ2_E_INVALID;
+  if (!disjoint_bytes(ids, ie, workspace, need)) return OZ2_E_INVALID;
   if ((st = oz2_device_ok()) != OZ2_OK) return st;
   return hip_status(oz2_launch_sort(tokens, top_k, num_experts, experts, wide_ids != 0, ldexperts, offsets,
                                     rows, slots, (int*)workspace, (hipStream_t)stream));

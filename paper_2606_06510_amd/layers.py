@@ -180,8 +180,12 @@ def _workspace(workspace, need, device):
             return None, None, 0
         workspace = _torch.empty(need, dtype=_torch.uint8, device=device)
         return workspace, workspace.data_ptr(), need
+    if not isinstance(workspace, _torch.Tensor):
+        raise TypeError(f"workspace: expected a torch tensor, got {type(workspace).__name__}")
     if workspace.device != device:
         raise ValueError("workspace: on another device")
+    if not workspace.is_contiguous():   # (its bytes would not all be there)
+        raise ValueError("workspace: expected a contiguous tensor")
     # the library checks its size
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 

@@ -108,6 +108,44 @@ def test_grouped_backward_refusals():
     assert L.ozaki2_grouped_linear_backward(*{**base, "ws": None}.values()) == _lib.OZ2_E_WORKSPACE
 
 
+def test_workspace_apart_from_what_the_call_reads_and_writes():
+    """the offsets of the groups, and all of the sort's arrays, are read or written
+    while the workspace is"""
+    L = oz.load()
+    G, S, N, K = 3, 4096, 64, 65   # odd rows: copied into the workspace
+    need = oz.ozaki2_grouped_linear_workspace_bytes(oz.OZ2_BF16, 0, S, G, N, K)
+    assert need
+    fwd = dict(dtype=oz.OZ2_BF16, act=0, gated=0, rows=S, groups=G, out=N, inp=K, off=AT + need - 16,
+               x=AT + 64 * MB, ldx=K, w=AT + 128 * MB, ldw=K, sw=N * K, bias=None, sb=0,
+               y=AT + 192 * MB, ldy=N, z=None, ldz=0, ws=AT, wsb=need, stream=None)
+    assert L.ozaki2_grouped_linear(*fwd.values()) == _lib.OZ2_E_INVALID
+    need = oz.ozaki2_grouped_linear_backward_workspace_bytes(oz.OZ2_BF16, 1, 0, S, G, N, K)
+    bwd = dict(dtype=oz.OZ2_BF16, act=1, gated=0, rows=S, groups=G, out=N, inp=K, off=AT + need - 16,
+               dy=AT + 64 * MB, lddy=N, x=AT + 80 * MB, ldx=K, w=AT + 128 * MB, ldw=K, sw=N * K,
+               z=AT + 144 * MB, ldz=N, dx=AT + 192 * MB, lddx=K, dw=AT + 208 * MB, lddw=K, sdw=N * K,
+               db=None, sdb=0, ws=AT, wsb=need, stream=None)
+    assert L.ozaki2_grouped_linear_backward(*bwd.values()) == _lib.OZ2_E_INVALID
+    need = oz.ozaki2_expert_sort_workspace_bytes(9000, 2, 4)
+    sort = dict(T=9000, k=2, E=4, ids=AT, wide=1, ld=2, off=AT + MB, rows=AT + 2 * MB,
+                slots=AT + 3 * MB, ws=AT + 4 * MB, wsb=need, s=None)
+    for name in ("ids", "off", "rows", "slots"):
+        over = {name: AT + 4 * MB + need - 8}
+        assert L.ozaki2_expert_sort(*{**sort, **over}.values()) == _lib.OZ2_E_INVALID, name
+
+
+def test_workspace_tensor_refusals():
+    """the library sees a pointer and a number of bytes: these must be there"""
+    from paper_2606_06510_amd import layers
+    layers._init()
+    cpu = torch.device("cpu")
+    with pytest.raises(ValueError, match="contiguous"):
+        layers._workspace(torch.zeros(1, dtype=torch.uint8).expand(1 << 20), 256, cpu)
+    with pytest.raises(TypeError, match="workspace"):
+        layers._workspace(b"0" * 512, 256, cpu)
+    ws = torch.zeros(512, dtype=torch.uint8)
+    assert layers._workspace(ws, 256, cpu)[1:] == (ws.data_ptr(), 512)
+
+
 def test_expert_refusals():
     L = oz.load()
     bad = _lib.OZ2_E_INVALID
