@@ -19,6 +19,7 @@
 // pieces of rows (unrolled over the accumulators it was 330 KB of code, run once a
 // tile: 30 us of instruction fetches).
 #include <algorithm>
+#include <type_traits>
 
 #include "oz2_layers.h"
 
@@ -898,8 +899,8 @@ k_join(Oz2Product p) {
 
 // ------------------------------------------------ few rows: one read of W
 // y = f(x W^T ..) for groups of a few rows each (single tokens, decoding): the bytes of
-// W bound it (4096 x 4096 bf16, one row: 7.5 us, 4.5 TB/s; 14 experts of 2 x 2048 x 4096:
-// 80-90 us, 5.2-5.9 TB/s).  A workgroup takes 16 columns of y of one group (gated: their gates and
+// W bound it (4096 x 4096 bf16, one row: 8.2-8.5 us, 4.0 TB/s; 14 experts of 2 x 2048 x
+// 4096: 75 us, 6.2 TB/s).  A workgroup takes 16 columns of y of one group (gated: their gates and
 // values), its eight waves share out the 128-byte chunks of l and read their rows of
 // W straight into fragments, UN chunks in flight; 16 TB rows of x at a time are the
 // other operand.  The waves' sums meet in LDS and are added in order.
@@ -942,14 +943,18 @@ k_rows(Oz2Product p) {
 #pragma unroll
       for (int b = 0; b < TB; ++b) acc[k][b] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
     typedef decltype(Frag<T>::v) V;
-    for (int c0 = w; c0 < full; c0 += RW * UN) {
+    // UN chunks of the wave from c0 on (WHOLE: all there).  One beyond the last full one
+    // must not meet W, whose infinities times zero are NaN: gated, it is the last one
+    // again and its products are left out (no branch between the loads and one loop's
+    // registers: 14 experts of 2 x 2048 x 4096 76 us against 83); else, where short sums
+    // count, zeros for both (5 x 1000 x 777 fp16 4.5 us against 6.5).
+    auto batch = [&](auto whole, int c0) {
+      constexpr bool WHOLE = decltype(whole)::value;
       Frag<T> wf[UN][2][G], xf[UN][2][TB];
 #pragma unroll
       for (int q = 0; q < UN; ++q) {
-        // chunks beyond the last full one: zeros for both (zeros times an infinity of W
-        // would be a NaN)
-        const bool on = c0 + RW * q < full;
-        const int k = (c0 + RW * q) * KC;
+        const bool on = GATED || WHOLE || c0 + RW * q < full;
+        const int k = (GATED ? min(c0 + RW * q, full - 1) : c0 + RW * q) * KC;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -968,15 +973,21 @@ k_rows(Oz2Product p) {
           }
         }
       }
+      if (!GATED) __builtin_amdgcn_sched_barrier(0);   // all loads first
 #pragma unroll
       for (int q = 0; q < UN; ++q)
+        if (!GATED || c0 + RW * q < full)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int e = 0; e < G; ++e)
+            for (int e = 0; e < G; ++e)
 #pragma unroll
-            for (int b = 0; b < TB; ++b) acc[e][b] = mma(wf[q][h][e], xf[q][h][b], acc[e][b]);
-    }
+              for (int b = 0; b < TB; ++b) acc[e][b] = mma(wf[q][h][e], xf[q][h][b], acc[e][b]);
+    };
+    int c0 = w;
+    if (!GATED)
+      for (; c0 + RW * (UN - 1) < full; c0 += RW * UN) batch(std::true_type{}, c0);
+    for (; c0 < full; c0 += RW * UN) batch(std::false_type{}, c0);
     if (nch > full && full % RW == w) {   // the last chunk, in part
       const int k = full * KC;
 #pragma unroll
