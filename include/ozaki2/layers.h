@@ -81,9 +81,9 @@ size_t ozaki2_linear_backward_workspace_bytes(int dtype, int activation, int gat
  * offsets[g] .. offsets[g+1] - 1 of X and Y belong to layer g, whose weights
  * start at w + g stride_w and bias at bias + g stride_bias (elements).
  * offsets is DEVICE memory, int [groups + 1], not read by the host: ascending from 0
- * and at most rows (other values are clamped to [0, rows] and to ascending
- * order, so that no access leaves the arrays, and the rows' results are then
- * undefined).  Rows from offsets[groups] on are not read, and written as
+ * and at most rows (other values are clamped to [0, rows] and, where groups are
+ * added up, to ascending order, so that no access leaves the arrays or the
+ * workspace; the results of such a call are undefined).  Rows from offsets[groups] on are not read, and written as
  * zeros in y and z.  1 <= groups <= OZ2_MAX_EXPERTS. */
 int ozaki2_grouped_linear(int dtype, int activation, int gated, int rows, int groups, int out,
                           int in, const int* offsets, const void* x, long long ldx, const void* w,

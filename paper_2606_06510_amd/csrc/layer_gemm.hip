@@ -1235,21 +1235,8 @@ k_sums(Oz2Slope p) {
   __shared__ float red[8][32];
   const int n2 = p.gated ? 2 * p.n : p.n, l = threadIdx.x & 31, run = threadIdx.x >> 5;
   const int c = (int)blockIdx.x * 32 + l, g = (int)blockIdx.y;
-  int first = 0, count;
-  if (!p.gr.offsets) {
-    count = (int)(((ll)p.gr.rows + p.sum_rows - 1) / p.sum_rows);
-  } else {
-    int s, e;
-    const int lane = threadIdx.x & 63;
-    for (int i = lane; i < g; i += 64) {
-      group_range(p.gr, i, s, e);
-      first += (e - s + p.sum_rows - 1) / p.sum_rows;
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) first += __shfl_xor(first, d);
-    group_range(p.gr, g, s, e);
-    count = (e - s + p.sum_rows - 1) / p.sum_rows;
-  }
+  int first, count;
+  group_tiles_before(p.gr, p.sum_rows, g, first, count);
   const int per = (count + 7) / 8, k0 = run * per, k1 = min(count, k0 + per);
   float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   if (c < n2) {

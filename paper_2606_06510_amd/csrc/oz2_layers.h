@@ -13,7 +13,8 @@ int oz2_device_cus();   // as in oz2_internal.h
 int oz2_device_ok();
 
 // Groups of rows: group g is rows [offsets[g], offsets[g+1]) of `rows`, clamped
-// so that whatever the array holds, no row index leaves [0, rows].
+// so that whatever the array holds, no row index leaves [0, rows] and no count of rows
+// over several groups passes `rows`.
 // offsets null: one group of all rows.
 struct Oz2Groups {
   const int* offsets;
@@ -223,14 +224,34 @@ __device__ __forceinline__ void group_range(const Oz2Groups& g, int i, int& star
   end = max(start, group_start(g, i + 1));
 }
 
+// Rows [start, end) of group i = g0 + lane, g0 = 0, 64, .. in turn, where what all groups
+// have is added up: a group starts no earlier than the ones before it, so that whatever
+// the array holds, all of them together are at most `rows` (ascending offsets: as
+// group_range).  high: 0 at first, then the end of the groups before.  Every lane of the
+// wave calls it; groups that do not exist are empty.
+__device__ __forceinline__ void ascending_ranges(const Oz2Groups& g, int g0, int& high, int& start,
+                                                 int& end) {
+  const int lane = threadIdx.x & 63, i = g0 + lane;
+  start = i < g.groups ? group_start(g, i) : 0;
+  end = i < g.groups ? group_start(g, i + 1) : 0;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int up = __shfl_up(start, d);
+    if (lane >= d) start = max(start, up);
+  }
+  start = max(start, high);
+  end = max(start, end);
+  high = __shfl(end, 63);
+}
+
 // Row tiles of `tile` rows that the groups have.  Every lane of the wave calls it;
 // the result is uniform.
 __device__ __forceinline__ int group_tiles(const Oz2Groups& g, int tile) {
   if (!g.offsets) return (int)(((ll)g.rows + tile - 1) / tile);
-  int n = 0;
-  for (int i = threadIdx.x & 63; i < g.groups; i += 64) {
+  int n = 0, high = 0;
+  for (int g0 = 0; g0 < g.groups; g0 += 64) {
     int s, e;
-    group_range(g, i, s, e);
+    ascending_ranges(g, g0, high, s, e);
     n += (e - s + tile - 1) / tile;
   }
 #pragma unroll
@@ -247,11 +268,10 @@ __device__ __forceinline__ void group_tile(const Oz2Groups& g, int tile, int t, 
   end = g.rows;
   if (!g.offsets) return;
   const int lane = threadIdx.x & 63;
-  int before = 0;
+  int before = 0, high = 0;
   for (int g0 = 0; g0 < g.groups; g0 += 64) {
-    const int i = g0 + lane;
-    int s = 0, e = 0;
-    if (i < g.groups) group_range(g, i, s, e);
+    int s, e;
+    ascending_ranges(g, g0, high, s, e);
     const int mine = (e - s + tile - 1) / tile;
     int sum = mine;
 #pragma unroll
@@ -270,6 +290,27 @@ __device__ __forceinline__ void group_tile(const Oz2Groups& g, int tile, int t, 
     }
     before += __shfl(sum, 63);
   }
+}
+
+// The row tiles of the groups before `group`, and its own.  Likewise uniform.
+__device__ __forceinline__ void group_tiles_before(const Oz2Groups& g, int tile, int group, int& first,
+                                                   int& count) {
+  first = 0;
+  if (!g.offsets) {
+    count = (int)(((ll)g.rows + tile - 1) / tile);
+    return;
+  }
+  const int lane = threadIdx.x & 63;
+  int high = 0;
+  for (int g0 = 0; g0 <= group; g0 += 64) {
+    int s, e;
+    ascending_ranges(g, g0, high, s, e);
+    const int mine = (e - s + tile - 1) / tile;
+    if (g0 + lane < group) first += mine;
+    count = __shfl(mine, (group - g0) & 63);   // (the last round's: of group itself)
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) first += __shfl_xor(first, d);
 }
 
 // Workgroup b's place in an order of n items in which each XCD (workgroups go

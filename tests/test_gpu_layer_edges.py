@@ -1,0 +1,54 @@
+"""The layer operators where arguments are at the edge of what they may be: offsets of
+groups that do not ascend."""
+import pytest
+import torch
+
+from tests import layer_util as lu
+from tests.gpu_util import device
+from tests.test_gpu_layers import check_grouped, grouped_case, oz
+
+pytestmark = pytest.mark.gpu
+
+GUARD = 4096   # bytes on either side of an output
+
+
+def guarded(shape, dtype):
+    """An output of the shape inside a buffer of bytes 0x5A, and the buffer"""
+    n = torch.empty(0, dtype=dtype).element_size()
+    for s in shape:
+        n *= s
+    buf = torch.full((n + 2 * GUARD,), 0x5A, dtype=torch.uint8, device=device())
+    return buf[GUARD:GUARD + n].view(dtype).view(shape), buf
+
+
+# rows, groups, in, out, gated: few rows a group, small and large tiles, copied operands
+NOT_ASCENDING = [(300, 64, 200, 136, False), (700, 64, 200, 136, True), (2600, 5, 520, 4104, False),
+                 (700, 64, 131, 137, False), (4096, 64, 64, 520, False)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("S,G,K,N,gated", NOT_ASCENDING)
+def test_offsets_that_do_not_ascend(S, G, K, N, gated, dtype):
+    """no result is promised, but nothing beside the outputs and the workspace is
+    written, and the next call is right"""
+    m, dt = oz(), lu.DTYPES[dtype]
+    off = [0] + [S * i // G for i in range(1, G)] + [S - 3]
+    c = grouped_case(off, 3, K, N, dtype, gated, seed=91)
+    n2 = 2 * N if gated else N
+    code = {"bf16": m.OZ2_BF16, "fp32": m.OZ2_F32}[dtype]
+    need = m.ozaki2_grouped_linear_backward_workspace_bytes(code, m.OZ2_ACT_SILU, gated, S, G, N, K)
+    g = torch.Generator().manual_seed(92)
+    for bad in ([0, S] * 600, [S, 0] * 600, [S - i for i in range(1200)], [-5, 2 ** 31 - 1, -2 ** 31] * 400,
+                torch.randint(-S, 2 * S, (1200,), generator=g).tolist()):
+        o = torch.tensor(bad[:G + 1], dtype=torch.int32, device=device())
+        bufs = dict(y=guarded((S, N), dt), dx=guarded((S, K), dt), dw=guarded((G, n2, K), dt),
+                    db=guarded((G, n2), dt), ws=guarded((need,), torch.uint8))
+        m.grouped_linear(c["x"], c["w"], o, bias=c["b"], activation="silu", gated=gated,
+                         out=bufs["y"][0])
+        m.grouped_linear_backward(c["dy"], c["x"], c["w"], o, preactivation=c["z"], activation="silu",
+                                  gated=gated, dx=bufs["dx"][0], dw=bufs["dw"][0],
+                                  dbias=bufs["db"][0], workspace=bufs["ws"][0])
+        torch.cuda.synchronize()
+        for name, (_, buf) in bufs.items():
+            assert bool((buf[:GUARD] == 0x5A).all()) and bool((buf[-GUARD:] == 0x5A).all()), name
+    check_grouped(off, 3, c, "silu", gated)
