@@ -1178,7 +1178,8 @@ k_slope(Oz2Slope p) {
         for (int i = 0; i < U * P; ++i) e[i] = d[i] * act_f<T>(to_f(a[i / P].v[i % P]), ACT);
 #pragma unroll
         for (int i = 0; i < U * P; ++i) {
-          su[i % P] += e[i];
+          // (rows past the end: d is 0, but 0 times an infinite f, or a slope of NaN, is not)
+          if (t0 + 8 * (i / P) < end) su[i % P] += e[i];
           d[i] *= to_f(u[i / P].v[i % P]);
           u[i / P].v[i % P] = from_f<T>(e[i]);
         }
@@ -1189,7 +1190,6 @@ k_slope(Oz2Slope p) {
       }
 #pragma unroll
       for (int i = 0; i < U * P; ++i) {
-        // (rows past the end: d is 0, but 0 times a slope of NaN is not)
         if (t0 + 8 * (i / P) < end) sg[i % P] += d[i];
         g[i / P].v[i % P] = from_f<T>(d[i]);
       }

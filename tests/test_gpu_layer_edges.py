@@ -1,14 +1,15 @@
 """The layer operators where arguments are at the edge of what they may be: offsets of
-groups that do not ascend."""
+groups that do not ascend, infinities in the last row before an end."""
 import pytest
 import torch
 
 from tests import layer_util as lu
 from tests.gpu_util import device
-from tests.test_gpu_layers import check_grouped, grouped_case, oz
+from tests.test_gpu_layers import case, check_grouped, grouped_case, oz
 
 pytestmark = pytest.mark.gpu
 
+INF = float("inf")
 GUARD = 4096   # bytes on either side of an output
 
 
@@ -52,3 +53,32 @@ def test_offsets_that_do_not_ascend(S, G, K, N, gated, dtype):
         for name, (_, buf) in bufs.items():
             assert bool((buf[:GUARD] == 0x5A).all()) and bool((buf[-GUARD:] == 0x5A).all()), name
     check_grouped(off, 3, c, "silu", gated)
+
+
+@pytest.mark.parametrize("dtype", list(lu.DTYPES))
+@pytest.mark.parametrize("act", lu.ACTS)
+def test_infinite_gate_in_the_last_row(act, dtype):
+    """a gate that was stored as infinity makes its values' bias gradients infinite, with
+    the sign of dY, whatever the number of rows is a multiple of"""
+    N = 40
+    for T in (1, 5, 8, 16, 17, 31, 33, 130):
+        c = case(T, 24, N, dtype, True, seed=93)
+        c["z"][T - 1, :N] = INF
+        _, _, db = oz().linear_backward(c["dy"], c["x"], c["w"], preactivation=c["z"], activation=act,
+                                        gated=True)
+        assert torch.equal(db[N:], c["dy"][T - 1].sign() * INF), T
+        assert bool(torch.isfinite(db[:N]).all()), T
+
+
+@pytest.mark.parametrize("dtype", list(lu.DTYPES))
+def test_infinite_gate_in_the_last_row_of_a_group(dtype):
+    off, N = [0, 5, 5, 38, 54, 84, 85], 40
+    for which in (0, 2, 4, 5):
+        c = grouped_case(off, 3, 24, N, dtype, True, seed=94)
+        last = off[which + 1] - 1
+        c["z"][last, :N] = INF
+        _, _, db = oz().grouped_linear_backward(c["dy"], c["x"], c["w"], c["off"], preactivation=c["z"],
+                                                activation="silu", gated=True)
+        assert torch.equal(db[which, N:], c["dy"][last].sign() * INF)
+        db[which, N:] = 0.0
+        assert bool(torch.isfinite(db).all())
