@@ -253,7 +253,8 @@ struct Tile {
 template <Oz2Side SIDE>
 __device__ __forceinline__ bool tile_of(const Oz2Product& p, int tile, int ncol, Tile& t) {
   const int cols = p.gated ? tile / 2 : tile;
-  const ll b = blockIdx.x;
+  // (grid y: the parts of a split sum, else the rest of a grid too long for x)
+  const ll b = blockIdx.x + (p.splits > 1 ? 0ll : (ll)blockIdx.y * gridDim.x);
   int r, c;
   t.split = 0;
   if (SIDE == OZ2_WGRAD) {
@@ -846,9 +847,10 @@ int direct(Oz2Side side, const Oz2Product& p, int tile) {
 dim3 tile_grid(Oz2Side side, const Oz2Product& p, int tile, int& ncol) {
   const int cols = p.gated && side == OZ2_FWD ? tile / 2 : tile, n = side == OZ2_FWD ? p.N : p.N2;
   ncol = (n + cols - 1) / cols;
-  if (side == OZ2_WGRAD)
-    return dim3((unsigned)(((ll)((p.M + tile - 1) / tile) * ncol + 7) / 8 * 8), 1, p.gr.groups);
-  return dim3((unsigned)oz2_tile_blocks(p.gr, tile, ncol));
+  const Oz2Grid g = oz2_grid(side == OZ2_WGRAD ? ((ll)((p.M + tile - 1) / tile) * ncol + 7) / 8 * 8
+                                               : oz2_tile_blocks(p.gr, tile, ncol));
+  // (split sums are of few tiles)
+  return dim3(g.x, p.splits > 1 ? p.splits : g.y, side == OZ2_WGRAD ? p.gr.groups : 1);
 }
 
 // The epilogue of W columns of one row from column col on (valid of them exist), v and
@@ -1107,8 +1109,7 @@ hipError_t launch_tiles(Oz2Side side, int tile, const Oz2Product& p, hipStream_t
   // (operands that direct loads do not take: 128 x 128 whatever the plan)
   const int pieces = direct<T>(side, p, tile);
   if (!pieces) tile = 0;
-  dim3 grid = tile_grid(side, p, tile ? tile : TM, ncol);
-  grid.y = p.splits;
+  const dim3 grid = tile_grid(side, p, tile ? tile : TM, ncol);
   if constexpr (sizeof(T) == 2) {
     if (tile == BT) OZ2_SIDES(k_product256);
   }
@@ -1149,7 +1150,9 @@ k_slope(Oz2Slope p) {
   constexpr bool SLOPED = GATED || ACT != OZ2_ACT_NONE;
   __shared__ float red[8][32 * 2 * P];
   // a row's pieces in a row of workgroups: whole rows are read at a time
-  const int cb = (p.n + 32 * P - 1) / (32 * P), tile = (int)(blockIdx.x / cb), cc = (int)blockIdx.x - tile * cb;
+  const int cb = (p.n + 32 * P - 1) / (32 * P);
+  const unsigned b = blockIdx.x + blockIdx.y * gridDim.x;
+  const int tile = (int)(b / cb), cc = (int)(b - (unsigned)tile * cb);
   if (tile >= group_tiles(p.gr, p.sum_rows)) return;
   int group, first, row, end;
   group_tile(p.gr, p.sum_rows, tile, group, first, row, end);
@@ -1267,7 +1270,8 @@ hipError_t launch_slope(Oz2Slope p, hipStream_t s) {
   while (p.sum_rows < 128 && (ll)p.gr.rows / p.sum_rows * cb > 8ll * oz2_device_cus()) p.sum_rows *= 2;
   const ll rt = oz2_row_tiles(p.gr, p.sum_rows);
   if (rt > 0 && cb > 0) {
-    const dim3 grid((unsigned)(rt * cb));
+    const Oz2Grid g = oz2_grid(rt * cb);
+    const dim3 grid(g.x, g.y);
 #define OZ2_SLOPE(ACT)                                                          \
   case ACT:                                                                     \
     if (p.gated)                                                                \

@@ -345,6 +345,18 @@ inline ll oz2_tile_blocks(const Oz2Groups& g, int tile, int ncol) {
   return (oz2_row_tiles(g, tile) * ncol + 7) / 8 * 8 + (g.offsets ? 8 : 0);
 }
 
+// A grid of `blocks` workgroups of 256 threads: HIP takes fewer than 2^32 threads along x
+// (2^30 rows in 64-row tiles are that many), so beyond 2^24 - 8 workgroups it goes on
+// along y, in whole rounds of the XCDs.
+struct Oz2Grid {
+  unsigned x, y;
+};
+inline Oz2Grid oz2_grid(ll blocks) {
+  const ll most = (1 << 24) - 8;
+  return blocks <= most ? Oz2Grid{(unsigned)blocks, 1u}
+                        : Oz2Grid{(unsigned)most, (unsigned)((blocks + most - 1) / most)};
+}
+
 // ---------------------------------------------------------------- launchers
 hipError_t oz2_launch_product(int dtype, Oz2Side side, const Oz2Plan& plan, const Oz2Product& p,
                               hipStream_t s);

@@ -1,5 +1,5 @@
 """The layer operators where arguments are at the edge of what they may be: offsets of
-groups that do not ascend, infinities in the last row before an end."""
+groups that do not ascend, infinities in the last row before an end, the most rows."""
 import pytest
 import torch
 
@@ -82,3 +82,33 @@ def test_infinite_gate_in_the_last_row_of_a_group(dtype):
         assert torch.equal(db[which, N:], c["dy"][last].sign() * INF)
         db[which, N:] = 0.0
         assert bool(torch.isfinite(db).all())
+
+
+def test_two_to_the_30_rows():
+    """the most rows there may be: more workgroups than one dimension of a grid takes.
+    All rows but 64 at the start, in the middle and at the end are zeros."""
+    m, T, n = oz(), 1 << 30, 64
+    c = case(3 * n, 8, 8, "bf16", False, seed=95)
+    at = [0, T // 2 - n // 2, T - n]
+
+    def spread(rows):
+        t = torch.zeros((T, 8), dtype=torch.bfloat16, device=device())
+        for i, a in enumerate(at):
+            t[a:a + n] = rows[n * i:n * (i + 1)]
+        return t
+
+    def gathered(t):
+        """the rows that are not zeros; the others are"""
+        got = torch.cat([t[a:a + n] for a in at])
+        for a in at:
+            t[a:a + n] = 0
+        assert not any(bool(part.any()) for part in t.split(T // 16))
+        return got
+    x = spread(c["x"])
+    y, _, ey, _ = lu.forward(c["x"], c["w"], None, None, "none", False)
+    lu.check(gathered(m.linear(x, c["w"])), y, ey, "y")
+    dx, dw, db, ex, ew, eb = lu.backward(c["dy"], c["x"], c["w"], None, "none", False, torch.bfloat16)
+    gx, gw, gb = m.linear_backward(spread(c["dy"]), x, c["w"])
+    lu.check(gathered(gx), dx, ex, "dx")
+    lu.check(gw, dw, ew, "dw")
+    lu.check(gb, db, eb, "db")
