@@ -20,7 +20,8 @@
  * calls may be captured into a graph.
  * Validation happens before any launch: on an error nothing is written
  * (OZ2_E_INVALID for sizes, types, leading dimensions, null pointers and
- * outputs or a workspace that overlap an input or another output; OZ2_E_WORKSPACE for a
+ * outputs or a workspace that overlap an input or another output (matrices may
+ * lie side by side in one buffer's rows, and stacks in between each other); OZ2_E_WORKSPACE for a
  * workspace that is smaller than the _workspace_bytes function says or not
  * 256-byte aligned).  A workspace of 0 bytes may be null.  Sizes of zero are
  * allowed: an empty sum is zero.  Limits: rows and token-expert pairs up to 2^30,

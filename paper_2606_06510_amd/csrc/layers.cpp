@@ -40,17 +40,31 @@ bool good(const Mat& m, size_t e, bool output = false) {
   return !output || m.stride >= (m.rows - 1) * m.ld + m.cols;
 }
 
-// no element in both.  Matrices of one leading dimension may lie side by side
-// (column ranges of one buffer).
+// bytes at [0, ca) and at [d, d + cb) of every `period`
+bool apart(ll d, ll ca, ll cb, ll period) {
+  if (period <= 0) return false;
+  d %= period;
+  if (d < 0) d += period;
+  return d >= ca && d + cb <= period;
+}
+
+// no element in both.  Matrices of one leading dimension may lie side by side (column
+// ranges of one buffer), also where they are stacked in whole rows of it, and stacks of
+// one stride may lie in between each other (a layer's parameters one after the other, for
+// every layer).
 bool disjoint(const Mat& a, const Mat& b, size_t e) {
   if (a.empty() || b.empty()) return true;
   const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p;
   if (a0 + a.span(e) <= b0 || b0 + b.span(e) <= a0) return true;
-  if (a.count > 1 || b.count > 1 || a.ld != b.ld) return false;
-  const ll pitch = a.ld * (ll)e;
-  ll d = ((ll)b0 - (ll)a0) % pitch;
-  if (d < 0) d += pitch;
-  return d >= a.cols * (ll)e && d + b.cols * (ll)e <= pitch;
+  const ll d = (ll)b0 - (ll)a0, size = (ll)e;
+  auto whole_rows = [](const Mat& m) { return m.count == 1 || m.stride % m.ld == 0; };
+  if (a.ld == b.ld && whole_rows(a) && whole_rows(b) &&
+      apart(d, a.cols * size, b.cols * size, a.ld * size))
+    return true;
+  if (a.count == 1 && b.count == 1) return false;
+  if (a.count > 1 && b.count > 1 && a.stride != b.stride) return false;
+  return apart(d, ((a.rows - 1) * a.ld + a.cols) * size, ((b.rows - 1) * b.ld + b.cols) * size,
+               (a.count > 1 ? a.stride : b.stride) * size);
 }
 bool disjoint_bytes(const Mat& a, size_t e, const void* p, size_t bytes) {
   if (a.empty() || !p || !bytes) return true;

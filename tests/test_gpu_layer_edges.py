@@ -1,5 +1,6 @@
 """The layer operators where arguments are at the edge of what they may be: offsets of
-groups that do not ascend, infinities in the last row before an end, the most rows."""
+groups that do not ascend, infinities in the last row before an end, the most rows, parameters and
+their gradients in one buffer."""
 import pytest
 import torch
 
@@ -112,3 +113,27 @@ def test_two_to_the_30_rows():
     lu.check(gathered(gx), dx, ex, "dx")
     lu.check(gw, dw, ew, "dw")
     lu.check(gb, db, eb, "db")
+
+
+@pytest.mark.parametrize("dtype", list(lu.DTYPES))
+@pytest.mark.parametrize("off,K,N", [([0, 40, 40, 301, 330], 72, 56), ([0, 3, 9], 136, 33)])
+def test_gradients_of_a_layer_in_one_buffer(off, K, N, dtype):
+    """[layer][dW, dbias, one more entry], [layer][row][W, dW]: the bits of the same call
+    with outputs of their own, and nothing beside them"""
+    m, dt, G = oz(), lu.DTYPES[dtype], len(off) - 1
+    c = grouped_case(off, 0, K, N, dtype, False, seed=96)
+    kw = dict(preactivation=c["z"], activation="gelu")
+    dx, dw, db = m.grouped_linear_backward(c["dy"], c["x"], c["w"], c["off"], **kw)
+    flat = torch.full((G, N * K + N + 1), 7.0, dtype=dt, device=device())
+    gw, gb = flat[:, :N * K].view(G, N, K), flat[:, N * K:-1]
+    got = m.grouped_linear_backward(c["dy"], c["x"], c["w"], c["off"], dw=gw, dbias=gb, **kw)
+    assert torch.equal(got[0], dx) and torch.equal(gw, dw) and torch.equal(gb, db)
+    assert bool((flat[:, -1] == 7).all())
+    wide = torch.full((G, N, 2 * K), 7.0, dtype=dt, device=device())
+    wide[..., :K] = c["w"]
+    got = m.grouped_linear_backward(c["dy"], c["x"], wide[..., :K], c["off"], dw=wide[..., K:], **kw)
+    assert torch.equal(wide[..., K:], dw) and torch.equal(wide[..., :K], c["w"])
+    for e in range(G):   # (W's rows may be read another way, so dx is not bit for bit the same)
+        r = slice(off[e], off[e + 1])
+        gx, _, _, ex, _, _ = lu.backward(c["dy"][r], c["x"][r], c["w"][e], c["z"][r], "gelu", False, dt)
+        lu.check(got[0][r], gx, ex, f"dx of {e}")
