@@ -191,9 +191,12 @@ def _workspace(workspace, need, device):
 
 
 def _dim2(name, t, n=2):
-    if t.dim() != n:
-        raise ValueError(f"{name}: expected {n} dimensions, got shape {tuple(t.shape)}")
-    return t.shape
+    try:
+        if t.dim() == n:
+            return t.shape
+    except AttributeError:
+        raise TypeError(f"{name}: expected a torch tensor, got {type(t).__name__}") from None
+    raise ValueError(f"{name}: expected {n} dimensions, got shape {tuple(t.shape)}")
 
 
 # ------------------------------------------------------------------ dense
