@@ -132,8 +132,8 @@ int ozaki2_expert_gather(int dtype, int tokens, int top_k, int width, const void
 
 /* Y[t] = residual[t] + sum over j ascending of weights[t][j] YS[slots[t][j]],
  * dropped pairs left out (their rows of YS are not read); weights null: 1;
- * residual null: 0; residual may be Y itself.  With weights and residual null
- * it is the gradient of ozaki2_expert_gather. */
+ * residual null: 0; residual may be Y itself.  With residual null it is the gradient
+ * of ozaki2_expert_gather with the same weights. */
 int ozaki2_expert_combine(int dtype, int tokens, int top_k, int width, const void* ys,
                           long long ldys, const int* slots, const int* kept, const float* weights,
                           const void* residual, long long ldr, void* y, long long ldy,
@@ -142,7 +142,8 @@ int ozaki2_expert_combine(int dtype, int tokens, int top_k, int width, const voi
 /* The gradients of ozaki2_expert_combine from dY: dys[slots[t][j]] =
  * weights[t][j] dY[t] (zeros for dropped pairs), and dweights[t][j] =
  * <dY[t], YS[slots[t][j]]> (float; 0 for dropped pairs).  weights must be given;
- * dys or dweights may be null (not wanted); ys is read for dweights alone. */
+ * dys or dweights may be null (not wanted); ys is read for dweights alone.
+ * dweights from X as dy and dXS as ys is the gradient of ozaki2_expert_gather's weights. */
 int ozaki2_expert_combine_backward(int dtype, int tokens, int top_k, int width, const void* dy,
                                    long long lddy, const void* ys, long long ldys,
                                    const int* slots, const int* kept, const float* weights,

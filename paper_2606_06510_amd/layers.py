@@ -8,6 +8,11 @@ be any number of elements apart, the elements of a row are adjacent.  All of a
 call's matrices have one dtype (float32, float16 or bfloat16) and one device.
 Outputs and workspaces that are not given are allocated on the stream of the call
 (``stream``, else torch's current one).
+
+Autograd does not see these calls: a result requires no gradient, whatever the
+inputs require, and nothing flows back through it by itself.  A training step calls the
+gradients by name (each docstring says which), or wraps a function and its gradients in a
+``torch.autograd.Function``.
 """
 from __future__ import annotations
 
@@ -209,7 +214,7 @@ def linear(x, w, bias=None, residual=None, activation="none", gated=False,
     gated: w has 2 out rows and bias 2 out entries, gates first, and the result
     is f(gates) * values + residual.  save_preactivation: returns (y, z) with z =
     x w^T + bias, rounded, as linear_backward takes it.  out may be residual
-    itself."""
+    itself.  Not recorded by autograd: its gradients are linear_backward's."""
     code, act, dev = _dtype("x", x), _act(activation), _device("x", x)
     T, K = _dim2("x", x)
     n2, _ = _dim2("w", w)
@@ -284,7 +289,8 @@ def grouped_linear(x, w, offsets, bias=None, activation="none", gated=False,
                    save_preactivation=False, out=None, workspace=None, stream=None):
     """``linear`` of a group of layers: rows offsets[g] .. offsets[g + 1] - 1 of x
     [S, in] through w[g] ([G, out, in], gated 2 out) and bias[g].  offsets is an int32
-    device tensor [G + 1]; the host never reads it.  Rows from offsets[G] on are zeros."""
+    device tensor [G + 1]; the host never reads it.  Rows from offsets[G] on are zeros.
+    Not recorded by autograd: its gradients are grouped_linear_backward's."""
     code, act, dev = _dtype("x", x), _act(activation), _device("x", x)
     S, K = _dim2("x", x)
     G, n2 = _dim2("w", w, 3)[:2]
@@ -395,7 +401,9 @@ def _weights(weights, like, shape):
 
 def expert_gather(x, order, weights=None, out=None, stream=None):
     """x[t] at the places of its pairs: [tokens * top_k, width], zeros for dropped
-    pairs; with weights (float32 [tokens, top_k]), times the pair's weight."""
+    pairs; with weights (float32 [tokens, top_k]), times the pair's weight.  Not recorded
+    by autograd.  The gradients from dxs: of x ``expert_combine(dxs, order, weights)``, of
+    the weights ``expert_combine_backward(x, dxs, order, weights, need_dys=False)[1]``."""
     code, dev = _dtype("x", x), _device("x", x)
     T0, width = _dim2("x", x)
     slots, kept, T, k = _order(order, x, T0)
@@ -414,8 +422,9 @@ def expert_gather(x, order, weights=None, out=None, stream=None):
 
 def expert_combine(ys, order, weights=None, residual=None, out=None, stream=None):
     """residual[t] + the sum over a token's pairs of weight * ys[place]: [tokens,
-    width].  Dropped pairs are left out.  Without weights it is the gradient of
-    expert_gather.  out may be residual itself."""
+    width].  Dropped pairs are left out.  It is the gradient of expert_gather with the same
+    weights, or without.  out may be residual itself.  Not recorded by autograd: its
+    gradients are expert_combine_backward's."""
     code, dev = _dtype("ys", ys), _device("ys", ys)
     S, width = _dim2("ys", ys)
     slots, kept, T, k = _order(order, ys)
