@@ -69,7 +69,8 @@ size_t ozaki2_linear_workspace_bytes(int dtype, int gated, int rows, int out, in
  * The residual's gradient is dY.  Each of dx, dw and dbias may be null (not
  * wanted); x is read for dw alone and w for dx alone, and may be null without
  * them.  dZ is rounded to dtype before the products (the matrix cores take
- * their operands in that type), but not before its column sums. */
+ * their operands in that type; beyond 65504 fp16 is infinite), but not before its column
+ * sums.  OZ2_F32 keeps dZ in 32 bits. */
 int ozaki2_linear_backward(int dtype, int activation, int gated, int rows, int out, int in,
                            const void* dy, long long lddy, const void* x, long long ldx,
                            const void* w, long long ldw, const void* z, long long ldz, void* dx,

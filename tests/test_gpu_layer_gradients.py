@@ -59,3 +59,31 @@ def test_inside_an_autograd_function():
     want = m.linear_backward(c["dy"].contiguous(), leaves[0], leaves[1], preactivation=z, activation="gelu")
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert all(t.device == device() for t in got)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+def test_precision_is_the_dtype_of_the_call(dtype):
+    """the gradient at the pre-activation is an operand in the call's dtype: 16 bits round it
+    once (lu.backward's bounds, which count that), the same values as float32 tensors do
+    not"""
+    m, c = oz(), case(150, 200, 88, dtype, False, seed=105)
+    args = [c[n] for n in ("dy", "x", "w", "z")]
+    for t in (args, [a.float() for a in args]):
+        dx, dw, db, ex, ew, eb = lu.backward(*t, "silu", False, t[0].dtype)
+        gx, gw, gb = m.linear_backward(t[0], t[1], t[2], preactivation=t[3], activation="silu")
+        lu.check(gx, dx, ex, "dx")
+        lu.check(gw, dw, ew, "dw")
+        lu.check(gb, db, eb, "db")
+
+
+def test_fp16_gradient_beyond_its_range():
+    """dZ = 120000: infinite as an fp16 operand, 120000 in fp32"""
+    m = oz()
+    one = torch.ones((20, 8), dtype=torch.float16, device=device())
+    args = [40000.0 * one[:, :4], one, 2.0 ** -6 * torch.cat([one, one])[:8], 3.0 * one]
+    dx, _, _ = m.linear_backward(args[0], args[1], args[2], preactivation=args[3], activation="none",
+                                 gated=True)
+    assert bool(torch.isinf(dx).all())
+    dx, _, _ = m.linear_backward(*(a.float() for a in args[:3]), preactivation=args[3].float(),
+                                 activation="none", gated=True)
+    assert bool((dx == 8 * 120000 / 64).all())
