@@ -20,10 +20,10 @@
  * calls may be captured into a graph.
  * Validation happens before any launch: on an error nothing is written
  * (OZ2_E_INVALID for sizes, types, leading dimensions, null pointers and
- * outputs or a workspace that overlap an input or another output (matrices may
- * lie side by side in one buffer's rows, and stacks in between each other); OZ2_E_WORKSPACE for a
+ * outputs or a workspace that overlap an input or another output; OZ2_E_WORKSPACE for a
  * workspace that is smaller than the _workspace_bytes function says or not
- * 256-byte aligned).  A workspace of 0 bytes may be null.  Sizes of zero are
+ * 256-byte aligned).  Matrices may lie side by side in the rows of one buffer, and stacks
+ * of one stride in between each other.  A workspace of 0 bytes may be null.  Sizes of zero are
  * allowed: an empty sum is zero.  Limits: rows and token-expert pairs up to 2^30,
  * in and out up to 2^21, and matrices (all groups' weights together) below 2^40
  * elements.
@@ -85,8 +85,9 @@ size_t ozaki2_linear_backward_workspace_bytes(int dtype, int activation, int gat
  * offsets is DEVICE memory, int [groups + 1], not read by the host: ascending from 0
  * and at most rows (other values are clamped to [0, rows] and, where groups are
  * added up, to ascending order, so that no access leaves the arrays or the
- * workspace; the results of such a call are undefined).  Rows from offsets[groups] on are not read, and written as
- * zeros in y and z.  1 <= groups <= OZ2_MAX_EXPERTS. */
+ * workspace; the results of such a call are undefined).  Rows of X from
+ * offsets[groups] on affect nothing, whatever they hold, and those of y and z are
+ * written as zeros.  1 <= groups <= OZ2_MAX_EXPERTS. */
 int ozaki2_grouped_linear(int dtype, int activation, int gated, int rows, int groups, int out,
                           int in, const int* offsets, const void* x, long long ldx, const void* w,
                           long long ldw, long long stride_w, const void* bias,

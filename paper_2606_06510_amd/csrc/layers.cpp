@@ -303,7 +303,11 @@ bool int_ok(const void* p) { return p && (uintptr_t)p % 4 == 0; }
 //   10.4 / 13, 32 rows 13.9 / 13.6; gated 11008 x 4096, 1 row 34 / 30, 16 rows 39 / 29.
 //   Tiles read W at no more than 6.2 TB/s.
 // Groups: their sizes are not known here; even ones that end half a tile early are
-// assumed, and the sum stays whole.  At most 8 rows a group on average: k_rows.
+// assumed, and the sum stays whole.  At most 8 rows a group on average: k_rows.  The same
+// rows in k_rows and in tiles, 1 and 8 a group: 16 gated bf16 experts, 4096 -> 2048, 90 and
+// 113 against 112; without gates tiles win (64 experts, 4096 -> 2048, 213 and 291 against
+// 178; 16 in fp32, 1024 -> 2048, 41 and 42 against 39), and so they do where most rows fall
+// to one group (k_rows reads W again for every 32 of them).
 Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr, bool padded) {
   const double cus = oz2_device_cus();
   const bool wide = dtype == OZ2_F32;
