@@ -37,7 +37,9 @@ bool good(const Mat& m, size_t e, bool output = false) {
   if (m.ld < m.cols || m.ld > kMaxLd) return false;
   if (m.count == 1) return true;
   if (m.stride < 0 || m.stride > kMaxLd) return false;
-  return !output || m.stride >= (m.rows - 1) * m.ld + m.cols;
+  // outputs: one matrix after the other, or all matrices' first rows, then their second ones
+  return !output || m.stride >= (m.rows - 1) * m.ld + m.cols ||
+         (m.stride >= m.cols && m.ld >= (m.count - 1) * m.stride + m.cols);
 }
 
 // bytes at [0, ca) and at [d, d + cb) of every `period`

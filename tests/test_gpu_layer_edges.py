@@ -118,7 +118,7 @@ def test_two_to_the_30_rows():
 @pytest.mark.parametrize("dtype", list(lu.DTYPES))
 @pytest.mark.parametrize("off,K,N", [([0, 40, 40, 301, 330], 72, 56), ([0, 3, 9], 136, 33)])
 def test_gradients_of_a_layer_in_one_buffer(off, K, N, dtype):
-    """[layer][dW, dbias, one more entry], [layer][row][W, dW]: the bits of the same call
+    """[layer][dW, dbias, one more entry], [layer][row][W, dW], [row][layer][dW]: the bits of the same call
     with outputs of their own, and nothing beside them"""
     m, dt, G = oz(), lu.DTYPES[dtype], len(off) - 1
     c = grouped_case(off, 0, K, N, dtype, False, seed=96)
@@ -129,6 +129,9 @@ def test_gradients_of_a_layer_in_one_buffer(off, K, N, dtype):
     got = m.grouped_linear_backward(c["dy"], c["x"], c["w"], c["off"], dw=gw, dbias=gb, **kw)
     assert torch.equal(got[0], dx) and torch.equal(gw, dw) and torch.equal(gb, db)
     assert bool((flat[:, -1] == 7).all())
+    rows = torch.full((N, G, K), 7.0, dtype=dt, device=device()).transpose(0, 1)
+    m.grouped_linear_backward(c["dy"], c["x"], c["w"], c["off"], dw=rows, need_dx=False, **kw)
+    assert torch.equal(rows, dw)
     wide = torch.full((G, N, 2 * K), 7.0, dtype=dt, device=device())
     wide[..., :K] = c["w"]
     got = m.grouped_linear_backward(c["dy"], c["x"], wide[..., :K], c["off"], dw=wide[..., K:], **kw)

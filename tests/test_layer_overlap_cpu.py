@@ -54,6 +54,17 @@ def test_weights_and_gradients_side_by_side():
     assert backward(1, N, K, N * K, 2 * N * K, K, w=0, sw=0, ldw=K, **kw) == _lib.OZ2_E_WORKSPACE
 
 
+@pytest.mark.parametrize("G", [2, 5])
+def test_gradients_row_by_row(G):
+    """[row][layer][dW]: no element is in two layers, though every layer's rows lie in
+    between the others'"""
+    N, K = 6, 8
+    assert backward(G, N, K, 0, K, G * K, 1 << 24, N) == _lib.OZ2_E_WORKSPACE
+    assert backward(G, N, K, 0, K, G * K - 1, 1 << 24, N) == _lib.OZ2_E_INVALID
+    assert backward(G, N, K, 0, K - 1, G * K, 1 << 24, N) == _lib.OZ2_E_INVALID
+    assert backward(G, N, K, 0, K, G * K, (N - 1) * G * K, N) == _lib.OZ2_E_INVALID    # dbias in a row
+
+
 def test_nothing_that_overlaps_is_taken():
     """random stacks: never taken where an element is in both; and the layouts that do not
     overlap by a common period are"""
