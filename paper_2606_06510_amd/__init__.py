@@ -10,3 +10,5 @@ from .tensor import (colmajor_empty, to_device_colmajor, from_device_colmajor,  
 from .layers import (ExpertOrder, linear, linear_backward, grouped_linear,  # noqa: F401
                      grouped_linear_backward, expert_sort, expert_gather, expert_combine,
                      expert_combine_backward)
+from .model import (expert_route, expert_route_backward, layer_norm,  # noqa: F401
+                    layer_norm_backward, linear_cross_entropy, linear_cross_entropy_backward)

@@ -60,6 +60,10 @@ OZ2_ACT_SILU = 4
 OZ2_MAX_EXPERTS = 1024
 OZ2_MAX_TOPK = 64
 
+# include/ozaki2/model.h
+OZ2_SCORE_SOFTMAX = 0
+OZ2_SCORE_SIGMOID = 1
+
 EXPORTS = [
     "ozaki2_dgemm", "ozaki2_dgemm_ex", "ozaki2_dgemm_static", "ozaki2_dgemm_strided_batched",
     "ozaki2_workspace_bytes", "ozaki2_moduli", "ozaki2_plan_create",
@@ -84,6 +88,14 @@ LAYER_EXPORTS = [
     "ozaki2_grouped_linear_backward_workspace_bytes", "ozaki2_expert_sort",
     "ozaki2_expert_sort_workspace_bytes", "ozaki2_expert_gather", "ozaki2_expert_combine",
     "ozaki2_expert_combine_backward",
+]
+
+# include/ozaki2/model.h
+MODEL_EXPORTS = [
+    "ozaki2_expert_route", "ozaki2_expert_route_backward", "ozaki2_layer_norm",
+    "ozaki2_layer_norm_backward", "ozaki2_layer_norm_backward_workspace_bytes",
+    "ozaki2_linear_cross_entropy", "ozaki2_linear_cross_entropy_workspace_bytes",
+    "ozaki2_linear_cross_entropy_backward", "ozaki2_linear_cross_entropy_backward_workspace_bytes",
 ]
 
 
@@ -111,6 +123,7 @@ def load():
     import torch  # noqa: F401
     L = ctypes.CDLL(LIB_PATH)
     i, u, p, sz, ll = ctypes.c_int, ctypes.c_uint, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_longlong
+    f = ctypes.c_float
     sig = {
         "ozaki2_dgemm": (i, [i, i, i, p, i, p, i, p, i, i, p]),
         "ozaki2_dgemm_ex": (i, [i, i, i, p, i, p, i, p, i, i, u, p, sz, p]),
@@ -153,11 +166,22 @@ def load():
         "ozaki2_expert_gather": (i, [i] * 4 + [p, ll, p, p, p, p, ll, p]),
         "ozaki2_expert_combine": (i, [i] * 4 + [p, ll, p, p, p, p, ll, p, ll, p]),
         "ozaki2_expert_combine_backward": (i, [i] * 4 + [p, ll, p, ll, p, p, p, p, ll, p, p]),
+        "ozaki2_expert_route": (i, [i] * 4 + [p, ll, p] + [i] * 5 + [f, p, p, p]),
+        "ozaki2_expert_route_backward": (i, [i] * 4 + [p, p, ll, p, i, i, f, p, ll, p]),
+        "ozaki2_layer_norm": (i, [i] * 3 + [p, ll, p, p, f, p, ll, p, p]),
+        "ozaki2_layer_norm_backward": (
+            i, [i] * 3 + [p, ll, p, ll, p, p, p, ll, p, ll, p, p, p, sz, p]),
+        "ozaki2_layer_norm_backward_workspace_bytes": (sz, [i] * 3),
+        "ozaki2_linear_cross_entropy": (i, [i] * 4 + [p, ll, p, ll, p, i, p, p, p, sz, p]),
+        "ozaki2_linear_cross_entropy_workspace_bytes": (sz, [i] * 4),
+        "ozaki2_linear_cross_entropy_backward": (
+            i, [i] * 4 + [p, p, ll, p, ll, p, i, p, p, ll, p, ll, p, sz, p]),
+        "ozaki2_linear_cross_entropy_backward_workspace_bytes": (sz, [i] * 4),
     }
     for name, (res, args) in sig.items():
-        f = getattr(L, name)
-        f.restype = res
-        f.argtypes = args
+        fn = getattr(L, name)
+        fn.restype = res
+        fn.argtypes = args
     _lib = L
     return L
 
@@ -389,6 +413,65 @@ def ozaki2_expert_combine_backward(dtype, tokens, top_k, width, dy, lddy, ys, ld
     return _check("ozaki2_expert_combine_backward", load().ozaki2_expert_combine_backward(
         dtype, tokens, top_k, width, _ptr(dy), lddy, _ptr(ys), ldys, _ptr(slots), _ptr(kept),
         _ptr(weights), _ptr(dys), lddys, _ptr(dweights), _stream(stream)))
+
+
+# -------------------------------------------------- model (ozaki2/model.h), same names
+
+def ozaki2_expert_route(dtype, tokens, num_experts, top_k, logits, ldl, bias, score, groups,
+                        top_groups, group_best, renormalize, scale, ids, weights, stream=None):
+    return _check("ozaki2_expert_route", load().ozaki2_expert_route(
+        dtype, tokens, num_experts, top_k, _ptr(logits), ldl, _ptr(bias), score, groups, top_groups,
+        group_best, renormalize, scale, _ptr(ids), _ptr(weights), _stream(stream)))
+
+
+def ozaki2_expert_route_backward(dtype, tokens, num_experts, top_k, dweights, logits, ldl, ids,
+                                 score, renormalize, scale, dlogits, lddl, stream=None):
+    return _check("ozaki2_expert_route_backward", load().ozaki2_expert_route_backward(
+        dtype, tokens, num_experts, top_k, _ptr(dweights), _ptr(logits), ldl, _ptr(ids), score,
+        renormalize, scale, _ptr(dlogits), lddl, _stream(stream)))
+
+
+def ozaki2_layer_norm(dtype, rows, width, x, ldx, weight, bias, eps, y, ldy, stats, stream=None):
+    return _check("ozaki2_layer_norm", load().ozaki2_layer_norm(
+        dtype, rows, width, _ptr(x), ldx, _ptr(weight), _ptr(bias), eps, _ptr(y), ldy, _ptr(stats),
+        _stream(stream)))
+
+
+def ozaki2_layer_norm_backward(dtype, rows, width, dy, lddy, x, ldx, stats, weight, residual, ldr,
+                               dx, lddx, dweight, dbias, workspace, ws_bytes, stream=None):
+    return _check("ozaki2_layer_norm_backward", load().ozaki2_layer_norm_backward(
+        dtype, rows, width, _ptr(dy), lddy, _ptr(x), ldx, _ptr(stats), _ptr(weight), _ptr(residual),
+        ldr, _ptr(dx), lddx, _ptr(dweight), _ptr(dbias), _ptr(workspace), ws_bytes,
+        _stream(stream)))
+
+
+def ozaki2_layer_norm_backward_workspace_bytes(dtype, rows, width):
+    return load().ozaki2_layer_norm_backward_workspace_bytes(dtype, rows, width)
+
+
+def ozaki2_linear_cross_entropy(dtype, rows, vocab, inp, x, ldx, w, ldw, targets, wide_targets,
+                                loss, lse, workspace, ws_bytes, stream=None):
+    return _check("ozaki2_linear_cross_entropy", load().ozaki2_linear_cross_entropy(
+        dtype, rows, vocab, inp, _ptr(x), ldx, _ptr(w), ldw, _ptr(targets), wide_targets, _ptr(loss),
+        _ptr(lse), _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def ozaki2_linear_cross_entropy_workspace_bytes(dtype, rows, vocab, inp):
+    return load().ozaki2_linear_cross_entropy_workspace_bytes(dtype, rows, vocab, inp)
+
+
+def ozaki2_linear_cross_entropy_backward(dtype, rows, vocab, inp, dloss, x, ldx, w, ldw, targets,
+                                         wide_targets, lse, dx, lddx, dw, lddw, workspace, ws_bytes,
+                                         stream=None):
+    return _check("ozaki2_linear_cross_entropy_backward",
+                  load().ozaki2_linear_cross_entropy_backward(
+                      dtype, rows, vocab, inp, _ptr(dloss), _ptr(x), ldx, _ptr(w), ldw,
+                      _ptr(targets), wide_targets, _ptr(lse), _ptr(dx), lddx, _ptr(dw), lddw,
+                      _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+def ozaki2_linear_cross_entropy_backward_workspace_bytes(dtype, rows, vocab, inp):
+    return load().ozaki2_linear_cross_entropy_backward_workspace_bytes(dtype, rows, vocab, inp)
 
 
 # ------------------------------------------------------------ probes (ozaki2_probes.h)

@@ -16,7 +16,7 @@ BUILD = os.path.join(os.path.dirname(HERE), "_build")
 LIB = os.path.join(HERE, "libozaki2.so")
 SOURCES = ["api.cpp", "deconstruct.hip", "gemm.hip", "reconstruct.hip", "batched.hip", "gemv.hip",
            "fused.hip", "bytes.hip", "bytegemm.hip", "bytefused.hip", "probes.hip",
-           "layers.cpp", "layer_gemm.hip", "experts.hip"]
+           "layers.cpp", "layer_gemm.hip", "experts.hip", "model.cpp", "router.hip", "norm.hip", "loss.hip"]
 
 
 def hipcc():

@@ -7,78 +7,9 @@
 
 #include "../../include/ozaki2.h"
 #include "oz2_layers.h"
+#include "oz2_operands.h"
 
 namespace {
-
-constexpr ll kMaxRows = 1ll << 30, kMaxWidth = 1ll << 21, kMaxLd = 1ll << 40, kMaxElems = 1ll << 40;
-
-size_t element(int dtype) { return dtype == OZ2_F32 ? 4 : 2; }
-size_t align256(size_t x) { return (x + 255) / 256 * 256; }
-
-// `count` matrices of rows x cols elements
-struct Mat {
-  const void* p;
-  ll rows, cols, ld;
-  int count;
-  ll stride;
-  bool empty() const { return !p || rows <= 0 || cols <= 0 || count <= 0; }
-  size_t span(size_t e) const { return (size_t)((count - 1) * stride + (rows - 1) * ld + cols) * e; }
-};
-
-Mat mat(const void* p, ll rows, ll cols, ll ld, int count = 1, ll stride = 0) {
-  return Mat{p, rows, cols, ld, count, stride};
-}
-
-// an operand that is needed: there, aligned to its elements, leading dimension
-// and stride in range
-bool good(const Mat& m, size_t e, bool output = false) {
-  if (m.rows <= 0 || m.cols <= 0 || m.count <= 0) return true;
-  if (!m.p || (uintptr_t)m.p % e) return false;
-  if (m.ld < m.cols || m.ld > kMaxLd) return false;
-  if (m.count == 1) return true;
-  if (m.stride < 0 || m.stride > kMaxLd) return false;
-  // outputs: one matrix after the other, or all matrices' first rows, then their second ones
-  return !output || m.stride >= (m.rows - 1) * m.ld + m.cols ||
-         (m.stride >= m.cols && m.ld >= (m.count - 1) * m.stride + m.cols);
-}
-
-// bytes at [0, ca) and at [d, d + cb) of every `period`
-bool apart(ll d, ll ca, ll cb, ll period) {
-  if (period <= 0) return false;
-  d %= period;
-  if (d < 0) d += period;
-  return d >= ca && d + cb <= period;
-}
-
-// no element in both.  Matrices of one leading dimension may lie side by side (column
-// ranges of one buffer), also where they are stacked in whole rows of it, and stacks of
-// one stride may lie in between each other (a layer's parameters one after the other, for
-// every layer).
-bool disjoint(const Mat& a, const Mat& b, size_t e) {
-  if (a.empty() || b.empty()) return true;
-  const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)b.p;
-  if (a0 + a.span(e) <= b0 || b0 + b.span(e) <= a0) return true;
-  const ll d = (ll)b0 - (ll)a0, size = (ll)e;
-  auto whole_rows = [](const Mat& m) { return m.count == 1 || m.stride % m.ld == 0; };
-  if (a.ld == b.ld && whole_rows(a) && whole_rows(b) &&
-      apart(d, a.cols * size, b.cols * size, a.ld * size))
-    return true;
-  if (a.count == 1 && b.count == 1) return false;
-  if (a.count > 1 && b.count > 1 && a.stride != b.stride) return false;
-  return apart(d, ((a.rows - 1) * a.ld + a.cols) * size, ((b.rows - 1) * b.ld + b.cols) * size,
-               (a.count > 1 ? a.stride : b.stride) * size);
-}
-bool disjoint_bytes(const Mat& a, size_t e, const void* p, size_t bytes) {
-  if (a.empty() || !p || !bytes) return true;
-  const uintptr_t a0 = (uintptr_t)a.p, b0 = (uintptr_t)p;
-  return a0 + a.span(e) <= b0 || b0 + bytes <= a0;
-}
-
-bool offsets_apart(const Oz2Groups& gr, const void* ws, size_t bytes) {
-  return !gr.offsets || disjoint_bytes(mat(gr.offsets, 1, gr.groups + 1, gr.groups + 1), 4, ws, bytes);
-}
-
-int hip_status(hipError_t e) { return e == hipSuccess ? OZ2_OK : OZ2_E_DEVICE; }
 
 bool sizes_ok(int dtype, int act, ll rows, ll groups, ll out, ll in, int gated) {
   if (dtype < OZ2_F32 || dtype > OZ2_BF16 || act < OZ2_ACT_NONE || act > OZ2_ACT_SILU) return false;
@@ -86,20 +17,6 @@ bool sizes_ok(int dtype, int act, ll rows, ll groups, ll out, ll in, int gated) 
   if (groups < 1 || groups > OZ2_MAX_EXPERTS) return false;
   const ll n2 = gated ? 2 * out : out;
   return rows * n2 < kMaxElems && rows * in < kMaxElems && (double)n2 * in * groups < (double)kMaxElems;
-}
-
-// pitch of dZ in the workspace: whole 64-byte pieces
-ll slope_pitch(ll n2, size_t e) {
-  const ll per = 64 / (ll)e;
-  return (n2 + per - 1) / per * per;
-}
-
-// the parts of a split sum, then the packed operands
-size_t part_bytes(const Oz2Plan& pl, ll M, ll N2) {
-  return pl.splits > 1 ? align256((size_t)pl.splits * M * N2 * 4) : 0;
-}
-size_t product_bytes(const Oz2Plan& pl, ll M, ll N2) {
-  return part_bytes(pl, M, N2) + align256(pl.packed_bytes);
 }
 
 struct BackwardLayout {
@@ -122,11 +39,6 @@ BackwardLayout backward_layout(int dtype, int act, int gated, const Oz2Groups& g
   o += std::max(product_bytes(L.dgrad, gr.rows, in), product_bytes(L.wgrad, n2, in));
   L.total = o;
   return L;
-}
-
-int check_workspace(const void* ws, size_t bytes, size_t need) {
-  if (!need) return OZ2_OK;
-  return ws && (uintptr_t)ws % 256 == 0 && bytes >= need ? OZ2_OK : OZ2_E_WORKSPACE;
 }
 
 size_t forward_bytes(int dtype, int gated, const Oz2Groups& gr, ll out, ll in) {
@@ -280,7 +192,6 @@ bool tokens_ok(int dtype, int tokens, int top_k, int width) {
          width >= 0 && width <= kMaxWidth && (ll)tokens * top_k <= kMaxRows &&
          (ll)tokens * top_k * width < kMaxElems;
 }
-bool int_ok(const void* p) { return p && (uintptr_t)p % 4 == 0; }
 
 }  // namespace
 
@@ -310,7 +221,8 @@ bool int_ok(const void* p) { return p && (uintptr_t)p % 4 == 0; }
 // 113 against 112; without gates tiles win (64 experts, 4096 -> 2048, 213 and 291 against
 // 178; 16 in fp32, 1024 -> 2048, 41 and 42 against 39), and so they do where most rows fall
 // to one group (k_rows reads W again for every 32 of them).
-Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr, bool padded) {
+Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr, bool padded,
+                 bool whole) {
   const double cus = oz2_device_cus();
   const bool wide = dtype == OZ2_F32;
   if (side == OZ2_FWD && gr.offsets && M <= 8ll * gr.groups)
@@ -338,7 +250,7 @@ Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr
     t_best = 2.0 + mb / 5.6 + (double)M * (0.05 + 0.003 * mb);
   }
   const double big = tiles(256.0);
-  const int most = gr.offsets ? 1 : (int)std::min(32.0, std::max(1.0, stages / 4.0));
+  const int most = gr.offsets || whole ? 1 : (int)std::min(32.0, std::max(1.0, stages / 4.0));
   for (int pack = 0; pack <= (odd ? 1 : 0); ++pack) {
     const double first = pack ? 4.0 + (double)packed / 2e6 : 0.0;
     const bool slow = odd && !pack;

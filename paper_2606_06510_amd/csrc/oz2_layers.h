@@ -29,6 +29,34 @@ enum Oz2Side {
   OZ2_WGRAD    // A = dZ, B = X: i and j contiguous
 };
 
+// What becomes of a product's sums
+enum Oz2End {
+  OZ2_END_Y,     // y (and z) with bias, activation and residual, or parts of a split sum
+  OZ2_END_LSE,   // FWD: of each row's columns, a chunk at a time, the largest and the sum of exponentials
+  OZ2_END_DZ,    // FWD: the gradient of the loss at the logits
+  OZ2_END_SUM    // DGRAD, WGRAD: y, or added to the parts of the sum so far
+};
+
+// The loss over a vocabulary: its rows, and how far its sums have come
+struct Oz2Chunk {
+  float top, sum;        // the largest logit; the sum of e^(z - largest)
+};
+struct alignas(16) Oz2LossRow {
+  float lse, factor;
+  int target;            // -1: the row does not count
+  int unused;
+};
+struct Oz2Loss {
+  const void* targets;   // LSE: one for each row, int or long long
+  int wide;
+  Oz2Chunk* chunks;      // LSE: [chunk][M]
+  float* picked;         // LSE: [M], the target's logit (where the row has one)
+  const Oz2LossRow* rows;   // DZ: [M]
+  int first;             // DZ: the vocabulary's index of column 0
+  const float* scale;    // SUM: null, or [1] is what the sums are multiplied by at last
+  int whole, more;       // SUM: y at once; added to what part holds already
+};
+
 struct Oz2Product {
   const void *A, *B;
   ll lda, ldb;           // elements between rows of A and B as they lie in memory
@@ -49,6 +77,7 @@ struct Oz2Product {
   void* packed;          // room for the copies that the plan asks for
   float* part;           // splits > 1: [split][M][N2] partial sums
   int splits, esize;     // (set by the launcher)
+  Oz2Loss loss;
 };
 
 // How a product runs: `rows` > 0: the kernel of few rows, that many blocks of 16 at a
@@ -63,8 +92,9 @@ struct Oz2Plan {
 };
 inline ll oz2_packed_pitch(ll cols, size_t e) { return (cols * (ll)e + 127) / 128 * 128 / (ll)e; }
 // padded: as in Oz2Product
+// whole: the sum is not split
 Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr,
-                 bool padded = false);
+                 bool padded = false, bool whole = false);
 // the plan of a product (side 0, 1, 2; groups 0: one product) as rows, tile, splits and
 // pack: a diagnostic for tests, not part of the public ABI
 extern "C" void oz2_plan_of(int dtype, int side, ll M, ll N2, ll L, int rows, int groups, int padded,

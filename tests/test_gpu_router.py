@@ -1,0 +1,239 @@
+"""expert_route and its gradient against the definition in Python's floats: choices
+exactly, weights and gradients within the bounds of model_util."""
+import itertools
+import math
+
+import pytest
+import torch
+
+from tests import layer_util as lu
+from tests import model_util as mu
+from tests.gpu_util import device
+
+pytestmark = pytest.mark.gpu
+
+INF, NAN = math.inf, math.nan
+
+
+def oz():
+    import paper_2606_06510_amd
+    return paper_2606_06510_amd
+
+
+def check_route(logits, bias, k, score="softmax", groups=1, top=1, best=2, renorm=True, scale=1.0, rows=None):
+    """logits on the device; rows: those compared (all)"""
+    ids, w = oz().expert_route(logits, k, bias=bias, score=score, groups=groups, top_groups=top,
+                               group_best=best, renormalize=renorm, scale=scale)
+    assert ids.dtype == torch.int32 and w.dtype == torch.float32 and ids.shape == w.shape == (logits.shape[0], k)
+    L, I, W = lu.d(logits).tolist(), ids.cpu().tolist(), w.cpu().tolist()
+    b = None if bias is None else lu.d(bias).tolist()
+    for t in rows if rows is not None else range(len(L)):
+        want, wt = mu.route_row(L[t], b, k, score, groups, top, best, renorm, scale)
+        assert I[t] == want, (t, I[t], want)
+        for j, v in enumerate(wt):
+            assert (math.isnan(v) and math.isnan(W[t][j])) or \
+                abs(W[t][j] - v) <= mu.route_weight_error(L[t], v), (t, j, W[t][j], v)
+    return ids, w
+
+
+def make(T, E, dtype, seed, spread=1.0):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((T, E), generator=g) * spread + torch.randn((1, E), generator=g) * 0.5
+    return x.to(lu.DTYPES[dtype]).to(device()), (torch.randn((E,), generator=g) * 0.1).to(device())
+
+
+@pytest.mark.parametrize("dtype", list(lu.DTYPES))
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 8, 2), (3, 5, 5), (7, 16, 4), (9, 33, 8), (70, 64, 6),
+                                   (33, 100, 10), (5, 129, 1), (18, 256, 8), (4, 300, 64), (3, 512, 12),
+                                   (2, 1000, 17), (3, 1024, 8)])
+def test_choices_and_weights(T, E, k, dtype):
+    logits, bias = make(T, E, dtype, 11 * T + E)
+    for score in ("softmax", "sigmoid"):
+        for b in (None, bias):
+            for renorm in (True, False):
+                check_route(logits, b, k, score, renorm=renorm, scale=1.5)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("E,groups,top,k", [(8, 8, 3, 3), (8, 2, 1, 4), (12, 4, 2, 5), (64, 8, 4, 8), (66, 3, 2, 7),
+                                            (256, 8, 4, 8), (256, 256, 9, 9), (1024, 32, 5, 16), (100, 1, 1, 3),
+                                            (40, 5, 5, 6), (258, 2, 1, 6), (510, 17, 3, 4)])
+def test_groups(E, groups, top, k, dtype):
+    logits, bias = make(21, E, dtype, E + groups)
+    for best in (1, 2):
+        check_route(logits, bias, k, "sigmoid", groups, top, best, scale=2.5)
+        check_route(logits, bias, k, "softmax", groups, top, best, renorm=False)
+        check_route(logits, None, k, "softmax", groups, top, best)
+
+
+@pytest.mark.parametrize("E", [6, 64, 200, 700])
+def test_equal_values_go_to_the_lowest_index(E):
+    """few distinct logits (and negative zeros): mostly ties"""
+    g = torch.Generator().manual_seed(E)
+    l = torch.randint(-1, 2, (40, E), generator=g).float() * 0.5
+    l[l == 0] *= torch.where(torch.rand(int((l == 0).sum()), generator=g) < 0.5, -1.0, 1.0)
+    l = l.to(device())
+    bias = (torch.randint(0, 2, (E,), generator=g).float() * 0.25).to(device())
+    for score in ("softmax", "sigmoid"):
+        check_route(l, None, 5, score)
+        check_route(l, bias * 0, 5, score)
+        check_route(l, bias, 5, score)
+        check_route(l, None, 2, score, 2, 1, 1)
+        check_route(torch.zeros_like(l), None, 3, score, 2, 1, 2)
+        check_route(torch.zeros_like(l), bias, 3, score, 2, 1, 2)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_neighbouring_scores(score):
+    """biases and logits a few steps of 32 bits apart: the order is that of 64 bits"""
+    g = torch.Generator().manual_seed(8)
+    step = torch.randint(-3, 4, (50, 96), generator=g)
+    l = (0.75 + step * 2.0 ** -24).float().to(device())
+    bias = (0.125 + torch.randint(-3, 4, (96,), generator=g) * 2.0 ** -26).float().to(device())
+    check_route(l, None, 9, score)
+    check_route(l, bias, 9, score)
+    check_route(l, None, 9, score, 4, 2, 1)
+    # Sums of two such values meet to within what 64 bits hold: with s = s0 (1 + h 2^-24 + h^2
+    # 2^-49 ..), two pairs of equal h and bias in all differ by s0 2^-48 at most, 4e-17 for s0 =
+    # 1 / 96 beside a value of 0.27, whose last place is 6e-17.  A value is off by its
+    # exponential (2), division, sum and bias (4 in all), and the pair's sum: 12 2^-53 of it;
+    # any two groups within twice that are as good.
+    for b in (bias, torch.zeros_like(bias)):
+        ids, _ = oz().expert_route(l, 9, bias=b, score=score, groups=4, top_groups=2)
+        for row, got in zip(lu.d(l).tolist(), ids.cpu().tolist()):
+            def pairs(value):
+                least = sorted(value)[-2]
+                near = 24 * 2.0 ** -53 * max(map(abs, value))
+                return [p for p in itertools.combinations(range(4), 2) if min(value[i] for i in p) >= least - near
+                        and max(value[i] for i in p) >= max(value) - near]
+            found, fits = [], []
+            mu.route_row(row, lu.d(b).tolist(), 9, score, 4, 2, 2, True, 1.0,
+                         chosen=lambda v: found.extend(pairs(v)) or [])
+            for p in found:
+                fits.append(mu.route_row(row, lu.d(b).tolist(), 9, score, 4, 2, 2, True, 1.0,
+                                         chosen=lambda v: p)[0])
+            assert got in fits
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("groups", [1, 4])
+def test_experts_that_are_out(score, groups):
+    """-infinity in logits or bias: rows with some, few and no experts left"""
+    l, bias = make(40, 32, "fp32", 5)
+    l[0] = -INF
+    l[1, :] = -INF
+    l[1, 9] = -3.0
+    l[2, 8:] = -INF
+    l[3:20, ::3] = -INF
+    l[20, 5] = l[21, 0] = -INF
+    off = bias.clone()
+    off[[1, 2, 30]] = -INF
+    for b in (None, bias, off):
+        for renorm in (True, False):
+            for best in (1, 2):
+                check_route(l, b, 6, score, groups, max(1, groups // 2), best, renorm)
+    ids, w = check_route(l, torch.full_like(bias, -INF), 2, score, groups, 1)
+    assert (ids == -1).all() and (w == 0).all()
+    order = oz().expert_sort(ids, 32)
+    assert int(order.offsets[-1]) == 0
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_nan_and_infinities(score):
+    l, bias = make(12, 24, "bf16", 6)
+    l[0, 3] = NAN
+    l[1, 5] = INF
+    l[2, [4, 7]] = INF
+    l[3, 1] = NAN
+    l[3, 2] = INF
+    l[4, :] = NAN
+    l[5, 11], l[5, 0] = INF, -INF
+    for b in (None, bias):
+        for renorm in (True, False):
+            check_route(l, b, 4, score, renorm=renorm)
+            check_route(l, b, 4, score, 3, 2, 1, renorm)
+            check_route(l, b, 4, score, 3, 2, 2, renorm)
+    odd = bias.clone()
+    odd[2], odd[9] = NAN, INF
+    check_route(l[6:], odd, 4, score)
+    check_route(l[6:], odd, 4, score, 3, 2, 2)
+
+
+def test_scores_too_small_for_32_bits():
+    """the bias chooses experts whose scores underflow: their shares are still theirs"""
+    l = torch.full((2, 8), 100.0)
+    l[:, 1], l[:, 2], l[:, 5] = -95.0, -96.0, -95.5
+    bias = torch.zeros(8)
+    bias[[1, 2, 5]] = 10.0
+    ids, w = check_route(l.to(device()), bias.to(device()), 3, "softmax")
+    assert ids[0].tolist() == [1, 2, 5]
+    ids, w = check_route((l - 100).to(device()), bias.to(device()), 3, "sigmoid")
+    assert abs(float(w.sum(1)[0]) - 1) < 1e-6 and float(w[0].min()) > 0.1
+
+
+def test_strided_and_unaligned_rows():
+    l, bias = make(50, 90, "fp16", 9)
+    big = torch.full((50, 131), NAN, dtype=l.dtype, device=l.device)
+    view = big[:, 5:95]
+    view.copy_(l)
+    for b in (None, bias):
+        a, c = check_route(view, b, 7, "sigmoid", 9, 4, 2), oz().expert_route(l, 7, bias=b, score="sigmoid",
+                                                                              groups=9, top_groups=4)
+        assert torch.equal(a[0], c[0]) and torch.equal(a[1], c[1])
+    dw = torch.randn((50, 7), device=l.device)
+    ids = c[0]
+    out = torch.full((50, 140), 7.0, dtype=l.dtype, device=l.device)
+    got = oz().expert_route_backward(dw, view, ids, dlogits=out[:, 3:93])
+    assert torch.equal(got, oz().expert_route_backward(dw, l, ids))
+    assert (out[:, :3] == 7).all() and (out[:, 93:] == 7).all()
+
+
+@pytest.mark.parametrize("T,E,k", [(4096, 64, 8), (20001, 128, 6), (6000, 256, 8), (3001, 1024, 4)])
+def test_many_tokens(T, E, k):
+    logits, bias = make(T, E, "bf16", 3)
+    rows = list(range(0, T, 61)) + [T - 2, T - 1]
+    check_route(logits, None, k, rows=rows)
+    check_route(logits, bias, k, "sigmoid", 8, 3, 2, rows=rows)
+    assert oz().expert_route(logits[:0], k)[0].shape == (0, k)
+
+
+def check_backward(dw, l, ids, score, renorm, scale):
+    got = oz().expert_route_backward(dw, l, ids, score=score, renormalize=renorm, scale=scale)
+    want = mu.route_backward(dw, l, ids, score, renorm, scale)
+    lu.check(got, want, mu.route_backward_error(dw, l, ids, scale), f"{score} {renorm}")
+    return got
+
+
+@pytest.mark.parametrize("dtype", list(lu.DTYPES))
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 8, 2), (5, 33, 4), (40, 64, 8), (9, 130, 6), (6, 256, 8),
+                                   (3, 700, 64), (4, 1024, 3)])
+def test_gradient(T, E, k, dtype):
+    l, bias = make(T, E, dtype, 31 * T + E)
+    dw = torch.randn((T, k), generator=torch.Generator().manual_seed(T)).to(device())
+    for score in ("softmax", "sigmoid"):
+        for renorm in (True, False):
+            ids, _ = oz().expert_route(l, k, bias=bias, score=score, renormalize=renorm, scale=1.5)
+            check_backward(dw, l, ids, score, renorm, 1.5)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renorm", [True, False])
+def test_gradient_of_dropped_repeated_and_masked_choices(score, renorm):
+    l, _ = make(8, 20, "fp32", 17)
+    l[:, 4] = -INF
+    l[7] = -INF
+    ids = torch.randint(0, 4, (8, 5), dtype=torch.int32)
+    ids[:, 0] = torch.arange(8) + 5
+    ids[1, 2] = -1
+    ids[2] = -1
+    ids[3, 1] = 20          # outside: no part
+    ids[4, 1] = ids[4, 0]   # the same expert twice
+    ids[7] = -1
+    dw = torch.randn((8, 5), generator=torch.Generator().manual_seed(2))
+    dw[1, 2] = dw[2, 0] = dw[3, 1] = NAN   # of choices that take no part
+    want = dw.clone()
+    want[torch.isnan(want)] = 0.0
+    ids = ids.to(device())
+    a = oz().expert_route_backward(dw.to(device()), l, ids, score=score, renormalize=renorm)
+    b = check_backward(want.to(device()), l, ids, score, renorm, 1.0)
+    assert torch.equal(a, b) and (a[2] == 0).all() and (a[7] == 0).all() and (a[:, 4] == 0).all()
