@@ -213,7 +213,7 @@ int ozaki2_layer_norm_backward(int dtype, int rows, int width, const void* dy, l
   if (sb && !disjoint_bytes(mat(stats, 1, 2 * (ll)rows, 2 * (ll)rows), 4, workspace, need)) return OZ2_E_INVALID;
   if ((st = oz2_device_ok()) != OZ2_OK) return st;
   return hip_status(oz2_launch_norm_backward(
-      dtype, Oz2NormBack{dy, lddy, x, ldx, stats, weight, residual, ldr, rows, width, dx, lddx, dweight, dbias,
+      dtype, Oz2NormBack{dy, lddy, mx.p, ldx, reads ? stats : nullptr, mw.p, residual, ldr, rows, width, dx, lddx, dweight, dbias,
                          (float*)workspace, 0},
       (hipStream_t)stream));
 }

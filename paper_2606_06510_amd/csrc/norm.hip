@@ -1,50 +1,130 @@
-// Layer norm of rows, and its gradients.
+// Layer norm of rows, and its gradients.  Both are bound by memory: every entry is read
+// once and kept in registers while its row's sums are taken, the variance about the mean.
+//
+// L lanes have a row, lane l its 16-byte pieces l, l + L, .., N of them at most.
 #include <algorithm>
 
+#include "oz2_lanes.h"
 #include "oz2_model.h"
 
 #pragma clang fp contract(fast)
 
 namespace {
 
-constexpr int NT = 256, SUM_ROWS = 256;   // rows of a partial column sum
 constexpr ll ROW_BLOCKS = 1 << 20;
 
-// The sum of v over the workgroup, in a fixed order, in all threads
-__device__ __forceinline__ float block_sum(float v, float* red) {
+// M sums over the L lanes of each row, in a fixed order, in all of them.  Beyond a wave by way
+// of LDS (red: M floats for each wave of the workgroup), and every thread calls it; red may
+// be written again after the next barrier.
+template <int L, int M>
+__device__ __forceinline__ void row_sums(float (&v)[M], float* red) {
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (red[0] + red[1]) + (red[2] + red[3]);
+  for (int i = 0; i < M; ++i) v[i] = across<(L < 64 ? L : 64), true>(v[i]);
+  if constexpr (L > 64) {
+    const int w = threadIdx.x >> 6, first = w / (L / 64) * (L / 64);
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int i = 0; i < M; ++i) red[w * M + i] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+      float s = 0.0f;
+#pragma unroll
+      for (int k = 0; k < L / 64; ++k) s += red[(first + k) * M + i];
+      v[i] = s;
+    }
+  }
 }
 
-template <class T>
-__global__ void __launch_bounds__(NT)
+template <class T, int L, int N>
+__global__ void __launch_bounds__(L < 256 ? 256 : L)
 k_norm(Oz2Norm a) {
-  constexpr int P = 16 / sizeof(T);
-  __shared__ float red[4];
+  constexpr int P = 16 / sizeof(T), NT = L < 256 ? 256 : L, G = NT / L;
+  __shared__ float red[2][NT / 64];
+  const int lane = threadIdx.x % L;
+  const float n = (float)a.width;
+  for (ll r = (ll)blockIdx.x * G + threadIdx.x / L; r < a.rows; r += (ll)gridDim.x * G) {
+    const T* x = (const T*)a.x + r * a.ldx;
+    Piece<T, P> v[N], w[N], b[N];
+    float sum[1] = {0.0f};
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int c = (lane + L * k) * P;
+      v[k] = load_piece<T>(x + c, a.width - c);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int c = (lane + L * k) * P;
+      if (a.weight) w[k] = load_piece<T>((const T*)a.weight + c, a.width - c);
+      if (a.bias) b[k] = load_piece<T>((const T*)a.bias + c, a.width - c);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int i = 0; i < P; ++i) sum[0] += to_f(v[k].v[i]);
+    row_sums<L>(sum, red[0]);
+    const float mean = sum[0] / n;
+    sum[0] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int valid = a.width - (lane + L * k) * P;
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const float d = to_f(v[k].v[i]) - mean;
+        if (i < valid) sum[0] += d * d;
+      }
+    }
+    row_sums<L>(sum, red[1]);
+    const float rstd = 1.0f / sqrtf(sum[0] / n + a.eps);
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const int c = (lane + L * k) * P, valid = a.width - c;
+      Piece<T, P> o;
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        float q = (to_f(v[k].v[i]) - mean) * rstd;
+        if (a.weight) q *= to_f(w[k].v[i]);
+        if (a.bias) q += to_f(b[k].v[i]);
+        o.v[i] = from_f<T>(q);
+      }
+      store_stream((T*)a.y + r * a.ldy + c, o, valid);
+    }
+    if (a.stats && lane == 0) {
+      a.stats[2 * r] = mean;
+      a.stats[2 * r + 1] = rstd;
+    }
+  }
+}
+
+// Longer rows: read three times, the second and third time from a cache
+template <class T>
+__global__ void __launch_bounds__(1024)
+k_norm_long(Oz2Norm a) {
+  constexpr int P = 16 / sizeof(T), NT = 1024;
+  __shared__ float red[2][NT / 64];
+  const float n = (float)a.width;
   for (ll r = blockIdx.x; r < a.rows; r += gridDim.x) {
     const T* x = (const T*)a.x + r * a.ldx;
-    T* y = (T*)a.y + r * a.ldy;
-    float sum = 0.0f;
+    float sum[1] = {0.0f};
     for (int c = threadIdx.x * P; c < a.width; c += NT * P) {
       const Piece<T, P> v = load_piece<T>(x + c, a.width - c);
 #pragma unroll
-      for (int i = 0; i < P; ++i) sum += to_f(v.v[i]);
+      for (int i = 0; i < P; ++i) sum[0] += to_f(v.v[i]);
     }
-    const float mean = block_sum(sum, red) / (float)a.width;
-    sum = 0.0f;
+    row_sums<NT>(sum, red[0]);
+    const float mean = sum[0] / n;
+    sum[0] = 0.0f;
     for (int c = threadIdx.x * P; c < a.width; c += NT * P) {
       const Piece<T, P> v = load_piece<T>(x + c, a.width - c);
 #pragma unroll
       for (int i = 0; i < P; ++i) {
         const float d = to_f(v.v[i]) - mean;
-        if (c + i < a.width) sum += d * d;
+        if (c + i < a.width) sum[0] += d * d;
       }
     }
-    const float rstd = 1.0f / sqrtf(block_sum(sum, red) / (float)a.width + a.eps);
+    row_sums<NT>(sum, red[1]);
+    const float rstd = 1.0f / sqrtf(sum[0] / n + a.eps);
     for (int c = threadIdx.x * P; c < a.width; c += NT * P) {
       const int valid = a.width - c;
       const Piece<T, P> v = load_piece<T>(x + c, valid);
@@ -58,22 +138,147 @@ k_norm(Oz2Norm a) {
         if (a.bias) q += to_f(b.v[i]);
         o.v[i] = from_f<T>(q);
       }
-      store_piece(y + c, o, valid);
+      store_stream((T*)a.y + r * a.ldy + c, o, valid);
     }
     if (a.stats && threadIdx.x == 0) {
       a.stats[2 * r] = mean;
       a.stats[2 * r + 1] = rstd;
     }
-    __syncthreads();
   }
 }
 
+// ---------------------------------------------------------------- gradients
+// A workgroup takes every gridDim-th of its G rows' groups, U of them at a time, and keeps
+// the column sums of its rows in registers; they leave as one partial row each of dweight
+// and dbias, which k_norm_join adds up in order.
+constexpr int U = 2;
+
+template <class T, int L, int N, int G>
+__global__ void __launch_bounds__(L* G)
+k_norm_backward(Oz2NormBack a) {
+  constexpr int P = 16 / sizeof(T), NT = L * G;
+  __shared__ float red[2][NT / 64 * 2 * U];
+  __shared__ float others[G > 1 ? (G - 1) * L * N * P : 1];
+  const int lane = threadIdx.x % L, grp = threadIdx.x / L;
+  const float n = (float)a.width;
+  const bool cols = a.dweight || a.dbias;
+  float dw[N * P], db[N * P];
+#pragma unroll
+  for (int i = 0; i < N * P; ++i) dw[i] = db[i] = 0.0f;
+  Piece<T, P> w[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const int c = (lane + L * k) * P;
+    if (a.weight) w[k] = load_piece<T>((const T*)a.weight + c, a.width - c);
+  }
+  const ll step = (ll)gridDim.x * G;
+  int turn = 0;
+  for (ll r0 = (ll)blockIdx.x * G; r0 < a.rows; r0 += step * U, turn ^= 1) {
+    Piece<T, P> x[U][N], dy[U][N], res[U][N];
+    float mean[U], rstd[U], sum[2 * U];
+    bool on[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const ll r = r0 + u * step + grp;
+      on[u] = r < a.rows;
+      const int width = on[u] ? a.width : 0;
+      mean[u] = on[u] && a.stats ? a.stats[2 * r] : 0.0f;
+      rstd[u] = on[u] && a.stats ? a.stats[2 * r + 1] : 0.0f;
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const int c = (lane + L * k) * P, valid = width - c;
+        dy[u][k] = load_stream<T>((const T*)a.dy + r * a.lddy + c, valid);
+        if (a.x) x[u][k] = load_stream<T>((const T*)a.x + r * a.ldx + c, valid);
+        if (a.residual) res[u][k] = load_stream<T>((const T*)a.residual + r * a.ldr + c, valid);
+      }
+    }
+    auto h_of = [&](int u, int k, int i) {
+      // (behind the row's end x reads as 0, which is not the mean)
+      return a.x && i < a.width - (lane + L * k) * P ? (to_f(x[u][k].v[i]) - mean[u]) * rstd[u] : 0.0f;
+    };
+    auto g_of = [&](int u, int k, int i) {
+      const float d = to_f(dy[u][k].v[i]);
+      return a.weight ? d * to_f(w[k].v[i]) : d;
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      sum[2 * u] = sum[2 * u + 1] = 0.0f;
+      if (!on[u]) continue;
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          const float h = h_of(u, k, i), g = g_of(u, k, i), d = to_f(dy[u][k].v[i]);
+          sum[2 * u] += g;
+          sum[2 * u + 1] += g * h;
+          dw[k * P + i] += d * h;
+          db[k * P + i] += d;
+        }
+    }
+    if (!a.dx) continue;
+    row_sums<L>(sum, red[turn]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (!on[u]) continue;
+      const ll r = r0 + u * step + grp;
+      const float mg = sum[2 * u] / n, mh = sum[2 * u + 1] / n;
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const int c = (lane + L * k) * P;
+        Piece<T, P> o;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          float d = rstd[u] * (g_of(u, k, i) - mg - h_of(u, k, i) * mh);
+          if (a.residual) d += to_f(res[u][k].v[i]);
+          o.v[i] = from_f<T>(d);
+        }
+        store_stream((T*)a.dx + r * a.lddx + c, o, a.width - c);
+      }
+    }
+  }
+  if (!cols) return;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float* mine = which ? db : dw;
+    if (G > 1) {
+      __syncthreads();
+      if (grp > 0) {
+#pragma unroll
+        for (int i = 0; i < N * P; ++i) others[(grp - 1) * L * N * P + i * L + lane] = mine[i];
+      }
+      __syncthreads();
+      if (grp == 0) {
+        for (int q = 0; q < G - 1; ++q)
+#pragma unroll
+          for (int i = 0; i < N * P; ++i) mine[i] += others[q * L * N * P + i * L + lane];
+      }
+    }
+    if (grp == 0) {
+      float* to = a.part + (2ll * blockIdx.x + which) * a.width;
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const int c = (lane + L * k) * P;
+        Piece<float, P> o;
+#pragma unroll
+        for (int i = 0; i < P; ++i) o.v[i] = mine[k * P + i];
+        if (c < a.width) store_piece(to + c, o, a.width - c);
+      }
+    }
+  }
+}
+
+// Longer rows: dX of a row by a workgroup, and partial column sums of LONG_ROWS rows, a column
+// a thread
+constexpr int LONG_ROWS = 64;
+
 template <class T>
-__global__ void __launch_bounds__(NT)
-k_norm_dx(Oz2NormBack a) {
-  constexpr int P = 16 / sizeof(T);
-  __shared__ float red[4];
-  for (ll r = blockIdx.x; r < a.rows; r += gridDim.x) {
+__global__ void __launch_bounds__(1024)
+k_norm_dx_long(Oz2NormBack a) {
+  constexpr int P = 16 / sizeof(T), NT = 1024;
+  __shared__ float red[2][NT / 64 * 2];
+  const float n = (float)a.width;
+  int turn = 0;
+  for (ll r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
     const T *x = (const T*)a.x + r * a.ldx, *dy = (const T*)a.dy + r * a.lddy;
     const float mean = a.stats[2 * r], rstd = a.stats[2 * r + 1];
     auto at = [&](int c, float* g, float* h) {
@@ -87,17 +292,17 @@ k_norm_dx(Oz2NormBack a) {
         h[i] = i < valid ? (to_f(v.v[i]) - mean) * rstd : 0.0f;
       }
     };
-    float sg = 0.0f, sh = 0.0f, g[P], h[P];
+    float sum[2] = {0.0f, 0.0f}, g[P], h[P];
     for (int c = threadIdx.x * P; c < a.width; c += NT * P) {
       at(c, g, h);
 #pragma unroll
       for (int i = 0; i < P; ++i) {
-        sg += g[i];
-        sh += g[i] * h[i];
+        sum[0] += g[i];
+        sum[1] += g[i] * h[i];
       }
     }
-    sg = block_sum(sg, red) / (float)a.width;
-    sh = block_sum(sh, red) / (float)a.width;
+    row_sums<NT>(sum, red[turn]);
+    const float mg = sum[0] / n, mh = sum[1] / n;
     for (int c = threadIdx.x * P; c < a.width; c += NT * P) {
       const int valid = a.width - c;
       at(c, g, h);
@@ -105,28 +310,26 @@ k_norm_dx(Oz2NormBack a) {
       if (a.residual) q = load_piece<T>((const T*)a.residual + r * a.ldr + c, valid);
 #pragma unroll
       for (int i = 0; i < P; ++i) {
-        float d = rstd * (g[i] - sg - h[i] * sh);
+        float d = rstd * (g[i] - mg - h[i] * mh);
         if (a.residual) d += to_f(q.v[i]);
         o.v[i] = from_f<T>(d);
       }
-      store_piece((T*)a.dx + r * a.lddx + c, o, valid);
+      store_stream((T*)a.dx + r * a.lddx + c, o, valid);
     }
-    __syncthreads();
   }
 }
 
-// partial column sums of SUM_ROWS rows, a column a thread
 template <class T>
-__global__ void __launch_bounds__(NT)
-k_norm_columns(Oz2NormBack a) {
-  const int c = (int)blockIdx.x * NT + threadIdx.x;
+__global__ void __launch_bounds__(256)
+k_norm_columns_long(Oz2NormBack a) {
+  const int c = (int)blockIdx.x * 256 + threadIdx.x;
   if (c >= a.width) return;
   for (int q = blockIdx.y; q < a.parts; q += gridDim.y) {
-    const ll r0 = (ll)q * SUM_ROWS, r1 = min(r0 + SUM_ROWS, (ll)a.rows);
+    const ll r0 = (ll)q * LONG_ROWS, r1 = min(r0 + LONG_ROWS, (ll)a.rows);
     float sw = 0.0f, sb = 0.0f;
     for (ll r = r0; r < r1; ++r) {
       const float d = to_f(((const T*)a.dy)[r * a.lddy + c]);
-      if (a.dweight) sw += d * (to_f(((const T*)a.x)[r * a.ldx + c]) - a.stats[2 * r]) * a.stats[2 * r + 1];
+      if (a.dweight) sw += d * ((to_f(((const T*)a.x)[r * a.ldx + c]) - a.stats[2 * r]) * a.stats[2 * r + 1]);
       sb += d;
     }
     a.part[(2ll * q) * a.width + c] = sw;
@@ -134,48 +337,132 @@ k_norm_columns(Oz2NormBack a) {
   }
 }
 
+// 32 columns of dweight (grid y 0) or dbias: the parts in eight runs, each in order, then the
+// runs in order
 template <class T>
-__global__ void __launch_bounds__(NT)
+__global__ void __launch_bounds__(256)
 k_norm_join(Oz2NormBack a) {
-  const int c = (int)blockIdx.x * NT + threadIdx.x;
-  if (c >= a.width) return;
-  float sw = 0.0f, sb = 0.0f;
-  for (int q = 0; q < a.parts; ++q) {
-    sw += a.part[(2ll * q) * a.width + c];
-    sb += a.part[(2ll * q + 1) * a.width + c];
+  __shared__ float red[8][32];
+  T* to = (T*)(blockIdx.y ? a.dbias : a.dweight);
+  if (!to) return;
+  const int l = threadIdx.x & 31, run = threadIdx.x >> 5, c = (int)blockIdx.x * 32 + l;
+  const int per = (a.parts + 7) / 8, k0 = run * per, k1 = min(a.parts, k0 + per);
+  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (c < a.width) {
+    const float* q = a.part + (ll)blockIdx.y * a.width + c;
+    int k = k0;
+    for (; k + 4 <= k1; k += 4)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) s[u] += q[2ll * (k + u) * a.width];
+    for (; k < k1; ++k) s[0] += q[2ll * k * a.width];
   }
-  if (a.dweight) ((T*)a.dweight)[c] = from_f<T>(sw);
-  if (a.dbias) ((T*)a.dbias)[c] = from_f<T>(sb);
+  red[run][l] = (s[0] + s[1]) + (s[2] + s[3]);
+  __syncthreads();
+  if (run || c >= a.width) return;
+  float sum = 0.0f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) sum += red[k][l];
+  to[c] = from_f<T>(sum);
+}
+
+// How the gradients run: lanes a row, pieces a lane (0: longer rows), rows a workgroup
+struct Shape {
+  int lanes, pieces, rows;
+};
+Shape backward_shape(int pieces) {
+  return pieces <= 16    ? Shape{16, 1, 16}
+         : pieces <= 64  ? Shape{64, 1, 4}
+         : pieces <= 128 ? Shape{64, 2, 4}
+         : pieces <= 256 ? Shape{64, 4, 4}
+         : pieces <= 512 ? Shape{256, 2, 2}
+         : pieces <= 1024 ? Shape{256, 4, 2}
+         : pieces <= 2048 ? Shape{256, 8, 1}
+         : pieces <= 4096 ? Shape{1024, 4, 1}
+                          : Shape{1024, 0, 1};
 }
 
 }  // namespace
 
-int oz2_norm_parts(int, int rows, int) { return (int)(((ll)rows + SUM_ROWS - 1) / SUM_ROWS); }
+// partial column sums: as many as workgroups, two on a CU at most (more would write and read
+// more parts than they save)
+int oz2_norm_parts(int dtype, int rows, int width) {
+  const Shape f = backward_shape((width + (dtype == OZ2_F32 ? 4 : 8) - 1) / (dtype == OZ2_F32 ? 4 : 8));
+  if (!f.pieces) return (int)(((ll)rows + LONG_ROWS - 1) / LONG_ROWS);
+  return (int)std::min<ll>(2 * oz2_device_cus(), ((ll)rows + f.rows - 1) / f.rows);
+}
+
+namespace {
+
+template <class T>
+hipError_t launch_norm(const Oz2Norm& a, hipStream_t s) {
+  constexpr int P = 16 / sizeof(T);
+  const int pieces = (a.width + P - 1) / P;
+  auto go = [&](auto* kernel, int lanes) {
+    const int threads = std::max(lanes, 256), g = threads / lanes;
+    const dim3 grid((unsigned)std::min<ll>(ROW_BLOCKS, ((ll)a.rows + g - 1) / g));
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, a);
+    return hipGetLastError();
+  };
+  // the fewest lanes, a wave mostly (no barrier), unless that leaves most of the chip idle
+  const bool few = (ll)a.rows * 64 <= 1024ll * oz2_device_cus();
+  if (pieces <= 16) return go(k_norm<T, 16, 1>, 16);
+  if (pieces <= 64) return go(k_norm<T, 64, 1>, 64);
+  if (!few || pieces <= 128) {
+    if (pieces <= 128) return go(k_norm<T, 64, 2>, 64);
+    if (pieces <= 256) return go(k_norm<T, 64, 4>, 64);
+    if (pieces <= 512) return go(k_norm<T, 64, 8>, 64);
+  }
+  if (pieces <= 256) return go(k_norm<T, 256, 1>, 256);
+  if (pieces <= 512) return go(k_norm<T, 256, 2>, 256);
+  if (pieces <= 1024) return go(k_norm<T, 256, 4>, 256);
+  if (pieces <= 2048) return go(k_norm<T, 256, 8>, 256);
+  if (pieces <= 4096) return go(k_norm<T, 1024, 4>, 1024);
+  return go(k_norm_long<T>, 1024);
+}
+
+template <class T>
+hipError_t launch_backward(const Oz2NormBack& a, const Shape& f, hipStream_t s) {
+  auto go = [&](auto* kernel, int threads) {
+    if (a.parts) hipLaunchKernelGGL(kernel, dim3((unsigned)a.parts), dim3(threads), 0, s, a);
+    return hipGetLastError();
+  };
+  switch (f.lanes + f.pieces) {
+    case 17: return go(k_norm_backward<T, 16, 1, 16>, 256);
+    case 65: return go(k_norm_backward<T, 64, 1, 4>, 256);
+    case 66: return go(k_norm_backward<T, 64, 2, 4>, 256);
+    case 68: return go(k_norm_backward<T, 64, 4, 4>, 256);
+    case 258: return go(k_norm_backward<T, 256, 2, 2>, 512);
+    case 260: return go(k_norm_backward<T, 256, 4, 2>, 512);
+    case 264: return go(k_norm_backward<T, 256, 8, 1>, 256);
+    case 1028: return go(k_norm_backward<T, 1024, 4, 1>, 1024);
+  }
+  hipError_t e = hipSuccess;
+  if ((a.dweight || a.dbias) && a.parts) {
+    hipLaunchKernelGGL(k_norm_columns_long<T>,
+                       dim3((unsigned)((a.width + 255) / 256), (unsigned)std::min(a.parts, 32768)), dim3(256), 0, s, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (a.dx) {
+    hipLaunchKernelGGL(k_norm_dx_long<T>, dim3((unsigned)std::min<ll>(ROW_BLOCKS, a.rows)), dim3(1024), 0, s, a);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace
 
 hipError_t oz2_launch_norm(int dtype, const Oz2Norm& a, hipStream_t s) {
-  const dim3 grid((unsigned)std::min<ll>(ROW_BLOCKS, a.rows));
-  OZ2_TYPED(dtype, hipLaunchKernelGGL(k_norm<T>, grid, dim3(NT), 0, s, a));
-  return hipGetLastError();
+  OZ2_TYPED(dtype, return launch_norm<T>(a, s));
 }
 
 hipError_t oz2_launch_norm_backward(int dtype, const Oz2NormBack& args, hipStream_t s) {
   Oz2NormBack a = args;
+  const int per = dtype == OZ2_F32 ? 4 : 8;
   a.parts = oz2_norm_parts(dtype, a.rows, a.width);
   hipError_t e = hipSuccess;
-  if (a.dweight || a.dbias) {
-    const unsigned cols = (unsigned)((a.width + NT - 1) / NT);
-    if (a.parts) {
-      OZ2_TYPED(dtype, hipLaunchKernelGGL(k_norm_columns<T>, dim3(cols, (unsigned)std::min(a.parts, 32768)),
-                                          dim3(NT), 0, s, a));
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-    }
-    OZ2_TYPED(dtype, hipLaunchKernelGGL(k_norm_join<T>, dim3(cols), dim3(NT), 0, s, a));
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  if (a.dx && a.rows) {
-    const dim3 grid((unsigned)std::min<ll>(ROW_BLOCKS, a.rows));
-    OZ2_TYPED(dtype, hipLaunchKernelGGL(k_norm_dx<T>, grid, dim3(NT), 0, s, a));
-    e = hipGetLastError();
-  }
-  return e;
+  OZ2_TYPED(dtype, e = launch_backward<T>(a, backward_shape((a.width + per - 1) / per), s));
+  if (e != hipSuccess || (!a.dweight && !a.dbias)) return e;
+  const dim3 grid((unsigned)((a.width + 31) / 32), 2);
+  OZ2_TYPED(dtype, hipLaunchKernelGGL(k_norm_join<T>, grid, dim3(256), 0, s, a));
+  return hipGetLastError();
 }

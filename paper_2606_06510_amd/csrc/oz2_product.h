@@ -22,6 +22,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "oz2_lanes.h"
 #include "oz2_layers.h"
 
 #pragma clang fp contract(fast)
@@ -342,22 +343,6 @@ __device__ __forceinline__ Piece<T, W> rounded(const float* v) {
 #pragma unroll
   for (int i = 0; i < W; ++i) o.v[i] = from_f<T>(v[i]);
   return o;
-}
-
-// The largest (sum) of v over N neighbouring lanes (N = 8 or 16, a multiple of N from the
-// wave's start on), in all of them: pairs, quads, then halves and rows mirrored.
-template <int N, bool SUM>
-__device__ __forceinline__ float across(float v) {
-  auto with = [&](auto ctrl) {
-    const int u = __builtin_bit_cast(int, v);
-    const float o = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(u, u, decltype(ctrl)::value, 0xf, 0xf, false));
-    v = SUM ? v + o : fmaxf(v, o);
-  };
-  with(std::integral_constant<int, 0xB1>{});
-  with(std::integral_constant<int, 0x4E>{});
-  with(std::integral_constant<int, 0x141>{});
-  if (N == 16) with(std::integral_constant<int, 0x140>{});
-  return v;
 }
 
 __device__ __forceinline__ ll target_of(const Oz2Loss& l, ll row) {

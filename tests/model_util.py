@@ -44,7 +44,7 @@ def route_row(l, bias, k, score, groups, top_groups, best, renorm, scale, chosen
                                              else _sigmoid(v)) for v in l]
     scored = bias is not None or (groups > 1 and best > 1)
     c = [(s[i] + b[i]) if scored else l[i] for i in range(E)]
-    inside = [i for i in range(E) if l[i] != -math.inf and c[i] != -math.inf]
+    inside = [i for i in range(E) if l[i] != -math.inf and b[i] != -math.inf]
     if groups > 1:
         per = E // groups
         value = []
