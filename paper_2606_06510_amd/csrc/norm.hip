@@ -37,7 +37,33 @@ __device__ __forceinline__ void row_sums(float (&v)[M], float* red) {
   }
 }
 
-template <class T, int L, int N>
+// Piece c / P of a row, without a branch between the loads of a row's pieces (each would wait
+// for the ones before): one that ends behind the row's end is read from where it ends with
+// the row (a row of a piece at least), and `settle` then moves its entries to their place and
+// zeros behind them.  TINY: rows shorter than a piece.
+template <class T, bool TINY, bool PAST>
+__device__ __forceinline__ Piece<T, 16 / sizeof(T)> row_piece(const T* row, int c, int width) {
+  constexpr int P = 16 / sizeof(T);
+  if (TINY) return load_piece<T>(row + c, width - c);
+  const T* p = row + min(c, width - P);
+  return PAST ? load_stream<T>(p, P) : load_piece<T>(p, P);   // (past the caches)
+}
+template <class T, bool TINY>
+__device__ __forceinline__ void settle(Piece<T, 16 / sizeof(T)>& v, int c, int width) {
+  constexpr int P = 16 / sizeof(T);
+  if (TINY) return;
+  struct Halves {
+    uint64_t lo, hi;
+  } h;
+  __builtin_memcpy(&h, &v, sizeof(v));
+  const int bits = 8 * (int)sizeof(T) * max(c - (width - P), 0);
+  const uint64_t up = bits >= 128 ? 0 : bits >= 64 ? h.hi >> (bits - 64) : bits ? h.lo >> bits | h.hi << (64 - bits) : h.lo;
+  h.hi = bits >= 64 ? 0 : h.hi >> bits;
+  h.lo = up;
+  __builtin_memcpy(&v, &h, sizeof(v));
+}
+
+template <class T, int L, int N, bool TINY = false>
 __global__ void __launch_bounds__(L < 256 ? 256 : L)
 k_norm(Oz2Norm a) {
   constexpr int P = 16 / sizeof(T), NT = L < 256 ? 256 : L, G = NT / L;
@@ -49,16 +75,22 @@ k_norm(Oz2Norm a) {
     Piece<T, P> v[N], w[N], b[N];
     float sum[1] = {0.0f};
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const int c = (lane + L * k) * P;
-      v[k] = load_piece<T>(x + c, a.width - c);
+    for (int k = 0; k < N; ++k) v[k] = row_piece<T, TINY, false>(x, (lane + L * k) * P, a.width);
+    if (a.weight) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) w[k] = row_piece<T, TINY, false>((const T*)a.weight, (lane + L * k) * P, a.width);
+    }
+    if (a.bias) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) b[k] = row_piece<T, TINY, false>((const T*)a.bias, (lane + L * k) * P, a.width);
     }
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const int c = (lane + L * k) * P;
-      if (a.weight) w[k] = load_piece<T>((const T*)a.weight + c, a.width - c);
-      if (a.bias) b[k] = load_piece<T>((const T*)a.bias + c, a.width - c);
-    }
+    for (int k = 0; k < N; ++k)
+      if (L * (k + 1) * P > a.width) {
+        settle<T, TINY>(v[k], (lane + L * k) * P, a.width);
+        if (a.weight) settle<T, TINY>(w[k], (lane + L * k) * P, a.width);
+        if (a.bias) settle<T, TINY>(b[k], (lane + L * k) * P, a.width);
+      }
 #pragma unroll
     for (int k = 0; k < N; ++k)
 #pragma unroll
@@ -148,16 +180,14 @@ k_norm_long(Oz2Norm a) {
 }
 
 // ---------------------------------------------------------------- gradients
-// A workgroup takes every gridDim-th of its G rows' groups, U of them at a time, and keeps
-// the column sums of its rows in registers; they leave as one partial row each of dweight
-// and dbias, which k_norm_join adds up in order.
-constexpr int U = 2;
-
-template <class T, int L, int N, int G>
+// A workgroup takes G rows of every gridDim G, and keeps the column sums of its rows in
+// registers; they leave as one partial row each of dweight and dbias, which k_norm_join adds
+// up in order.
+template <class T, int L, int N, int G, bool TINY = false>
 __global__ void __launch_bounds__(L* G)
 k_norm_backward(Oz2NormBack a) {
   constexpr int P = 16 / sizeof(T), NT = L * G;
-  __shared__ float red[2][NT / 64 * 2 * U];
+  __shared__ float red[2][NT / 64 * 2];
   __shared__ float others[G > 1 ? (G - 1) * L * N * P : 1];
   const int lane = threadIdx.x % L, grp = threadIdx.x / L;
   const float n = (float)a.width;
@@ -166,74 +196,76 @@ k_norm_backward(Oz2NormBack a) {
 #pragma unroll
   for (int i = 0; i < N * P; ++i) dw[i] = db[i] = 0.0f;
   Piece<T, P> w[N];
+  if (a.weight) {
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    const int c = (lane + L * k) * P;
-    if (a.weight) w[k] = load_piece<T>((const T*)a.weight + c, a.width - c);
-  }
-  const ll step = (ll)gridDim.x * G;
-  int turn = 0;
-  for (ll r0 = (ll)blockIdx.x * G; r0 < a.rows; r0 += step * U, turn ^= 1) {
-    Piece<T, P> x[U][N], dy[U][N], res[U][N];
-    float mean[U], rstd[U], sum[2 * U];
-    bool on[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const ll r = r0 + u * step + grp;
-      on[u] = r < a.rows;
-      const int width = on[u] ? a.width : 0;
-      mean[u] = on[u] && a.stats ? a.stats[2 * r] : 0.0f;
-      rstd[u] = on[u] && a.stats ? a.stats[2 * r + 1] : 0.0f;
-#pragma unroll
-      for (int k = 0; k < N; ++k) {
-        const int c = (lane + L * k) * P, valid = width - c;
-        dy[u][k] = load_stream<T>((const T*)a.dy + r * a.lddy + c, valid);
-        if (a.x) x[u][k] = load_stream<T>((const T*)a.x + r * a.ldx + c, valid);
-        if (a.residual) res[u][k] = load_stream<T>((const T*)a.residual + r * a.ldr + c, valid);
-      }
+    for (int k = 0; k < N; ++k) {
+      w[k] = row_piece<T, TINY, false>((const T*)a.weight, (lane + L * k) * P, a.width);
+      settle<T, TINY>(w[k], (lane + L * k) * P, a.width);
     }
-    auto h_of = [&](int u, int k, int i) {
+  }
+  int turn = 0;
+  for (ll r0 = (ll)blockIdx.x * G; r0 < a.rows; r0 += (ll)gridDim.x * G, turn ^= 1) {
+    const bool on = r0 + grp < a.rows;
+    const ll r = on ? r0 + grp : a.rows - 1;   // (read, and not used)
+    Piece<T, P> x[N], dy[N], res[N];
+    float mean = 0.0f, rstd = 0.0f, sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      dy[k] = row_piece<T, TINY, true>((const T*)a.dy + r * a.lddy, (lane + L * k) * P, a.width);
+    if (a.x) {
+      mean = a.stats[2 * r];
+      rstd = a.stats[2 * r + 1];
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        x[k] = row_piece<T, TINY, true>((const T*)a.x + r * a.ldx, (lane + L * k) * P, a.width);
+    }
+    if (a.residual) {
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        res[k] = row_piece<T, TINY, true>((const T*)a.residual + r * a.ldr, (lane + L * k) * P, a.width);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (L * (k + 1) * P > a.width) {
+        settle<T, TINY>(dy[k], (lane + L * k) * P, a.width);
+        if (a.x) settle<T, TINY>(x[k], (lane + L * k) * P, a.width);
+        if (a.residual) settle<T, TINY>(res[k], (lane + L * k) * P, a.width);
+      }
+    auto h_of = [&](int k, int i) {
       // (behind the row's end x reads as 0, which is not the mean)
-      return a.x && i < a.width - (lane + L * k) * P ? (to_f(x[u][k].v[i]) - mean[u]) * rstd[u] : 0.0f;
+      return a.x && i < a.width - (lane + L * k) * P ? (to_f(x[k].v[i]) - mean) * rstd : 0.0f;
     };
-    auto g_of = [&](int u, int k, int i) {
-      const float d = to_f(dy[u][k].v[i]);
+    auto g_of = [&](int k, int i) {
+      const float d = to_f(dy[k].v[i]);
       return a.weight ? d * to_f(w[k].v[i]) : d;
     };
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      sum[2 * u] = sum[2 * u + 1] = 0.0f;
-      if (!on[u]) continue;
+    if (on) {
 #pragma unroll
       for (int k = 0; k < N; ++k)
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-          const float h = h_of(u, k, i), g = g_of(u, k, i), d = to_f(dy[u][k].v[i]);
-          sum[2 * u] += g;
-          sum[2 * u + 1] += g * h;
+          const float h = h_of(k, i), g = g_of(k, i), d = to_f(dy[k].v[i]);
+          sum[0] += g;
+          sum[1] += g * h;
           dw[k * P + i] += d * h;
           db[k * P + i] += d;
         }
     }
     if (!a.dx) continue;
     row_sums<L>(sum, red[turn]);
+    if (!on) continue;
+    const float mg = sum[0] / n, mh = sum[1] / n;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (!on[u]) continue;
-      const ll r = r0 + u * step + grp;
-      const float mg = sum[2 * u] / n, mh = sum[2 * u + 1] / n;
+    for (int k = 0; k < N; ++k) {
+      const int c = (lane + L * k) * P;
+      Piece<T, P> o;
 #pragma unroll
-      for (int k = 0; k < N; ++k) {
-        const int c = (lane + L * k) * P;
-        Piece<T, P> o;
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-          float d = rstd[u] * (g_of(u, k, i) - mg - h_of(u, k, i) * mh);
-          if (a.residual) d += to_f(res[u][k].v[i]);
-          o.v[i] = from_f<T>(d);
-        }
-        store_stream((T*)a.dx + r * a.lddx + c, o, a.width - c);
+      for (int i = 0; i < P; ++i) {
+        float d = rstd * (g_of(k, i) - mg - h_of(k, i) * mh);
+        if (a.residual) d += to_f(res[k].v[i]);
+        o.v[i] = from_f<T>(d);
       }
+      store_stream((T*)a.dx + r * a.lddx + c, o, a.width - c);
     }
   }
   if (!cols) return;
@@ -347,16 +379,20 @@ k_norm_join(Oz2NormBack a) {
   if (!to) return;
   const int l = threadIdx.x & 31, run = threadIdx.x >> 5, c = (int)blockIdx.x * 32 + l;
   const int per = (a.parts + 7) / 8, k0 = run * per, k1 = min(a.parts, k0 + per);
-  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  float s = 0.0f;
   if (c < a.width) {
-    const float* q = a.part + (ll)blockIdx.y * a.width + c;
+    const ll stride = 2ll * a.width;
+    const float* q = a.part + (ll)blockIdx.y * a.width + c + k0 * stride;
     int k = k0;
-    for (; k + 4 <= k1; k += 4)
+    for (; k + 8 <= k1; k += 8, q += 8 * stride) {
+      float v[8];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) s[u] += q[2ll * (k + u) * a.width];
-    for (; k < k1; ++k) s[0] += q[2ll * k * a.width];
+      for (int u = 0; u < 8; ++u) v[u] = q[u * stride];
+      s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    }
+    for (; k < k1; ++k, q += stride) s += *q;
   }
-  red[run][l] = (s[0] + s[1]) + (s[2] + s[3]);
+  red[run][l] = s;
   __syncthreads();
   if (run || c >= a.width) return;
   float sum = 0.0f;
@@ -371,12 +407,12 @@ struct Shape {
 };
 Shape backward_shape(int pieces) {
   return pieces <= 16    ? Shape{16, 1, 16}
-         : pieces <= 64  ? Shape{64, 1, 4}
-         : pieces <= 128 ? Shape{64, 2, 4}
+         : pieces <= 64  ? Shape{64, 1, 8}
+         : pieces <= 128 ? Shape{64, 2, 8}
          : pieces <= 256 ? Shape{64, 4, 4}
          : pieces <= 512 ? Shape{256, 2, 2}
          : pieces <= 1024 ? Shape{256, 4, 2}
-         : pieces <= 2048 ? Shape{256, 8, 1}
+         : pieces <= 2048 ? Shape{512, 4, 1}
          : pieces <= 4096 ? Shape{1024, 4, 1}
                           : Shape{1024, 0, 1};
 }
@@ -405,13 +441,11 @@ hipError_t launch_norm(const Oz2Norm& a, hipStream_t s) {
   };
   // the fewest lanes, a wave mostly (no barrier), unless that leaves most of the chip idle
   const bool few = (ll)a.rows * 64 <= 1024ll * oz2_device_cus();
+  if (a.width < P) return go(k_norm<T, 16, 1, true>, 16);
   if (pieces <= 16) return go(k_norm<T, 16, 1>, 16);
   if (pieces <= 64) return go(k_norm<T, 64, 1>, 64);
-  if (!few || pieces <= 128) {
-    if (pieces <= 128) return go(k_norm<T, 64, 2>, 64);
-    if (pieces <= 256) return go(k_norm<T, 64, 4>, 64);
-    if (pieces <= 512) return go(k_norm<T, 64, 8>, 64);
-  }
+  if (pieces <= 128) return go(k_norm<T, 64, 2>, 64);
+  if (pieces <= 256 && !few) return go(k_norm<T, 64, 4>, 64);
   if (pieces <= 256) return go(k_norm<T, 256, 1>, 256);
   if (pieces <= 512) return go(k_norm<T, 256, 2>, 256);
   if (pieces <= 1024) return go(k_norm<T, 256, 4>, 256);
@@ -427,13 +461,15 @@ hipError_t launch_backward(const Oz2NormBack& a, const Shape& f, hipStream_t s) 
     return hipGetLastError();
   };
   switch (f.lanes + f.pieces) {
-    case 17: return go(k_norm_backward<T, 16, 1, 16>, 256);
-    case 65: return go(k_norm_backward<T, 64, 1, 4>, 256);
-    case 66: return go(k_norm_backward<T, 64, 2, 4>, 256);
+    case 17:
+      return a.width < 16 / (int)sizeof(T) ? go(k_norm_backward<T, 16, 1, 16, true>, 256)
+                                           : go(k_norm_backward<T, 16, 1, 16>, 256);
+    case 65: return go(k_norm_backward<T, 64, 1, 8>, 512);
+    case 66: return go(k_norm_backward<T, 64, 2, 8>, 512);
     case 68: return go(k_norm_backward<T, 64, 4, 4>, 256);
     case 258: return go(k_norm_backward<T, 256, 2, 2>, 512);
     case 260: return go(k_norm_backward<T, 256, 4, 2>, 512);
-    case 264: return go(k_norm_backward<T, 256, 8, 1>, 256);
+    case 516: return go(k_norm_backward<T, 512, 4, 1>, 512);
     case 1028: return go(k_norm_backward<T, 1024, 4, 1>, 1024);
   }
   hipError_t e = hipSuccess;

@@ -33,7 +33,19 @@ __device__ __forceinline__ void key_of(double c, double& k) {
   k = c != c ? INFINITY : fmin(c, kMost);
 }
 __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return max(a, b); }
-__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
+// (keys are no NaN: nothing is to be made quiet first)
+__device__ __forceinline__ double larger(double a, double b) {
+  double r;
+  asm("v_max_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ __forceinline__ double smaller(double a, double b) {
+  double r;
+  asm("v_min_f64 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t smaller(uint32_t a, uint32_t b) { return min(a, b); }
+__device__ __forceinline__ float value_of(uint32_t k) { return __builtin_bit_cast(float, k >> 31 ? k ^ 1u << 31 : ~k); }
 
 template <int CTRL>
 __device__ __forceinline__ uint32_t moved(uint32_t v) {
@@ -76,15 +88,18 @@ __device__ __forceinline__ uint64_t of_token(uint64_t ballot) {
 
 // The `n` largest of a token's keys, largest first, of equal ones the lower index, each taken
 // out of them: take(r, index) is called by the lane that has it.  Fewer where none are left.
+// Returns the last one.
 template <int L, int V, class KEY, class F>
-__device__ __forceinline__ void take_largest(KEY (&key)[V], int n, int lane, F take) {
-  KEY no;
+__device__ __forceinline__ KEY take_largest(KEY (&key)[V], int n, int lane, F take) {
+  KEY no, last;
   none(no);
+  none(last);
   for (int r = 0; r < n; ++r) {
     KEY mine = key[0];
 #pragma unroll
     for (int i = 1; i < V; ++i) mine = larger(mine, key[i]);
     const KEY best = largest<L>(mine);
+    if (best != no) last = best;
     const uint64_t have = of_token<L>(__ballot(mine == best));
     if (best != no && lane == __ffsll((unsigned long long)have) - 1) {
       int at = V - 1;
@@ -96,6 +111,7 @@ __device__ __forceinline__ void take_largest(KEY (&key)[V], int n, int lane, F t
       take(r, lane * V + at);
     }
   }
+  return last;
 }
 
 __device__ __forceinline__ float log_sigmoid(float l) { return fminf(l, 0.0f) - log1pf(expf(-fabsf(l))); }
@@ -113,17 +129,82 @@ __device__ __forceinline__ void load_logits(const T* row, int first, int E, floa
   }
 }
 
-// KEY: uint32_t where the order is that of the logits, double where scores are compared
-template <class T, class KEY, int L, int V>
+__device__ __forceinline__ double sigmoid64(float l) { return 1.0 / (1.0 + exp(-(double)l)); }
+
+// Those of a token's groups of `per` experts that do not stay have their experts' keys
+// taken out.  sum: a group's value is that of its two largest, joined by add.  Returns the last value
+// that stays, and in *next the largest that does not (none: there is none).
+template <int L, int V, class KEY, class F>
+__device__ __forceinline__ KEY keep_groups(KEY (&key)[V], KEY* keys, uint8_t* stays, int E, int groups, int top_groups,
+                                           bool sum, int lane, KEY* next, F add) {
+  const int per = E / groups, first = lane * V;
+  KEY no, last;
+  none(no);
+#pragma unroll
+  for (int i = 0; i < V; ++i) keys[first + i] = key[i];
+  for (int g = lane; g < groups; g += L) stays[g] = 0;
+  wave_fence();
+  // (each lane starts elsewhere in its group: LDS's banks)
+  auto group_key = [&](int g) {
+    KEY b1 = no, b2 = no;
+    int e = lane % per;
+    for (int n = 0; n < per; ++n) {
+      const KEY c = keys[g * per + e];
+      e = e + 1 == per ? 0 : e + 1;
+      b2 = larger(b2, smaller(b1, c));
+      b1 = larger(b1, c);
+    }
+    return sum && b2 != no ? add(b1, b2) : b1;
+  };
+  auto stay = [&](int, int g) { stays[g] = 1; };
+  if (groups <= L) {
+    KEY gk[1] = {no};
+    if (lane < groups) gk[0] = group_key(lane);
+    last = take_largest<L, 1>(gk, top_groups, lane, stay);
+    *next = largest<L>(gk[0]);
+  } else {
+    KEY gk[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) gk[i] = first + i < groups ? group_key(first + i) : no;
+    last = take_largest<L, V>(gk, top_groups, lane, stay);
+    KEY rest = gk[0];
+#pragma unroll
+    for (int i = 1; i < V; ++i) rest = larger(rest, gk[i]);
+    *next = largest<L>(rest);
+  }
+  wave_fence();
+  const uint32_t inverse = per > 1 ? 0xffffffffu / per + 1 : 0;   // e / per = e inverse / 2^32
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int e = min(first + i, E - 1);
+    if (!stays[per > 1 ? (int)__umulhi(e, inverse) : e]) key[i] = no;
+  }
+  wave_fence();
+  return last;
+}
+
+// LDS of a token: its choices, and one after the other its keys with the groups that stay, and
+// candidates with their scores
+constexpr int CAND = 64;
+template <int L, int V>
+constexpr int token_bytes() {
+  return OZ2_MAX_TOPK * 4 + std::max(L * V * 9, CAND * 12);
+}
+
+// Choices by scores (SCORED) or by the logits, whose order is that of scores without a bias.
+// Scores are compared as in 64 bits, but 64 bits are formed for few: 32 bits find those that
+// can be among the largest, within `near` of the last of them (A + 2^-23 |c|, the error of a
+// score and of its sum with the bias, twice).  Where that does not decide, too many are that
+// close or a group's value is, or there is a NaN or an infinity, all are formed.
+template <class T, bool SCORED, int L, int V>
 __global__ void __launch_bounds__(NT)
 k_route(Oz2Route a) {
   constexpr int TOKENS = NT / L, Q = OZ2_MAX_TOPK / L;
-  constexpr bool SCORED = sizeof(KEY) == 8;
   extern __shared__ double lds[];
-  int* const chosen = (int*)lds + threadIdx.x / L * OZ2_MAX_TOPK;
-  // groups: a token's keys, then which groups stay
-  KEY* const keys = (KEY*)((int*)lds + TOKENS * OZ2_MAX_TOPK) + threadIdx.x / L * (L * V);
-  uint8_t* const stays = (uint8_t*)((KEY*)((int*)lds + TOKENS * OZ2_MAX_TOPK) + NT * V) + threadIdx.x / L * (L * V);
+  uint8_t* const mine = (uint8_t*)lds + threadIdx.x / L * token_bytes<L, V>();
+  int* const chosen = (int*)mine;
+  uint8_t* const room = mine + OZ2_MAX_TOPK * 4;
+  uint8_t* const stays = room + L * V * 8;
   const int lane = threadIdx.x % L, E = a.experts, first = lane * V;
   const bool soft = a.score == OZ2_SCORE_SOFTMAX;
   const ll last = a.tokens - 1;
@@ -131,9 +212,17 @@ k_route(Oz2Route a) {
     const bool live = t0 + threadIdx.x / L <= last;
     const ll t = live ? t0 + threadIdx.x / L : last;
     const T* row = (const T*)a.logits + t * a.ld;
-    float l[V];
+    float l[V], b[V];
     load_logits<T, V>(row, first, E, l);
-    float top = l[0];
+    if (SCORED) {
+      if (a.bias) {
+        load_logits<float, V>(a.bias, first, E, b);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) b[i] = 0.0f;
+      }
+    }
+    float top = l[0], total = 1.0f;
     bool bad = !(l[0] < INFINITY);   // a logit that makes a softmax NaN
 #pragma unroll
     for (int i = 1; i < V; ++i) {
@@ -141,38 +230,9 @@ k_route(Oz2Route a) {
       top = fmaxf(top, l[i]);
     }
     bad = soft && of_token<L>(__ballot(bad));
-    float total = 1.0f;
-    KEY key[V], no;
-    none(no);
-    if constexpr (SCORED) {
-      float b[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) b[i] = a.bias && first + i < E ? a.bias[first + i] : 0.0f;
-      double s[V];
-      if (soft) {
-        top = across<L, false>(top);
-        double sum = 0.0;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          s[i] = l[i] == -INFINITY ? 0.0 : exp((double)l[i] - (double)top);
-          sum += s[i];
-        }
-        sum = total_of<L>(sum);
-        total = (float)sum;
-        const double share = bad ? __builtin_nan("") : 1.0;
-#pragma unroll
-        for (int i = 0; i < V; ++i) s[i] = s[i] / sum * share;
-      } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) s[i] = 1.0 / (1.0 + exp(-(double)l[i]));
-      }
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const double c = s[i] + (double)b[i];
-        key_of(c, key[i]);
-        if (l[i] == -INFINITY || b[i] == -INFINITY) key[i] = no;
-      }
-    } else {
+    for (int j = lane; j < a.top_k; j += L) chosen[j] = -1;
+    uint32_t key[V], after = 0;
+    if (!SCORED) {
       if (soft && !a.renormalize) {
         top = across<L, false>(top);
         float sum = 0.0f;
@@ -183,52 +243,115 @@ k_route(Oz2Route a) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         key_of(l[i], key[i]);
-        if (l[i] == -INFINITY) key[i] = no;
+        if (l[i] == -INFINITY) key[i] = 0;
       }
-    }
-    for (int j = lane; j < a.top_k; j += L) chosen[j] = -1;
-    if (a.groups > 1) {
-      const int per = E / a.groups;
-#pragma unroll
-      for (int i = 0; i < V; ++i) keys[first + i] = key[i];
-      for (int g = lane; g < a.groups; g += L) stays[g] = 0;
+      if (a.groups > 1)
+        keep_groups<L, V>(key, (uint32_t*)room, stays, E, a.groups, a.top_groups, false, lane, &after,
+                          [](uint32_t x, uint32_t) { return x; });
       wave_fence();
-      // lane l's groups: l W .. l W + W - 1, each lane starting elsewhere in them (LDS's banks)
-      auto group_key = [&](int g) {
-        KEY b1 = no, b2 = no;
-        int e = lane % per;
-        for (int n = 0; n < per; ++n) {
-          const KEY c = keys[g * per + e];
-          e = e + 1 == per ? 0 : e + 1;
-          if constexpr (SCORED) b2 = fmax(b2, fmin(b1, c));
-          b1 = larger(b1, c);
-        }
-        if constexpr (SCORED) {
-          if (a.group_best > 1 && b2 > -INFINITY && b1 < INFINITY) b1 = fmin(b1 + b2, kMost);
-        }
-        return b1;
-      };
-      auto stay = [&](int, int g) { stays[g] = 1; };
-      if (a.groups <= L) {
-        KEY gk[1] = {no};
-        if (lane < a.groups) gk[0] = group_key(lane);
-        take_largest<L, 1>(gk, a.top_groups, lane, stay);
-      } else {
-        KEY gk[V];
+      take_largest<L, V>(key, a.top_k, lane, [&](int r, int e) { chosen[r] = e; });
+    } else {
+      float c[V], far = 0.0f, A = 5e-7f;
+      double sum = 1.0;
+      if (soft) {
+        top = across<L, false>(top);
+        sum = 0.0;
 #pragma unroll
-        for (int i = 0; i < V; ++i) gk[i] = first + i < a.groups ? group_key(first + i) : no;
-        take_largest<L, V>(gk, a.top_groups, lane, stay);
+        for (int i = 0; i < V; ++i) sum += l[i] == -INFINITY ? 0.0 : exp((double)l[i] - (double)top);
+        sum = total_of<L>(sum);
+        total = (float)sum;
+        A /= total;   // (of the largest score; e^x in 32 bits is off by |x| 2^-24, and |x| e^x below 1)
       }
-      wave_fence();
-      const uint32_t inverse = per > 1 ? 0xffffffffu / per + 1 : 0;   // e / per = e inverse / 2^32
+      bool exact = false;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const int e = min(first + i, E - 1);
-        if (!stays[per > 1 ? (int)__umulhi(e, inverse) : e]) key[i] = no;
+        const float s = soft ? __expf(l[i] - top) / total : __builtin_amdgcn_rcpf(1.0f + __expf(-l[i]));
+        c[i] = s + b[i];
+        key_of(c[i], key[i]);
+        if (l[i] == -INFINITY || b[i] == -INFINITY) {
+          key[i] = 0;
+          c[i] = -INFINITY;
+        } else {
+          exact |= !(fabsf(c[i]) < INFINITY);
+          far = fmaxf(far, fabsf(c[i]));
+        }
+      }
+      far = across<L, false>(far);
+      const float near = 2.0f * (A + 2.4e-7f * far);
+      if (a.groups > 1) {
+        const uint32_t least = keep_groups<L, V>(
+            key, (uint32_t*)room, stays, E, a.groups, a.top_groups, a.group_best > 1, lane, &after,
+            [](uint32_t x, uint32_t y) {
+              uint32_t k;
+              key_of(value_of(x) + value_of(y), k);
+              return k;
+            });
+        // (sums of two)
+        exact |= after && value_of(least) - value_of(after) <= 3.0f * near;
+      }
+      // the k-th value, or the least there is
+      uint32_t kth = ~0u;
+      for (int r = 0; r < a.top_k; ++r) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) m = max(m, key[i] < kth ? key[i] : 0u);
+        m = largest<L>(m);
+        kth = m ? m : kth;
+      }
+      const float least = value_of(kth) - near;
+      int n = 0, before;
+      bool in[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        in[i] = key[i] && c[i] >= least;
+        n += in[i];
+      }
+      before = n;
+#pragma unroll
+      for (int d = 1; d < L; d *= 2) {
+        const int up = __shfl_up(before, d, L);
+        if (lane >= d) before += up;
+      }
+      const int count = __shfl(before, L - 1, L);
+      exact |= count > CAND;
+      if (!__any(exact)) {
+        double* const score = (double*)room;
+        int* const who = (int*)(score + CAND);
+        int at = before - n;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (in[i]) who[at++] = first + i;
+        wave_fence();
+        for (int j = lane; j < count; j += L) {
+          const int e = who[j];
+          const float z = to_f(row[e]);
+          const double s = soft ? exp((double)z - (double)top) / sum : sigmoid64(z);
+          score[j] = s + (a.bias ? (double)a.bias[e] : 0.0);
+        }
+        wave_fence();
+        for (int j = lane; j < count; j += L) {
+          const double mine = score[j];
+          const int e = who[j];
+          int rank = 0;
+          for (int i = 0; i < count; ++i) rank += score[i] > mine || (score[i] == mine && who[i] < e);
+          if (rank < a.top_k) chosen[rank] = e;
+        }
+      } else {
+        double all[V], beyond;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          double s = soft ? exp((double)l[i] - (double)top) / sum : sigmoid64(l[i]);
+          if (soft && bad) s = __builtin_nan("");
+          key_of(s + (double)b[i], all[i]);
+          if (l[i] == -INFINITY || b[i] == -INFINITY) none(all[i]);
+        }
+        if (a.groups > 1)
+          keep_groups<L, V>(all, (double*)room, stays, E, a.groups, a.top_groups, a.group_best > 1, lane, &beyond,
+                            [](double x, double y) { return x < INFINITY ? fmin(x + y, kMost) : x; });
+        wave_fence();
+        take_largest<L, V>(all, a.top_k, lane, [&](int r, int e) { chosen[r] = e; });
       }
     }
-    wave_fence();
-    take_largest<L, V>(key, a.top_k, lane, [&](int r, int e) { chosen[r] = e; });
     wave_fence();
     // the weights of choices lane, lane + L, ..
     int id[Q];
@@ -387,13 +510,12 @@ hipError_t for_experts(int E, F f) {
   return f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
 }
 
-template <class T, class KEY>
+template <class T, bool SCORED>
 hipError_t launch_route(const Oz2Route& a, hipStream_t s) {
   return for_experts(a.experts, [&](auto lanes, auto each) {
     constexpr int L = decltype(lanes)::value, V = decltype(each)::value, TOKENS = NT / L;
-    const size_t lds = TOKENS * OZ2_MAX_TOPK * 4 + (a.groups > 1 ? NT * V * (sizeof(KEY) + 1) : 0);
     const dim3 grid((unsigned)std::min<ll>(ROW_BLOCKS, ((ll)a.tokens + TOKENS - 1) / TOKENS));
-    hipLaunchKernelGGL((k_route<T, KEY, L, V>), grid, dim3(NT), lds, s, a);
+    hipLaunchKernelGGL((k_route<T, SCORED, L, V>), grid, dim3(NT), (TOKENS * token_bytes<L, V>()), s, a);
     return hipGetLastError();
   });
 }
@@ -401,9 +523,8 @@ hipError_t launch_route(const Oz2Route& a, hipStream_t s) {
 }  // namespace
 
 hipError_t oz2_launch_route(int dtype, const Oz2Route& a, hipStream_t s) {
-  // scores keep the order of the logits: they are formed only where they are added to
   const bool scored = a.bias || (a.groups > 1 && a.group_best > 1);
-  OZ2_TYPED(dtype, return scored ? (launch_route<T, double>(a, s)) : (launch_route<T, uint32_t>(a, s)));
+  OZ2_TYPED(dtype, return scored ? (launch_route<T, true>(a, s)) : (launch_route<T, false>(a, s)));
 }
 
 hipError_t oz2_launch_route_backward(int dtype, const Oz2RouteBack& a, hipStream_t s) {
