@@ -125,71 +125,159 @@ __device__ __forceinline__ void load_logits(const T* row, int first, int E, floa
     for (int i = 0; i < V; ++i) l[i] = to_f(p.v[i]);
   } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i) l[i] = first + i < E ? to_f(row[first + i]) : -INFINITY;
+    for (int i = 0; i < V; ++i) l[i] = to_f(row[min(first + i, E - 1)]);
+#pragma unroll
+    for (int i = 0; i < V; ++i) l[i] = first + i < E ? l[i] : -INFINITY;
   }
 }
 
 __device__ __forceinline__ double sigmoid64(float l) { return 1.0 / (1.0 + exp(-(double)l)); }
 
-// Those of a token's groups of `per` experts that do not stay have their experts' keys
-// taken out.  sum: a group's value is that of its two largest, joined by add.  Returns the last value
-// that stays, and in *next the largest that does not (none: there is none).
-template <int L, int V, class KEY, class F>
-__device__ __forceinline__ KEY keep_groups(KEY (&key)[V], KEY* keys, uint8_t* stays, int E, int groups, int top_groups,
-                                           bool sum, int lane, KEY* next, F add) {
-  const int per = E / groups, first = lane * V;
-  KEY no, last;
+// The keys of groups g = lane, lane + L, .. of `per` keys each; sum: of the two largest, joined by
+// add.  (Each lane starts elsewhere in its group: LDS's banks.)
+template <int L, class KEY, class F, class G>
+__device__ __forceinline__ void group_keys(const KEY* keys, int per, int first, int end, bool sum, int lane, F add,
+                                           G give) {
+  KEY no;
   none(no);
-#pragma unroll
-  for (int i = 0; i < V; ++i) keys[first + i] = key[i];
-  for (int g = lane; g < groups; g += L) stays[g] = 0;
-  wave_fence();
-  // (each lane starts elsewhere in its group: LDS's banks)
-  auto group_key = [&](int g) {
+#pragma clang loop unroll(disable)
+  for (int g = first; g < end; ++g) {
     KEY b1 = no, b2 = no;
     int e = lane % per;
+#pragma clang loop unroll_count(4)
     for (int n = 0; n < per; ++n) {
       const KEY c = keys[g * per + e];
       e = e + 1 == per ? 0 : e + 1;
       b2 = larger(b2, smaller(b1, c));
       b1 = larger(b1, c);
     }
-    return sum && b2 != no ? add(b1, b2) : b1;
-  };
+    give(g, sum && b2 != no ? add(b1, b2) : b1);
+  }
+}
+
+// Keys of experts in groups (of two at least) that do not stay are taken out
+template <int L, int V>
+__device__ __forceinline__ void drop_groups(uint32_t (&key)[V], const uint8_t* stays, int E, int groups, int lane) {
+  const uint32_t inverse = 0xffffffffu / (uint32_t)(E / groups) + 1;   // e / per = e inverse / 2^32
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (!stays[__umulhi(min(lane * V + i, E - 1), inverse)]) key[i] = 0;
+}
+
+// The same from the keys themselves.  Returns the last group's value
+// that stays, and in *next the largest that does not (none: there is none).
+template <int L, int V, class F>
+__device__ __forceinline__ uint32_t keep_groups(uint32_t (&key)[V], uint32_t* keys, uint8_t* stays, int E, int groups,
+                                                int top_groups, bool sum, int lane, uint32_t* next, F add) {
+  const int per = E / groups, first = lane * V;
+#pragma unroll
+  for (int i = 0; i < V; ++i) keys[first + i] = key[i];
+  for (int g = lane; g < groups; g += L) stays[g] = 0;
+  wave_fence();
   auto stay = [&](int, int g) { stays[g] = 1; };
+  uint32_t last;
   if (groups <= L) {
-    KEY gk[1] = {no};
-    if (lane < groups) gk[0] = group_key(lane);
+    uint32_t gk[1] = {0};
+    group_keys<L>(keys, per, lane, min(groups, lane + 1), sum, lane, add, [&](int, uint32_t k) { gk[0] = k; });
     last = take_largest<L, 1>(gk, top_groups, lane, stay);
     *next = largest<L>(gk[0]);
   } else {
-    KEY gk[V];
+    // (by way of LDS, behind the experts' keys: there is room for V a lane)
+    uint32_t* const values = keys + L * V;
+    group_keys<L>(keys, per, first, min(groups, first + V), sum, lane, add, [&](int g, uint32_t k) { values[g] = k; });
+    wave_fence();
+    uint32_t gk[V], rest = 0;
 #pragma unroll
-    for (int i = 0; i < V; ++i) gk[i] = first + i < groups ? group_key(first + i) : no;
+    for (int i = 0; i < V; ++i) gk[i] = first + i < groups ? values[first + i] : 0;
     last = take_largest<L, V>(gk, top_groups, lane, stay);
-    KEY rest = gk[0];
 #pragma unroll
-    for (int i = 1; i < V; ++i) rest = larger(rest, gk[i]);
+    for (int i = 0; i < V; ++i) rest = larger(rest, gk[i]);
     *next = largest<L>(rest);
   }
   wave_fence();
-  const uint32_t inverse = per > 1 ? 0xffffffffu / per + 1 : 0;   // e / per = e inverse / 2^32
-#pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const int e = min(first + i, E - 1);
-    if (!stays[per > 1 ? (int)__umulhi(e, inverse) : e]) key[i] = no;
-  }
+  drop_groups<L, V>(key, stays, E, groups, lane);
   wave_fence();
   return last;
 }
 
-// LDS of a token: its choices, and one after the other its keys with the groups that stay, and
-// candidates with their scores
+// The groups that stay, where 32 bits do not tell them from the next one: their values from the
+// scores in 64 bits of the experts that can be a group's two largest.  keys: as keep_groups left them.
+// False where there are too many of either (a lane has a group and four such experts).
+template <int L, int V, class F>
+__device__ __forceinline__ bool settle_groups(uint32_t (&key)[V], const uint32_t* keys, uint8_t* stays, int E,
+                                              int groups, int top_groups, bool sum, float near, int lane, F score64) {
+  if (groups > L) return false;
+  const int per = E / groups;
+  double value[1] = {-INFINITY};
+  int hits = 0;
+  if (lane < groups) {
+    const uint32_t* mine = keys + lane * per;
+    uint32_t b1 = 0, b2 = 0;
+    for (int e = 0; e < per; ++e) {
+      b2 = max(b2, min(b1, mine[e]));
+      b1 = max(b1, mine[e]);
+    }
+    const float least = value_of(sum && b2 ? b2 : b1) - near;
+    uint64_t which = 0;
+    for (int e = 0; e < per; ++e)
+      if (mine[e] && value_of(mine[e]) >= least) {
+        if (hits < 4) which |= (uint64_t)(lane * per + e) << 16 * hits;
+        ++hits;
+      }
+    double d1 = -INFINITY, d2 = -INFINITY;
+#pragma clang loop unroll(disable)
+    for (int h = 0; h < min(hits, 4); ++h) {
+      const double s = score64((int)(which >> 16 * h) & 0xffff);
+      d2 = larger(d2, smaller(d1, s));
+      d1 = larger(d1, s);
+    }
+    value[0] = sum && d2 > -INFINITY ? d1 + d2 : d1;
+    stays[lane] = 0;
+  }
+  if (of_token<L>(__ballot(hits > 4))) return false;
+  take_largest<L, 1>(value, top_groups, lane, [&](int, int g) { stays[g] = 1; });
+  wave_fence();
+#pragma unroll
+  for (int i = 0; i < V; ++i) key[i] = keys[lane * V + i];
+  drop_groups<L, V>(key, stays, E, groups, lane);
+  return true;
+}
+
+// take_largest of n keys in LDS (each lane a run of them): seldom called, and in few registers,
+// which the rest would have to do without
+template <int L, class F>
+__device__ __forceinline__ void take_largest_lds(double* keys, int n, int k, int lane, F take) {
+  const int each = (n + L - 1) / L, first = lane * each, end = min(n, first + each);
+#pragma clang loop unroll(disable)
+  for (int r = 0; r < k; ++r) {
+    double mine = -INFINITY;
+    int at = first;
+#pragma clang loop unroll_count(4)
+    for (int e = first; e < end; ++e) {
+      const double c = keys[e];
+      at = c > mine ? e : at;
+      mine = larger(mine, c);
+    }
+    const double best = largest<L>(mine);
+    const uint64_t have = of_token<L>(__ballot(mine == best));
+    if (best > -INFINITY && lane == __ffsll((unsigned long long)have) - 1) {
+      keys[at] = -INFINITY;
+      take(r, at);
+    }
+    wave_fence();
+  }
+}
+
+// LDS of a wave: its tokens' choices, which of their groups stay, and room for one thing after the
+// other: of each token the keys of experts and groups of 32 bits, or candidates with
+// their scores; keys of 64 bits of one token at a time.  (Groups are of two experts at least.)
 constexpr int CAND = 64;
 template <int L, int V>
-constexpr int token_bytes() {
-  return OZ2_MAX_TOPK * 4 + std::max(L * V * 9, CAND * 12);
-}
+struct Lds {
+  static constexpr int TOKENS = 64 / L, STAYS = TOKENS * OZ2_MAX_TOPK * 4, ROOM = STAYS + TOKENS * L * V;
+  static constexpr int EACH = std::max(L * V * (L < 64 ? 6 : 12), CAND * 12), WAVE = ROOM + TOKENS * EACH;
+  static_assert(TOKENS * EACH >= L * V * 12 && ROOM % 8 == 0 && EACH % 8 == 0 && WAVE % 8 == 0, "room");
+};
 
 // Choices by scores (SCORED) or by the logits, whose order is that of scores without a bias.
 // Scores are compared as in 64 bits, but 64 bits are formed for few: 32 bits find those that
@@ -197,20 +285,22 @@ constexpr int token_bytes() {
 // score and of its sum with the bias, twice).  Where that does not decide, too many are that
 // close or a group's value is, or there is a NaN or an infinity, all are formed.
 template <class T, bool SCORED, int L, int V>
-__global__ void __launch_bounds__(NT)
+__global__ void __launch_bounds__(NT, 4)
 k_route(Oz2Route a) {
   constexpr int TOKENS = NT / L, Q = OZ2_MAX_TOPK / L;
-  extern __shared__ double lds[];
-  uint8_t* const mine = (uint8_t*)lds + threadIdx.x / L * token_bytes<L, V>();
-  int* const chosen = (int*)mine;
-  uint8_t* const room = mine + OZ2_MAX_TOPK * 4;
-  uint8_t* const stays = room + L * V * 8;
-  const int lane = threadIdx.x % L, E = a.experts, first = lane * V;
+  typedef Lds<L, V> Part;
+  __shared__ __attribute__((aligned(8))) uint8_t lds[NT / 64 * Part::WAVE];
+  const int lane = threadIdx.x % L, tok = threadIdx.x % 64 / L, E = a.experts, first = lane * V;
+  uint8_t* const mine = lds + threadIdx.x / 64 * Part::WAVE;
+  int* const chosen = (int*)mine + tok * OZ2_MAX_TOPK;
+  uint8_t* const stays = mine + Part::STAYS + tok * L * V;
+  uint8_t* const room = mine + Part::ROOM + tok * Part::EACH;
+  const bool grouped = a.groups > 1 && a.groups < E;   // (groups of one: the experts themselves)
   const bool soft = a.score == OZ2_SCORE_SOFTMAX;
-  const ll last = a.tokens - 1;
-  for (ll t0 = (ll)blockIdx.x * TOKENS; t0 <= last; t0 += (ll)gridDim.x * TOKENS) {
-    const bool live = t0 + threadIdx.x / L <= last;
-    const ll t = live ? t0 + threadIdx.x / L : last;
+  {
+    const int own = (int)blockIdx.x * TOKENS + (int)threadIdx.x / L;
+    const bool live = own < a.tokens;
+    const ll t = live ? own : a.tokens - 1;
     const T* row = (const T*)a.logits + t * a.ld;
     float l[V], b[V];
     load_logits<T, V>(row, first, E, l);
@@ -245,7 +335,7 @@ k_route(Oz2Route a) {
         key_of(l[i], key[i]);
         if (l[i] == -INFINITY) key[i] = 0;
       }
-      if (a.groups > 1)
+      if (grouped)
         keep_groups<L, V>(key, (uint32_t*)room, stays, E, a.groups, a.top_groups, false, lane, &after,
                           [](uint32_t x, uint32_t) { return x; });
       wave_fence();
@@ -256,17 +346,31 @@ k_route(Oz2Route a) {
       if (soft) {
         top = across<L, false>(top);
         sum = 0.0;
+        // (a loop, its logits in LDS: the exponential of 64 bits is long)
+        float* const z = (float*)room;
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum += l[i] == -INFINITY ? 0.0 : exp((double)l[i] - (double)top);
+        for (int i = 0; i < V; ++i) z[first + i] = l[i];
+        wave_fence();
+#pragma clang loop unroll(disable)
+        for (int i = 0; i < V; ++i) {
+          const float v = z[first + i];
+          sum += v == -INFINITY ? 0.0 : exp((double)v - (double)top);
+        }
+        wave_fence();
         sum = total_of<L>(sum);
         total = (float)sum;
         A /= total;   // (of the largest score; e^x in 32 bits is off by |x| 2^-24, and |x| e^x below 1)
+        const float share = 1.0f / total;
+#pragma unroll
+        for (int i = 0; i < V; ++i) c[i] = __expf(l[i] - top) * share;
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) c[i] = __builtin_amdgcn_rcpf(1.0f + __expf(-l[i]));
       }
       bool exact = false;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float s = soft ? __expf(l[i] - top) / total : __builtin_amdgcn_rcpf(1.0f + __expf(-l[i]));
-        c[i] = s + b[i];
+        c[i] += b[i];
         key_of(c[i], key[i]);
         if (l[i] == -INFINITY || b[i] == -INFINITY) {
           key[i] = 0;
@@ -276,9 +380,16 @@ k_route(Oz2Route a) {
           far = fmaxf(far, fabsf(c[i]));
         }
       }
+      exact = of_token<L>(__ballot(exact));
       far = across<L, false>(far);
       const float near = 2.0f * (A + 2.4e-7f * far);
-      if (a.groups > 1) {
+      // expert e's score and bias in 64 bits
+      auto score64 = [&](int e) {
+        const float z = to_f(row[e]);
+        const double s = soft ? exp((double)z - (double)top) / sum : sigmoid64(z);
+        return s + (a.bias ? (double)a.bias[e] : 0.0);
+      };
+      if (grouped) {
         const uint32_t least = keep_groups<L, V>(
             key, (uint32_t*)room, stays, E, a.groups, a.top_groups, a.group_best > 1, lane, &after,
             [](uint32_t x, uint32_t y) {
@@ -287,7 +398,9 @@ k_route(Oz2Route a) {
               return k;
             });
         // (sums of two)
-        exact |= after && value_of(least) - value_of(after) <= 3.0f * near;
+        if (!exact && after && value_of(least) - value_of(after) <= 3.0f * near)
+          exact = !settle_groups<L, V>(key, (uint32_t*)room, stays, E, a.groups, a.top_groups, a.group_best > 1, near,
+                                       lane, score64);
       }
       // the k-th value, or the least there is
       uint32_t kth = ~0u;
@@ -314,7 +427,8 @@ k_route(Oz2Route a) {
       }
       const int count = __shfl(before, L - 1, L);
       exact |= count > CAND;
-      if (!__any(exact)) {
+      wave_fence();
+      if (!exact) {
         double* const score = (double*)room;
         int* const who = (int*)(score + CAND);
         int at = before - n;
@@ -322,12 +436,7 @@ k_route(Oz2Route a) {
         for (int i = 0; i < V; ++i)
           if (in[i]) who[at++] = first + i;
         wave_fence();
-        for (int j = lane; j < count; j += L) {
-          const int e = who[j];
-          const float z = to_f(row[e]);
-          const double s = soft ? exp((double)z - (double)top) / sum : sigmoid64(z);
-          score[j] = s + (a.bias ? (double)a.bias[e] : 0.0);
-        }
+        for (int j = lane; j < count; j += L) score[j] = score64(who[j]);
         wave_fence();
         for (int j = lane; j < count; j += L) {
           const double mine = score[j];
@@ -336,20 +445,35 @@ k_route(Oz2Route a) {
           for (int i = 0; i < count; ++i) rank += score[i] > mine || (score[i] == mine && who[i] < e);
           if (rank < a.top_k) chosen[rank] = e;
         }
-      } else {
-        double all[V], beyond;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          double s = soft ? exp((double)l[i] - (double)top) / sum : sigmoid64(l[i]);
-          if (soft && bad) s = __builtin_nan("");
-          key_of(s + (double)b[i], all[i]);
-          if (l[i] == -INFINITY || b[i] == -INFINITY) none(all[i]);
+      }
+      wave_fence();
+      for (int q = 0; q < 64 / L; ++q) {
+        if (q != tok || !exact) continue;
+        // all of a token's keys in 64 bits: in few registers, which the rest would have to do without
+        double* const keys = (double*)(mine + Part::ROOM);
+#pragma clang loop unroll(disable)
+        for (int e = lane; e < E; e += L) {
+          const float z = to_f(row[e]), d = a.bias ? a.bias[e] : 0.0f;
+          key_of(soft && bad ? __builtin_nan("") : score64(e), keys[e]);
+          if (z == -INFINITY || d == -INFINITY) none(keys[e]);
         }
-        if (a.groups > 1)
-          keep_groups<L, V>(all, (double*)room, stays, E, a.groups, a.top_groups, a.group_best > 1, lane, &beyond,
-                            [](double x, double y) { return x < INFINITY ? fmin(x + y, kMost) : x; });
         wave_fence();
-        take_largest<L, V>(all, a.top_k, lane, [&](int r, int e) { chosen[r] = e; });
+        if (grouped) {
+          const int per = E / a.groups, each = (a.groups + L - 1) / L;
+          double* const values = keys + L * V;
+          for (int g = lane; g < a.groups; g += L) stays[g] = 0;
+          group_keys<L>(keys, per, min(a.groups, lane * each), min(a.groups, lane * each + each), a.group_best > 1,
+                        lane, [](double x, double y) { return x < INFINITY ? fmin(x + y, kMost) : x; },
+                        [&](int g, double v) { values[g] = v; });
+          wave_fence();
+          take_largest_lds<L>(values, a.groups, a.top_groups, lane, [&](int, int g) { stays[g] = 1; });
+#pragma clang loop unroll(disable)
+          for (int e = lane; e < E; e += L)
+            if (!stays[e / per]) keys[e] = -INFINITY;
+          wave_fence();
+        }
+        take_largest_lds<L>(keys, E, a.top_k, lane, [&](int r, int e) { chosen[r] = e; });
+        wave_fence();
       }
     }
     wave_fence();
@@ -389,7 +513,6 @@ k_route(Oz2Route a) {
       a.ids[t * a.top_k + j] = id[q];
       a.weights[t * a.top_k + j] = id[q] < 0 ? 0.0f : bad ? __builtin_nanf("") : a.scale * w[q];
     }
-    wave_fence();
   }
 }
 
@@ -497,26 +620,38 @@ k_route_backward(Oz2RouteBack a) {
   }
 }
 
-// f(lanes a token, experts a lane) as types
+// f(lanes a token, experts a lane) as types.  The fewest lanes that keep a lane's experts in
+// registers: 16 experts and their scores do not fit beside what scores take
 template <class F>
-hipError_t for_experts(int E, F f) {
+hipError_t for_experts(int E, bool scored, F f) {
   using std::integral_constant;
   if (E <= 16) return f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
   if (E <= 32) return f(integral_constant<int, 16>{}, integral_constant<int, 2>{});
   if (E <= 64) return f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
   if (E <= 128) return f(integral_constant<int, 16>{}, integral_constant<int, 8>{});
-  if (E <= 256) return f(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+  if (E <= 256 && !scored) return f(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+  if (E <= 256) return f(integral_constant<int, 32>{}, integral_constant<int, 8>{});
   if (E <= 512) return f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
   return f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
 }
 
 template <class T, bool SCORED>
 hipError_t launch_route(const Oz2Route& a, hipStream_t s) {
-  return for_experts(a.experts, [&](auto lanes, auto each) {
+  return for_experts(a.experts, SCORED, [&](auto lanes, auto each) {
     constexpr int L = decltype(lanes)::value, V = decltype(each)::value, TOKENS = NT / L;
-    const dim3 grid((unsigned)std::min<ll>(ROW_BLOCKS, ((ll)a.tokens + TOKENS - 1) / TOKENS));
-    hipLaunchKernelGGL((k_route<T, SCORED, L, V>), grid, dim3(NT), (TOKENS * token_bytes<L, V>()), s, a);
-    return hipGetLastError();
+    hipError_t e = hipSuccess;
+    // (launches of no more than a grid's workgroups)
+    for (ll t = 0; t < a.tokens && e == hipSuccess; t += ROW_BLOCKS * TOKENS) {
+      Oz2Route part = a;
+      part.tokens = (int)std::min<ll>(ROW_BLOCKS * TOKENS, a.tokens - t);
+      part.logits = (const T*)a.logits + t * a.ld;
+      part.ids += t * a.top_k;
+      part.weights += t * a.top_k;
+      hipLaunchKernelGGL((k_route<T, SCORED, L, V>), dim3((unsigned)((part.tokens + TOKENS - 1) / TOKENS)), dim3(NT),
+                         0, s, part);
+      e = hipGetLastError();
+    }
+    return e;
   });
 }
 
@@ -528,7 +663,7 @@ hipError_t oz2_launch_route(int dtype, const Oz2Route& a, hipStream_t s) {
 }
 
 hipError_t oz2_launch_route_backward(int dtype, const Oz2RouteBack& a, hipStream_t s) {
-  OZ2_TYPED(dtype, return for_experts(a.experts, [&](auto lanes, auto each) {
+  OZ2_TYPED(dtype, return for_experts(a.experts, false, [&](auto lanes, auto each) {
               constexpr int L = decltype(lanes)::value, V = decltype(each)::value, TOKENS = NT / L;
               const dim3 grid((unsigned)std::min<ll>(ROW_BLOCKS, ((ll)a.tokens + TOKENS - 1) / TOKENS));
               hipLaunchKernelGGL((k_route_backward<T, L, V>), grid, dim3(NT), 0, s, a);
