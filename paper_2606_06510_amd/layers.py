@@ -39,6 +39,7 @@ class ExpertOrder(NamedTuple):
 
 _torch = None
 _raw_stream = None
+_current_device = None
 _codes = {}
 
 # bytes of workspace, functions of types and sizes alone
@@ -53,11 +54,12 @@ _sort_bytes = lru_cache(4096)(lambda *a: _lib.ozaki2_expert_sort_workspace_bytes
 
 def _init():
     """torch is imported by the first call, as everywhere in this package"""
-    global _torch, _raw_stream
+    global _torch, _raw_stream, _current_device
     import torch
     # the handle alone, where torch offers it (a Stream object takes 2.5 us to make)
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                           lambda index: torch.cuda.current_stream(index).cuda_stream)
+    _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
     _codes.update({torch.float32: _lib.OZ2_F32, torch.float16: _lib.OZ2_F16,
                    torch.bfloat16: _lib.OZ2_BF16})
     _torch = torch
@@ -163,12 +165,12 @@ def _p(t):
 def _launch(device, stream, call):
     """call(stream handle) with ``device`` and the stream current, so that what
     it allocates belongs to the stream that uses it."""
-    cuda = _torch.cuda
     if stream is None:
-        if device.index == cuda.current_device():
+        if device.index == _current_device():
             return call(_raw_stream(device.index))
-        with cuda.device(device):
+        with _torch.cuda.device(device):
             return call(_raw_stream(device.index))
+    cuda = _torch.cuda
     if isinstance(stream, int):
         stream = (cuda.ExternalStream(stream, device=device) if stream
                   else cuda.default_stream(device))

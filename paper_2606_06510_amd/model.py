@@ -36,19 +36,39 @@ def _range(name, value, lo, hi):
         raise ValueError(f"{name}: expected {lo} to {hi}, got {value}")
 
 
-def _vector(name, t, like, n, dtype=None):
-    """A contiguous vector, or None"""
-    if t is not None:
-        _dense(name, t, like, (n,), dtype or like.dtype)
+# A small call is mostly the host's: what holds for nearly every tensor is asked first and
+# in few steps, and where it does not the checks that name the fault follow.
+
+def _rows(name, t):
+    """(type code, device, rows, columns, leading dimension) of a matrix"""
+    try:
+        T, K = t.shape
+        code = layers._codes[t.dtype]
+        if t.is_cuda and t.is_contiguous():
+            return code, t.device, T, K, K or 1
+    except (AttributeError, KeyError, TypeError, ValueError):
+        pass
+    return (_dtype(name, t), _device(name, t), *_dim2(name, t), _ld(name, t))
+
+
+def _same(name, t, like, shape, dtype):
+    """A contiguous tensor of this shape and type on the device of ``like``"""
+    try:
+        if (t.shape == shape and t.dtype is dtype and t.is_contiguous()
+                and t.get_device() == like.get_device()):
+            return
+    except AttributeError:
+        pass
+    _dense(name, t, like, shape, dtype)
 
 
 # ----------------------------------------------------------------- router
 
 def _experts(logits):
-    T, E = _dim2("logits", logits)
+    code, dev, T, E, ld = _rows("logits", logits)
     if E < 1 or E > _lib.OZ2_MAX_EXPERTS:
         raise ValueError(f"logits: expected 1 to {_lib.OZ2_MAX_EXPERTS} experts, got {E}")
-    return T, E
+    return code, dev, T, E, ld
 
 
 def expert_route(logits, top_k, bias=None, score="softmax", groups=1, top_groups=1, group_best=2,
@@ -67,21 +87,23 @@ def expert_route(logits, top_k, bias=None, score="softmax", groups=1, top_groups
     An expert whose logit or bias is -inf is out.  Where fewer than top_k are left (all, in
     a row of padding), ids is -1, which drops the pair, and the weight 0.  NaN is larger than
     every number.  Not recorded by autograd: the gradient is expert_route_backward's."""
-    code, kind, dev = _dtype("logits", logits), _score(score), _device("logits", logits)
-    T, E = _experts(logits)
-    _range("groups", groups, 1, E)
-    if E % groups:
-        raise ValueError(f"groups: {E} experts are no {groups} equal groups")
-    _range("top_groups", top_groups, 1, groups)
-    _range("group_best", group_best, 1, 2)
+    code, dev, T, E, ld = _experts(logits)
+    kind = _score(score)
+    if groups != 1 or top_groups != 1:
+        _range("groups", groups, 1, E)
+        if E % groups:
+            raise ValueError(f"groups: {E} experts are no {groups} equal groups")
+        _range("top_groups", top_groups, 1, groups)
+    if group_best not in (1, 2):
+        raise ValueError(f"group_best: expected 1 or 2, got {group_best}")
     _range("top_k", top_k, 1, min(_lib.OZ2_MAX_TOPK, E // groups * top_groups))
-    ld = _ld("logits", logits)
     torch = layers._torch
-    _vector("bias", bias, logits, E, torch.float32)
+    if bias is not None:
+        _same("bias", bias, logits, (E,), torch.float32)
 
     def call(s):
-        ids = torch.empty((T, top_k), dtype=torch.int32, device=dev)
-        weights = torch.empty((T, top_k), dtype=torch.float32, device=dev)
+        ids = torch.empty(T, top_k, dtype=torch.int32, device=dev)
+        weights = torch.empty(T, top_k, dtype=torch.float32, device=dev)
         _call("ozaki2_expert_route", code, T, E, top_k, logits.data_ptr(), ld, _p(bias), kind, groups,
               top_groups, group_best, bool(renormalize), scale, ids.data_ptr(), weights.data_ptr(), s)
         return ids, weights
@@ -94,20 +116,19 @@ def expert_route_backward(dweights, logits, ids, score="softmax", renormalize=Tr
     top_k], as expert_combine_backward gives them) and the ids that expert_route chose with the
     same score, renormalize and scale.  Choices of -1 take no part.  The bias has no
     gradient.  dlogits: an output to write into."""
-    code, kind, dev = _dtype("logits", logits), _score(score), _device("logits", logits)
-    T, E = _experts(logits)
+    code, dev, T, E, ld = _experts(logits)
+    kind = _score(score)
     T0, k = _dim2("ids", ids)
     if T0 != T:
         raise ValueError(f"ids: expected {T} tokens, got {T0}")
     _range("top_k", k, 1, min(_lib.OZ2_MAX_TOPK, E))
     torch = layers._torch
-    _dense("ids", ids, logits, (T, k), torch.int32)
-    _dense("dweights", dweights, logits, (T, k), torch.float32)
-    ld = _ld("logits", logits)
+    _same("ids", ids, logits, (T, k), torch.int32)
+    _same("dweights", dweights, logits, (T, k), torch.float32)
     ldd = _matrix("dlogits", dlogits, logits, (T, E)) if dlogits is not None else E
 
     def call(s):
-        d = logits.new_empty((T, E)) if dlogits is None else dlogits
+        d = torch.empty(T, E, dtype=logits.dtype, device=dev) if dlogits is None else dlogits
         _call("ozaki2_expert_route_backward", code, T, E, k, dweights.data_ptr(), logits.data_ptr(),
               ld, ids.data_ptr(), kind, bool(renormalize), scale, d.data_ptr(), ldd, s)
         return d
@@ -123,18 +144,19 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, save_stats=False, out=None, 
     save_stats: returns (y, stats) with stats float32 [T, 2], each row's mean and 1 /
     sqrt(variance + eps), as layer_norm_backward takes them.  out may be x itself.  Not
     recorded by autograd: its gradients are layer_norm_backward's."""
-    code, dev = _dtype("x", x), _device("x", x)
-    T, K = _dim2("x", x)
+    code, dev, T, K, ldx = _rows("x", x)
     if not eps >= 0.0:
         raise ValueError(f"eps: expected a number of at least 0, got {eps}")
-    ldx = _ld("x", x)
-    _vector("weight", weight, x, K)
-    _vector("bias", bias, x, K)
-    ldy = _matrix("out", out, x, (T, K)) if out is not None else max(K, 1)
+    if weight is not None:
+        _same("weight", weight, x, (K,), x.dtype)
+    if bias is not None:
+        _same("bias", bias, x, (K,), x.dtype)
+    ldy = _matrix("out", out, x, (T, K)) if out is not None else K or 1
+    torch = layers._torch
 
     def call(s):
-        y = x.new_empty((T, K)) if out is None else out
-        stats = x.new_empty((T, 2), dtype=layers._torch.float32) if save_stats else None
+        y = torch.empty(T, K, dtype=x.dtype, device=dev) if out is None else out
+        stats = torch.empty(T, 2, dtype=torch.float32, device=dev) if save_stats else None
         _call("ozaki2_layer_norm", code, T, K, x.data_ptr(), ldx, _p(weight), _p(bias), eps,
               y.data_ptr(), ldy, _p(stats), s)
         return (y, stats) if save_stats else y
@@ -147,16 +169,15 @@ def layer_norm_backward(dy, x, stats, weight=None, residual=None, need_dx=True, 
     """(dx, dweight, dbias) of ``layer_norm`` from dy [T, width] and the stats it saved;
     None for what is not needed.  residual [T, width], the gradient that flows past the norm, is
     added to dx (dx may be residual itself).  dx, dweight, dbias: outputs to write into."""
-    code, dev = _dtype("dy", dy), _device("dy", dy)
-    T, K = _dim2("dy", dy)
-    lddy, ldx = _ld("dy", dy), _matrix("x", x, dy, (T, K))
-    _dense("stats", stats, dy, (T, 2), layers._torch.float32)
-    _vector("weight", weight, dy, K)
+    code, dev, T, K, lddy = _rows("dy", dy)
+    ldx = _matrix("x", x, dy, (T, K))
+    _same("stats", stats, dy, (T, 2), layers._torch.float32)
     ldr = _matrix("residual", residual, dy, (T, K)) if residual is not None else 0
     if dx is not None:
         _matrix("dx", dx, dy, (T, K))
-    _vector("dweight", dweight, dy, K)
-    _vector("dbias", dbias, dy, K)
+    for name, t in (("weight", weight), ("dweight", dweight), ("dbias", dbias)):
+        if t is not None:
+            _same(name, t, dy, (K,), dy.dtype)
     need = _norm_bytes(code, T, K) if need_dweight or need_dbias or dweight is not None \
         or dbias is not None else 0
 
@@ -175,6 +196,12 @@ def layer_norm_backward(dy, x, stats, weight=None, residual=None, need_dx=True, 
 # ------------------------------------------------------------------- loss
 
 def _targets(targets, like, T):
+    try:
+        if (targets.dtype is layers._torch.int64 and targets.shape == (T,) and targets.is_contiguous()
+                and targets.get_device() == like.get_device()):
+            return True
+    except AttributeError:
+        pass
     if not isinstance(targets, layers._torch.Tensor):
         raise TypeError(f"targets: expected a torch tensor, got {type(targets).__name__}")
     if targets.dtype not in (layers._torch.int32, layers._torch.int64):
@@ -190,10 +217,9 @@ def linear_cross_entropy(x, w, targets, workspace=None, stream=None):
 
     The logits are kept in 32 bits in the product's epilogue and never stored.  Not recorded
     by autograd: its gradients are linear_cross_entropy_backward's."""
-    code, dev = _dtype("x", x), _device("x", x)
-    T, K = _dim2("x", x)
+    code, dev, T, K, ldx = _rows("x", x)
     V, _ = _dim2("w", w)
-    ldx, ldw = _ld("x", x), _matrix("w", w, x, (V, K))
+    ldw = _matrix("w", w, x, (V, K))
     wide = _targets(targets, x, T)
     need = _loss_bytes(code, T, V, K)
 
@@ -217,14 +243,13 @@ def linear_cross_entropy_backward(dloss, x, w, targets, lse, need_dx=True, need_
     The logits are computed again, a piece of the vocabulary at a time.  Their gradient is
     rounded to the tensors' dtype before the products, as every operand of theirs, in
     float16 times a power of two that keeps it in range."""
-    code, dev = _dtype("x", x), _device("x", x)
-    T, K = _dim2("x", x)
+    code, dev, T, K, ldx = _rows("x", x)
     V, _ = _dim2("w", w)
-    ldx, ldw = _ld("x", x), _matrix("w", w, x, (V, K))
+    ldw = _matrix("w", w, x, (V, K))
     wide = _targets(targets, x, T)
     f32 = layers._torch.float32
-    _dense("dloss", dloss, x, (T,), f32)
-    _dense("lse", lse, x, (T,), f32)
+    _same("dloss", dloss, x, (T,), f32)
+    _same("lse", lse, x, (T,), f32)
     if dx is not None:
         _matrix("dx", dx, x, (T, K))
     if dw is not None:
