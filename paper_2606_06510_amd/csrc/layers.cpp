@@ -221,7 +221,7 @@ bool tokens_ok(int dtype, int tokens, int top_k, int width) {
 // 113 against 112; without gates tiles win (64 experts, 4096 -> 2048, 213 and 291 against
 // 178; 16 in fp32, 1024 -> 2048, 41 and 42 against 39), and so they do where most rows fall
 // to one group (k_rows reads W again for every 32 of them).
-Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr, bool padded,
+Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr, int padded,
                  bool whole) {
   const double cus = oz2_device_cus();
   const bool wide = dtype == OZ2_F32;
@@ -233,7 +233,7 @@ Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr
   // rows of A and B as they lie in memory
   const ll wa = side == OZ2_WGRAD ? M : L, wb = side == OZ2_FWD ? L : N2;
   const ll ra = side == OZ2_WGRAD ? L : M, rb = side == OZ2_FWD ? groups * N2 : side == OZ2_DGRAD ? groups * L : L;
-  const int odd = (!padded && wa * e % 16 ? 1 : 0) | (wb * e % 16 ? 2 : 0);
+  const int odd = (!(padded & 1) && wa * e % 16 ? 1 : 0) | (!(padded & 2) && wb * e % 16 ? 2 : 0);
   const size_t packed = (odd & 1 ? (size_t)ra * oz2_packed_pitch(wa, e) * e : 0) +
                         (odd & 2 ? (size_t)rb * oz2_packed_pitch(wb, e) * e : 0);
   auto tiles = [&](double t) {
@@ -288,7 +288,7 @@ extern "C" {
 void oz2_plan_of(int dtype, int side, ll M, ll N2, ll L, int rows, int groups, int padded, int* out) {
   static const int any = 0;
   const Oz2Plan p = oz2_plan(dtype, (Oz2Side)side, M, N2, L,
-                             Oz2Groups{groups ? &any : nullptr, groups ? groups : 1, rows}, padded != 0);
+                             Oz2Groups{groups ? &any : nullptr, groups ? groups : 1, rows}, padded ? 1 : 0);
   out[0] = p.rows;
   out[1] = p.tile;
   out[2] = p.splits;

@@ -11,7 +11,7 @@ constexpr int JT = 256;
 // (top, sum) and another one's: the larger top, both sums as seen from it
 __device__ __forceinline__ void join(float& top, float& sum, float t, float s) {
   const float m = fmaxf(top, t), m0 = m == -INFINITY ? 0.0f : m;
-  sum = sum * expf(top - m0) + s * expf(t - m0);
+  sum = sum * __builtin_amdgcn_exp2f(top - m0) + s * __builtin_amdgcn_exp2f(t - m0);
   top = m;
 }
 
@@ -50,24 +50,23 @@ k_lse_join(Oz2Loss l, int rows, int vocab, int n, float* __restrict__ loss, floa
     }
   }
   if (run || r >= rows) return;
-  const float rest = logf(s);
   const ll t = target_of(l, r);
-  lse[r] = m + rest;
-  // (the difference first: the logarithm keeps its low bits)
-  loss[r] = t >= 0 && t < vocab ? m - l.picked[r] + rest : 0.0f;
+  // (in 64 bits until the end: of a large lse and a target close to it little is left)
+  const double whole = (double)m * 0.69314718055994530942 + (double)logf(s);
+  lse[r] = (float)whole;
+  loss[r] = t >= 0 && t < vocab ? (float)(whole - (double)l.picked[r]) : 0.0f;
 }
 
-// scale[0]: the power of two that takes the largest |dloss| of the rows that count to
-// [2^14, 2^15), 1 where there is none or it is no number; scale[1] its inverse
-__global__ void __launch_bounds__(1024)
-k_loss_scale(Oz2LossRows a) {
-  __shared__ float red[16];
+// The exponent of the power of two that takes the largest |dloss| of the rows that count to
+// [2^14, 2^15), 0 where there is none or it is no number.  Every one of NT threads calls it.
+template <int NT>
+__device__ __forceinline__ int slope_exponent(const Oz2LossRows& a, float* red) {
   Oz2Loss l{};
   l.targets = a.targets;
   l.wide = a.wide;
   float m = 0.0f;
   bool bad = false;
-  for (ll r = threadIdx.x; r < a.rows; r += 1024) {
+  for (ll r = threadIdx.x; r < a.rows; r += NT) {
     const ll t = target_of(l, r);
     if (t < 0 || t >= a.vocab) continue;
     const float g = fabsf(a.dloss[r]);
@@ -79,36 +78,65 @@ k_loss_scale(Oz2LossRows a) {
   for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
   __syncthreads();
-  if (threadIdx.x) return;
-  for (int i = 1; i < 16; ++i) m = fmaxf(m, red[i]);
+  m = red[0];
+  for (int i = 1; i < NT / 64; ++i) m = fmaxf(m, red[i]);
   int e = 0;
   if (m > 0.0f && m < INFINITY) {
     frexpf(m, &e);           // m in [2^(e - 1), 2^e)
     e = min(15 - e, 126);
   }
+  return e;
+}
+
+__global__ void __launch_bounds__(1024)
+k_loss_scale(Oz2LossRows a) {
+  __shared__ float red[16];
+  const int e = slope_exponent<1024>(a, red);
+  if (threadIdx.x) return;
   a.scale[0] = ldexpf(1.0f, e);
   a.scale[1] = ldexpf(1.0f, -e);
 }
 
-// Rows of X at whole lines, zeros at their ends and for rows that do not count (whatever
-// such a row holds, it meets the slopes' zeros as a zero)
+// Rows of X (and of W) at whole lines, zeros at their ends and for rows of X that do not count
+// (whatever such a row holds, it meets the slopes' zeros as a zero)
 template <class T>
 __global__ void __launch_bounds__(256)
 k_loss_rows(Oz2LossRows a) {
   constexpr int P = 16 / sizeof(T);
+  __shared__ float red[4];
+  float scale = 1.0f;
+  if (a.scale && a.rows) {
+    if (a.rows <= OZ2_SCALE_ROWS) {
+      const int e = slope_exponent<256>(a, red);
+      scale = ldexpf(1.0f, e);
+      if (blockIdx.x == 0 && threadIdx.x == 0) {
+        a.scale[0] = scale;
+        a.scale[1] = ldexpf(1.0f, -e);
+      }
+    } else {
+      scale = a.scale[0];
+    }
+  }
   Oz2Loss l{};
   l.targets = a.targets;
   l.wide = a.wide;
-  for (ll r = (ll)blockIdx.x * 4 + (threadIdx.x >> 6); r < a.rows; r += (ll)gridDim.x * 4) {
-    const ll t = target_of(l, r);
-    const bool on = t >= 0 && t < a.vocab;
-    if ((threadIdx.x & 63) == 0)
-      a.out[r] = Oz2LossRow{on ? a.lse[r] : 0.0f, on ? a.dloss[r] * (a.scale ? a.scale[0] : 1.0f) : 0.0f,
-                            on ? (int)t : -1, 0};
-    const T* x = (const T*)a.x + r * a.ldx;
-    T* d = (T*)a.dst + r * a.pitch;
-    for (int c = (threadIdx.x & 63) * P; c < a.pitch; c += 64 * P)
-      store_piece(d + c, load_piece<T>(x + c, on ? a.in - c : 0), P);
+  const ll all = (ll)a.rows + (a.w ? a.words : 0);
+  for (ll r = (ll)blockIdx.x * 4 + (threadIdx.x >> 6); r < all; r += (ll)gridDim.x * 4) {
+    const bool of_w = r >= a.rows;
+    bool on = true;
+    if (!of_w) {
+      const ll t = target_of(l, r);
+      on = t >= 0 && t < a.vocab;
+      if ((threadIdx.x & 63) == 0)
+        a.out[r] = Oz2LossRow{on ? a.lse[r] : 0.0f, on ? a.dloss[r] * scale : 0.0f, on ? (int)t : -1, 0};
+    }
+    const T* from = of_w ? (const T*)a.w + (r - a.rows) * a.ldw : (const T*)a.x + r * a.ldx;
+    T* to = of_w ? (T*)a.dst_w + (r - a.rows) * a.pitch : (T*)a.dst + r * a.pitch;
+    for (int c = (threadIdx.x & 63) * P; c < a.pitch; c += 64 * P) {
+      const Piece<T, P> v = load_piece<T>(from + c, on ? a.in - c : 0);
+      store_piece(to + c, v, P);
+      if (a.twin && !of_w) store_piece(to + a.rows * a.pitch + c, v, P);
+    }
   }
 }
 
@@ -153,18 +181,25 @@ hipError_t launch_sum(const Oz2Plan& plan, Oz2Product p, bool last, hipStream_t 
   p.splits = plan.splits;
   hipError_t e = plan.pack ? pack<T>(SIDE, plan, p, s) : hipSuccess;
   if (e == hipSuccess) e = launch_tiles<T, SIDE, OZ2_END_SUM>(plan.tile, p, s);
-  return e != hipSuccess || p.loss.whole || !last ? e : launch_join<T>(p, s);
+  if (e != hipSuccess || p.loss.whole || !last) return e;
+  if (p.loss.twin) {   // both halves of a part are parts
+    p.M /= 2;
+    p.splits *= 2;
+  }
+  return launch_join<T>(p, s);
 }
 
 }  // namespace
 
 hipError_t oz2_launch_loss_rows(int dtype, const Oz2LossRows& a, hipStream_t s) {
-  if (a.scale) {
+  if (a.scale && a.rows > OZ2_SCALE_ROWS) {
     hipLaunchKernelGGL(k_loss_scale, dim3(1), dim3(1024), 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  const dim3 grid((unsigned)std::min<ll>(1 << 20, ((ll)a.rows + 3) / 4));
+  const ll all = (ll)a.rows + (a.w ? a.words : 0);
+  if (all == 0) return hipSuccess;
+  const dim3 grid((unsigned)std::min<ll>(1 << 20, (all + 3) / 4));
   OZ2_TYPED(dtype, hipLaunchKernelGGL(k_loss_rows<T>, grid, dim3(256), 0, s, a));
   return hipGetLastError();
 }

@@ -60,22 +60,30 @@ LseLayout lse_layout(int dtype, int rows, int vocab, int in) {
 // The gradients of the loss, `step` words of the vocabulary at a time
 constexpr size_t kSlopeBytes = 256u << 20;
 
+// Up to so many tokens the slopes are kept in two 16-bit parts, for the products are bound by
+// W there (65536 x 4096 bf16 at 100 tokens: the three products 416 us instead of 404).  The errors
+// of a few tokens' roundings do not average out: with one, dW is off by up to 2^-8 everywhere.  Beyond,
+// the gradients' error in bf16 is 0.0023 where their own rounding is 0.0017.
+constexpr int kTwinRows = 64;
+
 struct LossLayout {
-  size_t rows, scale, x, dz, dx, work, total;
+  size_t rows, scale, x, w, dz, dx, work, total;
   ll pitch, pitch_dz;
-  int step;
+  int step, lines;       // lines: rows of the slopes, and of X beside them
+  int padded;            // of the products with W: 1, and 2 where W is copied as X is
   bool whole;            // dX of one piece in one product
   Oz2Plan dgrad;         // of the first piece, for all (their parts add up)
 };
-Oz2Plan slope_plan(int dtype, int rows, int n, int in) {
-  return oz2_plan(dtype, OZ2_FWD, rows, n, in, all(rows), true, true);
+Oz2Plan slope_plan(int dtype, const LossLayout& L, int rows, int n, int in) {
+  return oz2_plan(dtype, OZ2_FWD, rows, n, in, all(rows), L.padded, true);
 }
-Oz2Plan wgrad_plan(int dtype, int rows, int n, int in) {
-  return oz2_plan(dtype, OZ2_WGRAD, n, in, rows, all(rows), true);
+Oz2Plan wgrad_plan(int dtype, const LossLayout& L, int n, int in) {
+  return oz2_plan(dtype, OZ2_WGRAD, n, in, L.lines, all(L.lines), 3);
 }
-size_t piece_bytes(int dtype, int rows, int n, int in, const Oz2Plan& dgrad) {
-  return std::max(std::max(align256(slope_plan(dtype, rows, n, in).packed_bytes), align256(dgrad.packed_bytes)),
-                  product_bytes(wgrad_plan(dtype, rows, n, in), n, in));
+size_t piece_bytes(int dtype, const LossLayout& L, int rows, int n, int in) {
+  return std::max(
+      std::max(align256(slope_plan(dtype, L, rows, n, in).packed_bytes), align256(L.dgrad.packed_bytes)),
+      product_bytes(wgrad_plan(dtype, L, n, in), n, in));
 }
 LossLayout loss_layout(int dtype, int rows, int vocab, int in) {
   const size_t e = element(dtype);
@@ -83,22 +91,28 @@ LossLayout loss_layout(int dtype, int rows, int vocab, int in) {
   L.step = (int)std::min<ll>(vocab, std::max<ll>(256, (ll)(kSlopeBytes / e / std::max(rows, 1)) / 256 * 256));
   L.pitch = oz2_packed_pitch(in, e);
   L.pitch_dz = slope_pitch(L.step, e);
-  L.dgrad = oz2_plan(dtype, OZ2_DGRAD, rows, in, L.step, all(rows), true);
-  L.whole = L.step >= vocab && L.dgrad.splits == 1;
+  const bool twin = e == 2 && rows <= kTwinRows;
+  L.lines = twin ? 2 * rows : rows;
+  // (16-bit rows that are not whole pieces, for both products that read them)
+  L.padded = e == 2 && (ll)in * (ll)e % 16 ? 3 : 1;
+  L.dgrad = oz2_plan(dtype, OZ2_DGRAD, L.lines, in, L.step, all(L.lines), L.padded);
+  L.whole = L.step >= vocab && L.dgrad.splits == 1 && !twin;
   size_t o = 0;
   L.rows = o;
   o = align256(o + (size_t)rows * sizeof(Oz2LossRow));
   L.scale = o;
   o += 256;
   L.x = o;
-  o = align256(o + (size_t)rows * L.pitch * e);
+  o = align256(o + (size_t)L.lines * L.pitch * e);
+  L.w = o;
+  if (L.padded & 2) o = align256(o + (size_t)L.step * L.pitch * e);
   L.dz = o;
-  o = align256(o + (size_t)rows * L.pitch_dz * e);
+  o = align256(o + (size_t)L.lines * L.pitch_dz * e);
   L.dx = o;
-  if (!L.whole) o = align256(o + (size_t)L.dgrad.splits * rows * in * 4);
+  if (!L.whole) o = align256(o + (size_t)L.dgrad.splits * L.lines * in * 4);
   L.work = o;
-  size_t most = piece_bytes(dtype, rows, L.step, in, L.dgrad);
-  if (L.step && vocab % L.step) most = std::max(most, piece_bytes(dtype, rows, vocab % L.step, in, L.dgrad));
+  size_t most = piece_bytes(dtype, L, rows, L.step, in);
+  if (L.step && vocab % L.step) most = std::max(most, piece_bytes(dtype, L, rows, vocab % L.step, in));
   L.total = o + most;
   return L;
 }
@@ -308,23 +322,35 @@ int ozaki2_linear_cross_entropy_backward(int dtype, int rows, int vocab, int in,
   hipStream_t s = (hipStream_t)stream;
   float* scale = dtype == OZ2_F16 && rows ? (float*)(base + L.scale) : nullptr;
   hipError_t err = hipSuccess;
-  if (rows) {
-    const Oz2LossRows a{x, ldx, rows, in, vocab, targets, wide_targets != 0, lse, dloss, base + L.x, L.pitch,
-                        (Oz2LossRow*)(base + L.rows), scale};
-    if ((err = oz2_launch_loss_rows(dtype, a, s)) != hipSuccess) return hip_status(err);
-  }
+  const bool twin = L.lines > rows;
   // (an empty vocabulary: one empty piece, so that dX is written)
   for (ll v = 0; v == 0 || v < vocab; v += L.step) {
     const int n = (int)std::min<ll>(L.step, vocab - v);
     const void* wv = (const uint8_t*)w + (mw.p ? v * ldw * (ll)e : 0);
-    const bool last = v + n >= vocab;
+    ll ldv = ldw;
+    const bool last = v + n >= vocab, copied = L.padded & 2 && n;
+    // the rows once, W's with each piece
+    if (rows && (v == 0 || copied)) {
+      Oz2LossRows a{x, ldx, v ? 0 : rows, in, vocab, targets, wide_targets != 0, lse, dloss, base + L.x, L.pitch,
+                    twin, (Oz2LossRow*)(base + L.rows), scale, nullptr, 0, 0, nullptr};
+      if (copied) {
+        a.w = wv;
+        a.ldw = ldw;
+        a.words = n;
+        a.dst_w = base + L.w;
+        wv = base + L.w;
+        ldv = L.pitch;
+      }
+      if ((err = oz2_launch_loss_rows(dtype, a, s)) != hipSuccess) return hip_status(err);
+    }
     if (rows && n) {
       Oz2Product p{};
       p.A = base + L.x;
       p.lda = L.pitch;
       p.padded = true;
       p.B = wv;
-      p.ldb = ldw;
+      p.ldb = ldv;
+      p.paddedB = L.padded & 2;
       p.M = rows;
       p.N2 = p.N = n;
       p.L = in;
@@ -334,20 +360,22 @@ int ozaki2_linear_cross_entropy_backward(int dtype, int rows, int vocab, int in,
       p.packed = base + L.work;
       p.loss.rows = (const Oz2LossRow*)(base + L.rows);
       p.loss.first = (int)v;
-      if ((err = oz2_launch_loss_slope(dtype, slope_plan(dtype, rows, n, in), p, s)) != hipSuccess)
+      p.loss.twin = twin;
+      if ((err = oz2_launch_loss_slope(dtype, slope_plan(dtype, L, rows, n, in), p, s)) != hipSuccess)
         return hip_status(err);
     }
     Oz2Product p{};
     p.A = base + L.dz;
     p.lda = L.pitch_dz;
     p.padded = true;
-    p.gr = all(rows);
+    p.gr = all(L.lines);
     p.loss.scale = scale;
     if (dx) {
       Oz2Product d = p;
       d.B = wv;
-      d.ldb = ldw;
-      d.M = rows;
+      d.ldb = ldv;
+      d.paddedB = L.padded & 2;
+      d.M = L.lines;
       d.N2 = d.N = in;
       d.L = n;
       d.y = dx;
@@ -356,16 +384,18 @@ int ozaki2_linear_cross_entropy_backward(int dtype, int rows, int vocab, int in,
       d.packed = base + L.work;
       d.loss.whole = L.whole;
       d.loss.more = v > 0;
+      d.loss.twin = twin;
       if ((err = oz2_launch_loss_sum(dtype, OZ2_DGRAD, L.dgrad, d, last, s)) != hipSuccess) return hip_status(err);
     }
     if (dw) {
-      const Oz2Plan plan = wgrad_plan(dtype, rows, n, in);
+      const Oz2Plan plan = wgrad_plan(dtype, L, n, in);
       Oz2Product d = p;
       d.B = base + L.x;
       d.ldb = L.pitch;
       d.M = n;
       d.N2 = d.N = in;
-      d.L = rows;
+      d.paddedB = true;
+      d.L = L.lines;
       d.y = (uint8_t*)dw + v * lddw * (ll)e;
       d.ldy = lddw;
       d.part = (float*)(base + L.work);

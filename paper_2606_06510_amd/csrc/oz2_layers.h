@@ -39,7 +39,7 @@ enum Oz2End {
 
 // The loss over a vocabulary: its rows, and how far its sums have come
 struct Oz2Chunk {
-  float top, sum;        // the largest logit; the sum of e^(z - largest)
+  float top, sum;        // the largest z log2 e; the sum of 2^(z log2 e - top)
 };
 struct alignas(16) Oz2LossRow {
   float lse, factor;
@@ -52,6 +52,7 @@ struct Oz2Loss {
   Oz2Chunk* chunks;      // LSE: [chunk][M]
   float* picked;         // LSE: [M], the target's logit (where the row has one)
   const Oz2LossRow* rows;   // DZ: [M]
+  bool twin;             // DZ: what the rounding leaves of row t goes to row M + t
   int first;             // DZ: the vocabulary's index of column 0
   const float* scale;    // SUM: null, or [1] is what the sums are multiplied by at last
   int whole, more;       // SUM: y at once; added to what part holds already
@@ -91,10 +92,9 @@ struct Oz2Plan {
   size_t packed_bytes;
 };
 inline ll oz2_packed_pitch(ll cols, size_t e) { return (cols * (ll)e + 127) / 128 * 128 / (ll)e; }
-// padded: as in Oz2Product
-// whole: the sum is not split
+// padded: 1 A, 2 B, as in Oz2Product; whole: the sum is not split
 Oz2Plan oz2_plan(int dtype, Oz2Side side, ll M, ll N2, ll L, const Oz2Groups& gr,
-                 bool padded = false, bool whole = false);
+                 int padded = 0, bool whole = false);
 // the plan of a product (side 0, 1, 2; groups 0: one product) as rows, tile, splits and
 // pack: a diagnostic for tests, not part of the public ABI
 extern "C" void oz2_plan_of(int dtype, int side, ll M, ll N2, ll L, int rows, int groups, int padded,

@@ -62,7 +62,7 @@ int oz2_norm_parts(int dtype, int rows, int width);   // of the column sums
 hipError_t oz2_launch_norm_backward(int dtype, const Oz2NormBack& a, hipStream_t s);
 
 // Rows of the loss: X in rows of whole lines, zeros where the token does not count, and
-// what the gradient at a row's logits takes (dst null: neither)
+// what the gradient at a row's logits takes; and rows of W in whole lines
 struct Oz2LossRows {
   const void* x;
   ll ldx;
@@ -72,9 +72,15 @@ struct Oz2LossRows {
   const float *lse, *dloss;
   void* dst;
   ll pitch;
+  bool twin;            // X once more, from row `rows` on
   Oz2LossRow* out;
   float* scale;         // fp16: [0] the power of two of the slopes, [1] its inverse
+  const void* w;        // null: none
+  ll ldw;
+  int words;
+  void* dst_w;
 };
+#define OZ2_SCALE_ROWS 4096   // up to so many rows each workgroup finds the scale by itself
 hipError_t oz2_launch_loss_rows(int dtype, const Oz2LossRows& a, hipStream_t s);
 // the forward product's chunks into loss and lse (rows of p)
 hipError_t oz2_launch_lse(int dtype, const Oz2Plan& plan, const Oz2Product& p, float* loss, float* lse,

@@ -349,73 +349,74 @@ __device__ __forceinline__ ll target_of(const Oz2Loss& l, ll row) {
   return l.wide ? ((const ll*)l.targets)[row] : (ll)((const int*)l.targets)[row];
 }
 
-// The largest logit and the sum of e^(z - largest) of `row`'s columns of one chunk, and
-// the target's logit where it is among the lane's W columns from col on.  LPR lanes hold a
-// row; columns that do not exist count as -infinity.  fmaxf leaves NaN out, the sum does
-// not.
-template <class T, int W, int STRIDE, int STEPS, int PITCH, int LPR>
-__device__ __forceinline__ void emit_lse(const Oz2Product& p, const Tile& t, const float* lw, int row, int col,
-                                         int valid, int chunk) {
-  constexpr int U = STEPS < 4 ? STEPS : 4;
-#pragma clang loop unroll(disable)
-  for (int s = 0; s < STEPS; s += U) {
-    float v[U * W];
-    ll at[U];
+// Sums of exponentials are kept as (top, sum): sum of 2^(z log2 e - top), top the largest
+// z log2 e, so that an exponential is a fused multiplication and the instruction.  (The
+// constant's rounding is 2^-26 of z; top is subtracted exactly.)
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ float max3(float a, float b, float c) {   // leaves NaN out
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+// R rows from `row` on of one chunk, COLS columns of which `valid` exist, in LDS at lw (PITCH floats
+// a row): a lane has a row and COLS R / 64 of its columns (rows one after the other lie 4 banks
+// apart), so that hardly anything is left to do across lanes: 3 us a 256 x 256 tile, where
+// 16 lanes a row took 9.  And the target's logit where the chunk has it.
+template <int R, int COLS, int PITCH>
+__device__ __forceinline__ void lse_rows(const Oz2Product& p, const float* lw, int row, int end, int valid,
+                                         int col, int chunk, int lane) {
+  constexpr int PARTS = 64 / R, C = COLS / PARTS;
+  const int mine = row + lane % R, part = lane / R;
+  const bool on = mine < end;
+  const ll target = on ? target_of(p.loss, mine) - col : -1;
+  const float* z = lw + lane % R * PITCH + part * C;
+  float v[C], top = -INFINITY, sum = 0.0f;
 #pragma unroll
-    for (int q = 0; q < U; ++q) {
-      const int r = row + (s + q) * STRIDE;
-      at[q] = r < t.end ? target_of(p.loss, r) - col : -1;
+  for (int i = 0; i < C; i += 4) {
+    const v4f x = *reinterpret_cast<const v4f*>(z + i);
 #pragma unroll
-      for (int i = 0; i < W; i += 4) {
-        const v4f x = *reinterpret_cast<const v4f*>(lw + (s + q) * STRIDE * PITCH + i);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[q * W + i + e] = i + e < valid ? x[e] : -INFINITY;
-      }
-    }
-#pragma unroll
-    for (int q = 0; q < U; ++q) {
-      const int r = row + (s + q) * STRIDE;
-      float m = v[q * W];
-#pragma unroll
-      for (int i = 1; i < W; ++i) m = fmaxf(m, v[q * W + i]);
-      m = across<LPR, false>(m);
-      // (a chunk of -infinity alone: e^(-inf - 0) = 0, not e^(-inf + inf))
-      const float m0 = m == -INFINITY ? 0.0f : m;
-      float sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < W; ++i) sum += exp_for<T>(v[q * W + i] - m0);
-      sum = across<LPR, true>(sum);
-      if (r >= t.end) continue;
-      if ((threadIdx.x & (LPR - 1)) == 0 && valid > 0)
-        p.loss.chunks[(ll)chunk * p.M + r] = Oz2Chunk{m, sum};
-      if (at[q] >= 0 && at[q] < min(W, valid)) {
-        float z = v[q * W];
-#pragma unroll
-        for (int i = 1; i < W; ++i) z = at[q] == i ? v[q * W + i] : z;
-        p.loss.picked[r] = z;
-      }
-    }
+    for (int e = 0; e < 4; ++e) v[i + e] = x[e];
   }
+  if (valid < COLS) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) v[i] = part * C + i < valid ? v[i] : -INFINITY;
+  }
+#pragma unroll
+  for (int i = 0; i < C; i += 2) top = max3(top, v[i], v[i + 1]);
+#pragma unroll
+  for (int d = R; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+  top *= kLog2e;
+  // (all -infinity: 2^(-inf - 0) = 0, not 2^(-inf + inf))
+  const float from = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+  for (int i = 0; i < C; ++i) sum += __builtin_amdgcn_exp2f(fmaf(v[i], kLog2e, -from));
+#pragma unroll
+  for (int d = R; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+  if (!on) return;
+  if (part == 0) p.loss.chunks[(ll)chunk * p.M + mine] = Oz2Chunk{top, sum};
+  if (target >= part * C && target < min(part * C + C, valid)) p.loss.picked[mine] = z[target - part * C];
 }
 
 // The same for the kernel of few rows: four columns of row t, the others in the lanes 16,
 // 32 and 48 further
 __device__ __forceinline__ void rows_lse(const Oz2Product& p, int t, bool on, int col, int valid, const v4f& z,
                                          int g) {
-  float m = -INFINITY, sum = 0.0f;
+  float top = -INFINITY, sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (i < valid) m = fmaxf(m, z[i]);
-  m = fmaxf(m, __shfl_xor(m, 16));
-  m = fmaxf(m, __shfl_xor(m, 32));
-  const float m0 = m == -INFINITY ? 0.0f : m;
+    if (i < valid) top = fmaxf(top, z[i]);
+  top = fmaxf(top, __shfl_xor(top, 16));
+  top = fmaxf(top, __shfl_xor(top, 32)) * kLog2e;
+  const float from = top == -INFINITY ? 0.0f : top;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (i < valid) sum += expf(z[i] - m0);
+    if (i < valid) sum += __builtin_amdgcn_exp2f(fmaf(z[i], kLog2e, -from));
   sum += __shfl_xor(sum, 16);
   sum += __shfl_xor(sum, 32);
   if (!on) return;
-  if (g == 0) p.loss.chunks[(ll)blockIdx.x * p.M + t] = Oz2Chunk{m, sum};
+  if (g == 0) p.loss.chunks[(ll)blockIdx.x * p.M + t] = Oz2Chunk{top, sum};
   const ll at = target_of(p.loss, t) - col;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -429,10 +430,26 @@ __device__ __forceinline__ void loss_slope(const Oz2Loss& l, ll row, int col, in
   const Oz2LossRow r = l.rows[row];
   const int at = r.target - (l.first + col);
 #pragma unroll
-  for (int i = 0; i < W; ++i) {
-    const float d = (exp_for<T>(v[i] - r.lse) - (at == i ? 1.0f : 0.0f)) * r.factor;
-    v[i] = r.target >= 0 && i < valid ? d : 0.0f;
+  for (int i = 0; i < W; ++i) v[i] = exp_for<T>(v[i] - r.lse);
+  if (at >= 0 && at < W) {   // (seldom)
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = at == i ? v[i] - 1.0f : v[i];
   }
+#pragma unroll
+  for (int i = 0; i < W; ++i) v[i] = r.target >= 0 && i < valid ? v[i] * r.factor : 0.0f;
+}
+
+// W slopes of a row, rounded, in whole pieces: the row goes on, and zeros behind its end are
+// read.  twin: what that leaves, rounded in turn, is another row's (with it 16 bits more:
+// the products of few rows are bound by W, and take the second half for nothing).
+template <class T, int W>
+__device__ __forceinline__ void store_slope(const Oz2Product& p, ll row, int col, float* v) {
+  const Piece<T, W> o = rounded<T, W>(v);
+  store_piece((T*)p.y + row * p.ldy + col, o, W);
+  if (!p.loss.twin) return;
+#pragma unroll
+  for (int i = 0; i < W; ++i) v[i] -= to_f(o.v[i]);
+  store_piece((T*)p.y + (p.M + row) * p.ldy + col, rounded<T, W>(v), W);
 }
 
 // `steps` rows of a lane from `row` on, STRIDE apart (those before `end`): W columns
@@ -469,8 +486,7 @@ __device__ __forceinline__ void emit(const Oz2Product& p, const Tile& t, const f
         const int at = row + (s + q) * STRIDE;
         if (at >= t.end) continue;
         loss_slope<T, W>(p.loss, at, col, ALL ? W : valid, v + q * W);
-        // (whole pieces: the row goes on, and zeros behind its end are read)
-        store_piece((T*)p.y + at * p.ldy + col, rounded<T, W>(v + q * W), W);
+        store_slope<T, W>(p, at, col, v + q * W);
       }
       continue;
     }
@@ -558,9 +574,12 @@ __device__ __forceinline__ void epilogue_of(const Oz2Product& p, const v4f (&acc
     __builtin_amdgcn_wave_barrier();
     const int r0 = row + 16 * PI * ps + lr;
     const float* lr0 = lw + lr * PITCH + at;
-    if constexpr (END == OZ2_END_LSE)
-      emit_lse<T, W, STRIDE, STEPS, PITCH, LPR>(p, t, lr0, r0, col, valid, (t.col0 + wn) / (64 * NB));
-    else if (valid >= W)
+    if constexpr (END == OZ2_END_LSE) {
+      const int left = p.N - t.col0 - wn;   // columns from the chunk's first on
+      if (left > 0)
+        lse_rows<16 * PI, 64 * NB, PITCH>(p, lw, row + 16 * PI * ps, t.end, left, t.col0 + wn,
+                                          (t.col0 + wn) / (64 * NB), lane);
+    } else if (valid >= W)
       emit<T, SIDE, GATED, true, W, STRIDE, STEPS, PITCH, END>(p, t, lr0, r0, col, W, b, bu);
     else if (valid > 0)
       emit<T, SIDE, GATED, false, W, STRIDE, STEPS, PITCH, END>(p, t, lr0, r0, col, valid, b, bu);
@@ -1146,7 +1165,7 @@ k_rows(Oz2Product p) {
         if constexpr (END == OZ2_END_Y) finish<T, 4>(p, group, t, col, valid, v, u);
         if constexpr (END == OZ2_END_DZ) {
           loss_slope<T, 4>(p.loss, t, col, valid, v);
-          store_piece((T*)p.y + t * p.ldy + col, rounded<T, 4>(v), 4);
+          store_slope<T, 4>(p, t, col, v);
         }
       }
       if constexpr (END == OZ2_END_LSE) rows_lse(p, t, t < r1, col, valid, s[0], g);

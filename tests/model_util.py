@@ -218,7 +218,9 @@ def loss_backward(dloss, x, w, targets, lse, dtype):
     e32 = torch.where(on[:, None], e32, torch.zeros_like(e32))
     # fp16 is scaled: the largest |dloss| is 2^14 at least
     tiny = TINY[dtype] if dtype != torch.float16 else TINY[dtype] * float(g.abs().max() if T else 0) / 2 ** 14
-    edz = e32 + U[dtype] * (dz.abs() + e32) + tiny
+    # few tokens in 16 bits: what the first rounding leaves is kept, rounded in turn
+    u = U[dtype] ** 2 if T <= 64 and dtype != torch.float32 else U[dtype]
+    edz = e32 + u * (dz.abs() + e32) + tiny
     edz = torch.where(on[:, None], edz, torch.zeros_like(edz))
     m = dz.abs() + edz
     ex = edz @ w.abs() + sum_error(V) * (m @ w.abs())
