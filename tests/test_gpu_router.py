@@ -81,6 +81,10 @@ def test_equal_values_go_to_the_lowest_index(E):
         check_route(l, None, 2, score, 2, 1, 1)
         check_route(torch.zeros_like(l), None, 3, score, 2, 1, 2)
         check_route(torch.zeros_like(l), bias, 3, score, 2, 1, 2)
+        # more groups than a token has lanes, all of one value, and few values
+        check_route(torch.zeros_like(l), bias * 0, 3, score, E // 2, 3, 2)
+        check_route(l, bias, 3, score, E // 2, 3, 2)
+        check_route(l, bias, 3, score, E // 2, 3, 1)
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
