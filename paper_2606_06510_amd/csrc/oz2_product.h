@@ -423,12 +423,11 @@ __device__ __forceinline__ void rows_lse(const Oz2Product& p, int t, bool on, in
     if (i < valid && at == i) p.loss.picked[t] = z[i];
 }
 
-// The gradient at W logits of a row, from its logits: (e^(z - lse) - [target]) times the
-// row's factor; 0 where the row does not count, and behind the row's end
+// The gradient at W logits of a row (col: of the vocabulary), from its logits: (e^(z - lse) -
+// [target]) times the row's factor; 0 where the row does not count, and behind the row's end
 template <class T, int W>
-__device__ __forceinline__ void loss_slope(const Oz2Loss& l, ll row, int col, int valid, float* v) {
-  const Oz2LossRow r = l.rows[row];
-  const int at = r.target - (l.first + col);
+__device__ __forceinline__ void loss_slope(const Oz2LossRow& r, int col, int valid, float* v) {
+  const int at = r.target - col;
 #pragma unroll
   for (int i = 0; i < W; ++i) v[i] = exp_for<T>(v[i] - r.lse);
   if (at >= 0 && at < W) {   // (seldom)
@@ -456,7 +455,7 @@ __device__ __forceinline__ void store_slope(const Oz2Product& p, ll row, int col
 // from col on, read from lw (PITCH floats a row), U rows in flight.  y may be res.
 template <class T, Oz2Side SIDE, bool GATED, bool ALL, int W, int STRIDE, int STEPS, int PITCH, Oz2End END>
 __device__ __forceinline__ void emit(const Oz2Product& p, const Tile& t, const float* lw, int row, int col,
-                                     int valid, const float* b, const float* bu) {
+                                     int valid, const float* b, const float* bu, int behind) {
   constexpr int U = STEPS < 4 ? STEPS : 4;
 #pragma clang loop unroll(disable)
   for (int s = 0; s < STEPS; s += U) {
@@ -485,7 +484,11 @@ __device__ __forceinline__ void emit(const Oz2Product& p, const Tile& t, const f
       for (int q = 0; q < U; ++q) {
         const int at = row + (s + q) * STRIDE;
         if (at >= t.end) continue;
-        loss_slope<T, W>(p.loss, at, col, ALL ? W : valid, v + q * W);
+        // (what the row takes lies behind its sums in LDS)
+        const float* info = lw + (s + q) * STRIDE * PITCH + behind;
+        const v4f r = *reinterpret_cast<const v4f*>(info);
+        loss_slope<T, W>(Oz2LossRow{r[0], r[1], __float_as_int(r[2]), 0}, p.loss.first + col, ALL ? W : valid,
+                         v + q * W);
         store_slope<T, W>(p, at, col, v + q * W);
       }
       continue;
@@ -558,6 +561,13 @@ __device__ __forceinline__ void epilogue_of(const Oz2Product& p, const v4f (&acc
     add_to<T, W, false>(b, bp, valid);
     if (GATED) add_to<T, W, false>(bu, bp + p.N, valid);
   }
+  // of the rows of each pass: loaded before any is waited for
+  v4f info[END == OZ2_END_DZ ? MI / PI : 1];
+  if constexpr (END == OZ2_END_DZ) {
+#pragma unroll
+    for (int k = 0; k < MI / PI; ++k)
+      info[k] = reinterpret_cast<const v4f*>(p.loss.rows)[min(row + 16 * PI * k + lane % (16 * PI), t.end - 1)];
+  }
   float* lq = lw + (lane & 15) * PITCH + 4 * (lane >> 4);
 #pragma clang loop unroll(disable)
   for (int ps = 0; ps < MI / PI; ++ps) {
@@ -569,6 +579,9 @@ __device__ __forceinline__ void epilogue_of(const Oz2Product& p, const v4f (&acc
 #pragma unroll
           for (int j = 0; j < 4 * NB; ++j)
             *reinterpret_cast<v4f*>(lq + 16 * i * PITCH + 16 * j) = acc[j][k * PI + i];
+        if constexpr (END == OZ2_END_DZ) {
+          if (lane < 16 * PI) *reinterpret_cast<v4f*>(lw + lane * PITCH + 64 * NB) = info[k];
+        }
       }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -580,9 +593,9 @@ __device__ __forceinline__ void epilogue_of(const Oz2Product& p, const v4f (&acc
         lse_rows<16 * PI, 64 * NB, PITCH>(p, lw, row + 16 * PI * ps, t.end, left, t.col0 + wn,
                                           (t.col0 + wn) / (64 * NB), lane);
     } else if (valid >= W)
-      emit<T, SIDE, GATED, true, W, STRIDE, STEPS, PITCH, END>(p, t, lr0, r0, col, W, b, bu);
+      emit<T, SIDE, GATED, true, W, STRIDE, STEPS, PITCH, END>(p, t, lr0, r0, col, W, b, bu, 64 * NB - at);
     else if (valid > 0)
-      emit<T, SIDE, GATED, false, W, STRIDE, STEPS, PITCH, END>(p, t, lr0, r0, col, valid, b, bu);
+      emit<T, SIDE, GATED, false, W, STRIDE, STEPS, PITCH, END>(p, t, lr0, r0, col, valid, b, bu, 64 * NB - at);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
@@ -1164,7 +1177,7 @@ k_rows(Oz2Product p) {
         }
         if constexpr (END == OZ2_END_Y) finish<T, 4>(p, group, t, col, valid, v, u);
         if constexpr (END == OZ2_END_DZ) {
-          loss_slope<T, 4>(p.loss, t, col, valid, v);
+          loss_slope<T, 4>(p.loss.rows[t], p.loss.first + col, valid, v);
           store_slope<T, 4>(p, t, col, v);
         }
       }
