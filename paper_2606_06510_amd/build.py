@@ -1,4 +1,5 @@
-"""Build the gfx950 shared library libozaki2.so in-tree with hipcc.
+"""Build the gfx950 shared library libozaki2.so in-tree with hipcc, and beside it the Python
+extension of the small calls (host code against torch's headers).
 
 Every call recompiles all sources (objects go to _build/ beside the package).
 """
@@ -14,6 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(os.path.dirname(HERE), "_build")
 LIB = os.path.join(HERE, "libozaki2.so")
+FASTCALL = os.path.join(HERE, "_fastcall.so")
 SOURCES = ["api.cpp", "deconstruct.hip", "gemm.hip", "reconstruct.hip", "batched.hip", "gemv.hip",
            "fused.hip", "bytes.hip", "bytegemm.hip", "bytefused.hip", "probes.hip",
            "layers.cpp", "layer_gemm.hip", "experts.hip", "model.cpp", "router.hip", "norm.hip", "loss.hip"]
@@ -45,10 +47,31 @@ def _compile(src):
     return obj
 
 
+def _fastcall():
+    """_fastcall.so: nothing of it runs on the GPU, so the host's compiler is enough"""
+    import sysconfig
+    import torch
+    from torch.utils import cpp_extension
+    tmp = FASTCALL + ".tmp"
+    cmd = [shutil.which("g++") or hipcc(), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}"]
+    for d in [*cpp_extension.include_paths(), sysconfig.get_paths()["include"]]:
+        cmd += ["-isystem", d]
+    cmd += [os.path.join(CSRC, "fastcall.cpp"), "-o", tmp]
+    cmd += [f"-L{d}" for d in cpp_extension.library_paths()]
+    cmd += ["-ltorch_python", "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, FASTCALL)
+
+
 def build(verbose=False):
     os.makedirs(BUILD, exist_ok=True)
-    with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as ex:
+    with ThreadPoolExecutor(max_workers=min(8, len(SOURCES) + 1)) as ex:
+        fast = ex.submit(_fastcall)
         objs = list(ex.map(_compile, SOURCES))
+        fast.result()
     tmp = LIB + ".tmp"
     cmd = [hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -56,7 +79,7 @@ def build(verbose=False):
         raise RuntimeError(f"link failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
     if verbose:
-        print("built", LIB)
+        print("built", LIB, FASTCALL)
     return LIB
 
 

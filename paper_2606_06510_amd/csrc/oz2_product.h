@@ -1028,7 +1028,7 @@ __global__ void __launch_bounds__(256)
 k_join(Oz2Product p) {
   constexpr int W = 16 / sizeof(T);
   const int pieces = (p.N + W - 1) / W;
-  const ll id = (ll)blockIdx.x * 256 + threadIdx.x, row = id / pieces;
+  const ll id = (blockIdx.x + (ll)blockIdx.y * gridDim.x) * 256 + threadIdx.x, row = id / pieces;
   if (row >= p.M) return;
   const int col = (int)(id - row * pieces) * W, valid = p.N - col;
   float v[W], u[W];
@@ -1284,7 +1284,8 @@ template <class T>
 hipError_t launch_join(const Oz2Product& p, hipStream_t s) {
   constexpr int W = 16 / sizeof(T);
   const ll items = (ll)p.M * ((p.N + W - 1) / W);
-  hipLaunchKernelGGL(k_join<T>, dim3((unsigned)((items + 255) / 256)), dim3(256), 0, s, p);
+  const Oz2Grid g = oz2_grid((items + 255) / 256);
+  hipLaunchKernelGGL(k_join<T>, dim3(g.x, g.y), dim3(256), 0, s, p);
   return hipGetLastError();
 }
 

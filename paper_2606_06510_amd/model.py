@@ -10,6 +10,7 @@ call; autograd records none of these calls (each docstring names the gradient).
 """
 from __future__ import annotations
 
+import ctypes
 from functools import lru_cache
 
 from . import _lib, layers
@@ -36,8 +37,32 @@ def _range(name, value, lo, hi):
         raise ValueError(f"{name}: expected {lo} to {hi}, got {value}")
 
 
-# A small call is mostly the host's: what holds for nearly every tensor is asked first and
-# in few steps, and where it does not the checks that name the fault follow.
+# A small call is mostly the host's.  Its plain form (dense tensors, nothing given to write
+# into, the current device and stream) goes through the extension csrc/fastcall.cpp in one
+# step, which answers None to every other; there, what holds for nearly every tensor is asked
+# first and in few steps, and where it does not the checks that name the fault follow.
+
+_fast = None
+
+
+def _bind():
+    """The extension, with the library's entry points (built beside the library, and as needed
+    as it is)"""
+    global _fast
+    lib = _lib.load()
+    if layers._torch is None:
+        layers._init()
+    try:
+        from . import _fastcall
+    except ImportError as e:
+        raise RuntimeError(f"{_lib.HERE}/_fastcall.so is missing or cannot be loaded ({e}): build "
+                           "it with __graft_entry__.build()") from e
+    names = ("ozaki2_layer_norm", "ozaki2_expert_route", "ozaki2_expert_route_backward")
+    _fastcall.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names),
+                   layers._raw_stream, layers._current_device)
+    _fast = _fastcall
+    return _fast
+
 
 def _rows(name, t):
     """(type code, device, rows, columns, leading dimension) of a matrix"""
@@ -87,8 +112,13 @@ def expert_route(logits, top_k, bias=None, score="softmax", groups=1, top_groups
     An expert whose logit or bias is -inf is out.  Where fewer than top_k are left (all, in
     a row of padding), ids is -1, which drops the pair, and the weight 0.  NaN is larger than
     every number.  Not recorded by autograd: the gradient is expert_route_backward's."""
-    code, dev, T, E, ld = _experts(logits)
     kind = _score(score)
+    if stream is None:
+        done = (_fast or _bind()).expert_route(logits, top_k, bias, kind, groups, top_groups, group_best,
+                                               renormalize, scale)
+        if done is not None:
+            return done
+    code, dev, T, E, ld = _experts(logits)
     if groups != 1 or top_groups != 1:
         _range("groups", groups, 1, E)
         if E % groups:
@@ -116,8 +146,12 @@ def expert_route_backward(dweights, logits, ids, score="softmax", renormalize=Tr
     top_k], as expert_combine_backward gives them) and the ids that expert_route chose with the
     same score, renormalize and scale.  Choices of -1 take no part.  The bias has no
     gradient.  dlogits: an output to write into."""
-    code, dev, T, E, ld = _experts(logits)
     kind = _score(score)
+    if stream is None and dlogits is None:
+        done = (_fast or _bind()).expert_route_backward(dweights, logits, ids, kind, renormalize, scale)
+        if done is not None:
+            return done
+    code, dev, T, E, ld = _experts(logits)
     T0, k = _dim2("ids", ids)
     if T0 != T:
         raise ValueError(f"ids: expected {T} tokens, got {T0}")
@@ -144,6 +178,10 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, save_stats=False, out=None, 
     save_stats: returns (y, stats) with stats float32 [T, 2], each row's mean and 1 /
     sqrt(variance + eps), as layer_norm_backward takes them.  out may be x itself.  Not
     recorded by autograd: its gradients are layer_norm_backward's."""
+    if stream is None and out is None:
+        done = (_fast or _bind()).layer_norm(x, weight, bias, eps, bool(save_stats))
+        if done is not None:
+            return done
     code, dev, T, K, ldx = _rows("x", x)
     if not eps >= 0.0:
         raise ValueError(f"eps: expected a number of at least 0, got {eps}")

@@ -192,6 +192,36 @@ def test_streams():
                 assert all(torch.equal(a, b) for a, b in zip(o[k], eager[k])), k
 
 
+def test_short_path_gives_the_other_ones_bits():
+    """the extension's one step, and the path that a given stream takes; what both refuse"""
+    device()
+    m = oz()
+    here = torch.cuda.current_stream()
+    for dtype in (torch.bfloat16, torch.float16, torch.float32):
+        for T, E in ((1, 8), (70, 40), (0, 16)):
+            l, b = torch.randn((T, E), device="cuda").to(dtype), torch.randn(E, device="cuda")
+            for kw in (dict(), dict(bias=b, score="sigmoid", groups=4, top_groups=3, scale=2, renormalize=0)):
+                a, c = m.expert_route(l, 3, **kw), m.expert_route(l, 3, stream=here, **kw)
+                assert all(torch.equal(p, q) and p.dtype == q.dtype and p.shape == q.shape for p, q in zip(a, c))
+                kw = {k: v for k, v in kw.items() if k in ("score", "scale", "renormalize")}
+                dw = torch.randn((T, 3), device="cuda")
+                a, c = (m.expert_route_backward(dw, l, a[0], stream=s, **kw) for s in (None, here))
+                assert torch.equal(a, c) and a.dtype == dtype
+            for w in (None, l.new_ones(E)):
+                a, c = (m.layer_norm(l, w, w, save_stats=True, stream=s) for s in (None, here))
+                assert all(torch.equal(p, q) for p, q in zip(a, c))
+                assert torch.equal(m.layer_norm(l, w, w), a[0])
+    p = torch.nn.Parameter(torch.randn((5, 16), device="cuda"))
+    assert not m.layer_norm(p, p[0].detach()).requires_grad
+    l = torch.randn((6, 8), device="cuda")
+    for call in (lambda: m.layer_norm(l, l[0].half()), lambda: m.layer_norm(l, eps=-1.0), lambda: m.expert_route(l, 9),
+                 lambda: m.expert_route(l, 2, groups=3), lambda: m.expert_route(l, 2, bias=l[0].cpu()),
+                 lambda: m.expert_route_backward(l[:, :2].contiguous(), l, torch.zeros((5, 2), dtype=torch.int32,
+                                                                                       device="cuda"))):
+        with pytest.raises(ValueError):
+            call()
+
+
 def test_workspaces_of_the_caller():
     device()
     m = oz()

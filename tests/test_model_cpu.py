@@ -245,6 +245,31 @@ def test_no_tensor(wrong, no_device):
                 call()
 
 
+class Doubtful:
+    def __bool__(self):
+        raise ValueError("neither")
+
+
+def test_the_short_path_leaves_everything_else_to_the_other():
+    """tensors elsewhere, arguments of other types and numbers of arguments: None, and no exception"""
+    from paper_2606_06510_amd import model
+    f = model._bind()
+    x, ids, dw = torch.zeros(4, 8), torch.zeros(4, 2, dtype=torch.int32), torch.zeros(4, 2)
+    for wrong in (None, 3, "x", [1.0], np.zeros((4, 8), np.float32), x, x.to_sparse(), x.t(),
+                  torch.nn.Parameter(x), torch.zeros(4, 8, device="meta")):
+        assert f.layer_norm(wrong, None, None, 1e-5, False) is None
+        assert f.expert_route(wrong, 2, None, 0, 1, 1, 1, True, 1.0) is None
+        assert f.expert_route_backward(dw, wrong, ids, 0, True, 1.0) is None
+        assert f.expert_route_backward(wrong, x, ids, 0, True, 1.0) is None
+    assert f.layer_norm() is None and f.expert_route(x) is None and f.expert_route_backward() is None
+    assert f.layer_norm(x, None, None, "eps", False) is None
+    assert f.expert_route(x, 1 << 80, None, 0, 1, 1, 1, True, 1.0) is None
+    assert f.expert_route(x, 2, None, 0, 1, 1, 1, Doubtful(), 1.0) is None
+    assert f.expert_route(x, 2, None, 0, 1, 1, 1, True, 1 << 2000) is None
+    with pytest.raises(TypeError):
+        f.bind(1)
+
+
 # -------------------------------------------------- the plain forms agree with autograd
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
