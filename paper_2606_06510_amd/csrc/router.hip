@@ -1,7 +1,11 @@
 // The router: every token's experts and their weights from its logits, and the gradient.
 //
 // L lanes have a token, lane l of them its experts l V .. l V + V - 1, in registers; a wave has
-// 64 / L tokens.  Rows of logits are read once.
+// 64 / L tokens.  Rows of logits are read once, and the bytes are few (16384 tokens of 256
+// experts: 17 MB, 3 us): what bounds it is the search for the largest values, some 30
+// instructions a choice and token.  16384 tokens, 8 choices: of 256 experts by the logits'
+// order 10 us, by scores with a bias 19, in 8 groups 25; of 64 experts 5.9, 8.8 and 11.  (All
+// scores in 64 bits and a wave a token: 169 us in groups.)  Gradient, 16384 x 128 bf16: 7 us.
 #include <algorithm>
 
 #include "oz2_lanes.h"
@@ -280,10 +284,14 @@ struct Lds {
 };
 
 // Choices by scores (SCORED) or by the logits, whose order is that of scores without a bias.
-// Scores are compared as in 64 bits, but 64 bits are formed for few: 32 bits find those that
-// can be among the largest, within `near` of the last of them (A + 2^-23 |c|, the error of a
-// score and of its sum with the bias, twice).  Where that does not decide, too many are that
-// close or a group's value is, or there is a NaN or an infinity, all are formed.
+// Scores are compared as in 64 bits, for biased ones lie closer together than 32 bits tell, but
+// 64 bits are formed for few: 32 bits find those that can be among the largest, within `near`
+// of the last of them, and those are ranked.  near is twice the error of c = s + b: A of the score
+// (sigmoid: s (1 - s) (|l| 2^-24 + 2^-23) and two roundings, 3e-7 at most; softmax: of its
+// largest score, |x| e^x being below 0.37), and of the sum 2^-24 |c|.  Groups whose values are
+// that close are settled by the scores that can be their two largest.  Where none of that decides
+// (a NaN, an infinity, more than 64 so close), a token's scores are all formed, in LDS
+// and in loops: unrolled in registers they slowed down the rest (15 us to 35).
 template <class T, bool SCORED, int L, int V>
 __global__ void __launch_bounds__(NT, 4)
 k_route(Oz2Route a) {

@@ -78,9 +78,9 @@ def test_large_tiles(dtype, T, V, K):
 
 
 def pieces(T, V, K, dtype):
-    """words of a piece: 256 MiB of slopes"""
+    """words of a piece: 128 MiB of slopes"""
     e = 4 if dtype == "fp32" else 2
-    return min(V, max(256, (256 << 20) // e // T // 256 * 256))
+    return min(V, max(256, (128 << 20) // e // T // 256 * 256))
 
 
 @pytest.mark.parametrize("dtype,T,V,K", [("bf16", 9000, 40001, 72), ("fp16", 20000, 16000, 64),
