@@ -2,7 +2,7 @@
 // nearly every call passes, its outputs and the call, in one step from Python.  Anything else
 // (another layout, a stream or outputs that are given, an argument that is wrong) is answered
 // with None, or a status, and the binding's own path takes it, with the errors that name the
-// fault.  One token's layer norm through ctypes 7.4 us, of which its kernel 3.1, the launch 2.5.
+// fault.  One token's layer norm 4.7 us a call, through ctypes 7.4 (its kernel takes 3.1).
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -13,8 +13,14 @@ namespace {
 
 // set by bind()
 decltype(&ozaki2_layer_norm) norm;
+decltype(&ozaki2_layer_norm_backward) norm_backward;
+decltype(&ozaki2_layer_norm_backward_workspace_bytes) norm_backward_bytes;
 decltype(&ozaki2_expert_route) route;
 decltype(&ozaki2_expert_route_backward) route_backward;
+decltype(&ozaki2_linear_cross_entropy) loss;
+decltype(&ozaki2_linear_cross_entropy_workspace_bytes) loss_bytes;
+decltype(&ozaki2_linear_cross_entropy_backward) loss_backward;
+decltype(&ozaki2_linear_cross_entropy_backward_workspace_bytes) loss_backward_bytes;
 PyObject *raw_stream, *current_device;
 
 // a dense tensor on a GPU, and not of a class of its own
@@ -47,6 +53,21 @@ bool vector(PyObject* o, const at::Tensor& like, int64_t n, at::ScalarType type,
   p = t->const_data_ptr();
   return true;
 }
+
+// a plain matrix of this shape, of the type and on the device of `like`
+const at::Tensor* same(PyObject* o, const at::Tensor& like, int64_t rows, int64_t cols) {
+  const at::Tensor* t = plain(o);
+  return t && t->dim() == 2 && t->size(0) == rows && t->size(1) == cols && t->scalar_type() == like.scalar_type() &&
+                 t->device() == like.device()
+             ? t
+             : nullptr;
+}
+
+at::Tensor bytes(size_t n, const at::Tensor& like) {
+  return at::empty({(int64_t)n}, like.options().dtype(at::kByte));
+}
+void* at_or_null(at::Tensor& t) { return t.defined() ? t.mutable_data_ptr() : nullptr; }
+int64_t ld(int64_t cols) { return cols ? cols : 1; }
 
 // the tensor's device is the current one: its stream's handle
 bool here(const at::Tensor& t, void*& stream) {
@@ -89,16 +110,23 @@ PyObject* other_path() {
   Py_RETURN_NONE;
 }
 
-PyObject* pair(at::Tensor&& a, at::Tensor&& b) {
-  PyObject *x = THPVariable_Wrap(std::move(a)), *y = x ? THPVariable_Wrap(std::move(b)) : nullptr;
-  PyObject* r = y ? PyTuple_New(2) : nullptr;
-  if (!r) {
-    Py_XDECREF(x);
-    Py_XDECREF(y);
-    return nullptr;
+// a tuple of N tensors, None where there is none
+template <size_t N>
+PyObject* tuple(at::Tensor (&&t)[N]) {
+  PyObject* r = PyTuple_New(N);
+  for (size_t i = 0; r && i < N; ++i) {
+    PyObject* o;
+    if (t[i].defined()) {
+      o = THPVariable_Wrap(std::move(t[i]));
+    } else {
+      Py_INCREF(Py_None);
+      o = Py_None;
+    }
+    if (o)
+      PyTuple_SET_ITEM(r, i, o);
+    else
+      Py_CLEAR(r);
   }
-  PyTuple_SET_ITEM(r, 0, x);
-  PyTuple_SET_ITEM(r, 1, y);
   return r;
 }
 
@@ -124,7 +152,7 @@ PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) try {
   status = norm(code, (int)T, (int)K, px, K ? K : 1, w, b, eps, py, K ? K : 1, ps, stream);
   Py_END_ALLOW_THREADS
   if (status != 0) return other_path();
-  return save ? pair(std::move(y), std::move(stats)) : THPVariable_Wrap(std::move(y));
+  return save ? tuple<2>({std::move(y), std::move(stats)}) : THPVariable_Wrap(std::move(y));
 } catch (...) {
   return other_path();
 }
@@ -153,7 +181,7 @@ PyObject* expert_route(PyObject*, PyObject* const* a, Py_ssize_t n) try {
   status = route(code, (int)T, (int)E, k, pl, E, (const float*)bias, score, groups, top, best, renormalize, scale, pi,
                  pw, stream);
   Py_END_ALLOW_THREADS
-  return status != 0 ? other_path() : pair(std::move(ids), std::move(weights));
+  return status != 0 ? other_path() : tuple<2>({std::move(ids), std::move(weights)});
 } catch (...) {
   return other_path();
 }
@@ -189,14 +217,120 @@ PyObject* expert_route_backward(PyObject*, PyObject* const* a, Py_ssize_t n) try
   return other_path();
 }
 
-// bind(addresses of the three entry points, raw_stream, current_device)
+// layer_norm_backward(dy, x, stats, weight, residual, need_dx, need_dweight, need_dbias)
+PyObject* layer_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) try {
+  const at::Tensor* dy = n == 8 ? plain(a[0]) : nullptr;
+  if (!matrix(dy)) return other_path();
+  const int64_t T = dy->size(0), K = dy->size(1);
+  const at::Tensor *x = same(a[1], *dy, T, K), *stats = plain(a[2]), *res = nullptr;
+  const void* w;
+  bool need[3];
+  void* stream;
+  if (!x || !stats || stats->dim() != 2 || stats->size(0) != T || stats->size(1) != 2 ||
+      stats->scalar_type() != at::kFloat || stats->device() != dy->device() ||
+      !vector(a[3], *dy, K, dy->scalar_type(), w) || (a[4] != Py_None && !(res = same(a[4], *dy, T, K))) ||
+      !truth(a[5], need[0]) || !truth(a[6], need[1]) || !truth(a[7], need[2]) || !here(*dy, stream))
+    return other_path();
+  const int code = code_of(*dy);
+  const size_t bytes_needed = need[1] || need[2] ? norm_backward_bytes(code, (int)T, (int)K) : 0;
+  at::Tensor dx, dw, db, ws;
+  if (need[0]) dx = at::empty({T, K}, dy->options());
+  if (need[1]) dw = at::empty({K}, dy->options());
+  if (need[2]) db = at::empty({K}, dy->options());
+  if (bytes_needed) ws = bytes(bytes_needed, *dy);
+  const void *pd = dy->const_data_ptr(), *px = x->const_data_ptr(), *pr = res ? res->const_data_ptr() : nullptr;
+  const float* ps = (const float*)stats->const_data_ptr();
+  void *gx = at_or_null(dx), *gw = at_or_null(dw), *gb = at_or_null(db), *pw = at_or_null(ws);
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = norm_backward(code, (int)T, (int)K, pd, ld(K), px, ld(K), ps, w, pr, ld(K), gx, ld(K), gw, gb, pw,
+                         bytes_needed, stream);
+  Py_END_ALLOW_THREADS
+  return status != 0 ? other_path() : tuple<3>({std::move(dx), std::move(dw), std::move(db)});
+} catch (...) {
+  return other_path();
+}
+
+// x, w and targets of the loss
+struct LossArgs {
+  const at::Tensor *x, *w, *targets;
+  int64_t T, V, K;
+  int code, wide;
+  bool read(PyObject* ox, PyObject* ow, PyObject* ot) {
+    x = plain(ox);
+    w = plain(ow);
+    targets = plain(ot);
+    if (!matrix(x) || !matrix(w) || !targets) return false;
+    T = x->size(0);
+    K = x->size(1);
+    V = w->size(0);
+    code = code_of(*x);
+    wide = targets->scalar_type() == at::kLong;
+    return w->size(1) == K && w->scalar_type() == x->scalar_type() && w->device() == x->device() &&
+           targets->dim() == 1 && targets->size(0) == T && (wide || targets->scalar_type() == at::kInt) &&
+           targets->device() == x->device();
+  }
+};
+
+// linear_cross_entropy(x, w, targets)
+PyObject* linear_cross_entropy(PyObject*, PyObject* const* a, Py_ssize_t n) try {
+  LossArgs q;
+  void* stream;
+  if (n != 3 || !q.read(a[0], a[1], a[2]) || !here(*q.x, stream)) return other_path();
+  const int T = (int)q.T, V = (int)q.V, K = (int)q.K;
+  const size_t need = loss_bytes(q.code, T, V, K);
+  const auto f32 = q.x->options().dtype(at::kFloat);
+  at::Tensor l = at::empty({q.T}, f32), e = at::empty({q.T}, f32), ws;
+  if (need) ws = bytes(need, *q.x);
+  const void *px = q.x->const_data_ptr(), *pw = q.w->const_data_ptr(), *pt = q.targets->const_data_ptr();
+  float *pl = (float*)l.mutable_data_ptr(), *pe = (float*)e.mutable_data_ptr();
+  void* space = at_or_null(ws);
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = loss(q.code, T, V, K, px, ld(K), pw, ld(K), pt, q.wide, pl, pe, space, need, stream);
+  Py_END_ALLOW_THREADS
+  return status != 0 ? other_path() : tuple<2>({std::move(l), std::move(e)});
+} catch (...) {
+  return other_path();
+}
+
+// linear_cross_entropy_backward(dloss, x, w, targets, lse, need_dx, need_dw)
+PyObject* linear_cross_entropy_backward(PyObject*, PyObject* const* a, Py_ssize_t n) try {
+  LossArgs q;
+  void* stream;
+  const void *d, *e;
+  bool need_dx, need_dw;
+  if (n != 7 || !q.read(a[1], a[2], a[3]) || a[0] == Py_None || a[4] == Py_None ||
+      !vector(a[0], *q.x, q.T, at::kFloat, d) || !vector(a[4], *q.x, q.T, at::kFloat, e) || !truth(a[5], need_dx) ||
+      !truth(a[6], need_dw) || !here(*q.x, stream))
+    return other_path();
+  const int T = (int)q.T, V = (int)q.V, K = (int)q.K;
+  const size_t need = loss_backward_bytes(q.code, T, V, K);
+  at::Tensor dx, dw, ws;
+  if (need_dx) dx = at::empty({q.T, q.K}, q.x->options());
+  if (need_dw) dw = at::empty({q.V, q.K}, q.x->options());
+  if (need) ws = bytes(need, *q.x);
+  const void *px = q.x->const_data_ptr(), *pw = q.w->const_data_ptr(), *pt = q.targets->const_data_ptr();
+  void *gx = at_or_null(dx), *gw = at_or_null(dw), *space = at_or_null(ws);
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = loss_backward(q.code, T, V, K, (const float*)d, px, ld(K), pw, ld(K), pt, q.wide, (const float*)e, gx,
+                         ld(K), gw, ld(K), space, need, stream);
+  Py_END_ALLOW_THREADS
+  return status != 0 ? other_path() : tuple<2>({std::move(dx), std::move(dw)});
+} catch (...) {
+  return other_path();
+}
+
+// bind(addresses of the entry points, raw_stream, current_device)
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n != 5) {
-    PyErr_SetString(PyExc_TypeError, "bind takes 5 arguments");
+  constexpr int N = 9;
+  if (n != N + 2) {
+    PyErr_Format(PyExc_TypeError, "bind takes %d arguments", N + 2);
     return nullptr;
   }
-  void* p[3];
-  for (int i = 0; i < 3; ++i) {
+  void* p[N];
+  for (int i = 0; i < N; ++i) {
     p[i] = PyLong_AsVoidPtr(a[i]);
     if (!p[i]) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null entry point");
@@ -204,19 +338,25 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     }
   }
   norm = (decltype(norm))p[0];
-  route = (decltype(route))p[1];
-  route_backward = (decltype(route_backward))p[2];
-  Py_INCREF(a[3]);
-  Py_INCREF(a[4]);
-  raw_stream = a[3];
-  current_device = a[4];
+  norm_backward = (decltype(norm_backward))p[1];
+  norm_backward_bytes = (decltype(norm_backward_bytes))p[2];
+  route = (decltype(route))p[3];
+  route_backward = (decltype(route_backward))p[4];
+  loss = (decltype(loss))p[5];
+  loss_bytes = (decltype(loss_bytes))p[6];
+  loss_backward = (decltype(loss_backward))p[7];
+  loss_backward_bytes = (decltype(loss_backward_bytes))p[8];
+  Py_INCREF(a[N]);
+  Py_INCREF(a[N + 1]);
+  raw_stream = a[N];
+  current_device = a[N + 1];
   Py_RETURN_NONE;
 }
 
-PyMethodDef methods[] = {{"bind", (PyCFunction)(void*)bind, METH_FASTCALL, nullptr},
-                         {"layer_norm", (PyCFunction)(void*)layer_norm, METH_FASTCALL, nullptr},
-                         {"expert_route", (PyCFunction)(void*)expert_route, METH_FASTCALL, nullptr},
-                         {"expert_route_backward", (PyCFunction)(void*)expert_route_backward, METH_FASTCALL, nullptr},
+#define OZ2_METHOD(name) {#name, (PyCFunction)(void*)name, METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {OZ2_METHOD(bind), OZ2_METHOD(layer_norm), OZ2_METHOD(layer_norm_backward),
+                         OZ2_METHOD(expert_route), OZ2_METHOD(expert_route_backward),
+                         OZ2_METHOD(linear_cross_entropy), OZ2_METHOD(linear_cross_entropy_backward),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -57,8 +57,11 @@ def _bind():
     except ImportError as e:
         raise RuntimeError(f"{_lib.HERE}/_fastcall.so is missing or cannot be loaded ({e}): build "
                            "it with __graft_entry__.build()") from e
-    names = ("ozaki2_layer_norm", "ozaki2_expert_route", "ozaki2_expert_route_backward")
-    _fastcall.bind(*(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names),
+    names = ("layer_norm", "layer_norm_backward", "layer_norm_backward_workspace_bytes",
+             "expert_route", "expert_route_backward", "linear_cross_entropy",
+             "linear_cross_entropy_workspace_bytes", "linear_cross_entropy_backward",
+             "linear_cross_entropy_backward_workspace_bytes")
+    _fastcall.bind(*(ctypes.cast(getattr(lib, "ozaki2_" + n), ctypes.c_void_p).value for n in names),
                    layers._raw_stream, layers._current_device)
     _fast = _fastcall
     return _fast
@@ -207,6 +210,11 @@ def layer_norm_backward(dy, x, stats, weight=None, residual=None, need_dx=True, 
     """(dx, dweight, dbias) of ``layer_norm`` from dy [T, width] and the stats it saved;
     None for what is not needed.  residual [T, width], the gradient that flows past the norm, is
     added to dx (dx may be residual itself).  dx, dweight, dbias: outputs to write into."""
+    if stream is None and workspace is None and dx is None and dweight is None and dbias is None:
+        done = (_fast or _bind()).layer_norm_backward(dy, x, stats, weight, residual, need_dx,
+                                                      need_dweight, need_dbias)
+        if done is not None:
+            return done
     code, dev, T, K, lddy = _rows("dy", dy)
     ldx = _matrix("x", x, dy, (T, K))
     _same("stats", stats, dy, (T, 2), layers._torch.float32)
@@ -255,6 +263,10 @@ def linear_cross_entropy(x, w, targets, workspace=None, stream=None):
 
     The logits are kept in 32 bits in the product's epilogue and never stored.  Not recorded
     by autograd: its gradients are linear_cross_entropy_backward's."""
+    if stream is None and workspace is None:
+        done = (_fast or _bind()).linear_cross_entropy(x, w, targets)
+        if done is not None:
+            return done
     code, dev, T, K, ldx = _rows("x", x)
     V, _ = _dim2("w", w)
     ldw = _matrix("w", w, x, (V, K))
@@ -281,6 +293,11 @@ def linear_cross_entropy_backward(dloss, x, w, targets, lse, need_dx=True, need_
     The logits are computed again, a piece of the vocabulary at a time.  Their gradient is
     rounded to the tensors' dtype before the products, as every operand of theirs, in
     float16 times a power of two that keeps it in range."""
+    if stream is None and workspace is None and dx is None and dw is None:
+        done = (_fast or _bind()).linear_cross_entropy_backward(dloss, x, w, targets, lse, need_dx,
+                                                                need_dw)
+        if done is not None:
+            return done
     code, dev, T, K, ldx = _rows("x", x)
     V, _ = _dim2("w", w)
     ldw = _matrix("w", w, x, (V, K))

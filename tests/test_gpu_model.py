@@ -211,6 +211,17 @@ def test_short_path_gives_the_other_ones_bits():
                 a, c = (m.layer_norm(l, w, w, save_stats=True, stream=s) for s in (None, here))
                 assert all(torch.equal(p, q) for p, q in zip(a, c))
                 assert torch.equal(m.layer_norm(l, w, w), a[0])
+                for kw in (dict(weight=w), dict(residual=l, need_dbias=False), dict(need_dx=False, need_dweight=False)):
+                    p, q = (m.layer_norm_backward(a[0], l, a[1], stream=s, **kw) for s in (None, here))
+                    assert all((u is None and v is None) or torch.equal(u, v) for u, v in zip(p, q))
+            v, dl = torch.randn((50, E), device="cuda").to(dtype), torch.rand(T, device="cuda")
+            for t in (torch.randint(-1, 50, (T,), device="cuda"),
+                      torch.randint(-1, 50, (T,), device="cuda", dtype=torch.int32)):
+                a, c = (m.linear_cross_entropy(l, v, t, stream=s) for s in (None, here))
+                assert all(torch.equal(p, q) and p.shape == q.shape for p, q in zip(a, c))
+                for kw in (dict(), dict(need_dx=False), dict(need_dw=False)):
+                    p, q = (m.linear_cross_entropy_backward(dl, l, v, t, a[1], stream=s, **kw) for s in (None, here))
+                    assert all((x is None and y is None) or torch.equal(x, y) for x, y in zip(p, q))
     p = torch.nn.Parameter(torch.randn((5, 16), device="cuda"))
     assert not m.layer_norm(p, p[0].detach()).requires_grad
     l = torch.randn((6, 8), device="cuda")

@@ -261,6 +261,12 @@ def test_the_short_path_leaves_everything_else_to_the_other():
         assert f.expert_route(wrong, 2, None, 0, 1, 1, 1, True, 1.0) is None
         assert f.expert_route_backward(dw, wrong, ids, 0, True, 1.0) is None
         assert f.expert_route_backward(wrong, x, ids, 0, True, 1.0) is None
+        t = torch.zeros(4, dtype=torch.int64)
+        assert f.layer_norm_backward(wrong, x, dw, None, None, True, True, True) is None
+        assert f.linear_cross_entropy(x, wrong, t) is None
+        assert f.linear_cross_entropy_backward(x[0], x, wrong, t, x[0], True, True) is None
+    assert f.layer_norm_backward() is None and f.linear_cross_entropy() is None
+    assert f.linear_cross_entropy_backward(None) is None
     assert f.layer_norm() is None and f.expert_route(x) is None and f.expert_route_backward() is None
     assert f.layer_norm(x, None, None, "eps", False) is None
     assert f.expert_route(x, 1 << 80, None, 0, 1, 1, 1, True, 1.0) is None
