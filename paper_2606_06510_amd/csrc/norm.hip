@@ -6,7 +6,8 @@
 //
 // L lanes have a row, lane l its 16-byte pieces l, l + L, .., N of them at most.  As few lanes
 // as keep N small: more than four pieces a lane cost more in registers than the barrier of
-// several waves a row (4096 wide, forward: 64 lanes of 8 pieces 98 us, 256 of 2 46).
+// several waves a row (16384 x 4096 bf16, forward: 64 lanes of 8 pieces 99 us, 256 of 2 52; with
+// loads that wait for nothing 45).
 #include <algorithm>
 
 #include "oz2_lanes.h"
@@ -188,8 +189,7 @@ k_norm_long(Oz2Norm a) {
 // A workgroup takes G rows of every gridDim G, and keeps the column sums of its rows in
 // registers; they leave as one partial row each of dweight and dbias, which k_norm_join adds
 // up in order.  One read of dY and X serves all three gradients (dX and the column sums
-// apart: 483 us for 16384 x 4096 bf16, together 102).  Two rows of a group at a time took
-// longer (129 against 114), the loads in flight of other workgroups being enough.
+// apart: 483 us for 16384 x 4096 bf16, together 102).
 template <class T, int L, int N, int G, bool TINY = false>
 __global__ void __launch_bounds__(L* G)
 k_norm_backward(Oz2NormBack a) {

@@ -362,8 +362,8 @@ __device__ __forceinline__ float max3(float a, float b, float c) {   // leaves N
 
 // R rows from `row` on of one chunk, COLS columns of which `valid` exist, in LDS at lw (PITCH floats
 // a row): a lane has a row and COLS R / 64 of its columns (rows one after the other lie 4 banks
-// apart), so that hardly anything is left to do across lanes: 3 us a 256 x 256 tile, where
-// 16 lanes a row took 9.  And the target's logit where the chunk has it.
+// apart), so that hardly anything is left to do across lanes (instead of 16 lanes a row: 8192 x 131072
+// over 4096 bf16 6573 -> 6196 us, 777 x 32003 over 1024 85 -> 68).  And the target's logit where the chunk has it.
 template <int R, int COLS, int PITCH>
 __device__ __forceinline__ void lse_rows(const Oz2Product& p, const float* lw, int row, int end, int valid,
                                          int col, int chunk, int lane) {
