@@ -7,7 +7,8 @@
  *
  * The conventions of layers.h hold: row-major, one token per row; leading dimensions in
  * elements, any element-aligned pointer; DEVICE pointers that the caller owns; work is
- * enqueued on `stream`, nothing synchronises or is allocated, calls may be captured.
+ * enqueued on `stream`, nothing synchronises or is allocated, calls may be captured.  A
+ * workspace belongs to one call at a time: calls, or replays, that can run at once need one each.
  * Validation happens before any launch: OZ2_E_INVALID for sizes, types, leading dimensions, null pointers
  * and outputs or a workspace that overlap an input or another output, OZ2_E_WORKSPACE for a workspace
  * smaller than the _workspace_bytes function says or not 256-byte aligned.  Sums,
@@ -32,7 +33,9 @@ enum { OZ2_SCORE_SOFTMAX = 0, OZ2_SCORE_SIGMOID = 1 };
  * num_experts / groups; a group's value is the sum of its group_best (1 or 2) largest c, and only
  * experts of the top_groups largest groups can be chosen.
  *   ids [tokens][top_k]: the experts of largest c, descending; of equal ones the lower
- *     index comes first, among groups too.  c is compared as in 64 bits.
+ *     index comes first, among groups too.  c is compared as in 64 bits; without a bias, unless
+ *     group_best 2 compares groups by sums, by the logits, whose order it has: so also
+ *     where two scores are one number in 64 bits (sigmoid: logits beyond 37).
  *   weights [tokens][top_k]: scale s, or with renormalize scale s / (sum of the chosen s),
  *     which is formed from logarithms: scores too small for 32 bits still have weights.
  * An expert whose logit or bias is -infinity is out: it is never chosen, in groups too.

@@ -107,7 +107,8 @@ def expert_route(logits, top_k, bias=None, score="softmax", groups=1, top_groups
 
     An expert's score s is the softmax over all experts or the sigmoid of its logit; the
     experts of largest s + bias are chosen, largest first, of equal ones the lower index
-    (compared as in 64 bits).  bias [experts], float32, decides the choice alone.
+    (compared as in 64 bits; without a bias, unless groups are compared by sums of two, by the
+    logits, also where scores round to the same number).  bias [experts], float32, decides the choice alone.
     groups > 1: the experts are so many equal ranges, a group's value is the sum of its
     group_best (1 or 2) largest s + bias, and only the top_groups largest groups are chosen
     from.  The weights are scale * s, with renormalize scale * s / (the sum of the chosen s).

@@ -175,6 +175,28 @@ def test_scores_too_small_for_32_bits():
     assert abs(float(w.sum(1)[0]) - 1) < 1e-6 and float(w[0].min()) > 0.1
 
 
+@pytest.mark.parametrize("dtype", list(lu.DTYPES))
+@pytest.mark.parametrize("E,groups", [(8, 1), (8, 4), (96, 1), (96, 8), (300, 1), (600, 4)])
+def test_scores_that_are_one_number_in_64_bits(E, groups, dtype):
+    """sigmoid beyond 37 is 1, softmax 750 below the largest is 0: without a bias the logits
+    decide, and with one the lower index, for the sums are equal"""
+    l = torch.full((2, E), -2000.0)
+    l[0, 1], l[0, E // 2], l[0, E // 2 + 1] = 40.0, 44.0, 56.0
+    l[1, 0], l[1, 1], l[1, E // 2], l[1, E // 2 + 1] = 0.0, -900.0, -1000.0, -800.0
+    l = l.to(lu.DTYPES[dtype]).to(device())
+    kw = dict(groups=groups, top_groups=groups, group_best=1)
+    ids, _ = oz().expert_route(l, 3, score="sigmoid", **kw)
+    assert ids[0].tolist() == [E // 2 + 1, E // 2, 1]
+    ids, _ = oz().expert_route(l, 4, **kw)
+    assert ids[1].tolist() == [0, E // 2 + 1, 1, E // 2]
+    zero = torch.zeros(E, device=device())
+    ids, _ = oz().expert_route(l, 3, bias=zero, score="sigmoid", **kw)
+    assert ids[0].tolist() == [1, E // 2, E // 2 + 1]
+    ids, _ = oz().expert_route(l, 4, bias=zero, **kw)
+    # (every score but the first is 0: of all experts the lower index)
+    assert ids[1].tolist() == [0, 1, 2, 3]
+
+
 def test_strided_and_unaligned_rows():
     l, bias = make(50, 90, "fp16", 9)
     big = torch.full((50, 131), NAN, dtype=l.dtype, device=l.device)
