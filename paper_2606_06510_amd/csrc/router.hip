@@ -405,8 +405,8 @@ k_route(Oz2Route a) {
               key_of(value_of(x) + value_of(y), k);
               return k;
             });
-        // (sums of two)
-        if (!exact && after && value_of(least) - value_of(after) <= 3.0f * near)
+        // (sums of two; where both are beyond 32 bits their difference is no number)
+        if (!exact && after && !(value_of(least) - value_of(after) > 3.0f * near))
           exact = !settle_groups<L, V>(key, (uint32_t*)room, stays, E, a.groups, a.top_groups, a.group_best > 1, near,
                                        lane, score64);
       }
