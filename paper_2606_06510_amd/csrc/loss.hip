@@ -16,7 +16,7 @@ constexpr int JT = 256;
 // (top, sum) and another one's: the larger top, both sums as seen from it
 __device__ __forceinline__ void join(float& top, float& sum, float t, float s) {
   const float m = fmaxf(top, t), m0 = m == -INFINITY ? 0.0f : m;
-  sum = sum * __builtin_amdgcn_exp2f(top - m0) + s * __builtin_amdgcn_exp2f(t - m0);
+  sum = sum * __builtin_amdgcn_exp2f((top - m0) * kLog2e) + s * __builtin_amdgcn_exp2f((t - m0) * kLog2e);
   top = m;
 }
 
@@ -57,10 +57,11 @@ k_lse_join(Oz2Loss l, int rows, int vocab, int n, float* __restrict__ loss, floa
   }
   if (run || r >= rows) return;
   const ll t = target_of(l, r);
-  // (in 64 bits until the end: of a large lse and a target close to it little is left)
-  const double whole = (double)m * 0.69314718055994530942 + (double)logf(s);
-  lse[r] = (float)whole;
-  loss[r] = t >= 0 && t < vocab ? (float)(whole - (double)l.picked[r]) : 0.0f;
+  // (the target's logit from the largest first, in 64 bits: of a large lse and a target close to
+  // it little is left)
+  const double more = (double)logf(s);
+  lse[r] = (float)((double)m + more);
+  loss[r] = t >= 0 && t < vocab ? (float)((double)m - (double)l.picked[r] + more) : 0.0f;
 }
 
 // The exponent of the power of two that takes the largest |dloss| of the rows that count to

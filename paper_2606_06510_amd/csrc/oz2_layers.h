@@ -39,7 +39,7 @@ enum Oz2End {
 
 // The loss over a vocabulary: its rows, and how far its sums have come
 struct Oz2Chunk {
-  float top, sum;        // the largest z log2 e; the sum of 2^(z log2 e - top)
+  float top, sum;        // the largest z; the sum of e^(z - top)
 };
 struct alignas(16) Oz2LossRow {
   float lse, factor;

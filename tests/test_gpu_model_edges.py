@@ -1,11 +1,19 @@
 """The model operators at the ends of their range."""
+import math
+
 import pytest
 import torch
 
+from tests import layer_util as lu
 from tests.gpu_util import device
 from tests.test_gpu_router import check_route
 
 pytestmark = pytest.mark.gpu
+
+
+def oz():
+    import paper_2606_06510_amd
+    return paper_2606_06510_amd
 
 
 # ----------------------------------------------------------------- router
@@ -45,3 +53,44 @@ def test_finite_masks(mask, score):
         check_route(l, b, 8, score)
         check_route(l, b, 8, score, 8, 4, 2)
         check_route(l, b, 8, score, 8, 4, 1, renorm=False)
+
+
+# ------------------------------------------------------------------- loss
+
+def exact_logits(z, T, dtype, K=16):
+    """x and w whose logits are exactly the rows' z [V]: one product of 1 with z, zeros beside"""
+    dt = lu.DTYPES[dtype]
+    w = torch.zeros((z.numel(), K))
+    w[:, K // 2] = z
+    x = torch.zeros((T, K))
+    x[:, K // 2] = 1.0
+    assert torch.equal(w.to(dt).float(), w)
+    return x.to(dt).to(device()), w.to(dt).to(device())
+
+
+@pytest.mark.parametrize("dtype", list(lu.DTYPES))
+@pytest.mark.parametrize("T,V", [(1, 1), (3, 40), (30, 700), (150, 900), (2048, 8192)])
+def test_confident_tokens(T, V, dtype):
+    """One word, or two, far above all others: a loss of 0 or log 2, whatever the logit's size.
+
+    The sum of exponentials is 1 or 2, the others' share is below e^-40 V.  Off by: an
+    exponential 2^-23, one for a chunk and one for the join, the sum and the logarithm
+    2^-23 each, relative to a sum of 2 at most: 2^-20 in all, and the result's rounding."""
+    sizes = [20.0, 100.0, 300.0, 1000.0]
+    if dtype != "fp16":
+        sizes += [2.0 ** 17, 1.5 * 2.0 ** 24, 1.25 * 2.0 ** 29, 1.75 * 2.0 ** 30, 2.0 ** 40, 3.0 * 2.0 ** 126]
+    for size in sizes:
+        for top in (size, -size):
+            z = torch.full((V,), top - max(60.0, 2 * abs(top)) if abs(top) < 1e30 else -1.875 * 2.0 ** 127)
+            z = z.to(lu.DTYPES[dtype]).float()
+            z[V // 3] = top
+            x, w = exact_logits(z, T, dtype)
+            t = torch.full((T,), V // 3, device=device())
+            loss, lse = oz().linear_cross_entropy(x, w, t)
+            assert float(loss.abs().max()) <= 2.0 ** -20, (size, top, loss[0])
+            assert float((lse.double() - top).abs().max()) <= 2.0 ** -20 + 2.0 ** -24 * abs(top)
+            if V > 1:
+                z[V - 1] = top
+                x, w = exact_logits(z, T, dtype)
+                loss, lse = oz().linear_cross_entropy(x, w, t)
+                assert float((loss.double() - math.log(2)).abs().max()) <= 2.0 ** -20, (size, top, loss[0])
