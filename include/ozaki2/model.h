@@ -97,7 +97,7 @@ size_t ozaki2_linear_cross_entropy_workspace_bytes(int dtype, int rows, int voca
 /* The gradients from dloss (float [rows]) and the forward call's lse:
  *   dZ = (e^(Z - lse) - [target]) dloss, dX = dZ W, dW = dZ^T X.
  * The logits are computed again, a piece of the vocabulary at a time; dZ is rounded to dtype for
- * the products (fp16: times a power of two that keeps the largest dloss near 2^14, taken
+ * the products (fp16: times a power of two that keeps the largest finite dloss near 2^14, taken
  * back in 32 bits), and the pieces' shares of dX are added up in 32 bits.  Tokens that do not
  * count have a zero row of dX and no part in dW, whatever their rows of X, lse and dloss hold.
  * dx or dw may be null (not wanted). */

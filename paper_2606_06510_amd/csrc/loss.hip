@@ -64,23 +64,21 @@ k_lse_join(Oz2Loss l, int rows, int vocab, int n, float* __restrict__ loss, floa
   loss[r] = t >= 0 && t < vocab ? (float)((double)m - (double)l.picked[r] + more) : 0.0f;
 }
 
-// The exponent of the power of two that takes the largest |dloss| of the rows that count to
-// [2^14, 2^15), 0 where there is none or it is no number.  Every one of NT threads calls it.
+// The exponent of the power of two that takes the largest finite |dloss| of the rows that count
+// to [2^14, 2^15), 0 where there is none: a row whose dloss is infinite or no number has such
+// slopes with any factor, and the others' stay in range.  Every one of NT threads calls it.
 template <int NT>
 __device__ __forceinline__ int slope_exponent(const Oz2LossRows& a, float* red) {
   Oz2Loss l{};
   l.targets = a.targets;
   l.wide = a.wide;
   float m = 0.0f;
-  bool bad = false;
   for (ll r = threadIdx.x; r < a.rows; r += NT) {
     const ll t = target_of(l, r);
     if (t < 0 || t >= a.vocab) continue;
     const float g = fabsf(a.dloss[r]);
-    bad |= !(g < INFINITY);
-    m = fmaxf(m, g);
+    if (g < INFINITY) m = fmaxf(m, g);
   }
-  if (bad) m = INFINITY;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
@@ -88,7 +86,7 @@ __device__ __forceinline__ int slope_exponent(const Oz2LossRows& a, float* red) 
   m = red[0];
   for (int i = 1; i < NT / 64; ++i) m = fmaxf(m, red[i]);
   int e = 0;
-  if (m > 0.0f && m < INFINITY) {
+  if (m > 0.0f) {
     frexpf(m, &e);           // m in [2^(e - 1), 2^e)
     e = min(15 - e, 126);
   }

@@ -10,6 +10,8 @@ from tests.test_gpu_router import check_route
 
 pytestmark = pytest.mark.gpu
 
+INF, NAN = math.inf, math.nan
+
 
 def oz():
     import paper_2606_06510_amd
@@ -94,3 +96,31 @@ def test_confident_tokens(T, V, dtype):
                 x, w = exact_logits(z, T, dtype)
                 loss, lse = oz().linear_cross_entropy(x, w, t)
                 assert float((loss.double() - math.log(2)).abs().max()) <= 2.0 ** -20, (size, top, loss[0])
+
+
+@pytest.mark.parametrize("value", [INF, -INF, NAN])
+@pytest.mark.parametrize("T", [5, 40, 200, 4500])
+def test_gradients_beside_one_that_is_no_number(T, value):
+    """fp16: a counted token's dloss that is not finite leaves the others' rows of dX as they are.
+    (Slopes are near 1e-8, below fp16's least number: without their power of two all would be 0.)"""
+    g = torch.Generator().manual_seed(T)
+    V, K = 3000, 64
+    x = torch.randn((T, K), generator=g).half().to(device())
+    w = (torch.randn((V, K), generator=g) * 0.1).half().to(device())
+    t = torch.randint(0, V, (T,), generator=g).to(device())
+    t[::9] = -1
+    dl = ((0.5 + torch.rand((T,), generator=g)) * 1e-5).to(device())
+    r = 2
+    dl[r] = 4e-6                    # (not the largest, which gives the power of two)
+    _, lse = oz().linear_cross_entropy(x, w, t)
+    clean = oz().linear_cross_entropy_backward(dl, x, w, t, lse)
+    assert float(clean[0][1].abs().max()) > 0
+    d2 = dl.clone()
+    d2[r] = value
+    dx, dw = oz().linear_cross_entropy_backward(d2, x, w, t, lse)
+    keep = torch.arange(T, device=x.device) != r
+    assert torch.equal(dx[keep], clean[0][keep])
+    assert not torch.isfinite(dx[r]).any() and not torch.isfinite(dw).any()
+    only = torch.where(keep, torch.full_like(t, -1), t)      # the only one that counts
+    dx, dw = oz().linear_cross_entropy_backward(d2, x, w, only, lse)
+    assert (dx[keep] == 0).all() and not torch.isfinite(dx[r]).any()
