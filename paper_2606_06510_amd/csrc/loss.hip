@@ -13,9 +13,10 @@ namespace {
 
 constexpr int JT = 256;
 
-// (top, sum) and another one's: the larger top, both sums as seen from it
+// (top, sum) and another one's: the larger top, both sums as seen from it (from 0 where it is
+// infinite)
 __device__ __forceinline__ void join(float& top, float& sum, float t, float s) {
-  const float m = fmaxf(top, t), m0 = m == -INFINITY ? 0.0f : m;
+  const float m = fmaxf(top, t), m0 = fabsf(m) == INFINITY ? 0.0f : m;
   sum = sum * __builtin_amdgcn_exp2f((top - m0) * kLog2e) + s * __builtin_amdgcn_exp2f((t - m0) * kLog2e);
   top = m;
 }

@@ -388,8 +388,9 @@ __device__ __forceinline__ void lse_rows(const Oz2Product& p, const float* lw, i
   for (int i = 0; i < C; i += 2) top = max3(top, v[i], v[i + 1]);
 #pragma unroll
   for (int d = R; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-  // (all -infinity: 2^(-inf - 0) = 0, not 2^(-inf + inf))
-  const float from = top == -INFINITY ? 0.0f : top;
+  // (infinities as they are: 2^(-inf - 0) = 0 where all are -infinity, 2^(inf - 0) where one is
+  // infinite, not 2^(inf - inf))
+  const float from = fabsf(top) == INFINITY ? 0.0f : top;
   // from k is rounded, and what that leaves (64 at most) taken back from the sum: a
   // multiplication and addition in one for every column (a difference first: 0.7% of 8192 x 131072
   // over 4096 bf16, 6276 us beside 6230).  From 2^30 on two logits are equal or 64 apart at
@@ -415,7 +416,7 @@ __device__ __forceinline__ void rows_lse(const Oz2Product& p, int t, bool on, in
     if (i < valid) top = fmaxf(top, z[i]);
   top = fmaxf(top, __shfl_xor(top, 16));
   top = fmaxf(top, __shfl_xor(top, 32));
-  const float from = top == -INFINITY ? 0.0f : top;
+  const float from = fabsf(top) == INFINITY ? 0.0f : top;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (i < valid) sum += __builtin_amdgcn_exp2f((z[i] - from) * kLog2e);

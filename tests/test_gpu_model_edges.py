@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from tests import layer_util as lu
+from tests import model_util as mu
 from tests.gpu_util import device
 from tests.test_gpu_router import check_route
 
@@ -124,3 +125,38 @@ def test_gradients_beside_one_that_is_no_number(T, value):
     only = torch.where(keep, torch.full_like(t, -1), t)      # the only one that counts
     dx, dw = oz().linear_cross_entropy_backward(d2, x, w, only, lse)
     assert (dx[keep] == 0).all() and not torch.isfinite(dx[r]).any()
+
+
+@pytest.mark.parametrize("dtype", list(lu.DTYPES))
+@pytest.mark.parametrize("T", [2, 40, 150, 2048])
+def test_infinite_logits(T, dtype):
+    """lse = log sum e^z is infinite where a logit is, and the loss with it, but for a target
+    whose own logit is infinite (no number)"""
+    g = torch.Generator().manual_seed(T)
+    dt = lu.DTYPES[dtype]
+    V, K = 900 if T < 2048 else 8192, 64
+    x, w = torch.randn((T, K), generator=g), torch.randn((V, K), generator=g) * 0.2
+    x[:, 3] = x[:, 3].abs() + 0.5
+    x[T - 1, 3] *= -1.0            # the last row has the logit -infinity
+    t = torch.randint(0, V, (T,), generator=g)
+    bad = 450
+    t[t == bad] = 451
+    if T > 2:
+        t[1] = bad
+    x, w, t = x.to(dt).to(device()), w.to(dt).to(device()), t.to(device())
+    w[bad] = 0.0
+    w[bad, 3] = INF
+    clean = mu.loss(x[T - 1:], torch.cat([w[:bad], w[bad + 1:]]), t[T - 1:] - (t[T - 1:] > bad).long())
+    loss, lse = oz().linear_cross_entropy(x, w, t)
+    assert (lse[:T - 1] == INF).all()
+    hit = t[:T - 1] == bad
+    assert torch.isnan(loss[:T - 1][hit]).all() and (loss[:T - 1][~hit] == INF).all()
+    lu.check(lse[T - 1:], clean[1], clean[3], "lse")
+    lu.check(loss[T - 1:], clean[0], clean[2], "loss")
+    w[bad + 9] = w[bad]            # and in another chunk's sums, and NaN over all
+    w[7] = w[bad]
+    loss, lse = oz().linear_cross_entropy(x, w, t)
+    assert (lse[:T - 1] == INF).all()
+    w[8, 3] = NAN
+    loss, lse = oz().linear_cross_entropy(x, w, t)
+    assert torch.isnan(lse).all() and torch.isnan(loss).all()
