@@ -454,7 +454,10 @@ __device__ __forceinline__ void store_slope(const Oz2Product& p, ll row, int col
   store_piece((T*)p.y + row * p.ldy + col, o, W);
   if (!p.loss.twin) return;
 #pragma unroll
-  for (int i = 0; i < W; ++i) v[i] -= to_f(o.v[i]);
+  for (int i = 0; i < W; ++i) {
+    const float f = to_f(o.v[i]);
+    v[i] = fabsf(f) == INFINITY ? 0.0f : v[i] - f;   // (of an infinity nothing, not inf - inf)
+  }
   store_piece((T*)p.y + (p.M + row) * p.ldy + col, rounded<T, W>(v), W);
 }
 

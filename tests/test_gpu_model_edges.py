@@ -160,3 +160,26 @@ def test_infinite_logits(T, dtype):
     w[8, 3] = NAN
     loss, lse = oz().linear_cross_entropy(x, w, t)
     assert torch.isnan(lse).all() and torch.isnan(loss).all()
+
+
+@pytest.mark.parametrize("dtype", list(lu.DTYPES))
+@pytest.mark.parametrize("T", [1, 3, 64, 65, 300])
+def test_infinite_gradients(T, dtype):
+    """an infinite dloss: the slopes are infinities of both signs, and so are the sums where
+    none meets another sign's, or a zero"""
+    dt, K = lu.DTYPES[dtype], 24
+    g = torch.Generator().manual_seed(T)
+    x = (torch.rand((T, K), generator=g) * 0.2 + 0.1).to(dt).to(device())
+    w = torch.stack([torch.full((K,), 0.25), torch.full((K,), -0.5)]).to(dt).to(device())
+    t = torch.ones(T, dtype=torch.int64, device=device())
+    dl = torch.full((T,), 1e-3, device=device())
+    _, lse = oz().linear_cross_entropy(x, w, t)
+    clean = oz().linear_cross_entropy_backward(dl, x, w, t, lse)
+    for sign in (1.0, -1.0):
+        dl[0] = sign * INF
+        dx, dw = oz().linear_cross_entropy_backward(dl, x, w, t, lse)
+        # dz = (p, p' - 1) dloss = (+, -) infinity; dX = dz W, dW = dz^T x
+        assert (dx[0] == sign * INF).all()
+        assert (dw[0] == sign * INF).all() and (dw[1] == -sign * INF).all()
+        if dtype != "fp16":        # (fp16: the power of two is that of the finite ones)
+            assert torch.equal(dx[1:], clean[0][1:])
