@@ -65,7 +65,8 @@ int ozaki2_expert_route_backward(int dtype, int tokens, int num_experts, int top
 /* Y = (X - mean) rstd weight + bias for X and Y (rows x width), mean and variance of each
  * row (the variance about the mean, over width), rstd = 1 / sqrt(variance + eps); weight and bias
  * (width, type dtype) may be null.  stats (float [rows][2], may be null) receives mean and
- * rstd.  Y may be X itself (same pointer and leading dimension). */
+ * rstd.  Y may be X itself (same pointer and leading dimension).  width 0: nothing is
+ * written, stats neither. */
 int ozaki2_layer_norm(int dtype, int rows, int width, const void* x, long long ldx,
                       const void* weight, const void* bias, float eps, void* y, long long ldy,
                       float* stats, void* stream);

@@ -141,6 +141,7 @@ PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) try {
   if (!vector(a[1], *x, K, x->scalar_type(), w) || !vector(a[2], *x, K, x->scalar_type(), b) || !here(*x, stream))
     return other_path();
   const bool save = a[4] == Py_True;
+  if (save && K == 0) return other_path();   // (statistics of nothing)
   at::Tensor y = at::empty({T, K}, x->options()), stats;
   if (save) stats = at::empty({T, 2}, x->options().dtype(at::kFloat));
   const void* px = x->const_data_ptr();

@@ -11,6 +11,7 @@ call; autograd records none of these calls (each docstring names the gradient).
 from __future__ import annotations
 
 import ctypes
+import math
 from functools import lru_cache
 
 from . import _lib, layers
@@ -180,7 +181,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, save_stats=False, out=None, 
     weight and bias [width].
 
     save_stats: returns (y, stats) with stats float32 [T, 2], each row's mean and 1 /
-    sqrt(variance + eps), as layer_norm_backward takes them.  out may be x itself.  Not
+    sqrt(variance + eps), as layer_norm_backward takes them (NaN of rows of no width).  out may be x itself.  Not
     recorded by autograd: its gradients are layer_norm_backward's."""
     if stream is None and out is None:
         done = (_fast or _bind()).layer_norm(x, weight, bias, eps, bool(save_stats))
@@ -199,6 +200,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, save_stats=False, out=None, 
     def call(s):
         y = torch.empty(T, K, dtype=x.dtype, device=dev) if out is None else out
         stats = torch.empty(T, 2, dtype=torch.float32, device=dev) if save_stats else None
+        if save_stats and K == 0:
+            stats.fill_(math.nan)   # 0 / 0: the library writes nothing where there is no width
         _call("ozaki2_layer_norm", code, T, K, x.data_ptr(), ldx, _p(weight), _p(bias), eps,
               y.data_ptr(), ldy, _p(stats), s)
         return (y, stats) if save_stats else y

@@ -183,3 +183,19 @@ def test_infinite_gradients(T, dtype):
         assert (dw[0] == sign * INF).all() and (dw[1] == -sign * INF).all()
         if dtype != "fp16":        # (fp16: the power of two is that of the finite ones)
             assert torch.equal(dx[1:], clean[0][1:])
+
+
+# ------------------------------------------------------------------- norm
+
+def test_rows_of_no_width():
+    """the mean and variance of nothing are 0 / 0"""
+    for stream in (None, torch.cuda.current_stream()):
+        for dtype in lu.DTYPES.values():
+            x = torch.ones((6, 8), dtype=dtype, device=device())[:, :0]
+            torch.full((4096,), 7.0, device=device())       # (freed memory that holds numbers)
+            y, stats = oz().layer_norm(x, save_stats=True, stream=stream)
+            assert y.shape == (6, 0) and stats.shape == (6, 2) and torch.isnan(stats).all()
+            got = oz().layer_norm_backward(x, x, stats, stream=stream)
+            assert got[0].shape == (6, 0) and got[1].shape == got[2].shape == (0,)
+            y, stats = oz().layer_norm(x[:0], save_stats=True, stream=stream)
+            assert stats.shape == (0, 2)
