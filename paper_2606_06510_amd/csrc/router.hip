@@ -630,22 +630,21 @@ k_route_backward(Oz2RouteBack a) {
 
 // f(lanes a token, experts a lane) as types.  The fewest lanes that keep a lane's experts in
 // registers: 16 experts and their scores do not fit beside what scores take
-template <class F>
-hipError_t for_experts(int E, bool scored, F f) {
+template <bool SCORED, class F>
+hipError_t for_experts(int E, F f) {
   using std::integral_constant;
   if (E <= 16) return f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
   if (E <= 32) return f(integral_constant<int, 16>{}, integral_constant<int, 2>{});
   if (E <= 64) return f(integral_constant<int, 16>{}, integral_constant<int, 4>{});
   if (E <= 128) return f(integral_constant<int, 16>{}, integral_constant<int, 8>{});
-  if (E <= 256 && !scored) return f(integral_constant<int, 16>{}, integral_constant<int, 16>{});
-  if (E <= 256) return f(integral_constant<int, 32>{}, integral_constant<int, 8>{});
+  if (E <= 256) return f(integral_constant<int, SCORED ? 32 : 16>{}, integral_constant<int, SCORED ? 8 : 16>{});
   if (E <= 512) return f(integral_constant<int, 64>{}, integral_constant<int, 8>{});
   return f(integral_constant<int, 64>{}, integral_constant<int, 16>{});
 }
 
 template <class T, bool SCORED>
 hipError_t launch_route(const Oz2Route& a, hipStream_t s) {
-  return for_experts(a.experts, SCORED, [&](auto lanes, auto each) {
+  return for_experts<SCORED>(a.experts, [&](auto lanes, auto each) {
     constexpr int L = decltype(lanes)::value, V = decltype(each)::value, TOKENS = NT / L;
     hipError_t e = hipSuccess;
     // (launches of no more than a grid's workgroups)
@@ -671,7 +670,7 @@ hipError_t oz2_launch_route(int dtype, const Oz2Route& a, hipStream_t s) {
 }
 
 hipError_t oz2_launch_route_backward(int dtype, const Oz2RouteBack& a, hipStream_t s) {
-  OZ2_TYPED(dtype, return for_experts(a.experts, false, [&](auto lanes, auto each) {
+  OZ2_TYPED(dtype, return for_experts<false>(a.experts, [&](auto lanes, auto each) {
               constexpr int L = decltype(lanes)::value, V = decltype(each)::value, TOKENS = NT / L;
               const dim3 grid((unsigned)std::min<ll>(ROW_BLOCKS, ((ll)a.tokens + TOKENS - 1) / TOKENS));
               hipLaunchKernelGGL((k_route_backward<T, L, V>), grid, dim3(NT), 0, s, a);
