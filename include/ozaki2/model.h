@@ -38,7 +38,9 @@ enum { OZ2_SCORE_SOFTMAX = 0, OZ2_SCORE_SIGMOID = 1 };
  *     where two scores are one number in 64 bits (sigmoid: logits beyond 37).
  *   weights [tokens][top_k]: scale s, or with renormalize scale s / (sum of the chosen s),
  *     which is formed from logarithms: scores too small for 32 bits still have weights.
- * An expert whose logit or bias is -infinity is out: it is never chosen, in groups too.
+ * An expert whose logit or bias is -infinity is out: it is never chosen, in groups too.  (Masks
+ * are better -infinity than a large finite bias: what 32-bit scores may be off grows with the
+ * largest |c|, and beside -1e9 all of a token's are formed in 64.)
  * Where none is left (fewer experts than top_k; a padding row of -infinity) the id is -1,
  * which ozaki2_expert_sort drops, and the weight 0.  A NaN is larger than every number:
  * it is chosen, and shows in the weights; with softmax a NaN or +infinity makes all of the
@@ -99,7 +101,9 @@ size_t ozaki2_linear_cross_entropy_workspace_bytes(int dtype, int rows, int voca
  *   dZ = (e^(Z - lse) - [target]) dloss, dX = dZ W, dW = dZ^T X.
  * The logits are computed again, a piece of the vocabulary at a time; dZ is rounded to dtype for
  * the products (fp16: times a power of two that keeps the largest finite dloss near 2^14, taken
- * back in 32 bits), and the pieces' shares of dX are added up in 32 bits.  Tokens that do not
+ * back in 32 bits; of up to 64 rows in 16 bits what the rounding leaves is added, rounded in turn),
+ * and the pieces' shares of dX are added up in 32 bits.  A caller that needs dZ in 32 bits for
+ * more rows passes X and W in OZ2_F32.  Tokens that do not
  * count have a zero row of dX and no part in dW, whatever their rows of X, lse and dloss hold.
  * dx or dw may be null (not wanted). */
 int ozaki2_linear_cross_entropy_backward(int dtype, int rows, int vocab, int in,

@@ -2,9 +2,11 @@
 // the gradients' sums (oz2_product.h), and the rows beside them.  With z = x W^T,
 //   lse = log sum e^z, loss = lse - z[target], dz = (e^(z - lse) - [target]) dloss,
 //   dx = dz W, dW = dz^T x.
-// The products are all of it: 8192 x 131072 over 4096 bf16 6.2-6.4 ms (1.37-1.42 PFLOP/s, the
-// library's rate for a product alone), 4096 x 65536 over 4096 and both gradients 4.5-5.0 ms
-// (three such products, a quarter of the vocabulary 442, 428 and 444 us).
+// The products are all of it: 8192 x 131072 over 4096 bf16 6.2-6.4 ms by card (1.37-1.42 PFLOP/s,
+// the library's rate for a product alone), 4096 x 65536 over 4096 and both gradients 4.5-5.0 ms.
+// (Under the profiler with pauses between, the first takes 6.3-6.6 ms and of the second, a quarter
+// of the vocabulary each, the slopes 414-442 us, dX 389-428 and dW 414-447.)  fp32: 2048 x 32768
+// over 2048 1.97 ms (140 TFLOP/s), its gradients 6.2 (133).
 #include "oz2_product.h"
 
 #include "oz2_model.h"

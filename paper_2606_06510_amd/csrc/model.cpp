@@ -60,14 +60,19 @@ LseLayout lse_layout(int dtype, int rows, int vocab, int in) {
 // The gradients of the loss, `step` words of the vocabulary at a time: so many bytes of slopes,
 // half of the memory-side cache, which holds them for the products that read them.  4096 x 65536
 // over 4096 bf16 and 8192 x 131072 over 1024: 64 MiB 4498 and 6607 us, 128 4458 and 5859, 256 4610
-// and 6266, 1 GiB 4603 and 6671.
+// and 6266, 1 GiB 4603 and 6671.  Longer batches were not measured: pieces get shorter, and each
+// reads and writes all of dX's 32-bit sums (16384 tokens of 131072 words over 4096: 32 pieces, 17
+// GB; 65536 tokens: 128, 275 GB).  Nor does a piece of few tokens leave W in the cache for dX: it is
+// read twice from memory.
 constexpr size_t kSlopeBytes = 128u << 20;
 
 // Up to so many tokens the slopes are kept in two 16-bit parts, for the products are bound by W
 // there (65536 x 4096 bf16, all gradients: 16 tokens 389 us instead of 382, 64 tokens 419 instead of
 // 399; 100 tokens 508 instead of 408).  Of few tokens one rounding is that of all of dW:
-// relatively 2^-8 at most, where it is 0.0017 on average.  With more tokens the gradients' error in
-// bf16 is 0.0023 on average, of which their own rounding is 0.0017.
+// relatively 2^-8 at most, where it is 0.0017 on average.  With more tokens the gradients' error
+// (8192 words over 1024, its norm by theirs) is that of two roundings: bf16 0.0020 of 100 and 0.0025
+// of 777 tokens, fp16 0.0003 and 0.0004, of which their own is 0.0017 and 0.0002 to 0.00025; from fp32
+// operands 2e-6 at most.
 constexpr int kTwinRows = 64;
 
 struct LossLayout {

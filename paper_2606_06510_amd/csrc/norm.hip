@@ -1,13 +1,19 @@
 // Layer norm of rows, y = (x - mean) rstd w + b, and its gradients,
 //   dx = rstd (g - mean g - h mean(g h)), g = dy w, h = (x - mean) rstd; dw = sum dy h, db = sum dy.
 // Both are bound by memory: every entry is read once and kept in registers while its
-// row's sums are taken, the variance about the mean.  16384 x 4096 bf16: forward 45 us (6.0
-// TB/s), the gradients with a residual 97 (5.5) and 5 for the join of the column sums.
+// row's sums are taken, the variance about the mean.  16384 x 4096 bf16: forward 53 us a call on
+// inputs that no cache holds (5.0 TB/s; the same inputs again 45), the gradients 81, with a
+// residual 101-102 (5.0 and 5.3 TB/s, the join of the column sums, 5 of them, included).
 //
 // L lanes have a row, lane l its 16-byte pieces l, l + L, .., N of them at most.  As few lanes
-// as keep N small: more than four pieces a lane cost more in registers than the barrier of
-// several waves a row (16384 x 4096 bf16, forward: 64 lanes of 8 pieces 99 us, 256 of 2 52; with
-// loads that wait for nothing 45).
+// as keep N small: many pieces a lane cost more in registers than the barrier of several waves a
+// row (16384 x 4096 bf16, forward: 64 lanes of 8 pieces 99 us, 256 of 2 52; with
+// loads that wait for nothing 45).  Forward, 1025 to 2048 pieces: 256 lanes of 8, for 512 of 4
+// are slower in 16 bits (16384 x 12288 231 us against 304, 4096 x 8200 63 against 77) and faster
+// in fp32 (8000 x 8000 116 against 102, 300 x 5000 7.6 against 6.0).  1024 lanes have 128 registers
+// each, into which four pieces do not fit but for the forward pass in fp32: 12 spill forward in 16
+// bits, and of the gradients 148 in fp32 and 288 in 16 bits (4096 x 12000 fp32 396 us, 1.5 TB/s;
+// 4096 x 20000 bf16 982, 0.5).
 #include <algorithm>
 
 #include "oz2_lanes.h"
@@ -189,7 +195,7 @@ k_norm_long(Oz2Norm a) {
 // A workgroup takes G rows of every gridDim G, and keeps the column sums of its rows in
 // registers; they leave as one partial row each of dweight and dbias, which k_norm_join adds
 // up in order.  One read of dY and X serves all three gradients (dX and the column sums
-// apart: 483 us for 16384 x 4096 bf16, together 102).
+// apart: 483 us for 16384 x 4096 bf16 with a residual, together 102).
 template <class T, int L, int N, int G, bool TINY = false>
 __global__ void __launch_bounds__(L* G)
 k_norm_backward(Oz2NormBack a) {
@@ -428,7 +434,7 @@ Shape backward_shape(int pieces) {
 
 // Partial column sums, as many as workgroups: one on a CU, two where each has two turns of
 // rows.  More parts cost more than their workgroups save (1000 x 4096 bf16: 500 of them 24.6 us,
-// 250 17.8; 16384 x 4096: 1024 120, 512 114).
+// 250 17.8; 16384 x 4096 with a residual: 1024 109, 512 101; 4000 x 2048 fp32 36 and 28).
 int oz2_norm_parts(int dtype, int rows, int width) {
   const Shape f = backward_shape((width + (dtype == OZ2_F32 ? 4 : 8) - 1) / (dtype == OZ2_F32 ? 4 : 8));
   if (!f.pieces) return (int)(((ll)rows + LONG_ROWS - 1) / LONG_ROWS);

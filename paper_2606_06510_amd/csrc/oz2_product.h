@@ -431,7 +431,9 @@ __device__ __forceinline__ void rows_lse(const Oz2Product& p, int t, bool on, in
 }
 
 // The gradient at W logits of a row (col: of the vocabulary), from its logits: (e^(z - lse) -
-// [target]) times the row's factor; 0 where the row does not count, and behind the row's end
+// [target]) times the row's factor; 0 where the row does not count, and behind the row's end.
+// (exp_for: of 16-bit operands the hardware's, off by |z - lse| 2^-24 relatively, also where two
+// parts keep more than 16 bits of it: the products that take them are rounded to 2^-8 or 2^-11.)
 template <class T, int W>
 __device__ __forceinline__ void loss_slope(const Oz2LossRow& r, int col, int valid, float* v) {
   const int at = r.target - col;

@@ -4,7 +4,8 @@
 // 64 / L tokens.  Rows of logits are read once, and the bytes are few (16384 tokens of 256
 // experts: 17 MB, 3 us): what bounds it is the search for the largest values, some 30
 // instructions a choice and token.  16384 tokens, 8 choices: of 256 experts by the logits'
-// order 10 us, by scores with a bias 19, in 8 groups 25; of 64 experts 5.9, 8.8 and 11.  (All
+// order 10 us, by scores with a bias 19, in 8 groups 24-27 by card (a group's two largest are one
+// lane's search in LDS, so that 8 of a token's 32 lanes work); of 64 experts 5.9, 8.8 and 11.  (All
 // scores in 64 bits and a wave a token: 169 us in groups.)  Gradient, 16384 x 128 bf16: 7 us.
 #include <algorithm>
 
@@ -137,7 +138,7 @@ __device__ __forceinline__ void load_logits(const T* row, int first, int E, floa
 
 __device__ __forceinline__ double sigmoid64(float l) { return 1.0 / (1.0 + exp(-(double)l)); }
 
-// The keys of groups g = lane, lane + L, .. of `per` keys each; sum: of the two largest, joined by
+// The keys of groups first .. end - 1 of `per` keys each; sum: of the two largest, joined by
 // add.  (Each lane starts elsewhere in its group: LDS's banks.)
 template <int L, class KEY, class F, class G>
 __device__ __forceinline__ void group_keys(const KEY* keys, int per, int first, int end, bool sum, int lane, F add,
@@ -288,7 +289,9 @@ struct Lds {
 // 64 bits are formed for few: 32 bits find those that can be among the largest, within `near`
 // of the last of them, and those are ranked.  near is twice the error of c = s + b: A of the score
 // (sigmoid: s (1 - s) (|l| 2^-24 + 2^-23) and two roundings, 3e-7 at most; softmax: of its
-// largest score, |x| e^x being below 0.37), and of the sum 2^-24 |c|.  Groups whose values are
+// largest score, |x| e^x being below 0.37), and of the sum 2^-24 |c|, c the largest of the token's
+// experts: a finite bias of -1e9 makes all others candidates (16384 tokens of 256 experts 20 -> 57
+// us, in groups 25 -> 93), -infinity does not (19 and 27).  Groups whose values are
 // that close are settled by the scores that can be their two largest.  Where none of that decides
 // (a NaN, an infinity, more than 64 so close), a token's scores are all formed, in LDS
 // and in loops: unrolled in registers they slowed down the rest (15 us to 35).

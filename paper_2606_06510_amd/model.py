@@ -114,7 +114,8 @@ def expert_route(logits, top_k, bias=None, score="softmax", groups=1, top_groups
     group_best (1 or 2) largest s + bias, and only the top_groups largest groups are chosen
     from.  The weights are scale * s, with renormalize scale * s / (the sum of the chosen s).
 
-    An expert whose logit or bias is -inf is out.  Where fewer than top_k are left (all, in
+    An expert whose logit or bias is -inf is out (and costs nothing, where a large finite bias
+    makes the choice three times as slow).  Where fewer than top_k are left (all, in
     a row of padding), ids is -1, which drops the pair, and the weight 0.  NaN is larger than
     every number.  Not recorded by autograd: the gradient is expert_route_backward's."""
     kind = _score(score)
@@ -296,7 +297,9 @@ def linear_cross_entropy_backward(dloss, x, w, targets, lse, need_dx=True, need_
 
     The logits are computed again, a piece of the vocabulary at a time.  Their gradient is
     rounded to the tensors' dtype before the products, as every operand of theirs, in
-    float16 times a power of two that keeps it in range."""
+    float16 times a power of two that keeps it in range (of up to 64 tokens in two parts,
+    which hold twice the bits).  A caller that needs it in 32 bits for more tokens passes
+    x.float() and w.float()."""
     if stream is None and workspace is None and dx is None and dw is None:
         done = (_fast or _bind()).linear_cross_entropy_backward(dloss, x, w, targets, lse, need_dx,
                                                                 need_dw)
